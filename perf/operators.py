@@ -188,13 +188,17 @@ def _plain_act_grad(g, act):
     return (g > 0).float()
 
 
-def _plain_block8(x):
-    """What an 8-bit checkpoint holds of x: blocks of 32 along a row with one power of two, codes of -127 .. 127."""
+def _plain_block8(x, act=None):
+    """What an 8-bit checkpoint holds of x: blocks of 32 along a row with one power of two, codes of -127 .. 127.
+    Under a ReLU a positive value's code is at least 1: its derivative there is not lost to rounding."""
     rows, width = x.shape
     b = torch.nn.functional.pad(x.float(), (0, -width % BLOCK)).view(rows, -1, BLOCK)
     top = torch.frexp(b.abs().amax(-1, keepdim=True)).exponent - 1  # floor(log2)
-    step = torch.ldexp(torch.ones_like(top, dtype=torch.float32), (top - 6).clamp(min=-126))
-    return ((b / step).round().clamp(-127, 127) * step).view(rows, -1)[:, :width]
+    step = ((top + (127 - 6)).clamp(min=1) << 23).view(torch.float32)  # 2^(top - 6), by its bits: exact
+    codes = (b / step).round().clamp(-127, 127)
+    if act == "relu":
+        codes = torch.maximum(codes, (b > 0).float() + -127 * (b <= 0).float())
+    return (codes * step).view(rows, -1)[:, :width]
 
 
 def _plain(s):
@@ -212,7 +216,7 @@ def _plain(s):
     h = (_plain_act(g, c["act"]) * u).to(t)
     if c["kind"] == "forward":
         return h
-    x8, g, u, dh = _plain_block8(x), _plain_block8(g), _plain_block8(u), s["dh"].float()
+    x8, g, u, dh = _plain_block8(x), _plain_block8(g, c["act"]), _plain_block8(u), s["dh"].float()
     dg, du = dh * u * _plain_act_grad(g, c["act"]), dh * _plain_act(g, c["act"])
     return {"h": h, "dx": (dg @ wg + du @ wu).to(t), "dwg": (dg.t() @ x8).to(t), "dwu": (du.t() @ x8).to(t)}
 
@@ -272,14 +276,15 @@ def _exact_act(g, act):
     return torch.clamp(g, min=0), (g > 0).double()
 
 
-def _exact_block8(x):
+def _exact_block8(x, relu=False):
     rows, width = x.shape
     out = torch.zeros((rows, -(-width // BLOCK) * BLOCK), dtype=torch.float64, device=DEV)
     out[:, :width] = x
     b = out.view(rows, -1, BLOCK)
     top = b.abs().max(-1, keepdim=True).values.clamp_min(2.0 ** -120)
-    step = 2.0 ** (torch.floor(torch.log2(top)) - 6)
-    b.copy_((torch.round(b / step)).clamp(-127, 127) * step)
+    step = (top.view(torch.int64) >> 52 << 52).view(torch.float64) / 64  # the power of two below, six down
+    codes = torch.round(b / step).clamp(-127, 127)
+    b.copy_(torch.where((b > 0) & (codes < 1) & relu, torch.ones_like(b), codes) * step)
     return out[:, :width]
 
 
@@ -297,7 +302,7 @@ def exact(c, seed):
     h = _exact_act(g, c["act"])[0] * u
     if c["kind"] == "forward":
         return h
-    g, u = _exact_block8(g), _exact_block8(u)
+    g, u = _exact_block8(g, c["act"] == "relu"), _exact_block8(u)
     a, da = _exact_act(g, c["act"])
     dg, du, x8 = s["dh"].double() * u * da, s["dh"].double() * a, _exact_block8(x)
     return {"h": h, "dx": dg @ wg + du @ wu, "dwg": dg.t() @ x8, "dwu": du.t() @ x8}
