@@ -294,6 +294,140 @@ SAMD_API samd_status samd_maxpool2x2(samd_fmt f, const void *in, void *out, int 
                             samd_layout layout, samd_stream_t stream);
 
 /*
+ * ---- Matrix products of floating-point activations with packed weights, and
+ * ---- activations kept in 8 bits: the gated feed-forward block.
+ *
+ * The paper stops at integer lanes. The calls below put its packed lanes under
+ * the block that holds most weights of a language model,
+ *   h = act(x Wg^T) * (x Wu^T),
+ * served from 4-bit lanes with group scales (samd_matvec4,
+ * samd_gated_matvec4) and trained with its activations kept in 8-bit lanes
+ * (samd_block8_*, samd_gated_ffn_*). The conventions at the top of this file
+ * hold: device pointers of 16-byte alignment, the caller's stream, no
+ * allocation, checks on the host before any launch. Strides ld* are in
+ * elements, from one row to the next. Inputs may overlap one another; no output
+ * may overlap an input or another output.
+ */
+typedef enum { SAMD_F16 = 0, SAMD_BF16 = 1, SAMD_F32 = 2 } samd_dtype;
+
+/* act(g); Phi is the normal distribution function. */
+typedef enum {
+  SAMD_SILU = 0,      /* g / (1 + exp(-g)) */
+  SAMD_GELU = 1,      /* g * Phi(g) */
+  SAMD_GELU_TANH = 2, /* g * (1 + tanh(sqrt(2/pi) * (g + 0.044715 g^3))) / 2 */
+  SAMD_RELU_ACT = 3   /* max(g, 0); its derivative at 0 is 0 */
+} samd_act;
+
+/*
+ * M tokens of K inputs and N outputs: x is M rows of K elements (stride ldx),
+ * y M rows of N (stride ldy), both of `type` (SAMD_F16 or SAMD_BF16). `group`,
+ * a power of two of at least 32, is the number of neighbouring inputs that
+ * share a scale (at least K: one scale a row).
+ */
+typedef struct {
+  int M, N, K, group;
+  int64_t ldx, ldy;
+  samd_dtype type;
+} samd_matvec_desc;
+
+/*
+ * N rows of K weights: lanes as samd_pack writes them, in the format of the
+ * call; scales [N][ceil(K / group)] of the call's `type`; zeros the same shape
+ * in bytes (low 4 bits read), or NULL for none. The weight of lane q is
+ * scale * (q - zero).
+ */
+typedef struct {
+  const void *lanes;
+  const void *scales;
+  const uint8_t *zeros;
+} samd_weights4;
+
+/*
+ * samd_matvec4: y[m][n] = sum_k x[m][k] * weight[n][k], summed in fp32 and
+ * rounded once. fw: 4-bit lanes without spacers, 32- or 64-bit words; signed
+ * lanes take no zero points (SAMD_EINVAL). Made for few tokens (it reads the
+ * weights once for every 32 of them); any M >= 0 is right. Each output depends
+ * on its row of x and its row of weights alone, and the same inputs give the
+ * same bits.
+ */
+SAMD_API samd_status samd_matvec4(const samd_matvec_desc *desc, samd_fmt fw, const void *x, samd_weights4 w, void *y,
+                                  samd_stream_t stream);
+
+/*
+ * samd_gated_matvec4: y[m][n] = act(g) * u with g and u the products of row m
+ * with row n of wg and of wu, all in fp32, rounded once. Both weights have
+ * zero points or neither has.
+ */
+SAMD_API samd_status samd_gated_matvec4(const samd_matvec_desc *desc, samd_act act, samd_fmt fw, const void *x,
+                                        samd_weights4 wg, samd_weights4 wu, void *y, samd_stream_t stream);
+
+/*
+ * An activation tensor in 8 bits: rows x inner lanes of the format
+ * {8 bits, signed, no spacer, 32-bit words} (what samd_unpack reads), and one
+ * exponent byte for every 32 neighbouring elements of a row,
+ * exps[rows][ceil(inner / 32)]. A lane c of a block with exponent e stands
+ * for c * 2^(e - 127), which 16-bit types hold without rounding (fp16: where
+ * the values came from fp16).
+ *   e = max(E - 6, 0), E the biased fp32 exponent of the block's largest
+ *       magnitude; c = round-to-even(v * 2^(127 - e)), clamped to -127 .. 127.
+ *   A block with an infinity or a NaN has e = 255 and zero lanes, and stands
+ *   for NaNs.
+ */
+typedef struct {
+  void *lanes;
+  uint8_t *exps;
+} samd_block8;
+
+/* x (rows of `inner` elements of `type`, stride ldx) into its 8-bit form. */
+SAMD_API samd_status samd_block8_quantize(samd_dtype type, const void *x, int64_t ldx, int64_t rows, int64_t inner,
+                                          samd_block8 out, samd_stream_t stream);
+/* The values an 8-bit form stands for, rounded to `type`, as rows of stride ldy. */
+SAMD_API samd_status samd_block8_dequantize(samd_dtype type, samd_block8 in, int64_t rows, int64_t inner, void *y,
+                                            int64_t ldy, samd_stream_t stream);
+
+/*
+ * The gated block of M tokens, K inputs and F hidden columns. x (and dx): M
+ * rows of K, stride ldx; wg, wu (and dwg, dwu): F rows of K, stride ldw; h (and
+ * dh): M rows of F, stride ldh; all of `type` (SAMD_F16 or SAMD_BF16). The
+ * strides are multiples of 8 (16-byte rows, else SAMD_EALIGN).
+ */
+typedef struct {
+  int M, K, F;
+  int64_t ldx, ldw, ldh;
+  samd_dtype type;
+  samd_act act;
+} samd_ffn_desc;
+
+/*
+ * samd_gated_ffn_forward: h = act(g) * u with g = x wg^T, u = x wu^T, in fp32
+ * and rounded once, in one kernel. ckpt_g, ckpt_u: the 8-bit forms of g and u
+ * (M rows of F), taken from the fp32 sums for the backward pass; NULL pointers
+ * in both: none are kept. With SAMD_RELU_ACT a positive g has a code of at
+ * least 1 in ckpt_g, so that no derivative is lost to rounding.
+ */
+SAMD_API samd_status samd_gated_ffn_forward(const samd_ffn_desc *desc, const void *x, const void *wg, const void *wu,
+                                            void *h, samd_block8 ckpt_g, samd_block8 ckpt_u, samd_stream_t stream);
+
+/* Bytes of workspace samd_gated_ffn_backward needs for this desc (0 on error). */
+SAMD_API size_t samd_gated_ffn_backward_workspace_size(const samd_ffn_desc *desc);
+
+/*
+ * samd_gated_ffn_backward: with x (M rows of K), g and u the values that the
+ * 8-bit forms stand for, dg = dh * u * act'(g) and du = dh * act(g) (fp32,
+ * rounded once to `type`, the operands of the products),
+ *   dx = dg wg + du wu,  dwg = dg^T x,  dwu = du^T x,  h = act(g) * u.
+ * Each output may be NULL if it is not wanted; those given are overwritten.
+ * ckpt_x is read for dwg and dwu only, wg and wu for dx only. With M = 0 the
+ * weights' gradients are zero. workspace: caller-owned device scratch.
+ * As with the convolution, a kernel that gives up on a bounded wait leaves its
+ * outputs undefined and records SAMD_ETIMEOUT for samd_device_status.
+ */
+SAMD_API samd_status samd_gated_ffn_backward(const samd_ffn_desc *desc, const void *dh, samd_block8 ckpt_x,
+                                             samd_block8 ckpt_g, samd_block8 ckpt_u, const void *wg, const void *wu,
+                                             void *dx, void *dwg, void *dwu, void *h, void *workspace,
+                                             size_t workspace_bytes, samd_stream_t stream);
+
+/*
  * samd_device_status: reads (and with reset=1 clears) the sticky status the
  * kernels of the current device record when a bounded wait runs out.
  * Synchronises `stream`. *status is SAMD_OK or SAMD_ETIMEOUT.

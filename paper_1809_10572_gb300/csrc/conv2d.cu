@@ -1140,6 +1140,15 @@ cudaError_t selftest_wait_timeout(uint64_t limit_ns, cudaStream_t s) {
   return cudaGetLastError();
 }
 
+cudaError_t device_status_ptr(int **out) {
+  void *p = nullptr;
+  const cudaError_t e = conv::g_status_addr.get(reinterpret_cast<const void *>(&g_conv_status), &p);
+  *out = static_cast<int *>(p);
+  return e;
+}
+
+conv::EncodeTiledFn tensor_map_encoder() { return conv::encode_tiled(); }
+
 cudaError_t read_device_status(int *status, int reset, cudaStream_t s) {
   int v = 0;
   cudaError_t e = cudaMemcpyFromSymbolAsync(&v, g_conv_status, sizeof(int), 0, cudaMemcpyDeviceToHost, s);

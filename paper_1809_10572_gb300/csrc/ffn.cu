@@ -1,0 +1,544 @@
+// ffn.cu -- the gated feed-forward block for training: forward with 8-bit
+// checkpoints, and the backward pass from them.
+//
+//   forward   g = x Wg^T, u = x Wu^T, h = act(g) * u
+//   backward  dg = dh * u * act'(g), du = dh * act(g)
+//             dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x
+//
+// Four large products (2 M K F multiply-adds forward, 4 M K F backward) on
+// tcgen05 with fp32 accumulators, through one persistent kernel in three forms:
+//   FWD  tile 128 tokens x 128 hidden columns of both projections: the B
+//        operand stacks 128 rows of Wg on 128 rows of Wu, so one MMA of N = 256
+//        fills g and u side by side in tensor memory, and the epilogue forms
+//        act(g) * u and the two 8-bit blocks of a row without leaving the chip.
+//   DX   tile 128 tokens x 256 inputs; the reduction runs over the hidden
+//        columns of dg and Wg, then of du and Wu, into the same accumulator.
+//        Wg and Wu are read as they lie (rows along the MMA's N).
+//   DW   tile 128 hidden columns x 256 inputs of either gradient; the reduction
+//        runs over the tokens, and both operands are read as they lie (rows
+//        along the MMA's M and N). x comes from its 8-bit form, whose values
+//        16-bit types hold without rounding.
+// Between FWD and the others an elementwise kernel forms dg and du, rounded to
+// the operands' type: with fp32 sums this is the one rounding between the
+// gradients' factors and their sums.
+#include <type_traits>
+
+#include "ffn_internal.cuh"
+#include "tc_ptx.cuh"
+
+namespace samd {
+namespace {
+
+enum Form { FWD = 0, DX = 1, DW = 2 };
+
+constexpr int BM = 128, BN = 256, BK = 64;
+constexpr int kStages = 4;
+constexpr int kABytes = BM * BK * 2, kBBytes = BN * BK * 2, kStageBytes = kABytes + kBBytes;
+constexpr int kEpiWarps = 8, kFirstEpiWarp = 4;
+constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
+constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + 256;
+constexpr uint64_t kWaitLimitNs = 1000000000ull;  // 1 s
+constexpr int kBand = 12;  // tiles along M that follow one another before the next along N
+
+struct GemmArgs {
+  int M, N;         // of an output: rows and columns
+  int steps;        // reduction steps of BK in a segment
+  int tiles_m, tiles_n, total;
+  int half_m;       // DW: rows of tiles of the first output; the rest are the second's
+  int64_t ld;       // of the output
+  void *out[2];     // FWD: h; DX: dx; DW: dwg, dwu
+  // FWD: the checkpoints (null: none), rows of `wpr` words and `bpr` exponents
+  uint32_t *lanes[2];
+  uint8_t *exps[2];
+  int64_t wpr, bpr;
+  int *status;
+};
+
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, int *status) {
+  return __all_sync(0xffffffffu,
+                    ptx::mbar_wait(bar, parity, status, static_cast<int>(SAMD_ETIMEOUT), kWaitLimitNs));
+}
+
+// Columns [c, c + 32) of a row of the output, rounded.
+template <typename T>
+__device__ __forceinline__ void store_row32(T *row, int c, int N, const float *v) {
+  if (c + 32 <= N) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<uint4 *>(row + c + 8 * i) =
+          make_uint4(pack2<T>(v[8 * i], v[8 * i + 1]), pack2<T>(v[8 * i + 2], v[8 * i + 3]),
+                     pack2<T>(v[8 * i + 4], v[8 * i + 5]), pack2<T>(v[8 * i + 6], v[8 * i + 7]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (c + i < N) row[c + i] = from_f32<T>(v[i]);
+  }
+}
+
+// The block [c, c + 32) of a row into its 8-bit form. Columns past N are zero.
+// kKeep: the code of a positive value is at least 1 (a ReLU's argument: rounded
+// to zero it would lose its derivative, which one in a hundred does on normal
+// data, a tenth of the gradient's norm).
+template <bool kKeep>
+__device__ __forceinline__ void store_block8(uint32_t *lanes, uint8_t *exps, int64_t wpr, int c, const float *v) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  const uint32_t e = block8_exp(top);
+  const float inv = block8_inv(e);
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    w[i] = block8_word(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
+    if constexpr (kKeep) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (e != 255u && v[4 * i + j] > 0.0f && (w[i] >> 8 * j & 255u) == 0u) w[i] |= 1u << 8 * j;
+    }
+  }
+  uint32_t *const out = lanes + c / 4;
+  if (wpr % 4 == 0 && c / 4 + 8 <= wpr) {
+    *reinterpret_cast<uint4 *>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4 *>(out + 4) = make_uint4(w[4], w[5], w[6], w[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c / 4 + i < wpr) out[i] = w[i];
+  }
+  exps[c / kBlock8] = static_cast<uint8_t>(e);
+}
+
+// One CTA per SM, looping over tiles; twelve warps: 0 loads operand tiles with
+// TMA, 1 issues the MMAs, 2 holds the tensor memory, 4-11 drain one of two
+// accumulators while the other fills. Every wait is bounded: a role that gives
+// up records it and stops, the others' waits then give up within one poll.
+template <int FORM, typename T, int ACT>
+__global__ void __launch_bounds__(kThreads, 1)
+    ffn_gemm_kernel(const __grid_constant__ CUtensorMap ma0, const __grid_constant__ CUtensorMap ma1,
+                    const __grid_constant__ CUtensorMap mb0, const __grid_constant__ CUtensorMap mb1,
+                    const GemmArgs a) {
+  constexpr bool kAMn = FORM == DW, kBMn = FORM != FWD;
+  constexpr int kSegs = FORM == DX ? 2 : 1;
+  constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *const smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t *const bars = reinterpret_cast<uint64_t *>(smem + kStages * kStageBytes);
+  const uint32_t full0 = ptx::smem_addr(bars), empty0 = full0 + 8 * kStages, accfull0 = empty0 + 8 * kStages,
+                 accempty0 = accfull0 + 16, drain = accempty0 + 16;
+  uint32_t *const holder = reinterpret_cast<uint32_t *>(bars + 2 * kStages + 5);
+  const uint32_t sbase = ptx::smem_addr(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (warp == 2) {
+    ptx::tmem_alloc(ptx::smem_addr(holder), 512);
+    ptx::tmem_relinquish();
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      ptx::mbar_init(full0 + 8 * s, 1);
+      ptx::mbar_init(empty0 + 8 * s, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(accfull0 + 8 * i, 1);
+      ptx::mbar_init(accempty0 + 8 * i, kEpiWarps);
+    }
+    ptx::mbar_init(drain, 1);
+    ptx::fence_barrier_init();
+  }
+  __syncwarp();
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *holder;
+  const int steps = a.steps * kSegs;
+
+  // tile -> its row and column of tiles: bands of kBand rows, down a band's
+  // column before the next, so that the tiles in flight share operands in L2
+  auto place = [&](int tile, int &tm, int &tn) {
+    const int band = tile / (kBand * a.tiles_n);
+    const int first = band * kBand;
+    const int rows = min(kBand, a.tiles_m - first);
+    const int r = tile - band * kBand * a.tiles_n;
+    tn = r / rows;
+    tm = first + (r - tn * rows);
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int s = 0, loaded = 0;
+      uint32_t par = 1;
+      bool ok = true;
+      for (int tile = blockIdx.x; ok && tile < a.total; tile += gridDim.x) {
+        int tm, tn;
+        place(tile, tm, tn);
+        const int second = FORM == DW && tm >= a.half_m;
+        const int m0 = (second ? tm - a.half_m : tm) * BM, n0 = tn * (FORM == FWD ? BN / 2 : BN);
+        for (int k = 0; k < steps; ++k) {
+          if (loaded == kStages) {
+            ok = ptx::mbar_wait(full0 + 8 * s, par, a.status, SAMD_ETIMEOUT, kWaitLimitNs) &&
+                 ptx::mbar_wait(empty0 + 8 * s, par, a.status, SAMD_ETIMEOUT, kWaitLimitNs);
+            if (!ok) break;
+          } else {
+            ++loaded;
+          }
+          const uint32_t full = full0 + 8 * s, sa = sbase + s * kStageBytes, sb = sa + kABytes;
+          ptx::mbar_arrive_expect_tx(full, kStageBytes);
+          const bool seg = FORM == DX && k >= a.steps;
+          const int kk = (seg ? k - a.steps : k) * BK;
+          const CUtensorMap *const A = (FORM == DX ? seg : FORM == DW ? second != 0 : false) ? &ma1 : &ma0;
+          const CUtensorMap *const B = FORM == DX && seg ? &mb1 : &mb0;
+          if constexpr (kAMn) {
+            ptx::tma_load_2d(sa, A, m0, kk, full);
+            ptx::tma_load_2d(sa + kABytes / 2, A, m0 + 64, kk, full);
+          } else {
+            ptx::tma_load_2d(sa, A, kk, m0, full);
+          }
+          if constexpr (FORM == FWD) {
+            ptx::tma_load_2d(sb, &mb0, kk, n0, full);
+            ptx::tma_load_2d(sb + kBBytes / 2, &mb1, kk, n0, full);
+          } else {
+#pragma unroll
+            for (int j = 0; j < BN / 64; ++j) ptx::tma_load_2d(sb + j * (kBBytes / 4), B, n0 + 64 * j, kk, full);
+          }
+          if (++s == kStages) {
+            s = 0;
+            par ^= 1;
+          }
+        }
+      }
+      // the CTA does not exit with a copy in flight: the ring's last round,
+      // oldest first
+      int quiet = 0;
+      for (int k = 0; k < loaded; ++k) {
+        int q = loaded == kStages ? s + k : k;
+        if (q >= kStages) q -= kStages;
+        ptx::mbar_wait_bounded(full0 + 8 * q, q < s ? par ^ 1u : par, &quiet, kWaitLimitNs / 10);
+      }
+    }
+  } else if (warp == 1) {
+    const uint32_t leader = ptx::elect_one() ? 1u : 0u;
+    constexpr uint32_t idesc = ptx::idesc_16_f32(kBf16, kAMn, kBMn, BM, BN);
+    // 16 reduction positions further: 32 bytes along a row, or 16 rows down
+    constexpr uint64_t kAStep = kAMn ? 2048 >> 4 : 32 >> 4, kBStep = kBMn ? 2048 >> 4 : 32 >> 4;
+    int s = 0, i = 0;
+    uint32_t par = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; ok && tile < a.total; tile += gridDim.x, ++i) {
+      const int acc = i & 1;
+      if (i >= 2) ok = warp_wait(accempty0 + 8 * acc, ((i >> 1) + 1) & 1u, a.status);
+      if (!ok) break;
+      ptx::tc_fence_after();
+      const uint32_t d = tmem + acc * BN;
+      for (int k = 0; k < steps; ++k) {
+        ok = warp_wait(full0 + 8 * s, par, a.status);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        const uint32_t sa = sbase + s * kStageBytes, sb = sa + kABytes;
+        const uint64_t da = kAMn ? ptx::sw128_mnmajor_desc(sa, kABytes / 2) : ptx::sw128_kmajor_desc(sa);
+        const uint64_t db = kBMn ? ptx::sw128_mnmajor_desc(sb, kBBytes / 4) : ptx::sw128_kmajor_desc(sb);
+#pragma unroll
+        for (int j = 0; j < BK / 16; ++j)
+          ptx::mma_f16(leader, d, da + j * kAStep, db + j * kBStep, idesc, k > 0 || j > 0);
+        ptx::mma_commit(leader, empty0 + 8 * s);
+        if (++s == kStages) {
+          s = 0;
+          par ^= 1;
+        }
+      }
+      if (ok) ptx::mma_commit(leader, accfull0 + 8 * acc);
+    }
+    // nothing of this CTA's reads shared memory or writes tensor memory after
+    // this: every MMA issued has completed
+    ptx::mma_commit(leader, drain);
+    int quiet = 0;
+    ptx::mbar_wait_bounded(drain, 0, &quiet, kWaitLimitNs / 10);
+  } else if (warp >= kFirstEpiWarp) {
+    const int ew = warp - kFirstEpiWarp;
+    const int quad = warp & 3, half = ew >> 2;  // rows 32 * quad .., the first or the second half of the columns
+    int i = 0;
+    for (int tile = blockIdx.x; tile < a.total; tile += gridDim.x, ++i) {
+      const int acc = i & 1;
+      if (!warp_wait(accfull0 + 8 * acc, (i >> 1) & 1u, a.status)) break;
+      ptx::tc_fence_after();
+      int tm, tn;
+      place(tile, tm, tn);
+      const int second = FORM == DW && tm >= a.half_m;
+      const int m = (second ? tm - a.half_m : tm) * BM + quad * 32 + lane;
+      const uint32_t t0 = tmem + acc * BN + (static_cast<uint32_t>(quad * 32) << 16);
+      if constexpr (FORM == FWD) {
+        const int n0 = tn * (BN / 2);
+#pragma unroll 1
+        for (int b = half * 2; b < half * 2 + 2; ++b) {
+          uint32_t rg[32], ru[32];
+          __syncwarp();
+          ptx::tmem_ld_32x32b_x32(t0 + b * 32, rg);
+          ptx::tmem_ld_32x32b_x32(t0 + BN / 2 + b * 32, ru);
+          ptx::tmem_wait_ld(rg);
+          ptx::tmem_wait_ld(ru);
+          const float *const gv = reinterpret_cast<const float *>(rg), *const uv = reinterpret_cast<const float *>(ru);
+          const int c = n0 + b * 32;
+          if (m < a.M && c < a.N) {
+            float h[32];
+#pragma unroll
+            for (int q = 0; q < 32; ++q) h[q] = act_value<ACT>(gv[q]) * uv[q];
+            store_row32<T>(static_cast<T *>(a.out[0]) + m * a.ld, c, a.N, h);
+            if (a.lanes[0]) {
+              store_block8<ACT == SAMD_RELU_ACT>(a.lanes[0] + m * a.wpr, a.exps[0] + m * a.bpr, a.wpr, c, gv);
+              store_block8<false>(a.lanes[1] + m * a.wpr, a.exps[1] + m * a.bpr, a.wpr, c, uv);
+            }
+          }
+        }
+      } else {
+        const int n0 = tn * BN;
+        T *const out = static_cast<T *>(second ? a.out[1] : a.out[0]) + m * a.ld;
+#pragma unroll 1
+        for (int b = half * 4; b < half * 4 + 4; ++b) {
+          uint32_t r[32];
+          __syncwarp();
+          ptx::tmem_ld_32x32b_x32(t0 + b * 32, r);
+          ptx::tmem_wait_ld(r);
+          const int c = n0 + b * 32;
+          if (m < a.M && c < a.N) store_row32<T>(out, c, a.N, reinterpret_cast<const float *>(r));
+        }
+      }
+      __syncwarp();
+      ptx::tc_fence_before();
+      if (lane == 0) ptx::mbar_arrive(accempty0 + 8 * acc);
+    }
+  }
+
+  __syncwarp();
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 2) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem, 512);
+  }
+}
+
+// dg = dh * u * act'(g) and du = dh * act(g) from the 8-bit forms of g and u,
+// rounded to T, in rows of `ldw` elements; h = act(g) * u again if wanted.
+// One pass over HBM: 4 1/16 bytes an element in, 4 or 6 out.
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256)
+    ffn_dgate_kernel(const T *__restrict__ dh, int64_t ldh, samd_block8 cg, samd_block8 cu, T *__restrict__ dg,
+                     T *__restrict__ du, int64_t ldw, T *__restrict__ h, int64_t M, int F, int segs, int64_t wpr,
+                     int64_t bpr) {
+  const int64_t nthreads = static_cast<int64_t>(gridDim.x) * blockDim.x;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < M * segs; i += nthreads) {
+    const int64_t m = i / segs;
+    const int c = static_cast<int>(i - m * segs) * 8;
+    const int n = F - c < 8 ? F - c : 8;
+    const uint32_t *const gl = static_cast<const uint32_t *>(cg.lanes) + m * wpr + c / 4;
+    const uint32_t *const ul = static_cast<const uint32_t *>(cu.lanes) + m * wpr + c / 4;
+    uint32_t gw[2], uw[2];
+    if (wpr % 2 == 0) {
+      const uint2 p = *reinterpret_cast<const uint2 *>(gl), q = *reinterpret_cast<const uint2 *>(ul);
+      gw[0] = p.x, gw[1] = p.y, uw[0] = q.x, uw[1] = q.y;
+    } else {
+      gw[0] = gl[0], uw[0] = ul[0];
+      gw[1] = n > 4 ? gl[1] : 0u, uw[1] = n > 4 ? ul[1] : 0u;
+    }
+    const float gs = block8_scale(cg.exps[m * bpr + c / kBlock8]), us = block8_scale(cu.exps[m * bpr + c / kBlock8]);
+    float d[8];
+    if (n == 8) {
+      const uint4 w = *reinterpret_cast<const uint4 *>(dh + m * ldh + c);
+      const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 f = unpack2<T>(ws[j]);
+        d[2 * j] = f.x;
+        d[2 * j + 1] = f.y;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) d[j] = j < n ? to_f32<T>(dh[m * ldh + c + j]) : 0.0f;
+    }
+    float vg[8], vu[8], vh[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float g = block8_value(gw[j >> 2], j & 3, gs), u = block8_value(uw[j >> 2], j & 3, us);
+      float da;
+      const float av = act_value_grad<ACT>(g, da);
+      vg[j] = d[j] * u * da;
+      vu[j] = d[j] * av;
+      vh[j] = av * u;
+    }
+    // the workspace's rows hold whole units of eight; past F they are not read
+    auto pack = [](const float *v) {
+      return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+    };
+    *reinterpret_cast<uint4 *>(dg + m * ldw + c) = pack(vg);
+    *reinterpret_cast<uint4 *>(du + m * ldw + c) = pack(vu);
+    if (h) {
+      if (n == 8) {
+        *reinterpret_cast<uint4 *>(h + m * ldh + c) = pack(vh);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < n) h[m * ldh + c + j] = from_f32<T>(vh[j]);
+      }
+    }
+  }
+}
+
+// ---- host side -------------------------------------------------------------------
+
+int64_t round_up8(int64_t v) { return (v + 7) / 8 * 8; }
+size_t round_up256(size_t v) { return (v + 255) / 256 * 256; }
+
+// A tensor of `rows` rows of `cols` 16-bit elements, read in boxes of 64
+// columns by box_rows rows with the 128-byte swizzle.
+bool make_map(CUtensorMap *map, samd_dtype t, const void *p, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+  const EncodeTiledFn enc = tensor_map_encoder();
+  if (!enc) return false;
+  const cuuint64_t dim[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t stride[1] = {static_cast<cuuint64_t>(ld) * 2};
+  const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)}, es[2] = {1, 1};
+  return enc(map, t == SAMD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+             const_cast<void *>(p), dim, stride, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int FORM, typename T, int ACT>
+cudaError_t launch_gemm(const CUtensorMap (&m)[4], GemmArgs &a, cudaStream_t s) {
+  a.total = a.tiles_m * a.tiles_n;
+  cudaError_t e = device_status_ptr(&a.status);
+  if (e != cudaSuccess) return e;
+  const auto kern = ffn_gemm_kernel<FORM, T, ACT>;
+  e = conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), kSmemBytes);
+  if (e != cudaSuccess) return e;
+  const int grid = a.total < sm_count() ? a.total : sm_count();
+  kern<<<grid, kThreads, kSmemBytes, s>>>(m[0], m[1], m[2], m[3], a);
+  return cudaGetLastError();
+}
+
+template <typename F>
+cudaError_t by_act(int act, F f) {
+  switch (act) {
+    case SAMD_SILU: return f(std::integral_constant<int, SAMD_SILU>());
+    case SAMD_GELU: return f(std::integral_constant<int, SAMD_GELU>());
+    case SAMD_GELU_TANH: return f(std::integral_constant<int, SAMD_GELU_TANH>());
+    default: return f(std::integral_constant<int, SAMD_RELU_ACT>());
+  }
+}
+
+template <typename T>
+cudaError_t forward(const samd_ffn_desc &d, const void *x, const void *wg, const void *wu, void *h, samd_block8 cg,
+                    samd_block8 cu, cudaStream_t s) {
+  CUtensorMap m[4];
+  if (!make_map(&m[0], d.type, x, d.M, d.K, d.ldx, BM) || !make_map(&m[2], d.type, wg, d.F, d.K, d.ldw, BN / 2) ||
+      !make_map(&m[3], d.type, wu, d.F, d.K, d.ldw, BN / 2))
+    return cudaErrorInvalidValue;
+  m[1] = m[0];
+  GemmArgs a = {};
+  a.M = d.M;
+  a.N = d.F;
+  a.steps = (d.K + BK - 1) / BK;
+  a.tiles_m = (d.M + BM - 1) / BM;
+  a.tiles_n = (d.F + BN / 2 - 1) / (BN / 2);
+  a.ld = d.ldh;
+  a.out[0] = h;
+  a.lanes[0] = static_cast<uint32_t *>(cg.lanes);
+  a.lanes[1] = static_cast<uint32_t *>(cu.lanes);
+  a.exps[0] = cg.exps;
+  a.exps[1] = cu.exps;
+  a.wpr = block8_words(d.F);
+  a.bpr = block8_blocks(d.F);
+  return by_act(d.act, [&](auto act) { return launch_gemm<FWD, T, decltype(act)::value>(m, a, s); });
+}
+
+// The workspace: dg and du (M rows of F) and x (M rows of K), each row a
+// multiple of eight elements.
+struct Workspace {
+  size_t dg, du, x, bytes;
+  int64_t ldf, ldk;
+};
+Workspace plan_workspace(const samd_ffn_desc &d) {
+  Workspace w;
+  w.ldf = round_up8(d.F);
+  w.ldk = round_up8(d.K);
+  const size_t f = round_up256(static_cast<size_t>(d.M) * w.ldf * 2), k = round_up256(static_cast<size_t>(d.M) * w.ldk * 2);
+  w.dg = 0;
+  w.du = f;
+  w.x = 2 * f;
+  w.bytes = 2 * f + k;
+  return w;
+}
+
+template <typename T>
+cudaError_t backward(const samd_ffn_desc &d, const void *dh, samd_block8 cx, samd_block8 cg, samd_block8 cu,
+                     const void *wg, const void *wu, void *dx, void *dwg, void *dwu, void *h, void *workspace,
+                     cudaStream_t s) {
+  const Workspace w = plan_workspace(d);
+  uint8_t *const ws = static_cast<uint8_t *>(workspace);
+  T *const dg = reinterpret_cast<T *>(ws + w.dg), *const du = reinterpret_cast<T *>(ws + w.du);
+  const int segs = (d.F + 7) / 8;
+  cudaError_t e = by_act(d.act, [&](auto act) {
+    constexpr int kAct = decltype(act)::value;
+    const int grid = resident_grid<ffn_dgate_kernel<T, kAct>>(static_cast<int64_t>(d.M) * segs, 256);
+    ffn_dgate_kernel<T, kAct><<<grid, 256, 0, s>>>(static_cast<const T *>(dh), d.ldh, cg, cu, dg, du, w.ldf,
+                                                   static_cast<T *>(h), d.M, d.F, segs, block8_words(d.F),
+                                                   block8_blocks(d.F));
+    return cudaGetLastError();
+  });
+  if (e != cudaSuccess) return e;
+  CUtensorMap m[4];
+  if (dx) {
+    if (!make_map(&m[0], d.type, dg, d.M, d.F, w.ldf, BM) || !make_map(&m[1], d.type, du, d.M, d.F, w.ldf, BM) ||
+        !make_map(&m[2], d.type, wg, d.F, d.K, d.ldw, BK) || !make_map(&m[3], d.type, wu, d.F, d.K, d.ldw, BK))
+      return cudaErrorInvalidValue;
+    GemmArgs a = {};
+    a.M = d.M;
+    a.N = d.K;
+    a.steps = (d.F + BK - 1) / BK;
+    a.tiles_m = (d.M + BM - 1) / BM;
+    a.tiles_n = (d.K + BN - 1) / BN;
+    a.ld = d.ldx;
+    a.out[0] = dx;
+    e = launch_gemm<DX, T, 0>(m, a, s);
+    if (e != cudaSuccess) return e;
+  }
+  if (dwg || dwu) {
+    e = launch_block8_dequantize(d.type, cx, d.M, d.K, ws + w.x, w.ldk, s);
+    if (e != cudaSuccess) return e;
+    const T *const first = dwg ? dg : du;
+    if (!make_map(&m[0], d.type, first, d.M, d.F, w.ldf, BK) || !make_map(&m[1], d.type, du, d.M, d.F, w.ldf, BK) ||
+        !make_map(&m[2], d.type, ws + w.x, d.M, d.K, w.ldk, BK))
+      return cudaErrorInvalidValue;
+    m[3] = m[2];
+    GemmArgs a = {};
+    a.M = d.F;
+    a.N = d.K;
+    a.steps = (d.M + BK - 1) / BK;
+    a.tiles_m = (d.F + BM - 1) / BM;
+    a.tiles_n = (d.K + BN - 1) / BN;
+    a.ld = d.ldw;
+    a.out[0] = dwg ? dwg : dwu;
+    a.out[1] = dwu;
+    a.half_m = a.tiles_m;
+    if (dwg && dwu) a.tiles_m *= 2;
+    e = launch_gemm<DW, T, 0>(m, a, s);
+  }
+  return e;
+}
+
+}  // namespace
+
+size_t ffn_backward_workspace(const samd_ffn_desc &d) { return plan_workspace(d).bytes; }
+
+cudaError_t launch_ffn_forward(const samd_ffn_desc &d, const void *x, const void *wg, const void *wu, void *h,
+                               samd_block8 cg, samd_block8 cu, cudaStream_t s) {
+  return d.type == SAMD_BF16 ? forward<__nv_bfloat16>(d, x, wg, wu, h, cg, cu, s)
+                             : forward<__half>(d, x, wg, wu, h, cg, cu, s);
+}
+
+cudaError_t launch_ffn_backward(const samd_ffn_desc &d, const void *dh, samd_block8 cx, samd_block8 cg, samd_block8 cu,
+                                const void *wg, const void *wu, void *dx, void *dwg, void *dwu, void *h,
+                                void *workspace, cudaStream_t s) {
+  return d.type == SAMD_BF16
+             ? backward<__nv_bfloat16>(d, dh, cx, cg, cu, wg, wu, dx, dwg, dwu, h, workspace, s)
+             : backward<__half>(d, dh, cx, cg, cu, wg, wu, dx, dwg, dwu, h, workspace, s);
+}
+
+}  // namespace samd

@@ -3,6 +3,7 @@
 // stream. See include/samd.h for the contract of each call.
 #include <mutex>
 
+#include "ffn_internal.cuh"
 #include "samd_internal.cuh"
 
 namespace samd {
@@ -220,6 +221,132 @@ samd_status samd_maxpool2x2(samd_fmt f, const void *in, void *out, int N, int C,
   if (!in || !out) return SAMD_EINVAL;
   if (!aligned16(in) || !aligned16(out)) return SAMD_EALIGN;
   return from_cuda(launch_maxpool2x2_nhwc(f, in, out, N, C, H, W, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+constexpr int kMaxDim = 1 << 30;  // of a matrix product: the kernels' tile coordinates stay within an int
+
+bool type16(samd_dtype t) { return t == SAMD_F16 || t == SAMD_BF16; }
+bool act_ok(samd_act a) { return a >= SAMD_SILU && a <= SAMD_RELU_ACT; }
+
+// Checks shared by the two matrix-vector calls; *empty: there is nothing to do.
+samd_status matvec4_checks(const samd_matvec_desc *d, samd_fmt fw, const void *x, const samd_weights4 *w, int n_w,
+                           const void *y, bool *empty) {
+  *empty = false;
+  if (!d || !type16(d->type) || !fmt_valid(fw)) return SAMD_EINVAL;
+  if (d->group < 32 || (d->group & (d->group - 1)) != 0) return SAMD_EINVAL;
+  if (fw.bits != 4 || fw.spacer != 0) return SAMD_EUNSUP;
+  if (d->M < 0 || d->N < 0 || d->K < 1 || d->ldx < d->K || d->ldy < d->N) return SAMD_ESHAPE;
+  if (d->M > kMaxDim || d->N > kMaxDim || d->K > kMaxDim) return SAMD_EUNSUP;
+  *empty = d->M == 0 || d->N == 0;
+  if (*empty) return SAMD_OK;
+  if (!x || !y) return SAMD_EINVAL;
+  for (int i = 0; i < n_w; ++i) {
+    if (!w[i].lanes || !w[i].scales) return SAMD_EINVAL;
+    if (w[i].zeros && fw.is_signed) return SAMD_EINVAL;
+    if (!w[i].zeros != !w[0].zeros) return SAMD_EINVAL;
+  }
+  if (!aligned16(x) || !aligned16(y)) return SAMD_EALIGN;
+  for (int i = 0; i < n_w; ++i)
+    if (!aligned16(w[i].lanes) || !aligned16(w[i].scales) || !aligned16(w[i].zeros)) return SAMD_EALIGN;
+  return SAMD_OK;
+}
+
+// Sizes and strides of the gated block.
+samd_status ffn_shape_checks(const samd_ffn_desc *d) {
+  if (!d || !type16(d->type) || !act_ok(d->act)) return SAMD_EINVAL;
+  if (d->M < 0 || d->K < 1 || d->F < 1 || d->ldx < d->K || d->ldw < d->K || d->ldh < d->F) return SAMD_ESHAPE;
+  if (d->ldx % 8 != 0 || d->ldw % 8 != 0 || d->ldh % 8 != 0) return SAMD_EALIGN;
+  if (d->M > kMaxDim || d->K > kMaxDim || d->F > kMaxDim) return SAMD_EUNSUP;
+  // tiles of an output are counted in an int, strides in bytes by the tensor maps in 40 bits
+  const int64_t m = d->M / 128 + 1, k = d->K / 128 + 1, f = d->F / 128 + 1;
+  if (m * f >= kMaxDim || m * k >= kMaxDim || 2 * f * k >= kMaxDim) return SAMD_EUNSUP;
+  const int64_t ld = (int64_t(1) << 38);
+  if (d->ldx >= ld || d->ldw >= ld || d->ldh >= ld) return SAMD_EUNSUP;
+  return SAMD_OK;
+}
+}  // namespace
+
+samd_status samd_matvec4(const samd_matvec_desc *d, samd_fmt fw, const void *x, samd_weights4 w, void *y,
+                         samd_stream_t stream) {
+  bool empty;
+  const samd_status st = matvec4_checks(d, fw, x, &w, 1, y, &empty);
+  if (st != SAMD_OK || empty) return st;
+  return from_cuda(launch_matvec4(*d, -1, fw, x, w, nullptr, y, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+samd_status samd_gated_matvec4(const samd_matvec_desc *d, samd_act act, samd_fmt fw, const void *x, samd_weights4 wg,
+                               samd_weights4 wu, void *y, samd_stream_t stream) {
+  if (!act_ok(act)) return SAMD_EINVAL;
+  const samd_weights4 w[2] = {wg, wu};
+  bool empty;
+  const samd_status st = matvec4_checks(d, fw, x, w, 2, y, &empty);
+  if (st != SAMD_OK || empty) return st;
+  return from_cuda(launch_matvec4(*d, act, fw, x, wg, &wu, y, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+samd_status samd_block8_quantize(samd_dtype type, const void *x, int64_t ldx, int64_t rows, int64_t inner,
+                                 samd_block8 out, samd_stream_t stream) {
+  if (!type16(type) && type != SAMD_F32) return SAMD_EINVAL;
+  if (!shape_ok(rows, inner) || ldx < inner || (rows > 0 && ldx > INT64_MAX / 8 / rows)) return SAMD_ESHAPE;
+  if (rows == 0 || inner == 0) return SAMD_OK;
+  if (!x || !out.lanes || !out.exps) return SAMD_EINVAL;
+  if (!aligned16(x) || !aligned16(out.lanes) || !aligned16(out.exps)) return SAMD_EALIGN;
+  return from_cuda(launch_block8_quantize(type, x, ldx, rows, inner, out, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+samd_status samd_block8_dequantize(samd_dtype type, samd_block8 in, int64_t rows, int64_t inner, void *y, int64_t ldy,
+                                   samd_stream_t stream) {
+  if (!type16(type) && type != SAMD_F32) return SAMD_EINVAL;
+  if (!shape_ok(rows, inner) || ldy < inner || (rows > 0 && ldy > INT64_MAX / 8 / rows)) return SAMD_ESHAPE;
+  if (rows == 0 || inner == 0) return SAMD_OK;
+  if (!y || !in.lanes || !in.exps) return SAMD_EINVAL;
+  if (!aligned16(y) || !aligned16(in.lanes) || !aligned16(in.exps)) return SAMD_EALIGN;
+  return from_cuda(launch_block8_dequantize(type, in, rows, inner, y, ldy, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+samd_status samd_gated_ffn_forward(const samd_ffn_desc *d, const void *x, const void *wg, const void *wu, void *h,
+                                   samd_block8 cg, samd_block8 cu, samd_stream_t stream) {
+  const samd_status st = ffn_shape_checks(d);
+  if (st != SAMD_OK) return st;
+  if (d->M == 0) return SAMD_OK;
+  if (!x || !wg || !wu || !h) return SAMD_EINVAL;
+  const bool keep = cg.lanes != nullptr;  // all four pointers, or none
+  if ((cg.exps != nullptr) != keep || (cu.lanes != nullptr) != keep || (cu.exps != nullptr) != keep)
+    return SAMD_EINVAL;
+  if (!aligned16(x) || !aligned16(wg) || !aligned16(wu) || !aligned16(h) || !aligned16(cg.lanes) ||
+      !aligned16(cg.exps) || !aligned16(cu.lanes) || !aligned16(cu.exps))
+    return SAMD_EALIGN;
+  return from_cuda(launch_ffn_forward(*d, x, wg, wu, h, cg, cu, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+size_t samd_gated_ffn_backward_workspace_size(const samd_ffn_desc *d) {
+  return ffn_shape_checks(d) == SAMD_OK ? ffn_backward_workspace(*d) : 0;
+}
+
+samd_status samd_gated_ffn_backward(const samd_ffn_desc *d, const void *dh, samd_block8 cx, samd_block8 cg,
+                                    samd_block8 cu, const void *wg, const void *wu, void *dx, void *dwg, void *dwu,
+                                    void *h, void *workspace, size_t workspace_bytes, samd_stream_t stream) {
+  const samd_status st = ffn_shape_checks(d);
+  if (st != SAMD_OK) return st;
+  const bool weights = dwg || dwu;
+  if (!dx && !weights && !h) return SAMD_EINVAL;
+  if (!aligned16(dx) || !aligned16(dwg) || !aligned16(dwu) || !aligned16(h)) return SAMD_EALIGN;
+  const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (d->M == 0) {  // a sum over no tokens
+    for (void *w : {dwg, dwu})
+      if (w && cudaMemset2DAsync(w, static_cast<size_t>(d->ldw) * 2, 0, static_cast<size_t>(d->K) * 2, d->F, s) !=
+                   cudaSuccess)
+        return SAMD_ECUDA;
+    return SAMD_OK;
+  }
+  if (!dh || !cg.lanes || !cg.exps || !cu.lanes || !cu.exps || !workspace) return SAMD_EINVAL;
+  if ((dx && (!wg || !wu)) || (weights && (!cx.lanes || !cx.exps))) return SAMD_EINVAL;
+  if (!aligned16(dh) || !aligned16(cx.lanes) || !aligned16(cx.exps) || !aligned16(cg.lanes) || !aligned16(cg.exps) ||
+      !aligned16(cu.lanes) || !aligned16(cu.exps) || !aligned16(wg) || !aligned16(wu) || !aligned16(workspace))
+    return SAMD_EALIGN;
+  if (workspace_bytes < ffn_backward_workspace(*d)) return SAMD_ESHAPE;
+  return from_cuda(launch_ffn_backward(*d, dh, cx, cg, cu, wg, wu, dx, dwg, dwu, h, workspace, s));
 }
 
 samd_status samd_device_status(int *status, int reset, samd_stream_t stream) {

@@ -12,9 +12,11 @@ fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -37,14 +39,38 @@ class samd_conv_desc(ctypes.Structure):
                 ("pad", ctypes.c_int), ("layout", ctypes.c_int)]
 
 
+class samd_matvec_desc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int), ("N", ctypes.c_int), ("K", ctypes.c_int), ("group", ctypes.c_int),
+                ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64), ("type", ctypes.c_int)]
+
+
+class samd_weights4(ctypes.Structure):
+    _fields_ = [("lanes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("zeros", ctypes.c_void_p)]
+
+
+class samd_block8(ctypes.Structure):
+    _fields_ = [("lanes", ctypes.c_void_p), ("exps", ctypes.c_void_p)]
+
+
+class samd_ffn_desc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int), ("K", ctypes.c_int), ("F", ctypes.c_int), ("ldx", ctypes.c_int64),
+                ("ldw", ctypes.c_int64), ("ldh", ctypes.c_int64), ("type", ctypes.c_int), ("act", ctypes.c_int)]
+
+
 SAMD_OK, SAMD_EINVAL, SAMD_EALIGN, SAMD_ESHAPE, SAMD_EUNSUP, SAMD_ECUDA, SAMD_ETIMEOUT = range(7)
 SAMD_ADD, SAMD_SUB, SAMD_MUL, SAMD_RELU, SAMD_REQUANT = range(5)
 SAMD_NCHW, SAMD_NHWC = 0, 1
+SAMD_F16, SAMD_BF16, SAMD_F32 = range(3)
+DTYPES = {torch.float16: SAMD_F16, torch.bfloat16: SAMD_BF16, torch.float32: SAMD_F32}
+SAMD_SILU, SAMD_GELU, SAMD_GELU_TANH, SAMD_RELU_ACT = range(4)
+ACTS = {"silu": SAMD_SILU, "gelu": SAMD_GELU, "gelu_tanh": SAMD_GELU_TANH, "relu": SAMD_RELU_ACT}
 OPS = {"add": SAMD_ADD, "sub": SAMD_SUB, "mul": SAMD_MUL, "relu": SAMD_RELU, "requant": SAMD_REQUANT}
 
 EXPORTED = ["samd_lanes_per_word", "samd_packed_words", "samd_pack", "samd_unpack", "samd_elementwise",
             "samd_conv2d", "samd_conv2d_workspace_size", "samd_conv2d_operand_bits", "samd_conv2d_set_min_tiles_per_cta", "samd_conv2d_prepare", "samd_conv2d_prepared",
             "samd_conv2d_noalloc", "samd_conv2d_prepared_pool2x2", "samd_conv2d_pool2x2_supported",
+            "samd_matvec4", "samd_gated_matvec4", "samd_block8_quantize", "samd_block8_dequantize",
+            "samd_gated_ffn_forward", "samd_gated_ffn_backward", "samd_gated_ffn_backward_workspace_size",
             "samd_maxpool2x2", "samd_device_status", "samd_selftest_wait_timeout", "samd_status_str", "samd_version"]
 FMT_NONE = (0, 0, 0, 0)
 
@@ -104,6 +130,18 @@ def load(build_if_missing: bool = True):
     lib.samd_conv2d_set_min_tiles_per_cta.restype = i32
     lib.samd_maxpool2x2.argtypes = [samd_fmt, vp, vp, i32, i32, i32, i32, i32, vp]
     lib.samd_maxpool2x2.restype = i32
+    mvp, w4, b8, fdp = c.POINTER(samd_matvec_desc), samd_weights4, samd_block8, c.POINTER(samd_ffn_desc)
+    lib.samd_matvec4.argtypes, lib.samd_matvec4.restype = [mvp, samd_fmt, vp, w4, vp, vp], i32
+    lib.samd_gated_matvec4.argtypes = [mvp, i32, samd_fmt, vp, w4, w4, vp, vp]
+    lib.samd_gated_matvec4.restype = i32
+    lib.samd_block8_quantize.argtypes, lib.samd_block8_quantize.restype = [i32, vp, i64, i64, i64, b8, vp], i32
+    lib.samd_block8_dequantize.argtypes, lib.samd_block8_dequantize.restype = [i32, b8, i64, i64, vp, i64, vp], i32
+    lib.samd_gated_ffn_forward.argtypes = [fdp, vp, vp, vp, vp, b8, b8, vp]
+    lib.samd_gated_ffn_forward.restype = i32
+    lib.samd_gated_ffn_backward.argtypes = [fdp, vp, b8, b8, b8, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.samd_gated_ffn_backward.restype = i32
+    lib.samd_gated_ffn_backward_workspace_size.argtypes = [fdp]
+    lib.samd_gated_ffn_backward_workspace_size.restype = sz
     lib.samd_device_status.argtypes, lib.samd_device_status.restype = [c.POINTER(c.c_int), i32, vp], i32
     lib.samd_selftest_wait_timeout.argtypes, lib.samd_selftest_wait_timeout.restype = [c.c_uint64, vp], i32
     lib.samd_status_str.argtypes, lib.samd_status_str.restype = [i32], c.c_char_p
@@ -239,6 +277,57 @@ def samd_conv2d_pool2x2_supported(desc, fa, fw, fo) -> bool:
 def samd_maxpool2x2(f, inp, out, N, C, H, W, layout=SAMD_NHWC, stream=None):
     _check(load().samd_maxpool2x2(f, _ptr(inp), _ptr(out), N, C, H, W, layout, _stream(stream)),
            "samd_maxpool2x2")
+
+
+def _weights4(lanes, scales, zeros) -> samd_weights4:
+    return samd_weights4(_ptr(lanes), _ptr(scales), _ptr(zeros))
+
+
+def _block8(b) -> samd_block8:
+    """Of a Block8, a pair (lanes, exps) of tensors or addresses, or None."""
+    return samd_block8(None, None) if b is None else samd_block8(_ptr(b[0]), _ptr(b[1]))
+
+
+def _act(act) -> int:
+    return ACTS[act] if isinstance(act, str) else act
+
+
+def samd_matvec4(desc: samd_matvec_desc, fw, x, lanes, scales, zeros, y, stream=None):
+    _check(load().samd_matvec4(ctypes.byref(desc), fw, _ptr(x), _weights4(lanes, scales, zeros), _ptr(y),
+                               _stream(stream)), "samd_matvec4")
+
+
+def samd_gated_matvec4(desc: samd_matvec_desc, act, fw, x, wg, wu, y, stream=None):
+    """wg, wu: (lanes, scales, zeros or None)."""
+    _check(load().samd_gated_matvec4(ctypes.byref(desc), _act(act), fw, _ptr(x), _weights4(*wg), _weights4(*wu),
+                                     _ptr(y), _stream(stream)), "samd_gated_matvec4")
+
+
+def samd_block8_quantize(dtype, x, ldx, rows, inner, out, stream=None):
+    _check(load().samd_block8_quantize(DTYPES.get(dtype, dtype), _ptr(x), ldx, rows, inner, _block8(out),
+                                       _stream(stream)), "samd_block8_quantize")
+
+
+def samd_block8_dequantize(dtype, b, rows, inner, y, ldy, stream=None):
+    _check(load().samd_block8_dequantize(DTYPES.get(dtype, dtype), _block8(b), rows, inner, _ptr(y), ldy,
+                                         _stream(stream)), "samd_block8_dequantize")
+
+
+def samd_gated_ffn_forward(desc: samd_ffn_desc, x, wg, wu, h, ckpt_g=None, ckpt_u=None, stream=None):
+    _check(load().samd_gated_ffn_forward(ctypes.byref(desc), _ptr(x), _ptr(wg), _ptr(wu), _ptr(h), _block8(ckpt_g),
+                                         _block8(ckpt_u), _stream(stream)), "samd_gated_ffn_forward")
+
+
+def samd_gated_ffn_backward_workspace_size(desc: samd_ffn_desc) -> int:
+    return int(load().samd_gated_ffn_backward_workspace_size(ctypes.byref(desc)))
+
+
+def samd_gated_ffn_backward(desc: samd_ffn_desc, dh, ckpt_x, ckpt_g, ckpt_u, wg, wu, dx, dwg, dwu, h, workspace,
+                            workspace_bytes=None, stream=None):
+    nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(load().samd_gated_ffn_backward(ctypes.byref(desc), _ptr(dh), _block8(ckpt_x), _block8(ckpt_g),
+                                          _block8(ckpt_u), _ptr(wg), _ptr(wu), _ptr(dx), _ptr(dwg), _ptr(dwu), _ptr(h),
+                                          _ptr(workspace), nb, _stream(stream)), "samd_gated_ffn_backward")
 
 
 def samd_device_status(reset: bool = False, stream=None) -> int:
@@ -390,3 +479,193 @@ def maxpool2x2(words, f: samd_fmt, N: int, C: int, H: int, W: int, stream=None):
     out = empty_words(f, N * (H // 2) * (W // 2), C, words.device)
     samd_maxpool2x2(f, words, out, N, C, H, W, SAMD_NHWC, stream)
     return out
+
+
+# ---- the gated feed-forward block -------------------------------------------------
+
+
+def _on(stream):
+    """Allocations made inside belong to the stream that uses them."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
+def _rows(t: torch.Tensor, what: str, cols: int | None = None, rows: int | None = None, dtype=None) -> int:
+    """Checks a matrix whose rows lie contiguous in memory and returns its row stride in elements."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(t.shape)}, "
+                         f"strides {t.stride()}")
+    if (cols is not None and t.shape[1] != cols) or (rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, wanted ({rows if rows is not None else 'any'}, "
+                         f"{cols if cols is not None else 'any'})")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what}: {t.dtype}, wanted {dtype}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _check_weights4(lanes, scales, zeros, N, K, group, f, dtype):
+    groups = -(-K // group)
+    if lanes.dtype != word_dtype(f) or not lanes.is_contiguous() or lanes.numel() != N * -(-K // (f.word_bits // 4)):
+        raise ValueError(f"lanes: {N} packed rows of {K} 4-bit lanes are wanted")
+    if scales.dtype != dtype or not scales.is_contiguous() or tuple(scales.shape) != (N, groups):
+        raise ValueError(f"scales: a contiguous ({N}, {groups}) {dtype} tensor is wanted")
+    if zeros is not None and (zeros.dtype != torch.uint8 or not zeros.is_contiguous() or
+                              tuple(zeros.shape) != (N, groups)):
+        raise ValueError(f"zeros: a contiguous ({N}, {groups}) uint8 tensor is wanted")
+
+
+def _matvec_desc(x, scales, group, out):
+    if x.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError(f"x: {x.dtype}, wanted float16 or bfloat16")
+    if group < 32 or group & (group - 1):
+        raise ValueError(f"group: {group}, wanted a power of two of at least 32")
+    M, N, K = x.shape[0], scales.shape[0], x.shape[1]
+    ldx = _rows(x, "x")
+    ldy = _rows(out, "out", N, M, x.dtype) if out is not None else N
+    return samd_matvec_desc(M, N, K, group, ldx, ldy, DTYPES[x.dtype])
+
+
+def matvec4(x, lanes, scales, group: int, f: samd_fmt, zeros=None, out=None, stream=None):
+    """x (M, K) times N rows of K packed 4-bit weights, scales (N, ceil(K / group)) of x's type and, for unsigned
+    lanes, zero points of the same shape (uint8): out (M, N), y = x @ (scale * (lane - zero)).T."""
+    d = _matvec_desc(x, scales, group, out)
+    _check_weights4(lanes, scales, zeros, d.N, d.K, group, f, x.dtype)
+    if out is None:
+        with _on(stream):
+            out = torch.empty((d.M, d.N), dtype=x.dtype, device=x.device)
+    samd_matvec4(d, f, x, lanes, scales, zeros, out, stream)
+    return out
+
+
+def gated_matvec4(x, lanes_g, scales_g, lanes_u, scales_u, group: int, f: samd_fmt, act="silu", zeros_g=None,
+                  zeros_u=None, out=None, stream=None):
+    """act(x @ Wg.T) * (x @ Wu.T) over two sets of packed 4-bit weights, as matvec4 takes one."""
+    d = _matvec_desc(x, scales_g, group, out)
+    _check_weights4(lanes_g, scales_g, zeros_g, d.N, d.K, group, f, x.dtype)
+    _check_weights4(lanes_u, scales_u, zeros_u, d.N, d.K, group, f, x.dtype)
+    if out is None:
+        with _on(stream):
+            out = torch.empty((d.M, d.N), dtype=x.dtype, device=x.device)
+    samd_gated_matvec4(d, act, f, x, (lanes_g, scales_g, zeros_g), (lanes_u, scales_u, zeros_u), out, stream)
+    return out
+
+
+class Block8(NamedTuple):
+    """An activation tensor in 8 bits (samd_block8): packed lanes (format block8_fmt()) and block exponents."""
+    lanes: torch.Tensor
+    exps: torch.Tensor
+    inner: int
+
+
+def block8_fmt() -> samd_fmt:
+    return fmt(8, True, 0, 32)
+
+
+def block8_empty(rows: int, inner: int, device="cuda") -> Block8:
+    return Block8(torch.empty((rows, -(-inner // 4)), dtype=torch.int32, device=device),
+                  torch.empty((rows, -(-inner // 32)), dtype=torch.uint8, device=device), inner)
+
+
+def _check_block8(b: Block8, what: str, rows: int, inner: int):
+    if b.inner != inner or tuple(b.lanes.shape) != (rows, -(-inner // 4)) or \
+            tuple(b.exps.shape) != (rows, -(-inner // 32)) or not b.lanes.is_contiguous() or \
+            not b.exps.is_contiguous() or b.lanes.dtype != torch.int32 or b.exps.dtype != torch.uint8:
+        raise ValueError(f"{what}: the 8-bit form of a ({rows}, {inner}) tensor is wanted")
+
+
+def block8_quantize(x: torch.Tensor, out: Block8 | None = None, stream=None) -> Block8:
+    """The 8-bit form of a matrix (float16, bfloat16 or float32)."""
+    if x.dtype not in DTYPES:
+        raise ValueError(f"x: {x.dtype}, wanted float16, bfloat16 or float32")
+    ldx = _rows(x, "x")
+    rows, inner = x.shape
+    if out is None:
+        with _on(stream):
+            out = block8_empty(rows, inner, x.device)
+    else:
+        _check_block8(out, "out", rows, inner)
+    samd_block8_quantize(x.dtype, x, ldx, rows, inner, out, stream)
+    return out
+
+
+def block8_dequantize(b: Block8, dtype: torch.dtype, out=None, stream=None) -> torch.Tensor:
+    """The values an 8-bit form stands for, as a matrix of `dtype`."""
+    if dtype not in DTYPES:
+        raise ValueError(f"dtype: {dtype}, wanted float16, bfloat16 or float32")
+    rows = b.lanes.shape[0]
+    _check_block8(b, "b", rows, b.inner)
+    if out is None:
+        with _on(stream):
+            out = torch.empty((rows, b.inner), dtype=dtype, device=b.lanes.device)
+    samd_block8_dequantize(dtype, b, rows, b.inner, out, _rows(out, "out", b.inner, rows, dtype), stream)
+    return out
+
+
+def _aligned8(n: int) -> int:
+    return -(-n // 8) * 8
+
+
+def _empty_rows(rows: int, cols: int, like: torch.Tensor) -> torch.Tensor:
+    """A (rows, cols) matrix whose rows start 16-byte units apart."""
+    return torch.empty((rows, _aligned8(cols)), dtype=like.dtype, device=like.device)[:, :cols]
+
+
+def _ffn_desc(M, K, F, t, act, ldx, ldw, ldh) -> samd_ffn_desc:
+    if t not in (torch.float16, torch.bfloat16):
+        raise ValueError(f"{t}: float16 or bfloat16 is wanted")
+    return samd_ffn_desc(M, K, F, ldx, ldw, ldh, DTYPES[t], _act(act))
+
+
+def _ld8(t: torch.Tensor, what: str, rows: int, cols: int, dtype) -> int:
+    """The row stride of a matrix of the block, rounded up where a single row leaves it open."""
+    ld = _rows(t, what, cols, rows, dtype)
+    return ld if rows > 1 else _aligned8(ld)
+
+
+def _same_ld(a: int, b: int, what: str) -> int:
+    if a != b:
+        raise ValueError(f"{what}: one row stride for both is wanted, got {a} and {b}")
+    return a
+
+
+def gated_ffn_forward(x, wg, wu, act="silu", checkpoints: bool = False, out=None, stream=None):
+    """h = act(x @ wg.T) * (x @ wu.T) for x (M, K), wg and wu (F, K), whose rows start 16-byte units apart (a row
+    stride that is a multiple of 8). With checkpoints: (h, ckpt_g, ckpt_u), the two products in 8 bits for
+    gated_ffn_backward."""
+    (M, K), F, t = x.shape, wg.shape[0], x.dtype
+    with _on(stream):
+        h = _empty_rows(M, F, x) if out is None else out
+        g8, u8 = (block8_empty(M, F, x.device), block8_empty(M, F, x.device)) if checkpoints else (None, None)
+    d = _ffn_desc(M, K, F, t, act, _ld8(x, "x", M, K, t),
+                  _same_ld(_ld8(wg, "wg", F, K, t), _ld8(wu, "wu", F, K, t), "wg, wu"), _ld8(h, "out", M, F, t))
+    samd_gated_ffn_forward(d, x, wg, wu, h, g8, u8, stream)
+    return (h, g8, u8) if checkpoints else h
+
+
+def gated_ffn_backward(dh, ckpt_x: Block8, ckpt_g: Block8, ckpt_u: Block8, wg, wu, act="silu", need_dx: bool = True,
+                       need_dw: bool = True, need_h: bool = False, workspace=None, stream=None):
+    """Gradients of gated_ffn_forward from dh (M, F) and the 8-bit forms of x, g and u: (dx, dwg, dwu), None for those
+    not wanted, and with need_h also h formed again from the checkpoints (for the next layer's weight gradient)."""
+    (M, F), K, t = dh.shape, wg.shape[1], dh.dtype
+    if need_dw:
+        _check_block8(ckpt_x, "ckpt_x", M, K)
+    _check_block8(ckpt_g, "ckpt_g", M, F)
+    _check_block8(ckpt_u, "ckpt_u", M, F)
+    ldw = _same_ld(_ld8(wg, "wg", F, K, t), _ld8(wu, "wu", F, K, t), "wg, wu")
+    ldh = _ld8(dh, "dh", M, F, t)
+    d = _ffn_desc(M, K, F, t, act, _aligned8(K), ldw, ldh)
+    with _on(stream):
+        dx = _empty_rows(M, K, dh) if need_dx else None
+        dwg, dwu = (_empty_strided(F, K, ldw, dh), _empty_strided(F, K, ldw, dh)) if need_dw else (None, None)
+        h = _empty_strided(M, F, ldh, dh) if need_h else None
+        if workspace is None:
+            workspace = torch.empty(samd_gated_ffn_backward_workspace_size(d), dtype=torch.uint8, device=dh.device)
+        if dx is None and dwg is None and h is None:
+            raise ValueError("nothing is wanted")
+        samd_gated_ffn_backward(d, dh, ckpt_x, ckpt_g, ckpt_u, wg, wu, dx, dwg, dwu, h, workspace, stream=stream)
+    return (dx, dwg, dwu, h) if need_h else (dx, dwg, dwu)
+
+
+def _empty_strided(rows: int, cols: int, ld: int, like: torch.Tensor) -> torch.Tensor:
+    return torch.empty_strided((rows, cols), (ld, 1), dtype=like.dtype, device=like.device)
