@@ -24,10 +24,12 @@
 // 32 inputs is four words of a row, which ldmatrix deals out as the MMA wants
 // them: word t of row r to lane 4 r + t.
 //
-// Split: a CTA takes 16 * RT rows (of both matrices of the pair) and its eight
-// warps take blocks of KB inputs in turn, each through its own ring of cp.async
-// stages (weights, tokens, scales, zero points), without a barrier until their
-// sums are joined, in a fixed order, at the end.
+// Split: the grid is at most one wave of resident CTAs, each taking tiles of
+// 16 * RT rows (of both matrices of the pair) in turn. Its eight warps share a
+// tile's blocks of KB inputs, each through its own ring of cp.async stages
+// (weights, scales, zero points) that runs on into the next tile; their sums
+// are joined in a fixed order behind the tile's one barrier. Tokens come
+// through L1, which holds a CTA's x from tile to tile.
 #include "ffn_internal.cuh"
 #include "tc_ptx.cuh"
 
@@ -49,14 +51,12 @@ struct MvArgs {
   int64_t n_scales;   // of a matrix
   int M, N, K;
   int group_shift;    // log2(group)
-  int nb;             // groups that a block of KB inputs touches
   int nblk;           // blocks of KB inputs
-  int s_words, z_words;  // 4-byte words staged for a row's scales and zero points of a block
-  int x_rows;         // tokens staged
+  int tiles;          // of 16 * RT rows
   int w_vec, x_vec;   // rows are 16-byte aligned
+  int s_vec;          // a row's scales of a block lie on a multiple of their size
   int is_signed;
   int act;            // of the gated pair; -1: one matrix
-  int x_off, s_off, z_off, stage_bytes;  // of a warp's stage
 };
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
@@ -131,256 +131,401 @@ __device__ __forceinline__ float f32_of_bits(uint16_t v) {
   return to_f32<T>(reinterpret_cast<const T &>(v));
 }
 
-// CH: chunks of 32 inputs in a block.
-template <typename T, bool kGated, int RT, int NT, int CH, int STAGES>
-__global__ void __launch_bounds__(kThreads) matvec4_kernel(const MvArgs a) {
-  constexpr int kMats = kGated ? 2 : 1;
-  constexpr int kTiles = RT * kMats;  // 16-row tiles of a CTA: those of the first matrix, then the second's
-  constexpr int kRows = 16 * kTiles;
-  constexpr int KB = 32 * CH;
-  constexpr int kPitch = 16 * CH;      // bytes of a row of weights in a stage
-  constexpr int kXPitch = 2 * KB + 64;  // of a token: eight lanes read two tokens' neighbouring 64 bytes without conflict
-  constexpr int kSwz = CH >= 8 ? 0 : CH == 4 ? 1 : 2;  // rows that share a 128-byte line
+// The lane's eight inputs k .. k + 7 of a token; those past K are zero and not read.
+template <typename T>
+__device__ __forceinline__ uint4 load_x8(const T *row, int64_t k, int K, bool vec) {
+  const int64_t left = K - k;
+  if (vec && left >= 8) return __ldg(reinterpret_cast<const uint4 *>(row + k));
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < left) w[i / 2] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t *>(row) + k + i)) << 16 * (i & 1);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// CH: chunks of 32 inputs in a block; CPG: chunks of a block that share a scale.
+template <typename T, bool kGated, bool kZeros, int RT, int NT, int CH, int CPG>
+struct Mv {
+  static constexpr int kMats = kGated ? 2 : 1;
+  static constexpr int kTiles = RT * kMats;  // 16-row tiles of a CTA's tile: the first matrix's, then the second's
+  static constexpr int kRows = 16 * kTiles;
+  static constexpr int KB = 32 * CH;
+  static constexpr int kStages = RT * kMats > 1 && CH == 8 ? 3 : 4;
+  static constexpr int kPitch = 16 * CH;  // bytes of a row of weights in a stage
+  static constexpr int kGroups = CH / CPG;  // scales of a row in a block
+  // bytes of a row's scales, and of its zero points, in a stage: the 4-byte
+  // words that hold them at any alignment, in a power of two
+  static constexpr int kSPitch = kGroups == 1 ? 4 : 4 * kGroups;
+  static constexpr int kZPitch = kGroups == 1 ? 4 : kGroups <= 4 ? 8 : 16;
+  static constexpr int kSOff = kRows * kPitch;
+  static constexpr int kZOff = kSOff + kRows * kSPitch;
+  static constexpr int kStageBytes = (kZOff + (kZeros ? kRows * kZPitch : 0) + 127) / 128 * 128;
+  static constexpr int kBufs = NT == 1 ? 2 : 1;
+  // the warps' sums: rows of an odd number of tokens, so that neighbouring rows lie in other banks
+  static __host__ __device__ int red_pitch(int tokens) { return tokens | 1; }
+  static __host__ __device__ int red_floats(int tokens) { return kWarps * kRows * red_pitch(tokens); }  // of one buffer
+  static size_t smem(int tokens) {
+    return static_cast<size_t>(kWarps) * kStages * kStageBytes + static_cast<size_t>(kBufs) * red_floats(tokens) * 4;
+  }
+};
+
+template <typename T, bool kGated, bool kZeros, int RT, int NT, int CH, int CPG>
+__global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
+  using P = Mv<T, kGated, kZeros, RT, NT, CH, CPG>;
+  constexpr int kTiles = P::kTiles, kRows = P::kRows, KB = P::KB, kPitch = P::kPitch, kStages = P::kStages;
+  constexpr int kSwz = CH >= 8 ? 0 : CH == 4 ? 1 : 2;  // rows that share a 128-byte line: 2^kSwz
   static_assert(CH == 2 || CH == 4 || CH == 8, "a row of a stage is 32, 64 or 128 bytes");
   extern __shared__ __align__(128) uint8_t smem[];
+  float *const red = reinterpret_cast<float *>(smem + static_cast<size_t>(kWarps) * kStages * P::kStageBytes);
+
+  // the tokens may come from the kernel before; the next one may be set up
+  ptx::grid_dependency_wait();
+  ptx::grid_dependents_launch();
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
-  const int n0 = blockIdx.x * (16 * RT);
   const int m0 = blockIdx.y * (8 * NT);
   const int tokens = min(a.M - m0, 8 * NT);
-  uint8_t *const mine = smem + static_cast<size_t>(warp) * STAGES * a.stage_bytes;
+  uint8_t *const mine = smem + static_cast<size_t>(warp) * kStages * P::kStageBytes;
+  const uint32_t mine_s = ptx::smem_addr(mine);
   const T *const x = static_cast<const T *>(a.x) + m0 * a.ldx;
 
-  // One block's weights, tokens, scales and zero points into a stage. Rows past
-  // N repeat row N - 1 (their sums are not stored); bytes past a row's end, and
-  // inputs past K, are zero.
-  auto load = [&](int blk, uint8_t *st) {
-    const int64_t k0 = static_cast<int64_t>(blk) * KB;
-    const uint32_t sw = ptx::smem_addr(st);
-    const int64_t off = k0 / 2;
+  // One block's weights, scales and zero points into a stage. Rows past N
+  // repeat row N - 1 (their sums are not stored); bytes past a row's end are
+  // zero. Where a row's scales of a block do not lie on their own size
+  // (s_vec = 0), the 4-byte words around them are copied, a word past the end
+  // of the array is clipped, and the reader finds its place in the first word
+  // from the same index.
+  auto load = [&](int n0, int blk, uint32_t st) {
+    const int last = a.N - 1 - n0;  // of the tile's rows
+    const uint32_t row_bytes = static_cast<uint32_t>(a.row_bytes), groups = static_cast<uint32_t>(a.groups);
     if (a.w_vec) {
+      constexpr int kStep = 32 / CH;  // rows a copy of the warp covers
+      const int lrow = lane / CH, ch = lane % CH;
+      const int64_t at = static_cast<int64_t>(blk) * (KB / 2) + ch * 16;
+      const bool in = at < a.row_bytes;  // whole 16-byte units: row_bytes is a multiple of 16
+      const uint32_t size = in ? 16u : 0u;
+      const int64_t from = static_cast<int64_t>(n0) * a.row_bytes + (in ? at : 0);
 #pragma unroll
-      for (int i = 0; i < kRows * CH / 32; ++i) {
-        const int idx = i * 32 + lane, row = idx / CH, ch = idx % CH;
-        const int mat = kGated ? row / (16 * RT) : 0;
-        const int64_t n = min(n0 + row - mat * 16 * RT, a.N - 1);
-        const int64_t at = off + ch * 16;
-        const bool in = at < a.row_bytes;  // whole 16-byte units: row_bytes is a multiple of 16
-        ptx::cp_async_16(sw + row * kPitch + ((ch ^ ((row >> kSwz) & (CH - 1))) * 16),
-                         a.lanes[mat] + n * a.row_bytes + (in ? at : 0), in ? 16u : 0u);
+      for (int i = 0; i < kRows / kStep; ++i) {
+        const int row = i * kStep + lrow, mat = kGated && i * kStep >= 16 * RT;
+        const uint32_t r = min(row - mat * 16 * RT, last);
+        ptx::cp_async_16(st + row * kPitch + ((ch ^ ((row >> kSwz) & (CH - 1))) * 16),
+                         a.lanes[mat] + from + static_cast<uint64_t>(r) * row_bytes, size);
       }
     } else {
-      for (int i = 0; i < kRows * CH * 4 / 32; ++i) {
-        const int idx = i * 32 + lane, row = idx / (4 * CH), w = idx % (4 * CH), ch = w >> 2;
-        const int mat = kGated ? row / (16 * RT) : 0;
-        const int64_t n = min(n0 + row - mat * 16 * RT, a.N - 1);
-        const int64_t at = off + w * 4;
+      constexpr int kPer = 4 * CH;  // words of a row
+      for (int i = 0; i < kRows * kPer / 32; ++i) {
+        const int idx = i * 32 + lane, row = idx / kPer, w = idx % kPer, ch = w >> 2;
+        const int mat = kGated && row >= 16 * RT;
+        const int64_t at = static_cast<int64_t>(blk) * (KB / 2) + w * 4;
         const bool in = at < a.row_bytes;
-        ptx::cp_async_4(sw + row * kPitch + ((ch ^ ((row >> kSwz) & (CH - 1))) * 16) + (w & 3) * 4,
-                        a.lanes[mat] + n * a.row_bytes + (in ? at : 0), in ? 4u : 0u);
+        ptx::cp_async_4(st + row * kPitch + ((ch ^ ((row >> kSwz) & (CH - 1))) * 16) + (w & 3) * 4,
+                        a.lanes[mat] + (n0 + min(row - mat * 16 * RT, last)) * a.row_bytes + (in ? at : 0),
+                        in ? 4u : 0u);
       }
     }
-    const uint32_t sx = sw + a.x_off;
-    if (a.x_vec) {
-      for (int idx = lane; idx < tokens * 4 * CH; idx += 32) {
-        const int m = idx / (4 * CH), p = idx % (4 * CH);
-        const int64_t k = k0 + p * 8, left = a.K - k;
-        const uint32_t bytes = left >= 8 ? 16u : left > 0 ? static_cast<uint32_t>(left) * 2u : 0u;
-        ptx::cp_async_16(sx + m * kXPitch + p * 16, x + m * a.ldx + (bytes ? k : 0), bytes);
+    const int64_t g0 = (static_cast<int64_t>(blk) * KB) >> a.group_shift;
+    const int64_t tile_g = n0 * a.groups + g0;
+    if (P::kGroups > 1 && a.s_vec) {
+#pragma unroll
+      for (int i = 0; i < (kRows + 31) / 32; ++i) {
+        const int row = i * 32 + lane, mat = kGated && row >= 16 * RT;
+        if (kRows % 32 == 0 || row < kRows) {
+          const int64_t n = tile_g + static_cast<uint64_t>(static_cast<uint32_t>(min(row - mat * 16 * RT, last))) * groups;
+          const uint32_t dst = st + P::kSOff + row * P::kSPitch;
+          if constexpr (P::kGroups == 8) ptx::cp_async_16(dst, a.scales[mat] + n * 2, 16);
+          if constexpr (P::kGroups == 4) ptx::cp_async_8(dst, a.scales[mat] + n * 2, 8);
+          if constexpr (P::kGroups == 2) ptx::cp_async_4(dst, a.scales[mat] + n * 2, 4);
+        }
       }
     } else {
-      for (int idx = lane; idx < tokens * KB; idx += 32) {
-        const int m = idx / KB, p = idx % KB;
-        uint16_t v = 0;
-        if (k0 + p < a.K) v = reinterpret_cast<const uint16_t *>(x)[m * a.ldx + k0 + p];
-        *reinterpret_cast<uint16_t *>(st + a.x_off + m * kXPitch + p * 2) = v;
+      constexpr int kWords = P::kGroups == 1 ? 1 : P::kGroups / 2 + 1;
+#pragma unroll
+      for (int i = 0; i < (kRows * kWords + 31) / 32; ++i) {
+        const int idx = i * 32 + lane, row = idx / kWords, w = idx % kWords, mat = kGated && row >= 16 * RT;
+        if (kRows * kWords % 32 == 0 || row < kRows) {
+          const int64_t n = tile_g + min(row - mat * 16 * RT, last) * a.groups;
+          const int64_t at = (n * 2 & ~int64_t(3)) + w * 4, left = a.n_scales * 2 - at;
+          ptx::cp_async_4(st + P::kSOff + row * P::kSPitch + w * 4, a.scales[mat] + (left > 0 ? at : 0),
+                          left >= 4 ? 4u : left > 0 ? static_cast<uint32_t>(left) : 0u);
+        }
       }
     }
-    // The 4-byte words that hold the row's scales of this block; the reader
-    // finds its place in the first word from the same index. A word past the
-    // end of the array is clipped.
-    const int64_t g0 = k0 >> a.group_shift;
-    for (int idx = lane; idx < kRows * a.s_words; idx += 32) {
-      const int row = idx / a.s_words, w = idx - row * a.s_words;
-      const int mat = kGated ? row / (16 * RT) : 0;
-      const int64_t n = min(n0 + row - mat * 16 * RT, a.N - 1);
-      const int64_t at = ((n * a.groups + g0) * 2 & ~int64_t(3)) + w * 4, left = a.n_scales * 2 - at;
-      ptx::cp_async_4(sw + a.s_off + idx * 4, a.scales[mat] + (left > 0 ? at : 0),
-                      left >= 4 ? 4u : left > 0 ? static_cast<uint32_t>(left) : 0u);
-    }
-    if (a.zeros[0]) {
-      for (int idx = lane; idx < kRows * a.z_words; idx += 32) {
-        const int row = idx / a.z_words, w = idx - row * a.z_words;
-        const int mat = kGated ? row / (16 * RT) : 0;
-        const int64_t n = min(n0 + row - mat * 16 * RT, a.N - 1);
-        const int64_t at = ((n * a.groups + g0) & ~int64_t(3)) + w * 4, left = a.n_scales - at;
-        ptx::cp_async_4(sw + a.z_off + idx * 4, a.zeros[mat] + (left > 0 ? at : 0),
-                        left >= 4 ? 4u : left > 0 ? static_cast<uint32_t>(left) : 0u);
+    if constexpr (kZeros) {
+      constexpr int kWords = P::kGroups == 1 ? 1 : P::kGroups <= 4 ? 2 : 3;
+#pragma unroll
+      for (int i = 0; i < (kRows * kWords + 31) / 32; ++i) {
+        const int idx = i * 32 + lane, row = idx / kWords, w = idx % kWords, mat = kGated && row >= 16 * RT;
+        if (kRows * kWords % 32 == 0 || row < kRows) {
+          const int64_t n = tile_g + min(row - mat * 16 * RT, last) * a.groups;
+          const int64_t at = (n & ~int64_t(3)) + w * 4, left = a.n_scales - at;
+          ptx::cp_async_4(st + P::kZOff + row * P::kZPitch + w * 4, a.zeros[mat] + (left > 0 ? at : 0),
+                          left >= 4 ? 4u : left > 0 ? static_cast<uint32_t>(left) : 0u);
+        }
       }
     }
   };
 
-  float acc[kTiles][NT][4];
-#pragma unroll
-  for (int r = 0; r < kTiles; ++r)
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[r][j][i] = 0.0f;
-
   const uint32_t flip = a.is_signed ? 0x00080008u : 0u;
-  const bool has_zeros = a.zeros[0] != nullptr;
+  Offset<T> plain;  // without zero points: offset binary's 8 for signed lanes, else 0
+  plain.set(flip & 15u);
 
-  int next = warp;
+  // the ring's next block to load, which runs ahead of the one in hand, over the CTA's tiles
+  int l_tile = blockIdx.x, l_blk = warp, fill = 0, slot = 0;
+  auto load_next = [&]() {
+    if (l_tile < a.tiles && l_blk < a.nblk) {
+      load(l_tile * (16 * RT), l_blk, mine_s + fill * P::kStageBytes);
+      l_blk += kWarps;
+      if (l_blk >= a.nblk) {
+        l_blk = warp;
+        l_tile += gridDim.x;
+      }
+    }
+    ptx::cp_async_commit();
+    fill = fill + 1 == kStages ? 0 : fill + 1;
+  };
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s) {
-    if (next < a.nblk) load(next, mine + s * a.stage_bytes);
-    ptx::cp_async_commit();
-    next += kWarps;
-  }
-  int slot = 0, fill = STAGES - 1;
-  for (int blk = warp; blk < a.nblk; blk += kWarps) {
-    ptx::cp_async_wait<STAGES - 2>();
-    __syncwarp();  // every lane's copies are in, and the slot filled next has been read by every lane
-    if (next < a.nblk) load(next, mine + fill * a.stage_bytes);
-    ptx::cp_async_commit();
-    next += kWarps;
-    fill = fill + 1 == STAGES ? 0 : fill + 1;
+  for (int s = 0; s < kStages - 1; ++s) load_next();
 
-    uint8_t *const st = mine + slot * a.stage_bytes;
-    slot = slot + 1 == STAGES ? 0 : slot + 1;
-    const uint32_t sw = ptx::smem_addr(st);
-    const int64_t k0 = static_cast<int64_t>(blk) * KB;
-    const int64_t g0 = k0 >> a.group_shift;
-    const int64_t left = a.K - k0;
-    const int nch = left >= KB ? CH : static_cast<int>((left + 31) / 32);
+  int buf = 0;
+  for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+    const int n0 = tile * (16 * RT);
+    float acc[kTiles][NT][4];
 #pragma unroll
-    for (int c2 = 0; c2 < CH; c2 += 2) {
-      if (c2 < nch) {
-        uint32_t words[kTiles][4];
+    for (int r = 0; r < kTiles; ++r)
 #pragma unroll
-        for (int r = 0; r < kTiles; ++r) {
-          const int row = r * 16 + (lane & 15), ch = c2 + (lane >> 4);
-          ldmatrix_x4(sw + row * kPitch + ((ch ^ ((row >> kSwz) & (CH - 1))) * 16), words[r]);
-        }
+      for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int cc = 0; cc < 2; ++cc) {
-          const int c = c2 + cc;
-          if (c < nch) {
-            uint32_t b[NT][4];
+        for (int i = 0; i < 4; ++i) acc[r][j][i] = 0.0f;
+    // index of the rows' first scales, low bits (the place in a staged word)
+    int first[kTiles][2];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-              uint4 q = make_uint4(0, 0, 0, 0);
-              if (8 * j + g < tokens)
-                q = *reinterpret_cast<const uint4 *>(st + a.x_off + (8 * j + g) * kXPitch + c * 64 + t * 16);
-              b[j][0] = __byte_perm(q.x, q.z, 0x5410);
-              b[j][1] = __byte_perm(q.x, q.z, 0x7632);
-              b[j][2] = __byte_perm(q.y, q.w, 0x5410);
-              b[j][3] = __byte_perm(q.y, q.w, 0x7632);
-            }
-            const int gi = static_cast<int>(((k0 + c * 32) >> a.group_shift) - g0);
+    for (int r = 0; r < kTiles; ++r)
 #pragma unroll
-            for (int r = 0; r < kTiles; ++r) {
-              const int mat_row = kGated && r >= RT ? r - RT : r;
-              uint32_t lo[4], hi[4];
-              float s[2];
-              Offset<T> o[2];
+      for (int h = 0; h < 2; ++h)
+        first[r][h] = static_cast<int>(min(n0 + (kGated && r >= RT ? r - RT : r) * 16 + g + 8 * h, a.N - 1) * a.groups & 3);
+
+    for (int blk = warp; blk < a.nblk; blk += kWarps) {
+      const int64_t k0 = static_cast<int64_t>(blk) * KB;
+      // tokens first: their way through L1 overlaps the wait for the stage
+      uint4 xq[NT == 1 ? CH : 1];
+      if constexpr (NT == 1) {
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int row = r * 16 + g + 8 * h;
-                const int64_t n = min(n0 + mat_row * 16 + g + 8 * h, a.N - 1);
-                const int64_t first = n * a.groups + g0;
-                s[h] = f32_of_bits<T>(*reinterpret_cast<const uint16_t *>(st + a.s_off + row * a.s_words * 4 +
-                                                                          (first & 1) * 2 + gi * 2));
-                o[h].set(has_zeros ? st[a.z_off + row * a.z_words * 4 + (first & 3) + gi] & 15u
-                                   : (flip & 15u));
-              }
-              widen(words[r][2 * cc], flip, o[0], lo);
-              widen(words[r][2 * cc + 1], flip, o[1], hi);
+        for (int c = 0; c < CH; ++c) xq[c] = make_uint4(0, 0, 0, 0);
+        if (g < tokens) {
+          const T *const xr = x + g * a.ldx + k0 + t * 8;
+          if (a.x_vec && k0 + KB <= a.K) {
 #pragma unroll
-              for (int j = 0; j < NT; ++j) {
-                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
-                mma16816<T>(d, a0, b[j][0], b[j][1]);
-                mma16816<T>(d, a1, b[j][2], b[j][3]);
-                acc[r][j][0] = fmaf(s[0], d[0], acc[r][j][0]);
-                acc[r][j][1] = fmaf(s[0], d[1], acc[r][j][1]);
-                acc[r][j][2] = fmaf(s[1], d[2], acc[r][j][2]);
-                acc[r][j][3] = fmaf(s[1], d[3], acc[r][j][3]);
-              }
-            }
+            for (int c = 0; c < CH; ++c) xq[c] = __ldg(reinterpret_cast<const uint4 *>(xr + c * 32));
+          } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) xq[c] = load_x8<T>(x + g * a.ldx, k0 + c * 32 + t * 8, a.K, a.x_vec);
           }
         }
       }
+      ptx::cp_async_wait<kStages - 2>();
+      __syncwarp();  // every lane's copies are in, and the slot filled next has been read by every lane
+      load_next();
+      const uint8_t *const st = mine + slot * P::kStageBytes;
+      const uint32_t sw = mine_s + slot * P::kStageBytes;
+      slot = slot + 1 == kStages ? 0 : slot + 1;
+      const int g0 = static_cast<int>((k0 >> a.group_shift) & 3);
+      const bool one_scale = P::kGroups > 1 && CPG == 4 && a.group_shift > 7;  // groups that hold whole blocks
+      // the rows' scales of the block, two in a word
+      constexpr int kSW = (P::kGroups + 1) / 2;
+      uint32_t sraw[kTiles][2][kSW];
+#pragma unroll
+      for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint8_t *const sp = st + P::kSOff + (r * 16 + g + 8 * h) * P::kSPitch;
+          if (P::kGroups > 1 && a.s_vec) {
+            if constexpr (P::kGroups == 8) {
+              const uint4 v = *reinterpret_cast<const uint4 *>(sp);
+              sraw[r][h][0] = v.x, sraw[r][h][1] = v.y, sraw[r][h][2] = v.z, sraw[r][h][3] = v.w;
+            }
+            if constexpr (P::kGroups == 4) {
+              const uint2 v = *reinterpret_cast<const uint2 *>(sp);
+              sraw[r][h][0] = v.x, sraw[r][h][1] = v.y;
+            }
+            if constexpr (P::kGroups == 2) sraw[r][h][0] = *reinterpret_cast<const uint32_t *>(sp);
+          } else {
+            const uint16_t *const sh = reinterpret_cast<const uint16_t *>(sp) + ((first[r][h] + g0) & 1);
+#pragma unroll
+            for (int i = 0; i < kSW; ++i) {
+              const int i0 = one_scale ? 0 : 2 * i;
+              sraw[r][h][i] = sh[i0];
+              if constexpr (P::kGroups > 1) sraw[r][h][i] |= static_cast<uint32_t>(sh[one_scale ? 0 : i0 + 1]) << 16;
+            }
+          }
+        }
+      if (k0 + KB > a.K) {
+        // The last block of a row: past the row's end lanes and tokens are zero
+        // and add nothing, whatever their scale, unless that is not finite.
+        const int ng = static_cast<int>((a.K - k0 + 32 * CPG - 1) / (32 * CPG));  // groups with inputs
+#pragma unroll
+        for (int gi = 0; gi < P::kGroups; ++gi)
+          if (gi >= ng) {
+#pragma unroll
+            for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) sraw[r][h][gi / 2] &= gi & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+          }
+      }
+      uint32_t words[kTiles][4];
+#pragma unroll
+      for (int gi = 0; gi < P::kGroups; ++gi) {
+        {
+          float s[kTiles][2], d[kTiles][NT][4];
+          Offset<T> o[kTiles][2];
+#pragma unroll
+          for (int r = 0; r < kTiles; ++r) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t w = sraw[r][h][gi / 2];
+              s[r][h] = f32_of_bits<T>(static_cast<uint16_t>(gi & 1 ? w >> 16 : w));
+              if constexpr (kZeros)
+                o[r][h].set(st[P::kZOff + (r * 16 + g + 8 * h) * P::kZPitch + ((first[r][h] + g0) & 3) + (one_scale ? 0 : gi)] & 15u);
+              else
+                o[r][h] = plain;
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) d[r][j][i] = 0.0f;
+          }
+#pragma unroll
+          for (int cc = 0; cc < CPG; ++cc) {
+            const int c = gi * CPG + cc;
+            {
+              if ((c & 1) == 0) {  // two chunks at a time
+#pragma unroll
+                for (int r = 0; r < kTiles; ++r) {
+                  const int row = r * 16 + (lane & 15), ch = c + (lane >> 4);
+                  ldmatrix_x4(sw + row * kPitch + ((ch ^ ((row >> kSwz) & (CH - 1))) * 16), words[r]);
+                }
+              }
+              uint32_t b[NT][4];
+#pragma unroll
+              for (int j = 0; j < NT; ++j) {
+                uint4 q = make_uint4(0, 0, 0, 0);
+                if constexpr (NT == 1) {
+                  q = xq[c];
+                } else {
+                  if (8 * j + g < tokens)
+                    q = load_x8<T>(x + (8 * j + g) * a.ldx, k0 + c * 32 + t * 8, a.K, a.x_vec);
+                }
+                b[j][0] = __byte_perm(q.x, q.z, 0x5410);
+                b[j][1] = __byte_perm(q.x, q.z, 0x7632);
+                b[j][2] = __byte_perm(q.y, q.w, 0x5410);
+                b[j][3] = __byte_perm(q.y, q.w, 0x7632);
+              }
+#pragma unroll
+              for (int r = 0; r < kTiles; ++r) {
+                uint32_t lo[4], hi[4];
+                widen(words[r][2 * (c & 1)], flip, o[r][0], lo);
+                widen(words[r][2 * (c & 1) + 1], flip, o[r][1], hi);
+                const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                  mma16816<T>(d[r][j], a0, b[j][0], b[j][1]);
+                  mma16816<T>(d[r][j], a1, b[j][2], b[j][3]);
+                }
+              }
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[r][j][i] = fmaf(s[r][i >> 1], d[r][j][i], acc[r][j][i]);
+        }
+      }
     }
-  }
 
-  // Join the warps' sums: [warp][row][token], rows one float apart from their
-  // neighbours' banks.
-  ptx::cp_async_wait<0>();
-  __syncthreads();
-  constexpr int kTok = 8 * NT, kRed = kTok + 1;
-  float *const red = reinterpret_cast<float *>(smem);
+    // Join the warps' sums: [warp][row][token].
+    const int pitch = P::red_pitch(tokens);
+    float *const rb = red + buf * P::red_floats(tokens);
+    if constexpr (P::kBufs == 2) buf ^= 1;
 #pragma unroll
-  for (int r = 0; r < kTiles; ++r)
+    for (int r = 0; r < kTiles; ++r)
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+      for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        red[(warp * kRows + r * 16 + g + (i >> 1) * 8) * kRed + 8 * j + 2 * t + (i & 1)] = acc[r][j][i];
-  __syncthreads();
-  T *const y = static_cast<T *>(a.y);
-  for (int idx = threadIdx.x; idx < 16 * RT * tokens; idx += kThreads) {
-    const int m = idx / (16 * RT), row = idx % (16 * RT);
-    if (n0 + row >= a.N) continue;
-    float v = 0.0f, u = 0.0f;
+        for (int i = 0; i < 4; ++i)
+          if (8 * j + 2 * t + (i & 1) < tokens)
+            rb[(warp * kRows + r * 16 + g + (i >> 1) * 8) * pitch + 8 * j + 2 * t + (i & 1)] = acc[r][j][i];
+    __syncthreads();
+    T *const y = static_cast<T *>(a.y);
+    for (int idx = threadIdx.x; idx < 16 * RT * tokens; idx += kThreads) {
+      const int m = idx / (16 * RT), row = idx % (16 * RT);
+      if (n0 + row < a.N) {
+        float v = 0.0f, u = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      v += red[(w * kRows + row) * kRed + m];
-      if constexpr (kGated) u += red[(w * kRows + 16 * RT + row) * kRed + m];
+        for (int w = 0; w < kWarps; ++w) {
+          v += rb[(w * kRows + row) * pitch + m];
+          if constexpr (kGated) u += rb[(w * kRows + 16 * RT + row) * pitch + m];
+        }
+        if constexpr (kGated) v = act_of(a.act, v) * u;
+        y[(m0 + m) * a.ldy + n0 + row] = from_f32<T>(v);
+      }
     }
-    if constexpr (kGated) v = act_of(a.act, v) * u;
-    y[(m0 + m) * a.ldy + n0 + row] = from_f32<T>(v);
+    if constexpr (P::kBufs == 1) __syncthreads();
   }
+  ptx::cp_async_wait<0>();
 }
 
-template <typename T, bool kGated, int RT, int NT, int CH, int STAGES>
+template <typename T, bool kGated, bool kZeros, int RT, int NT, int CH, int CPG>
 cudaError_t launch_as(MvArgs a, cudaStream_t s) {
-  constexpr int kRows = 16 * RT * (kGated ? 2 : 1), KB = 32 * CH;
-  const int group = 1 << a.group_shift;
-  a.nb = group >= KB ? 1 : KB / group;
-  a.nblk = (a.K + KB - 1) / KB;
-  a.s_words = a.nb == 1 ? 1 : a.nb / 2 + 1;
-  a.z_words = a.nb == 1 ? 1 : a.nb <= 4 ? 2 : 3;
-  a.x_rows = a.M < 8 * NT ? a.M : 8 * NT;
-  a.x_off = kRows * 16 * CH;
-  a.s_off = a.x_off + a.x_rows * (2 * KB + 64);
-  a.z_off = a.s_off + kRows * a.s_words * 4;
-  a.stage_bytes = (a.z_off + (a.zeros[0] ? kRows * a.z_words * 4 : 0) + 127) / 128 * 128;
-  size_t smem = static_cast<size_t>(kWarps) * STAGES * a.stage_bytes;
-  const size_t red = static_cast<size_t>(kWarps) * kRows * (8 * NT + 1) * 4;
-  if (red > smem) smem = red;
-  const auto kern = matvec4_kernel<T, kGated, RT, NT, CH, STAGES>;
+  using P = Mv<T, kGated, kZeros, RT, NT, CH, CPG>;
+  a.nblk = (a.K + P::KB - 1) / P::KB;
+  a.tiles = (a.N + 16 * RT - 1) / (16 * RT);
+  a.s_vec = a.groups % P::kGroups == 0 && (1 << a.group_shift) * P::kGroups == P::KB;
+  constexpr auto kern = matvec4_kernel<T, kGated, kZeros, RT, NT, CH, CPG>;
+  const int most = a.M < 8 * NT ? a.M : 8 * NT;  // tokens of a CTA
+  const size_t smem = P::smem(most);
   const cudaError_t e = conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), smem);
   if (e != cudaSuccess) return e;
-  const dim3 grid((a.N + 16 * RT - 1) / (16 * RT), (a.M + 8 * NT - 1) / (8 * NT));
-  kern<<<grid, kThreads, smem, s>>>(a);
-  return cudaGetLastError();
+  int per_sm = resident_ctas<kern>(kThreads, P::smem(1));
+  while (per_sm > 1 && per_sm * (smem + 1024) > (228u << 10)) --per_sm;  // (an SM's shared memory, 1 KB a CTA reserved)
+  const int cap = sm_count() * per_sm;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.tiles < cap ? a.tiles : cap, (a.M + 8 * NT - 1) / (8 * NT));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t le = cudaLaunchKernelEx(&cfg, kern, a);
+  return le != cudaSuccess ? le : cudaGetLastError();
 }
 
-template <typename T, bool kGated>
+template <typename T, bool kGated, bool kZeros, int RT, int NT, int CH>
+cudaError_t launch_grouped(const MvArgs &a, cudaStream_t s) {
+  if (a.group_shift == 5) return launch_as<T, kGated, kZeros, RT, NT, CH, 1>(a, s);
+  if (a.group_shift == 6) return launch_as<T, kGated, kZeros, RT, NT, CH, 2>(a, s);
+  return launch_as<T, kGated, kZeros, RT, NT, CH, 4>(a, s);
+}
+
+template <typename T, bool kGated, bool kZeros>
 cudaError_t launch_sized(const MvArgs &a, cudaStream_t s) {
   constexpr int kRT = kGated ? 1 : 2;
-  if (a.M <= 2) return launch_as<T, kGated, 1, 1, 8, 3>(a, s);
-  if (a.M <= 8) return launch_as<T, kGated, 1, 1, 4, 3>(a, s);
-  if (a.M <= 16) return launch_as<T, kGated, kRT, 2, 4, 3>(a, s);
-  return launch_as<T, kGated, kRT, 4, 2, 3>(a, s);
+  if (a.M > 16) return launch_grouped<T, kGated, kZeros, kRT, 4, 4>(a, s);
+  if (a.M > 8) return launch_grouped<T, kGated, kZeros, kRT, 2, 4>(a, s);
+  if (a.K < 2048) return launch_grouped<T, kGated, kZeros, 1, 1, 4>(a, s);
+  if (!kGated && a.N >= 9728) return launch_grouped<T, kGated, kZeros, kRT, 1, 8>(a, s);
+  return launch_grouped<T, kGated, kZeros, 1, 1, 8>(a, s);
 }
 
 template <typename T>
 cudaError_t launch_type(const MvArgs &a, cudaStream_t s) {
-  return a.act >= 0 ? launch_sized<T, true>(a, s) : launch_sized<T, false>(a, s);
+  if (a.zeros[0]) return a.act >= 0 ? launch_sized<T, true, true>(a, s) : launch_sized<T, false, true>(a, s);
+  return a.act >= 0 ? launch_sized<T, true, false>(a, s) : launch_sized<T, false, false>(a, s);
 }
 
 }  // namespace
