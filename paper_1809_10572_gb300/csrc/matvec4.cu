@@ -38,6 +38,7 @@ namespace {
 
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
+constexpr uint64_t kWaitLimitNs = 1000000000ull;  // 1 s
 
 struct MvArgs {
   const uint8_t *lanes[2];
@@ -53,7 +54,8 @@ struct MvArgs {
   int group_shift;    // log2(group)
   int nblk;           // blocks of KB inputs
   int tiles;          // of 16 * RT rows
-  int w_vec, x_vec;   // rows are 16-byte aligned
+  int tma, x_vec;     // rows of lanes are whole 16-byte units; rows of x are 16-byte aligned
+  int *status;        // of the device, for waits that give up
   int s_vec;          // a row's scales of a block lie on a multiple of their size
   int is_signed;
   int act;            // of the gated pair; -1: one matrix
@@ -157,61 +159,68 @@ struct Mv {
   // words that hold them at any alignment, in a power of two
   static constexpr int kSPitch = kGroups == 1 ? 4 : 4 * kGroups;
   static constexpr int kZPitch = kGroups == 1 ? 4 : kGroups <= 4 ? 8 : 16;
-  static constexpr int kSOff = kRows * kPitch;
-  static constexpr int kZOff = kSOff + kRows * kSPitch;
-  static constexpr int kStageBytes = (kZOff + (kZeros ? kRows * kZPitch : 0) + 127) / 128 * 128;
+  static constexpr int kWBytes = kRows * kPitch;  // a stage's weights (whole 1024- or 512-byte swizzle patterns)
+  static constexpr int kZOff = kRows * kSPitch;
+  static constexpr int kSzBytes = kZOff + (kZeros ? kRows * kZPitch : 0);  // its scales and zero points
+  // shared memory: [warp][stage] weights, [warp][stage] scales and zero points, [warp][stage] barriers, the sums
+  static constexpr int kSzAt = kWarps * kStages * kWBytes;
+  static constexpr int kBarAt = kSzAt + kWarps * kStages * kSzBytes;
+  static constexpr int kRedAt = kBarAt + kWarps * kStages * 8;
   static constexpr int kBufs = NT == 1 ? 2 : 1;
   // the warps' sums: rows of an odd number of tokens, so that neighbouring rows lie in other banks
   static __host__ __device__ int red_pitch(int tokens) { return tokens | 1; }
   static __host__ __device__ int red_floats(int tokens) { return kWarps * kRows * red_pitch(tokens); }  // of one buffer
   static size_t smem(int tokens) {
-    return static_cast<size_t>(kWarps) * kStages * kStageBytes + static_cast<size_t>(kBufs) * red_floats(tokens) * 4;
+    return static_cast<size_t>(kRedAt) + static_cast<size_t>(kBufs) * red_floats(tokens) * 4;
   }
 };
 
 template <typename T, bool kGated, bool kZeros, int RT, int NT, int CH, int CPG>
-__global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_constant__ CUtensorMap map0,
+                                                                const __grid_constant__ CUtensorMap map1,
+                                                                const MvArgs a) {
   using P = Mv<T, kGated, kZeros, RT, NT, CH, CPG>;
   constexpr int kTiles = P::kTiles, kRows = P::kRows, KB = P::KB, kPitch = P::kPitch, kStages = P::kStages;
-  constexpr int kSwz = CH >= 8 ? 0 : CH == 4 ? 1 : 2;  // rows that share a 128-byte line: 2^kSwz
-  static_assert(CH == 2 || CH == 4 || CH == 8, "a row of a stage is 32, 64 or 128 bytes");
-  extern __shared__ __align__(128) uint8_t smem[];
-  float *const red = reinterpret_cast<float *>(smem + static_cast<size_t>(kWarps) * kStages * P::kStageBytes);
+  constexpr int kSwz = CH >= 8 ? 0 : 1;  // rows that share a 128-byte line: 2^kSwz
+  static_assert(CH == 4 || CH == 8, "a row of a stage is 64 or 128 bytes");
+  extern __shared__ __align__(1024) uint8_t smem[];
+  float *const red = reinterpret_cast<float *>(smem + P::kRedAt);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t bar0 = ptx::smem_addr(smem + P::kBarAt) + warp * kStages * 8;  // this warp's stages' weights
+  if (a.tma && lane == 0) {
+    for (int i = 0; i < kStages; ++i) ptx::mbar_init(bar0 + 8 * i, 1);
+    ptx::fence_barrier_init();
+  }
+  __syncwarp();
 
   // the tokens may come from the kernel before; the next one may be set up
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
   const int m0 = blockIdx.y * (8 * NT);
   const int tokens = min(a.M - m0, 8 * NT);
-  uint8_t *const mine = smem + static_cast<size_t>(warp) * kStages * P::kStageBytes;
-  const uint32_t mine_s = ptx::smem_addr(mine);
+  const uint32_t w_s = ptx::smem_addr(smem) + warp * kStages * P::kWBytes;
+  const uint8_t *const sz = smem + P::kSzAt + warp * kStages * P::kSzBytes;
+  const uint32_t sz_s = ptx::smem_addr(sz);
   const T *const x = static_cast<const T *>(a.x) + m0 * a.ldx;
 
-  // One block's weights, scales and zero points into a stage. Rows past N
-  // repeat row N - 1 (their sums are not stored); bytes past a row's end are
-  // zero. Where a row's scales of a block do not lie on their own size
-  // (s_vec = 0), the 4-byte words around them are copied, a word past the end
-  // of the array is clipped, and the reader finds its place in the first word
-  // from the same index.
-  auto load = [&](int n0, int blk, uint32_t st) {
+  // One block's weights, scales and zero points into a stage: the weights by
+  // one TMA tile where rows are whole 16-byte units (rows past N and bytes past
+  // a row's end are zero), else by 4-byte copies (rows past N repeat row N - 1;
+  // their sums are not stored). Where a row's scales of a block do not lie on
+  // their own size (s_vec = 0), the 4-byte words around them are copied, a word
+  // past the end of the array is clipped, and the reader finds its place in the
+  // first word from the same index.
+  auto load = [&](int n0, int blk, int stage) {
     const int last = a.N - 1 - n0;  // of the tile's rows
-    const uint32_t row_bytes = static_cast<uint32_t>(a.row_bytes), groups = static_cast<uint32_t>(a.groups);
-    if (a.w_vec) {
-      constexpr int kStep = 32 / CH;  // rows a copy of the warp covers
-      const int lrow = lane / CH, ch = lane % CH;
-      const int64_t at = static_cast<int64_t>(blk) * (KB / 2) + ch * 16;
-      const bool in = at < a.row_bytes;  // whole 16-byte units: row_bytes is a multiple of 16
-      const uint32_t size = in ? 16u : 0u;
-      const int64_t from = static_cast<int64_t>(n0) * a.row_bytes + (in ? at : 0);
-#pragma unroll
-      for (int i = 0; i < kRows / kStep; ++i) {
-        const int row = i * kStep + lrow, mat = kGated && i * kStep >= 16 * RT;
-        const uint32_t r = min(row - mat * 16 * RT, last);
-        ptx::cp_async_16(st + row * kPitch + ((ch ^ ((row >> kSwz) & (CH - 1))) * 16),
-                         a.lanes[mat] + from + static_cast<uint64_t>(r) * row_bytes, size);
+    const uint32_t sw = w_s + stage * P::kWBytes, ss = sz_s + stage * P::kSzBytes;
+    if (a.tma) {
+      if (lane == 0) {
+        const uint32_t bar = bar0 + 8 * stage;
+        ptx::mbar_arrive_expect_tx(bar, P::kWBytes);
+        ptx::tma_load_2d(sw, &map0, blk * kPitch, n0, bar);
+        if constexpr (kGated) ptx::tma_load_2d(sw + P::kWBytes / 2, &map1, blk * kPitch, n0, bar);
       }
     } else {
       constexpr int kPer = 4 * CH;  // words of a row
@@ -220,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
         const int mat = kGated && row >= 16 * RT;
         const int64_t at = static_cast<int64_t>(blk) * (KB / 2) + w * 4;
         const bool in = at < a.row_bytes;
-        ptx::cp_async_4(st + row * kPitch + ((ch ^ ((row >> kSwz) & (CH - 1))) * 16) + (w & 3) * 4,
+        ptx::cp_async_4(sw + row * kPitch + ((ch ^ ((row >> kSwz) & (CH - 1))) * 16) + (w & 3) * 4,
                         a.lanes[mat] + (n0 + min(row - mat * 16 * RT, last)) * a.row_bytes + (in ? at : 0),
                         in ? 4u : 0u);
       }
@@ -232,8 +241,8 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
       for (int i = 0; i < (kRows + 31) / 32; ++i) {
         const int row = i * 32 + lane, mat = kGated && row >= 16 * RT;
         if (kRows % 32 == 0 || row < kRows) {
-          const int64_t n = tile_g + static_cast<uint64_t>(static_cast<uint32_t>(min(row - mat * 16 * RT, last))) * groups;
-          const uint32_t dst = st + P::kSOff + row * P::kSPitch;
+          const int64_t n = tile_g + static_cast<uint64_t>(static_cast<uint32_t>(min(row - mat * 16 * RT, last))) * static_cast<uint32_t>(a.groups);
+          const uint32_t dst = ss + row * P::kSPitch;
           if constexpr (P::kGroups == 8) ptx::cp_async_16(dst, a.scales[mat] + n * 2, 16);
           if constexpr (P::kGroups == 4) ptx::cp_async_8(dst, a.scales[mat] + n * 2, 8);
           if constexpr (P::kGroups == 2) ptx::cp_async_4(dst, a.scales[mat] + n * 2, 4);
@@ -247,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
         if (kRows * kWords % 32 == 0 || row < kRows) {
           const int64_t n = tile_g + min(row - mat * 16 * RT, last) * a.groups;
           const int64_t at = (n * 2 & ~int64_t(3)) + w * 4, left = a.n_scales * 2 - at;
-          ptx::cp_async_4(st + P::kSOff + row * P::kSPitch + w * 4, a.scales[mat] + (left > 0 ? at : 0),
+          ptx::cp_async_4(ss + row * P::kSPitch + w * 4, a.scales[mat] + (left > 0 ? at : 0),
                           left >= 4 ? 4u : left > 0 ? static_cast<uint32_t>(left) : 0u);
         }
       }
@@ -260,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
         if (kRows * kWords % 32 == 0 || row < kRows) {
           const int64_t n = tile_g + min(row - mat * 16 * RT, last) * a.groups;
           const int64_t at = (n & ~int64_t(3)) + w * 4, left = a.n_scales - at;
-          ptx::cp_async_4(st + P::kZOff + row * P::kZPitch + w * 4, a.zeros[mat] + (left > 0 ? at : 0),
+          ptx::cp_async_4(ss + P::kZOff + row * P::kZPitch + w * 4, a.zeros[mat] + (left > 0 ? at : 0),
                           left >= 4 ? 4u : left > 0 ? static_cast<uint32_t>(left) : 0u);
         }
       }
@@ -272,10 +281,13 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
   plain.set(flip & 15u);
 
   // the ring's next block to load, which runs ahead of the one in hand, over the CTA's tiles
-  int l_tile = blockIdx.x, l_blk = warp, fill = 0, slot = 0;
+  int l_tile = blockIdx.x, l_blk = warp, fill = 0, slot = 0, loaded = 0, used = 0;
+  uint32_t par = 0;  // of the ring's round in hand
+  bool ok = true;    // no wait has given up
   auto load_next = [&]() {
-    if (l_tile < a.tiles && l_blk < a.nblk) {
-      load(l_tile * (16 * RT), l_blk, mine_s + fill * P::kStageBytes);
+    if (l_tile < a.tiles && l_blk < a.nblk && ok) {
+      load(l_tile * (16 * RT), l_blk, fill);
+      ++loaded;
       l_blk += kWarps;
       if (l_blk >= a.nblk) {
         l_blk = warp;
@@ -285,9 +297,12 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
     ptx::cp_async_commit();
     fill = fill + 1 == kStages ? 0 : fill + 1;
   };
-#pragma unroll
+#pragma unroll 1
   for (int s = 0; s < kStages - 1; ++s) load_next();
 
+  uint4 xq[NT == 1 ? CH : 1];  // the block's tokens; lanes without one keep zeros
+#pragma unroll
+  for (int c = 0; c < (NT == 1 ? CH : 1); ++c) xq[c] = make_uint4(0, 0, 0, 0);
   int buf = 0;
   for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
     const int n0 = tile * (16 * RT);
@@ -300,19 +315,17 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
         for (int i = 0; i < 4; ++i) acc[r][j][i] = 0.0f;
     // index of the rows' first scales, low bits (the place in a staged word)
     int first[kTiles][2];
+    if (kZeros || P::kGroups == 1 || !a.s_vec)
 #pragma unroll
-    for (int r = 0; r < kTiles; ++r)
+      for (int r = 0; r < kTiles; ++r)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        first[r][h] = static_cast<int>(min(n0 + (kGated && r >= RT ? r - RT : r) * 16 + g + 8 * h, a.N - 1) * a.groups & 3);
+        for (int h = 0; h < 2; ++h)
+          first[r][h] = static_cast<int>(min(n0 + (kGated && r >= RT ? r - RT : r) * 16 + g + 8 * h, a.N - 1) * a.groups & 3);
 
     for (int blk = warp; blk < a.nblk; blk += kWarps) {
       const int64_t k0 = static_cast<int64_t>(blk) * KB;
       // tokens first: their way through L1 overlaps the wait for the stage
-      uint4 xq[NT == 1 ? CH : 1];
       if constexpr (NT == 1) {
-#pragma unroll
-        for (int c = 0; c < CH; ++c) xq[c] = make_uint4(0, 0, 0, 0);
         if (g < tokens) {
           const T *const xr = x + g * a.ldx + k0 + t * 8;
           if (a.x_vec && k0 + KB <= a.K) {
@@ -327,9 +340,16 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
       ptx::cp_async_wait<kStages - 2>();
       __syncwarp();  // every lane's copies are in, and the slot filled next has been read by every lane
       load_next();
-      const uint8_t *const st = mine + slot * P::kStageBytes;
-      const uint32_t sw = mine_s + slot * P::kStageBytes;
-      slot = slot + 1 == kStages ? 0 : slot + 1;
+      const uint8_t *const st = sz + slot * P::kSzBytes;
+      const uint32_t sw = w_s + slot * P::kWBytes;
+      if (a.tma && ok) {
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar0 + 8 * slot, par, a.status, SAMD_ETIMEOUT, kWaitLimitNs));
+        used += ok;
+      }
+      if (++slot == kStages) {
+        slot = 0;
+        par ^= 1;
+      }
       const int g0 = static_cast<int>((k0 >> a.group_shift) & 3);
       const bool one_scale = P::kGroups > 1 && CPG == 4 && a.group_shift > 7;  // groups that hold whole blocks
       // the rows' scales of the block, two in a word
@@ -339,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
       for (int r = 0; r < kTiles; ++r)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const uint8_t *const sp = st + P::kSOff + (r * 16 + g + 8 * h) * P::kSPitch;
+          const uint8_t *const sp = st + (r * 16 + g + 8 * h) * P::kSPitch;
           if (P::kGroups > 1 && a.s_vec) {
             if constexpr (P::kGroups == 8) {
               const uint4 v = *reinterpret_cast<const uint4 *>(sp);
@@ -475,6 +495,11 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const MvArgs a) {
     if constexpr (P::kBufs == 1) __syncthreads();
   }
   ptx::cp_async_wait<0>();
+  if (!ok) {  // the CTA does not exit with a copy in flight
+    int quiet = 0;
+    for (int i = used; i < loaded; ++i)
+      ptx::mbar_wait_bounded(bar0 + 8 * (i % kStages), (i / kStages) & 1, &quiet, kWaitLimitNs / 10);
+  }
 }
 
 template <typename T, bool kGated, bool kZeros, int RT, int NT, int CH, int CPG>
@@ -484,6 +509,21 @@ cudaError_t launch_as(MvArgs a, cudaStream_t s) {
   a.tiles = (a.N + 16 * RT - 1) / (16 * RT);
   a.s_vec = a.groups % P::kGroups == 0 && (1 << a.group_shift) * P::kGroups == P::KB;
   constexpr auto kern = matvec4_kernel<T, kGated, kZeros, RT, NT, CH, CPG>;
+  CUtensorMap map[2] = {};
+  if (a.tma) {
+    // bytes of a row by rows, in boxes of one block of one tile, swizzled as the kernel's ldmatrix reads them
+    const EncodeTiledFn enc = tensor_map_encoder();
+    if (!enc) return cudaErrorNotSupported;
+    for (int i = 0; i < P::kMats; ++i) {
+      const cuuint64_t dim[2] = {static_cast<cuuint64_t>(a.row_bytes), static_cast<cuuint64_t>(a.N)};
+      const cuuint64_t stride[1] = {static_cast<cuuint64_t>(a.row_bytes)};
+      const cuuint32_t box[2] = {P::kPitch, 16 * RT}, es[2] = {1, 1};
+      if (enc(&map[i], CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(a.lanes[i]), dim, stride, box, es,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CH == 8 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return cudaErrorInvalidValue;
+    }
+  }
   const int most = a.M < 8 * NT ? a.M : 8 * NT;  // tokens of a CTA
   const size_t smem = P::smem(most);
   const cudaError_t e = conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), smem);
@@ -501,7 +541,7 @@ cudaError_t launch_as(MvArgs a, cudaStream_t s) {
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t le = cudaLaunchKernelEx(&cfg, kern, a);
+  const cudaError_t le = cudaLaunchKernelEx(&cfg, kern, map[0], map[1], a);
   return le != cudaSuccess ? le : cudaGetLastError();
 }
 
@@ -518,7 +558,9 @@ cudaError_t launch_sized(const MvArgs &a, cudaStream_t s) {
   if (a.M > 16) return launch_grouped<T, kGated, kZeros, kRT, 4, 4>(a, s);
   if (a.M > 8) return launch_grouped<T, kGated, kZeros, kRT, 2, 4>(a, s);
   if (a.K < 2048) return launch_grouped<T, kGated, kZeros, 1, 1, 4>(a, s);
-  if (!kGated && a.N >= 9728) return launch_grouped<T, kGated, kZeros, kRT, 1, 8>(a, s);
+  if (!kGated && a.N >= 9728)
+    return a.M <= 2 ? launch_grouped<T, kGated, kZeros, kRT, 1, 8>(a, s)
+                    : launch_grouped<T, kGated, kZeros, kRT, 1, 4>(a, s);
   return launch_grouped<T, kGated, kZeros, 1, 1, 8>(a, s);
 }
 
@@ -549,7 +591,11 @@ cudaError_t launch_matvec4(const samd_matvec_desc &d, int act, samd_fmt fw, cons
   a.n_scales = a.groups * d.N;
   a.N = d.N;
   a.K = d.K;
-  a.w_vec = a.row_bytes % 16 == 0;
+  a.tma = a.row_bytes % 16 == 0;
+  if (a.tma) {
+    const cudaError_t e = device_status_ptr(&a.status);
+    if (e != cudaSuccess) return e;
+  }
   a.x_vec = d.M == 1 || d.ldx % 8 == 0;
   a.is_signed = fw.is_signed;
   a.act = act;
