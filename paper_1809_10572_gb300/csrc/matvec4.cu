@@ -33,6 +33,8 @@
 #include "ffn_internal.cuh"
 #include "tc_ptx.cuh"
 
+#include <type_traits>
+
 namespace samd {
 namespace {
 
@@ -68,24 +70,22 @@ __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
                : "memory");
 }
 
-template <typename T>
-__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
-template <>
-__device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
-                                                        uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-      "{%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-template <>
-__device__ __forceinline__ void mma16816<__half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-      "{%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// d = a b, or d += a b.
+template <typename T, bool kAdd>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  const float c0 = kAdd ? d[0] : 0.0f, c1 = kAdd ? d[1] : 0.0f, c2 = kAdd ? d[2] : 0.0f, c3 = kAdd ? d[3] : 0.0f;
+  if constexpr (std::is_same<T, __half>::value)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%10, %11, %12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%10, %11, %12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 
 // What is subtracted from the widened lanes of a group with zero point z.
@@ -212,7 +212,12 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
   // their own size (s_vec = 0), the 4-byte words around them are copied, a word
   // past the end of the array is clipped, and the reader finds its place in the
   // first word from the same index.
-  auto load = [&](int n0, int blk, int stage) {
+  auto scale_of = [&](int n0, int row, int blk) -> const uint8_t * {
+    const int mat = kGated && row >= 16 * RT;
+    const int64_t n = min(n0 + row - mat * 16 * RT, a.N - 1);
+    return a.scales[mat] + (n * a.groups + ((static_cast<int64_t>(blk) * KB) >> a.group_shift)) * 2;
+  };
+  auto load = [&](int n0, int blk, int stage, const uint8_t *scale) {
     const int last = a.N - 1 - n0;  // of the tile's rows
     const uint32_t sw = w_s + stage * P::kWBytes, ss = sz_s + stage * P::kSzBytes;
     if (a.tma) {
@@ -234,21 +239,19 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
                         in ? 4u : 0u);
       }
     }
-    const int64_t g0 = (static_cast<int64_t>(blk) * KB) >> a.group_shift;
-    const int64_t tile_g = n0 * a.groups + g0;
     if (P::kGroups > 1 && a.s_vec) {
+      // one copy for a row: lane r brings row r of the tile (and row r + 32)
 #pragma unroll
-      for (int i = 0; i < (kRows + 31) / 32; ++i) {
-        const int row = i * 32 + lane, mat = kGated && row >= 16 * RT;
-        if (kRows % 32 == 0 || row < kRows) {
-          const int64_t n = tile_g + static_cast<uint64_t>(static_cast<uint32_t>(min(row - mat * 16 * RT, last))) * static_cast<uint32_t>(a.groups);
-          const uint32_t dst = ss + row * P::kSPitch;
-          if constexpr (P::kGroups == 8) ptx::cp_async_16(dst, a.scales[mat] + n * 2, 16);
-          if constexpr (P::kGroups == 4) ptx::cp_async_8(dst, a.scales[mat] + n * 2, 8);
-          if constexpr (P::kGroups == 2) ptx::cp_async_4(dst, a.scales[mat] + n * 2, 4);
+      for (int i = 0; i < (kRows + 31) / 32; ++i)
+        if (kRows % 32 == 0 || lane < kRows) {
+          const uint32_t dst = ss + (i * 32 + lane) * P::kSPitch;
+          const uint8_t *const src = i == 0 ? scale : scale_of(n0, i * 32 + lane, blk);
+          if constexpr (P::kGroups == 8) ptx::cp_async_16(dst, src, 16);
+          if constexpr (P::kGroups == 4) ptx::cp_async_8(dst, src, 8);
+          if constexpr (P::kGroups == 2) ptx::cp_async_4(dst, src, 4);
         }
-      }
     } else {
+      const int64_t tile_g = n0 * a.groups + ((static_cast<int64_t>(blk) * KB) >> a.group_shift);
       constexpr int kWords = P::kGroups == 1 ? 1 : P::kGroups / 2 + 1;
 #pragma unroll
       for (int i = 0; i < (kRows * kWords + 31) / 32; ++i) {
@@ -262,6 +265,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
       }
     }
     if constexpr (kZeros) {
+      const int64_t tile_g = n0 * a.groups + ((static_cast<int64_t>(blk) * KB) >> a.group_shift);
       constexpr int kWords = P::kGroups == 1 ? 1 : P::kGroups <= 4 ? 2 : 3;
 #pragma unroll
       for (int i = 0; i < (kRows * kWords + 31) / 32; ++i) {
@@ -276,6 +280,12 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
     }
   };
 
+  // The lane's place in a stage for ldmatrix: row lane % 16, chunk lane / 16,
+  // with the row's swizzle. A row of tiles further is 16 rows, whole swizzle
+  // patterns, and chunk c is an exclusive or of the address (the weights start
+  // on a multiple of the pattern).
+  const uint32_t lm = (lane & 15) * kPitch + ((lane >> 4) ^ (((lane & 15) >> kSwz) & (CH - 1))) * 16;
+
   const uint32_t flip = a.is_signed ? 0x00080008u : 0u;
   Offset<T> plain;  // without zero points: offset binary's 8 for signed lanes, else 0
   plain.set(flip & 15u);
@@ -284,14 +294,18 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
   int l_tile = blockIdx.x, l_blk = warp, fill = 0, slot = 0, loaded = 0, used = 0;
   uint32_t par = 0;  // of the ring's round in hand
   bool ok = true;    // no wait has given up
+  if (warp >= a.nblk) l_tile = a.tiles;  // no block is this warp's
+  const uint8_t *l_scale = scale_of(l_tile * (16 * RT), lane, warp);  // the lane's row's, of the next block
   auto load_next = [&]() {
-    if (l_tile < a.tiles && l_blk < a.nblk && ok) {
-      load(l_tile * (16 * RT), l_blk, fill);
+    if (l_tile < a.tiles) {
+      load(l_tile * (16 * RT), l_blk, fill, l_scale);
       ++loaded;
       l_blk += kWarps;
+      l_scale += kWarps * P::kGroups * 2;
       if (l_blk >= a.nblk) {
         l_blk = warp;
         l_tile += gridDim.x;
+        l_scale = scale_of(l_tile * (16 * RT), lane, warp);
       }
     }
     ptx::cp_async_commit();
@@ -303,6 +317,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
   uint4 xq[NT == 1 ? CH : 1];  // the block's tokens; lanes without one keep zeros
 #pragma unroll
   for (int c = 0; c < (NT == 1 ? CH : 1); ++c) xq[c] = make_uint4(0, 0, 0, 0);
+  const T *const x_lane = x + g * a.ldx + t * 8;
   int buf = 0;
   for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
     const int n0 = tile * (16 * RT);
@@ -327,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
       // tokens first: their way through L1 overlaps the wait for the stage
       if constexpr (NT == 1) {
         if (g < tokens) {
-          const T *const xr = x + g * a.ldx + k0 + t * 8;
+          const T *const xr = x_lane + k0;
           if (a.x_vec && k0 + KB <= a.K) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) xq[c] = __ldg(reinterpret_cast<const uint4 *>(xr + c * 32));
@@ -345,6 +360,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
       if (a.tma && ok) {
         ok = __all_sync(0xffffffffu, ptx::mbar_wait(bar0 + 8 * slot, par, a.status, SAMD_ETIMEOUT, kWaitLimitNs));
         used += ok;
+        if (!ok) l_tile = a.tiles;  // nothing more is loaded
       }
       if (++slot == kStages) {
         slot = 0;
@@ -410,10 +426,6 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
               else
                 o[r][h] = plain;
             }
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) d[r][j][i] = 0.0f;
           }
 #pragma unroll
           for (int cc = 0; cc < CPG; ++cc) {
@@ -422,8 +434,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
               if ((c & 1) == 0) {  // two chunks at a time
 #pragma unroll
                 for (int r = 0; r < kTiles; ++r) {
-                  const int row = r * 16 + (lane & 15), ch = c + (lane >> 4);
-                  ldmatrix_x4(sw + row * kPitch + ((ch ^ ((row >> kSwz) & (CH - 1))) * 16), words[r]);
+                  ldmatrix_x4(((sw + lm) ^ (c * 16)) + r * (16 * kPitch), words[r]);
                 }
               }
               uint32_t b[NT][4];
@@ -449,8 +460,11 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
                 const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                  mma16816<T>(d[r][j], a0, b[j][0], b[j][1]);
-                  mma16816<T>(d[r][j], a1, b[j][2], b[j][3]);
+                  if (cc == 0)
+                    mma16816<T, false>(d[r][j], a0, b[j][0], b[j][1]);
+                  else
+                    mma16816<T, true>(d[r][j], a0, b[j][0], b[j][1]);
+                  mma16816<T, true>(d[r][j], a1, b[j][2], b[j][3]);
                 }
               }
             }
