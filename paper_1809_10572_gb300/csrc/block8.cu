@@ -2,39 +2,46 @@
 // of two, ffn_internal.cuh) and back.
 //
 // Both are one pass over HBM: 2 or 4 bytes an element on the wide side and
-// 33/32 on the other. Four neighbouring lanes hold a block, eight elements
-// each (one 16-byte load of a 16-bit type), and find its largest magnitude
-// with two shuffles; magnitudes are compared as bit patterns, which puts
-// infinities and NaNs above every number.
+// 33/32 on the other. Two neighbouring lanes hold a block, sixteen elements
+// each (two 16-byte loads of a 16-bit type, one 16-byte store of codes), and
+// find its largest magnitude with a shuffle.
 #include "ffn_internal.cuh"
+#include "tc_ptx.cuh"
 
 namespace samd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPer = 8;  // elements a thread handles at a time
+constexpr int kPer = 16;             // elements a thread handles at a time
 constexpr int kRowStep = 32 * kPer;  // elements of a row a warp handles at a time
 
 struct Block8Args {
   int64_t rows, inner, ld, segs;  // segs: warps' steps in a row
   int64_t wpr, bpr;               // words and blocks of a row
-  int x_vec, l_vec;               // rows of x are 16-byte, rows of lanes 8-byte aligned
+  IndexDiv by_segs;
+  int x_vec, l_vec;               // rows of x, and of lanes, are 16-byte aligned
 };
 
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, int n, bool vec, float *v) {
+__device__ __forceinline__ void load16(const T *p, int n, bool vec, float *v) {
   if (vec && n == kPer) {
     if constexpr (sizeof(T) == 4) {
-      const float4 a = __ldcs(reinterpret_cast<const float4 *>(p)), b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-      const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p));
-      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float2 f = unpack2<T>(w[i]);
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
+        const float4 f = __ldcs(reinterpret_cast<const float4 *>(p) + i);
+        v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
+      }
+    } else {
+      const uint4 q[2] = {__ldcs(reinterpret_cast<const uint4 *>(p)), __ldcs(reinterpret_cast<const uint4 *>(p) + 1)};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 f = unpack2<T>(w[k]);
+          v[8 * i + 2 * k] = f.x;
+          v[8 * i + 2 * k + 1] = f.y;
+        }
       }
     }
   } else {
@@ -44,14 +51,18 @@ __device__ __forceinline__ void load8(const T *p, int n, bool vec, float *v) {
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T *p, int n, bool vec, const float *v) {
+__device__ __forceinline__ void store16(T *p, int n, bool vec, const float *v) {
   if (vec && n == kPer) {
     if constexpr (sizeof(T) == 4) {
-      __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
-      __stcs(reinterpret_cast<float4 *>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        __stcs(reinterpret_cast<float4 *>(p) + i, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
     } else {
-      __stcs(reinterpret_cast<uint4 *>(p), make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]),
-                                                      pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])));
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        __stcs(reinterpret_cast<uint4 *>(p) + i,
+               make_uint4(pack2<T>(v[8 * i], v[8 * i + 1]), pack2<T>(v[8 * i + 2], v[8 * i + 3]),
+                          pack2<T>(v[8 * i + 4], v[8 * i + 5]), pack2<T>(v[8 * i + 6], v[8 * i + 7])));
     }
   } else {
 #pragma unroll
@@ -63,34 +74,35 @@ __device__ __forceinline__ void store8(T *p, int n, bool vec, const float *v) {
 template <typename T>
 __global__ void __launch_bounds__(kThreads) block8_quantize_kernel(const T *__restrict__ x, uint32_t *__restrict__ lanes,
                                                                    uint8_t *__restrict__ exps, const Block8Args a) {
+  ptx::grid_dependency_wait();
+  ptx::grid_dependents_launch();
   const int lane = threadIdx.x & 31;
   const int64_t nwarps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
   const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
   for (int64_t step = first; step < a.rows * a.segs; step += nwarps) {
-    const int64_t row = step / a.segs;
+    const int64_t row = idiv(step, a.by_segs);
     const int64_t col = (step - row * a.segs) * kRowStep + lane * kPer;
     const int64_t left = a.inner - col;
     const int n = left < 0 ? 0 : left < kPer ? static_cast<int>(left) : kPer;
     float v[kPer];
-    load8<T>(x + row * a.ld + (n ? col : 0), n, a.x_vec, v);
-    uint32_t top = 0;
+    load16<T>(x + row * a.ld + (n ? col : 0), n, a.x_vec, v);
+    float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    for (int i = 0; i < kPer; ++i) top = max_abs(top, v[i]);
+    top = max_abs(top, __shfl_xor_sync(0xffffffffu, top, 1));
     const uint32_t e = block8_exp(top);
-    const float inv = block8_inv(e);
     if (n) {
-      const uint32_t lo = block8_word(v[0], v[1], v[2], v[3], inv);
-      const uint32_t hi = block8_word(v[4], v[5], v[6], v[7], inv);
-      uint32_t *out = lanes + row * a.wpr + col / 4;
-      if (a.l_vec && n > 4) {
-        __stcs(reinterpret_cast<uint2 *>(out), make_uint2(lo, hi));
+      uint32_t w[4];
+      block8_words_of<false, kPer>(v, top, e, block8_inv(e), w);
+      uint32_t *const out = lanes + row * a.wpr + col / 4;
+      if (a.l_vec && n > 12) {
+        __stcs(reinterpret_cast<uint4 *>(out), make_uint4(w[0], w[1], w[2], w[3]));
       } else {
-        out[0] = lo;
-        if (n > 4) out[1] = hi;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (4 * i < n) out[i] = w[i];
       }
-      if ((lane & 3) == 0) exps[row * a.bpr + col / kBlock8] = static_cast<uint8_t>(e);
+      if ((lane & 1) == 0) exps[row * a.bpr + col / kBlock8] = static_cast<uint8_t>(e);
     }
   }
 }
@@ -99,26 +111,31 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads)
     block8_dequantize_kernel(const uint32_t *__restrict__ lanes, const uint8_t *__restrict__ exps, T *__restrict__ y,
                              const Block8Args a) {
+  ptx::grid_dependency_wait();
+  ptx::grid_dependents_launch();
   const int lane = threadIdx.x & 31;
   const int64_t nwarps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
   const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
   for (int64_t step = first; step < a.rows * a.segs; step += nwarps) {
-    const int64_t row = step / a.segs;
+    const int64_t row = idiv(step, a.by_segs);
     const int64_t col = (step - row * a.segs) * kRowStep + lane * kPer;
     const int64_t left = a.inner - col;
     const int n = left < 0 ? 0 : left < kPer ? static_cast<int>(left) : kPer;
     if (n) {
-      const uint32_t *in = lanes + row * a.wpr + col / 4;
-      uint2 w;
-      if (a.l_vec && n > 4)
-        w = __ldcs(reinterpret_cast<const uint2 *>(in));
-      else
-        w = make_uint2(in[0], n > 4 ? in[1] : 0u);
+      const uint32_t *const in = lanes + row * a.wpr + col / 4;
+      uint32_t w[4];
+      if (a.l_vec && n > 12) {
+        const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(in));
+        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = 4 * i < n ? in[i] : 0u;
+      }
       const float scale = block8_scale(exps[row * a.bpr + col / kBlock8]);
       float v[kPer];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) v[i] = block8_value(i < 4 ? w.x : w.y, i & 3, scale);
-      store8<T>(y + row * a.ld + col, n, a.x_vec, v);
+      for (int i = 0; i < 4; ++i) block8_values(w[i], scale, v + 4 * i);
+      store16<T>(y + row * a.ld + col, n, a.x_vec, v);
     }
   }
 }
@@ -129,10 +146,11 @@ Block8Args make_args(size_t esize, const void *x, int64_t ld, int64_t rows, int6
   a.inner = inner;
   a.ld = ld;
   a.segs = (inner + kRowStep - 1) / kRowStep;
+  a.by_segs = make_index_div(rows * a.segs, a.segs);
   a.wpr = block8_words(inner);
   a.bpr = block8_blocks(inner);
   a.x_vec = aligned16(x) && (rows == 1 || ld * static_cast<int64_t>(esize) % 16 == 0);
-  a.l_vec = aligned16(b.lanes) && (rows == 1 || a.wpr % 2 == 0);
+  a.l_vec = aligned16(b.lanes) && (rows == 1 || a.wpr % 4 == 0);
   return a;
 }
 
@@ -140,18 +158,16 @@ template <typename T>
 cudaError_t quantize(const void *x, int64_t ldx, int64_t rows, int64_t inner, samd_block8 out, cudaStream_t s) {
   const Block8Args a = make_args(sizeof(T), x, ldx, rows, inner, out);
   const int grid = resident_grid<block8_quantize_kernel<T>>(a.rows * a.segs * 32, kThreads);
-  block8_quantize_kernel<T><<<grid, kThreads, 0, s>>>(static_cast<const T *>(x), static_cast<uint32_t *>(out.lanes),
-                                                      out.exps, a);
-  return cudaGetLastError();
+  return launch_dependent(block8_quantize_kernel<T>, dim3(grid), kThreads, 0, s, static_cast<const T *>(x),
+                          static_cast<uint32_t *>(out.lanes), out.exps, a);
 }
 
 template <typename T>
 cudaError_t dequantize(samd_block8 in, int64_t rows, int64_t inner, void *y, int64_t ldy, cudaStream_t s) {
   const Block8Args a = make_args(sizeof(T), y, ldy, rows, inner, in);
   const int grid = resident_grid<block8_dequantize_kernel<T>>(a.rows * a.segs * 32, kThreads);
-  block8_dequantize_kernel<T><<<grid, kThreads, 0, s>>>(static_cast<const uint32_t *>(in.lanes), in.exps,
-                                                        static_cast<T *>(y), a);
-  return cudaGetLastError();
+  return launch_dependent(block8_dequantize_kernel<T>, dim3(grid), kThreads, 0, s,
+                          static_cast<const uint32_t *>(in.lanes), in.exps, static_cast<T *>(y), a);
 }
 
 }  // namespace

@@ -31,12 +31,18 @@ namespace {
 
 enum Form { FWD = 0, DX = 1, DW = 2 };
 
-constexpr int BM = 128, BN = 256, BK = 64;
-constexpr int kStages = 4;
-constexpr int kABytes = BM * BK * 2, kBBytes = BN * BK * 2, kStageBytes = kABytes + kBBytes;
+constexpr int BM = 128, BK = 64;
 constexpr int kEpiWarps = 8, kFirstEpiWarp = 4;
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
-constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + 256;
+
+// A tile's columns BN, and what follows from them: stages of 16 KB of A and
+// BN * 128 bytes of B, as many as 192 KB hold.
+template <int BN>
+struct Tile {
+  static constexpr int kABytes = BM * BK * 2, kBBytes = BN * BK * 2, kStageBytes = kABytes + kBBytes;
+  static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : 8;
+  static constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + 256;
+};
 constexpr uint64_t kWaitLimitNs = 1000000000ull;  // 1 s
 constexpr int kBand = 12;  // tiles along M that follow one another before the next along N
 
@@ -81,21 +87,12 @@ __device__ __forceinline__ void store_row32(T *row, int c, int N, const float *v
 // data, a tenth of the gradient's norm).
 template <bool kKeep>
 __device__ __forceinline__ void store_block8(uint32_t *lanes, uint8_t *exps, int64_t wpr, int c, const float *v) {
-  uint32_t top = 0;
+  float top = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  for (int i = 0; i < 32; ++i) top = max_abs(top, v[i]);
   const uint32_t e = block8_exp(top);
-  const float inv = block8_inv(e);
   uint32_t w[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    w[i] = block8_word(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inv);
-    if constexpr (kKeep) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (e != 255u && v[4 * i + j] > 0.0f && (w[i] >> 8 * j & 255u) == 0u) w[i] |= 1u << 8 * j;
-    }
-  }
+  block8_words_of<kKeep, 32>(v, top, e, block8_inv(e), w);
   uint32_t *const out = lanes + c / 4;
   if (wpr % 4 == 0 && c / 4 + 8 <= wpr) {
     *reinterpret_cast<uint4 *>(out) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -112,7 +109,7 @@ __device__ __forceinline__ void store_block8(uint32_t *lanes, uint8_t *exps, int
 // TMA, 1 issues the MMAs, 2 holds the tensor memory, 4-11 drain one of two
 // accumulators while the other fills. Every wait is bounded: a role that gives
 // up records it and stops, the others' waits then give up within one poll.
-template <int FORM, typename T, int ACT>
+template <int FORM, typename T, int ACT, int BN>
 __global__ void __launch_bounds__(kThreads, 1)
     ffn_gemm_kernel(const __grid_constant__ CUtensorMap ma0, const __grid_constant__ CUtensorMap ma1,
                     const __grid_constant__ CUtensorMap mb0, const __grid_constant__ CUtensorMap mb1,
@@ -120,6 +117,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr bool kAMn = FORM == DW, kBMn = FORM != FWD;
   constexpr int kSegs = FORM == DX ? 2 : 1;
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+  constexpr int kStages = Tile<BN>::kStages, kABytes = Tile<BN>::kABytes, kBBytes = Tile<BN>::kBBytes,
+                kStageBytes = Tile<BN>::kStageBytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *const smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t *const bars = reinterpret_cast<uint64_t *>(smem + kStages * kStageBytes);
@@ -130,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (warp == 2) {
-    ptx::tmem_alloc(ptx::smem_addr(holder), 512);
+    ptx::tmem_alloc(ptx::smem_addr(holder), 2 * BN);
     ptx::tmem_relinquish();
   }
   if (threadIdx.x == 0) {
@@ -150,6 +149,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = *holder;
+  // (every role, before it reads or writes global memory)
+  ptx::grid_dependency_wait();
+  ptx::grid_dependents_launch();
   const int steps = a.steps * kSegs;
 
   // tile -> its row and column of tiles: bands of kBand rows, down a band's
@@ -198,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             ptx::tma_load_2d(sb + kBBytes / 2, &mb1, kk, n0, full);
           } else {
 #pragma unroll
-            for (int j = 0; j < BN / 64; ++j) ptx::tma_load_2d(sb + j * (kBBytes / 4), B, n0 + 64 * j, kk, full);
+            for (int j = 0; j < BN / 64; ++j) ptx::tma_load_2d(sb + j * (64 * BK * 2), B, n0 + 64 * j, kk, full);
           }
           if (++s == kStages) {
             s = 0;
@@ -235,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         ptx::tc_fence_after();
         const uint32_t sa = sbase + s * kStageBytes, sb = sa + kABytes;
         const uint64_t da = kAMn ? ptx::sw128_mnmajor_desc(sa, kABytes / 2) : ptx::sw128_kmajor_desc(sa);
-        const uint64_t db = kBMn ? ptx::sw128_mnmajor_desc(sb, kBBytes / 4) : ptx::sw128_kmajor_desc(sb);
+        const uint64_t db = kBMn ? ptx::sw128_mnmajor_desc(sb, 64 * BK * 2) : ptx::sw128_kmajor_desc(sb);
 #pragma unroll
         for (int j = 0; j < BK / 16; ++j)
           ptx::mma_f16(leader, d, da + j * kAStep, db + j * kBStep, idesc, k > 0 || j > 0);
@@ -254,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     ptx::mbar_wait_bounded(drain, 0, &quiet, kWaitLimitNs / 10);
   } else if (warp >= kFirstEpiWarp) {
     const int ew = warp - kFirstEpiWarp;
-    const int quad = warp & 3, half = ew >> 2;  // rows 32 * quad .., the first or the second half of the columns
+    const int quad = warp & 3, half = ew >> 2;  // rows 32 * quad .., alternate blocks of 32 columns
     int i = 0;
     for (int tile = blockIdx.x; tile < a.total; tile += gridDim.x, ++i) {
       const int acc = i & 1;
@@ -268,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if constexpr (FORM == FWD) {
         const int n0 = tn * (BN / 2);
 #pragma unroll 1
-        for (int b = half * 2; b < half * 2 + 2; ++b) {
+        for (int b = half; b < BN / 64; b += 2) {
           uint32_t rg[32], ru[32];
           __syncwarp();
           ptx::tmem_ld_32x32b_x32(t0 + b * 32, rg);
@@ -292,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int n0 = tn * BN;
         T *const out = static_cast<T *>(second ? a.out[1] : a.out[0]) + m * a.ld;
 #pragma unroll 1
-        for (int b = half * 4; b < half * 4 + 4; ++b) {
+        for (int b = half; b < BN / 32; b += 2) {
           uint32_t r[32];
           __syncwarp();
           ptx::tmem_ld_32x32b_x32(t0 + b * 32, r);
@@ -312,71 +314,117 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   if (warp == 2) {
     ptx::tc_fence_after();
-    ptx::tmem_dealloc(tmem, 512);
+    ptx::tmem_dealloc(tmem, 2 * BN);
   }
 }
 
-// dg = dh * u * act'(g) and du = dh * act(g) from the 8-bit forms of g and u,
-// rounded to T, in rows of `ldw` elements; h = act(g) * u again if wanted.
-// One pass over HBM: 4 1/16 bytes an element in, 4 or 6 out.
+// The elementwise part of the backward pass, sixteen columns a thread:
+//   dg = dh * u * act'(g) and du = dh * act(g) from the 8-bit forms of g and u,
+//   rounded to T; h = act(g) * u again if wanted; and x from its 8-bit form
+//   (where the weights' gradients are wanted), which T holds without rounding.
+// One pass over HBM: 4 1/16 bytes an element of dh in and 4 or 6 out, 1 1/32 in
+// and 2 out for x. dg, du and xb are rows of whole units of eight; past F and K
+// their columns are not read.
+struct DgateArgs {
+  const void *dh;
+  void *dg, *du, *h, *xb;  // h, xb: null if not wanted
+  samd_block8 cg, cu, cx;
+  int64_t ldh, ldf, ldk, M, items_f, items;  // items: threads' pieces, those of dh first
+  int F, K, segs_f, segs_k;                  // pieces of a row
+  IndexDiv by_f, by_k;
+};
+
+__device__ __forceinline__ void load_words4(const void *lanes, int64_t at, bool vec, int n, uint32_t *w) {
+  const uint32_t *const p = static_cast<const uint32_t *>(lanes) + at;
+  if (vec && n > 12) {
+    const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(p));
+    w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = 4 * i < n ? p[i] : 0u;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 pack8(const float *v) {
+  return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+}
+
 template <typename T, int ACT>
-__global__ void __launch_bounds__(256)
-    ffn_dgate_kernel(const T *__restrict__ dh, int64_t ldh, samd_block8 cg, samd_block8 cu, T *__restrict__ dg,
-                     T *__restrict__ du, int64_t ldw, T *__restrict__ h, int64_t M, int F, int segs, int64_t wpr,
-                     int64_t bpr) {
+__global__ void __launch_bounds__(256) ffn_dgate_kernel(const DgateArgs a) {
+  ptx::grid_dependency_wait();
+  ptx::grid_dependents_launch();
   const int64_t nthreads = static_cast<int64_t>(gridDim.x) * blockDim.x;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < M * segs; i += nthreads) {
-    const int64_t m = i / segs;
-    const int c = static_cast<int>(i - m * segs) * 8;
-    const int n = F - c < 8 ? F - c : 8;
-    const uint32_t *const gl = static_cast<const uint32_t *>(cg.lanes) + m * wpr + c / 4;
-    const uint32_t *const ul = static_cast<const uint32_t *>(cu.lanes) + m * wpr + c / 4;
-    uint32_t gw[2], uw[2];
-    if (wpr % 2 == 0) {
-      const uint2 p = *reinterpret_cast<const uint2 *>(gl), q = *reinterpret_cast<const uint2 *>(ul);
-      gw[0] = p.x, gw[1] = p.y, uw[0] = q.x, uw[1] = q.y;
-    } else {
-      gw[0] = gl[0], uw[0] = ul[0];
-      gw[1] = n > 4 ? gl[1] : 0u, uw[1] = n > 4 ? ul[1] : 0u;
-    }
-    const float gs = block8_scale(cg.exps[m * bpr + c / kBlock8]), us = block8_scale(cu.exps[m * bpr + c / kBlock8]);
-    float d[8];
-    if (n == 8) {
-      const uint4 w = *reinterpret_cast<const uint4 *>(dh + m * ldh + c);
-      const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 f = unpack2<T>(ws[j]);
-        d[2 * j] = f.x;
-        d[2 * j + 1] = f.y;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) d[j] = j < n ? to_f32<T>(dh[m * ldh + c + j]) : 0.0f;
-    }
-    float vg[8], vu[8], vh[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float g = block8_value(gw[j >> 2], j & 3, gs), u = block8_value(uw[j >> 2], j & 3, us);
-      float da;
-      const float av = act_value_grad<ACT>(g, da);
-      vg[j] = d[j] * u * da;
-      vu[j] = d[j] * av;
-      vh[j] = av * u;
-    }
-    // the workspace's rows hold whole units of eight; past F they are not read
-    auto pack = [](const float *v) {
-      return make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
-    };
-    *reinterpret_cast<uint4 *>(dg + m * ldw + c) = pack(vg);
-    *reinterpret_cast<uint4 *>(du + m * ldw + c) = pack(vu);
-    if (h) {
-      if (n == 8) {
-        *reinterpret_cast<uint4 *>(h + m * ldh + c) = pack(vh);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < a.items; i += nthreads) {
+    if (i < a.items_f) {
+      const int64_t m = idiv(i, a.by_f);
+      const int c = static_cast<int>(i - m * a.segs_f) * 16;
+      const int n = a.F - c < 16 ? a.F - c : 16;
+      const int64_t wpr = (a.F + 3) / 4, bpr = (a.F + kBlock8 - 1) / kBlock8;
+      uint32_t gw[4], uw[4];
+      load_words4(a.cg.lanes, m * wpr + c / 4, wpr % 4 == 0, n, gw);
+      load_words4(a.cu.lanes, m * wpr + c / 4, wpr % 4 == 0, n, uw);
+      const float gs = block8_scale(a.cg.exps[m * bpr + c / kBlock8]), us = block8_scale(a.cu.exps[m * bpr + c / kBlock8]);
+      const T *const dh = static_cast<const T *>(a.dh) + m * a.ldh + c;
+      uint32_t dw[8];
+      if (n == 16) {
+        const uint4 p = __ldcs(reinterpret_cast<const uint4 *>(dh)), q = __ldcs(reinterpret_cast<const uint4 *>(dh) + 1);
+        dw[0] = p.x, dw[1] = p.y, dw[2] = p.z, dw[3] = p.w, dw[4] = q.x, dw[5] = q.y, dw[6] = q.z, dw[7] = q.w;
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < n) h[m * ldh + c + j] = from_f32<T>(vh[j]);
+        for (int j = 0; j < 8; ++j) {
+          const uint16_t *const p = reinterpret_cast<const uint16_t *>(dh) + 2 * j;
+          dw[j] = (2 * j < n ? p[0] : 0u) | (2 * j + 1 < n ? static_cast<uint32_t>(p[1]) << 16 : 0u);
+        }
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (half * 8 >= n) break;
+        float g[8], u[8], vg[8], vu[8];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          block8_values(gw[2 * half + j], gs, g + 4 * j);
+          block8_values(uw[2 * half + j], us, u + 4 * j);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 d2 = unpack2<T>(dw[4 * half + j / 2]);
+          const float d = j & 1 ? d2.y : d2.x;
+          float da;
+          const float av = act_value_grad<ACT>(g[j], da);
+          vg[j] = d * u[j] * da;
+          vu[j] = d * av;
+          g[j] = av * u[j];
+        }
+        const int64_t at = m * a.ldf + c + 8 * half;
+        *reinterpret_cast<uint4 *>(static_cast<T *>(a.dg) + at) = pack8<T>(vg);
+        *reinterpret_cast<uint4 *>(static_cast<T *>(a.du) + at) = pack8<T>(vu);
+        if (a.h) {
+          T *const h = static_cast<T *>(a.h) + m * a.ldh + c + 8 * half;
+          if (n - 8 * half >= 8) {
+            *reinterpret_cast<uint4 *>(h) = pack8<T>(g);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (8 * half + j < n) h[j] = from_f32<T>(g[j]);
+          }
+        }
+      }
+    } else {
+      const int64_t k = i - a.items_f, m = idiv(k, a.by_k);
+      const int c = static_cast<int>(k - m * a.segs_k) * 16;
+      const int n = a.K - c < 16 ? a.K - c : 16;
+      const int64_t wpr = (a.K + 3) / 4, bpr = (a.K + kBlock8 - 1) / kBlock8;
+      uint32_t w[4];
+      load_words4(a.cx.lanes, m * wpr + c / 4, wpr % 4 == 0, n, w);
+      const float s = block8_scale(a.cx.exps[m * bpr + c / kBlock8]);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (half * 8 >= n) break;
+        float v[8];
+        block8_values(w[2 * half], s, v);
+        block8_values(w[2 * half + 1], s, v + 4);
+        *reinterpret_cast<uint4 *>(static_cast<T *>(a.xb) + m * a.ldk + c + 8 * half) = pack8<T>(v);
       }
     }
   }
@@ -400,17 +448,56 @@ bool make_map(CUtensorMap *map, samd_dtype t, const void *p, int64_t rows, int64
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int FORM, typename T, int ACT>
-cudaError_t launch_gemm(const CUtensorMap (&m)[4], GemmArgs &a, cudaStream_t s) {
+// Columns of a tile for a product of `rows` rows of tiles, `cols` columns and
+// `steps` reduction steps: the fewest clocks over the waves of tiles. A step of
+// 256, 128 or 64 columns takes about 540, 340 or 250 clocks of an SM (the tensor
+// core bounds the first, the operands' way from L2 the others), and the last
+// tile's epilogue grows with its columns.
+int pick_columns(int64_t rows, int64_t cols, int64_t steps) {
+  int best = 256;
+  int64_t least = INT64_MAX;
+  for (const int bn : {256, 128, 64}) {
+    const int64_t tiles = rows * ((cols + bn - 1) / bn), waves = (tiles + sm_count() - 1) / sm_count();
+    const int64_t cost = waves * steps * (bn == 256 ? 540 : bn == 128 ? 340 : 250) + 12 * bn;
+    if (cost < least) {
+      least = cost;
+      best = bn;
+    }
+  }
+  return best;
+}
+
+// The operands of a product before its tile is picked.
+struct Operand {
+  const void *p;
+  int64_t rows, cols, ld;
+};
+
+template <int FORM, typename T, int ACT, int BN>
+cudaError_t launch_tiled(const Operand *op, samd_dtype t, GemmArgs &a, cudaStream_t s) {
+  constexpr int kARows = FORM == DW ? BK : BM, kBRows = FORM == FWD ? BN / 2 : BK;  // of a TMA box
+  CUtensorMap m[4];
+  for (int i = 0; i < 4; ++i)
+    if (!make_map(&m[i], t, op[i].p, op[i].rows, op[i].cols, op[i].ld, i < 2 ? kARows : kBRows))
+      return cudaErrorInvalidValue;
+  a.tiles_n = FORM == FWD ? (a.N + BN / 2 - 1) / (BN / 2) : (a.N + BN - 1) / BN;
   a.total = a.tiles_m * a.tiles_n;
+  const auto kern = ffn_gemm_kernel<FORM, T, ACT, BN>;
   cudaError_t e = device_status_ptr(&a.status);
-  if (e != cudaSuccess) return e;
-  const auto kern = ffn_gemm_kernel<FORM, T, ACT>;
-  e = conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), kSmemBytes);
+  if (e == cudaSuccess) e = conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), Tile<BN>::kSmemBytes);
   if (e != cudaSuccess) return e;
   const int grid = a.total < sm_count() ? a.total : sm_count();
-  kern<<<grid, kThreads, kSmemBytes, s>>>(m[0], m[1], m[2], m[3], a);
-  return cudaGetLastError();
+  return launch_dependent(kern, dim3(grid), kThreads, Tile<BN>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
+}
+
+template <int FORM, typename T, int ACT>
+cudaError_t launch_gemm(const Operand (&op)[4], samd_dtype t, GemmArgs &a, cudaStream_t s) {
+  const int cols = FORM == FWD ? 2 * a.N : a.N;  // of the MMA
+  switch (pick_columns(a.tiles_m, cols, static_cast<int64_t>(a.steps) * (FORM == DX ? 2 : 1))) {
+    case 64: return launch_tiled<FORM, T, ACT, 64>(op, t, a, s);
+    case 128: return launch_tiled<FORM, T, ACT, 128>(op, t, a, s);
+    default: return launch_tiled<FORM, T, ACT, 256>(op, t, a, s);
+  }
 }
 
 template <typename F>
@@ -426,17 +513,13 @@ cudaError_t by_act(int act, F f) {
 template <typename T>
 cudaError_t forward(const samd_ffn_desc &d, const void *x, const void *wg, const void *wu, void *h, samd_block8 cg,
                     samd_block8 cu, cudaStream_t s) {
-  CUtensorMap m[4];
-  if (!make_map(&m[0], d.type, x, d.M, d.K, d.ldx, BM) || !make_map(&m[2], d.type, wg, d.F, d.K, d.ldw, BN / 2) ||
-      !make_map(&m[3], d.type, wu, d.F, d.K, d.ldw, BN / 2))
-    return cudaErrorInvalidValue;
-  m[1] = m[0];
+  const Operand op[4] = {
+      {x, d.M, d.K, d.ldx}, {x, d.M, d.K, d.ldx}, {wg, d.F, d.K, d.ldw}, {wu, d.F, d.K, d.ldw}};
   GemmArgs a = {};
   a.M = d.M;
   a.N = d.F;
   a.steps = (d.K + BK - 1) / BK;
   a.tiles_m = (d.M + BM - 1) / BM;
-  a.tiles_n = (d.F + BN / 2 - 1) / (BN / 2);
   a.ld = d.ldh;
   a.out[0] = h;
   a.lanes[0] = static_cast<uint32_t *>(cg.lanes);
@@ -445,7 +528,7 @@ cudaError_t forward(const samd_ffn_desc &d, const void *x, const void *wg, const
   a.exps[1] = cu.exps;
   a.wpr = block8_words(d.F);
   a.bpr = block8_blocks(d.F);
-  return by_act(d.act, [&](auto act) { return launch_gemm<FWD, T, decltype(act)::value>(m, a, s); });
+  return by_act(d.act, [&](auto act) { return launch_gemm<FWD, T, decltype(act)::value>(op, d.type, a, s); });
 }
 
 // The workspace: dg and du (M rows of F) and x (M rows of K), each row a
@@ -473,52 +556,60 @@ cudaError_t backward(const samd_ffn_desc &d, const void *dh, samd_block8 cx, sam
   const Workspace w = plan_workspace(d);
   uint8_t *const ws = static_cast<uint8_t *>(workspace);
   T *const dg = reinterpret_cast<T *>(ws + w.dg), *const du = reinterpret_cast<T *>(ws + w.du);
-  const int segs = (d.F + 7) / 8;
+  T *const xb = reinterpret_cast<T *>(ws + w.x);
+  const bool weights = dwg || dwu;
+  DgateArgs g = {};
+  g.dh = dh;
+  g.dg = dg;
+  g.du = du;
+  g.h = h;
+  g.xb = weights ? xb : nullptr;
+  g.cg = cg;
+  g.cu = cu;
+  g.cx = cx;
+  g.ldh = d.ldh;
+  g.ldf = w.ldf;
+  g.ldk = w.ldk;
+  g.M = d.M;
+  g.F = d.F;
+  g.K = d.K;
+  g.segs_f = (d.F + 15) / 16;
+  g.segs_k = (d.K + 15) / 16;
+  g.items_f = static_cast<int64_t>(d.M) * g.segs_f;
+  const int64_t items_k = weights ? static_cast<int64_t>(d.M) * g.segs_k : 0;
+  g.items = g.items_f + items_k;
+  g.by_f = make_index_div(g.items_f, g.segs_f);
+  g.by_k = make_index_div(items_k, g.segs_k);
   cudaError_t e = by_act(d.act, [&](auto act) {
-    constexpr int kAct = decltype(act)::value;
-    const int grid = resident_grid<ffn_dgate_kernel<T, kAct>>(static_cast<int64_t>(d.M) * segs, 256);
-    ffn_dgate_kernel<T, kAct><<<grid, 256, 0, s>>>(static_cast<const T *>(dh), d.ldh, cg, cu, dg, du, w.ldf,
-                                                   static_cast<T *>(h), d.M, d.F, segs, block8_words(d.F),
-                                                   block8_blocks(d.F));
-    return cudaGetLastError();
+    constexpr auto kern = ffn_dgate_kernel<T, decltype(act)::value>;
+    return launch_dependent(kern, dim3(resident_grid<kern>(g.items, 256)), 256, 0, s, g);
   });
   if (e != cudaSuccess) return e;
-  CUtensorMap m[4];
+  const Operand odg = {dg, d.M, d.F, w.ldf}, odu = {du, d.M, d.F, w.ldf};
   if (dx) {
-    if (!make_map(&m[0], d.type, dg, d.M, d.F, w.ldf, BM) || !make_map(&m[1], d.type, du, d.M, d.F, w.ldf, BM) ||
-        !make_map(&m[2], d.type, wg, d.F, d.K, d.ldw, BK) || !make_map(&m[3], d.type, wu, d.F, d.K, d.ldw, BK))
-      return cudaErrorInvalidValue;
+    const Operand op[4] = {odg, odu, {wg, d.F, d.K, d.ldw}, {wu, d.F, d.K, d.ldw}};
     GemmArgs a = {};
     a.M = d.M;
     a.N = d.K;
     a.steps = (d.F + BK - 1) / BK;
     a.tiles_m = (d.M + BM - 1) / BM;
-    a.tiles_n = (d.K + BN - 1) / BN;
     a.ld = d.ldx;
     a.out[0] = dx;
-    e = launch_gemm<DX, T, 0>(m, a, s);
+    e = launch_gemm<DX, T, 0>(op, d.type, a, s);
     if (e != cudaSuccess) return e;
   }
-  if (dwg || dwu) {
-    e = launch_block8_dequantize(d.type, cx, d.M, d.K, ws + w.x, w.ldk, s);
-    if (e != cudaSuccess) return e;
-    const T *const first = dwg ? dg : du;
-    if (!make_map(&m[0], d.type, first, d.M, d.F, w.ldf, BK) || !make_map(&m[1], d.type, du, d.M, d.F, w.ldf, BK) ||
-        !make_map(&m[2], d.type, ws + w.x, d.M, d.K, w.ldk, BK))
-      return cudaErrorInvalidValue;
-    m[3] = m[2];
+  if (weights) {
+    const Operand ox = {xb, d.M, d.K, w.ldk}, op[4] = {dwg ? odg : odu, odu, ox, ox};
     GemmArgs a = {};
     a.M = d.F;
     a.N = d.K;
     a.steps = (d.M + BK - 1) / BK;
-    a.tiles_m = (d.F + BM - 1) / BM;
-    a.tiles_n = (d.K + BN - 1) / BN;
+    a.half_m = (d.F + BM - 1) / BM;
+    a.tiles_m = dwg && dwu ? 2 * a.half_m : a.half_m;
     a.ld = d.ldw;
     a.out[0] = dwg ? dwg : dwu;
     a.out[1] = dwu;
-    a.half_m = a.tiles_m;
-    if (dwg && dwu) a.tiles_m *= 2;
-    e = launch_gemm<DW, T, 0>(m, a, s);
+    e = launch_gemm<DW, T, 0>(op, d.type, a, s);
   }
   return e;
 }

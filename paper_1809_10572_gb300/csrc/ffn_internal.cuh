@@ -130,9 +130,9 @@ __device__ __forceinline__ float act_value_grad(float g, float &grad) {
 // cores take without another rounding.
 constexpr int kBlock8 = 32;
 
-// Exponent byte of a block from the bits of its largest magnitude.
-__device__ __forceinline__ uint32_t block8_exp(uint32_t amax_bits) {
-  const int E = static_cast<int>(amax_bits >> 23);
+// Exponent byte of a block from its largest magnitude.
+__device__ __forceinline__ uint32_t block8_exp(float top) {
+  const int E = static_cast<int>(__float_as_uint(top) >> 23);
   return E == 255 ? 255u : static_cast<uint32_t>(E > 6 ? E - 6 : 0);
 }
 // 2^(127 - e) for e <= 248 (a finite block has no larger one); a block of NaNs
@@ -142,20 +142,94 @@ __device__ __forceinline__ float block8_inv(uint32_t e) { return e == 255u ? 0.0
 __device__ __forceinline__ float block8_scale(uint32_t e) {
   return e == 255u ? __uint_as_float(0x7FC00000u) : e == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(e << 23);
 }
-__device__ __forceinline__ uint32_t block8_code(float v, float inv) {
-  const int c = __float2int_rn(v * inv);
-  return static_cast<uint32_t>(c > 127 ? 127 : c < -127 ? -127 : c) & 255u;
+
+// The larger magnitude; a NaN is larger than everything.
+__device__ __forceinline__ float max_abs(float top, float v) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(top), "f"(fabsf(v)));
+  return r;
 }
-// Four codes as a word of lanes (in a block of NaNs inf * 0 converts to 0).
-__device__ __forceinline__ uint32_t block8_word(float a, float b, float c, float d, float inv) {
-  return block8_code(a, inv) | block8_code(b, inv) << 8 | block8_code(c, inv) << 16 | block8_code(d, inv) << 24;
+
+// N values of a block (N a multiple of 4), whose largest magnitude is `top`,
+// as words of four lanes, with the block's exponent e and factor inv. Adding
+// 1.5 * 2^23 rounds v * inv to an integer (the product is exact, so this is
+// its one rounding) and leaves the code in the sum's low byte; a conversion
+// would take the quarter-rate pipe. Blocks with something to clamp (one in a
+// hundred or so) and blocks of NaNs go the long way round.
+// kKeep: the code of a positive value is at least 1.
+template <bool kKeep, int N>
+__device__ __forceinline__ void block8_words_of(const float *v, float top, uint32_t e, float inv, uint32_t *w) {
+  if (top * inv < 127.5f) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      uint32_t c[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        c[j] = __float_as_uint(fmaf(v[4 * i + j], inv, 12582912.0f));
+        if constexpr (kKeep)
+          if (v[4 * i + j] > 0.0f) c[j] = max(c[j], 0x4B400001u);
+      }
+      w[i] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      w[i] = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float f = fminf(fmaxf(v[4 * i + j] * inv, -127.0f), 127.0f);
+        if constexpr (kKeep)
+          if (v[4 * i + j] > 0.0f) f = fmaxf(f, 1.0f);
+        if (e != 255u) w[i] |= (__float_as_uint(f + 12582912.0f) & 255u) << 8 * j;
+      }
+    }
+  }
 }
-__device__ __forceinline__ float block8_value(uint32_t word, int lane, float scale) {
-  return static_cast<float>(static_cast<int>(word << (24 - 8 * lane)) >> 24) * scale;
+
+// The four values of a word: lane + 128 under the exponent of 2^23, less
+// 2^23 + 128 (exact, and not on the conversions' pipe).
+__device__ __forceinline__ void block8_values(uint32_t word, float scale, float *v) {
+  const uint32_t u = word ^ 0x80808080u;
+  v[0] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440)) - 8388736.0f) * scale;
+  v[1] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7441)) - 8388736.0f) * scale;
+  v[2] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7442)) - 8388736.0f) * scale;
+  v[3] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7443)) - 8388736.0f) * scale;
 }
 
 inline int64_t block8_words(int64_t inner) { return (inner + 3) / 4; }
 inline int64_t block8_blocks(int64_t inner) { return (inner + kBlock8 - 1) / kBlock8; }
+
+// Division of an index below `count` by d: in 32 bits where they suffice.
+struct IndexDiv {
+  FastDiv f;
+  int64_t d;
+  bool small;
+};
+inline IndexDiv make_index_div(int64_t count, int64_t d) {
+  const bool small = count < (int64_t(1) << 31) && d < (int64_t(1) << 31);
+  return IndexDiv{make_fastdiv(small ? static_cast<uint32_t>(d) : 1u), d, small};
+}
+__device__ __forceinline__ int64_t idiv(int64_t n, const IndexDiv &v) {
+  return v.small ? static_cast<int64_t>(fdiv(static_cast<uint32_t>(n), v.f)) : n / v.d;
+}
+
+// A launch that may be set up while the kernel before it in the stream drains
+// (the kernel calls grid_dependency_wait before it touches global memory).
+template <typename... P, typename... A>
+cudaError_t launch_dependent(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
 
 // ---- launchers -------------------------------------------------------------------
 
