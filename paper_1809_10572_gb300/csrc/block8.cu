@@ -23,8 +23,8 @@ struct Block8Args {
 };
 
 template <typename T>
-__device__ __forceinline__ void load16(const T *p, int n, bool vec, float *v) {
-  if (vec && n == kPer) {
+__device__ __forceinline__ void load16(const T *p, int n, float *v) {
+  if (n == kPer) {
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -51,8 +51,8 @@ __device__ __forceinline__ void load16(const T *p, int n, bool vec, float *v) {
 }
 
 template <typename T>
-__device__ __forceinline__ void store16(T *p, int n, bool vec, const float *v) {
-  if (vec && n == kPer) {
+__device__ __forceinline__ void store16(T *p, int n, const float *v) {
+  if (n == kPer) {
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -71,11 +71,46 @@ __device__ __forceinline__ void store16(T *p, int n, bool vec, const float *v) {
   }
 }
 
+// Rows that are not 16-byte aligned go through shared memory, so that a warp's
+// accesses are neighbouring elements: place i of the warp's 512 elements, one
+// word further behind every sixteen, which puts the lanes' runs of sixteen into
+// different banks.
+__device__ __forceinline__ int place(int i) { return i + (i >> 4); }
+constexpr int kStageWords = kRowStep + kRowStep / 16;
+
+// The warp's 512 elements from `p`, of which the row holds `left` (at least
+// one): sixteen for each lane, zeros past the row's end.
 template <typename T>
+__device__ __forceinline__ void load_staged(const T *p, int64_t left, float *stage, int lane, float *v) {
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int at = i * 32 + lane;
+    stage[place(at)] = at < left ? to_f32<T>(p[at]) : 0.0f;
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) v[i] = stage[place(lane * kPer) + i];
+  __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void store_staged(T *p, int64_t left, float *stage, int lane, const float *v) {
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) stage[place(lane * kPer) + i] = v[i];
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int at = i * 32 + lane;
+    if (at < left) p[at] = from_f32<T>(stage[place(at)]);
+  }
+  __syncwarp();
+}
+
+template <typename T, bool kVec>
 __global__ void __launch_bounds__(kThreads) block8_quantize_kernel(const T *__restrict__ x, uint32_t *__restrict__ lanes,
                                                                    uint8_t *__restrict__ exps, const Block8Args a) {
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
+  __shared__ float stage[kVec ? 1 : kThreads / 32][kVec ? 1 : kStageWords];
   const int lane = threadIdx.x & 31;
   const int64_t nwarps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
   const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
@@ -85,7 +120,10 @@ __global__ void __launch_bounds__(kThreads) block8_quantize_kernel(const T *__re
     const int64_t left = a.inner - col;
     const int n = left < 0 ? 0 : left < kPer ? static_cast<int>(left) : kPer;
     float v[kPer];
-    load16<T>(x + row * a.ld + (n ? col : 0), n, a.x_vec, v);
+    if constexpr (kVec)
+      load16<T>(x + row * a.ld + (n ? col : 0), n, v);
+    else
+      load_staged<T>(x + row * a.ld + col - lane * kPer, left + lane * kPer, stage[threadIdx.x >> 5], lane, v);
     float top = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) top = max_abs(top, v[i]);
@@ -107,12 +145,13 @@ __global__ void __launch_bounds__(kThreads) block8_quantize_kernel(const T *__re
   }
 }
 
-template <typename T>
+template <typename T, bool kVec>
 __global__ void __launch_bounds__(kThreads)
     block8_dequantize_kernel(const uint32_t *__restrict__ lanes, const uint8_t *__restrict__ exps, T *__restrict__ y,
                              const Block8Args a) {
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
+  __shared__ float stage[kVec ? 1 : kThreads / 32][kVec ? 1 : kStageWords];
   const int lane = threadIdx.x & 31;
   const int64_t nwarps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
   const int64_t first = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
@@ -121,6 +160,7 @@ __global__ void __launch_bounds__(kThreads)
     const int64_t col = (step - row * a.segs) * kRowStep + lane * kPer;
     const int64_t left = a.inner - col;
     const int n = left < 0 ? 0 : left < kPer ? static_cast<int>(left) : kPer;
+    float v[kPer];
     if (n) {
       const uint32_t *const in = lanes + row * a.wpr + col / 4;
       uint32_t w[4];
@@ -132,10 +172,16 @@ __global__ void __launch_bounds__(kThreads)
         for (int i = 0; i < 4; ++i) w[i] = 4 * i < n ? in[i] : 0u;
       }
       const float scale = block8_scale(exps[row * a.bpr + col / kBlock8]);
-      float v[kPer];
 #pragma unroll
       for (int i = 0; i < 4; ++i) block8_values(w[i], scale, v + 4 * i);
-      store16<T>(y + row * a.ld + col, n, a.x_vec, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) v[i] = 0.0f;
+    }
+    if constexpr (kVec) {
+      if (n) store16<T>(y + row * a.ld + col, n, v);
+    } else {
+      store_staged<T>(y + row * a.ld + col - lane * kPer, left + lane * kPer, stage[threadIdx.x >> 5], lane, v);
     }
   }
 }
@@ -154,20 +200,28 @@ Block8Args make_args(size_t esize, const void *x, int64_t ld, int64_t rows, int6
   return a;
 }
 
+template <typename T, bool kVec>
+cudaError_t quantize_as(const Block8Args &a, const void *x, samd_block8 out, cudaStream_t s) {
+  constexpr auto kern = block8_quantize_kernel<T, kVec>;
+  return launch_dependent(kern, dim3(resident_grid<kern>(a.rows * a.segs * 32, kThreads)), kThreads, 0, s,
+                          static_cast<const T *>(x), static_cast<uint32_t *>(out.lanes), out.exps, a);
+}
 template <typename T>
 cudaError_t quantize(const void *x, int64_t ldx, int64_t rows, int64_t inner, samd_block8 out, cudaStream_t s) {
   const Block8Args a = make_args(sizeof(T), x, ldx, rows, inner, out);
-  const int grid = resident_grid<block8_quantize_kernel<T>>(a.rows * a.segs * 32, kThreads);
-  return launch_dependent(block8_quantize_kernel<T>, dim3(grid), kThreads, 0, s, static_cast<const T *>(x),
-                          static_cast<uint32_t *>(out.lanes), out.exps, a);
+  return a.x_vec ? quantize_as<T, true>(a, x, out, s) : quantize_as<T, false>(a, x, out, s);
 }
 
+template <typename T, bool kVec>
+cudaError_t dequantize_as(const Block8Args &a, samd_block8 in, void *y, cudaStream_t s) {
+  constexpr auto kern = block8_dequantize_kernel<T, kVec>;
+  return launch_dependent(kern, dim3(resident_grid<kern>(a.rows * a.segs * 32, kThreads)), kThreads, 0, s,
+                          static_cast<const uint32_t *>(in.lanes), in.exps, static_cast<T *>(y), a);
+}
 template <typename T>
 cudaError_t dequantize(samd_block8 in, int64_t rows, int64_t inner, void *y, int64_t ldy, cudaStream_t s) {
   const Block8Args a = make_args(sizeof(T), y, ldy, rows, inner, in);
-  const int grid = resident_grid<block8_dequantize_kernel<T>>(a.rows * a.segs * 32, kThreads);
-  return launch_dependent(block8_dequantize_kernel<T>, dim3(grid), kThreads, 0, s,
-                          static_cast<const uint32_t *>(in.lanes), in.exps, static_cast<T *>(y), a);
+  return a.x_vec ? dequantize_as<T, true>(a, in, y, s) : dequantize_as<T, false>(a, in, y, s);
 }
 
 }  // namespace
