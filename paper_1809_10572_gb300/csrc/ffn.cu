@@ -35,12 +35,16 @@ constexpr int BM = 128, BK = 64;
 constexpr int kEpiWarps = 8, kFirstEpiWarp = 4;
 constexpr int kThreads = 32 * (kFirstEpiWarp + kEpiWarps);
 
-// A tile's columns BN, and what follows from them: stages of 16 KB of A and
-// BN * 128 bytes of B, as many as 192 KB hold.
+// A tile's columns BN, and what follows from them: stages of KS reduction steps,
+// each 16 KB of A and BN * 128 bytes of B, as many as 192 KB hold. Narrow tiles
+// take two steps a stage: their MMAs are over before the barriers and the issue
+// of the next ones are.
 template <int BN>
 struct Tile {
-  static constexpr int kABytes = BM * BK * 2, kBBytes = BN * BK * 2, kStageBytes = kABytes + kBBytes;
-  static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : 8;
+  static constexpr int KS = BN == 256 ? 1 : 2;
+  static constexpr int kABytes = BM * BK * 2, kBBytes = BN * BK * 2, kStepBytes = kABytes + kBBytes;
+  static constexpr int kStageBytes = KS * kStepBytes;
+  static constexpr int kStages = BN == 128 ? 3 : 4;
   static constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + 256;
 };
 constexpr uint64_t kWaitLimitNs = 1000000000ull;  // 1 s
@@ -118,7 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   constexpr int kSegs = FORM == DX ? 2 : 1;
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   constexpr int kStages = Tile<BN>::kStages, kABytes = Tile<BN>::kABytes, kBBytes = Tile<BN>::kBBytes,
-                kStageBytes = Tile<BN>::kStageBytes;
+                kStepBytes = Tile<BN>::kStepBytes, kStageBytes = Tile<BN>::kStageBytes, KS = Tile<BN>::KS;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *const smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t *const bars = reinterpret_cast<uint64_t *>(smem + kStages * kStageBytes);
@@ -175,32 +179,40 @@ __global__ void __launch_bounds__(kThreads, 1)
         place(tile, tm, tn);
         const int second = FORM == DW && tm >= a.half_m;
         const int m0 = (second ? tm - a.half_m : tm) * BM, n0 = tn * (FORM == FWD ? BN / 2 : BN);
-        for (int k = 0; k < steps; ++k) {
+        for (int k = 0; k < steps; k += KS) {
+          // A stage is armed again when the MMAs that read it have completed,
+          // and they were issued behind a wait for its copies.
           if (loaded == kStages) {
-            ok = ptx::mbar_wait(full0 + 8 * s, par, a.status, SAMD_ETIMEOUT, kWaitLimitNs) &&
-                 ptx::mbar_wait(empty0 + 8 * s, par, a.status, SAMD_ETIMEOUT, kWaitLimitNs);
+            ok = ptx::mbar_wait(empty0 + 8 * s, par, a.status, SAMD_ETIMEOUT, kWaitLimitNs);
             if (!ok) break;
           } else {
             ++loaded;
           }
-          const uint32_t full = full0 + 8 * s, sa = sbase + s * kStageBytes, sb = sa + kABytes;
-          ptx::mbar_arrive_expect_tx(full, kStageBytes);
-          const bool seg = FORM == DX && k >= a.steps;
-          const int kk = (seg ? k - a.steps : k) * BK;
-          const CUtensorMap *const A = (FORM == DX ? seg : FORM == DW ? second != 0 : false) ? &ma1 : &ma0;
-          const CUtensorMap *const B = FORM == DX && seg ? &mb1 : &mb0;
-          if constexpr (kAMn) {
-            ptx::tma_load_2d(sa, A, m0, kk, full);
-            ptx::tma_load_2d(sa + kABytes / 2, A, m0 + 64, kk, full);
-          } else {
-            ptx::tma_load_2d(sa, A, kk, m0, full);
-          }
-          if constexpr (FORM == FWD) {
-            ptx::tma_load_2d(sb, &mb0, kk, n0, full);
-            ptx::tma_load_2d(sb + kBBytes / 2, &mb1, kk, n0, full);
-          } else {
+          const int now = KS == 1 ? 1 : min(KS, steps - k);  // steps of this stage
+          const uint32_t full = full0 + 8 * s;
+          ptx::mbar_arrive_expect_tx(full, now * kStepBytes);
 #pragma unroll
-            for (int j = 0; j < BN / 64; ++j) ptx::tma_load_2d(sb + j * (64 * BK * 2), B, n0 + 64 * j, kk, full);
+          for (int j = 0; j < KS; ++j) {
+            if (j < now) {
+              const uint32_t sa = sbase + s * kStageBytes + j * kStepBytes, sb = sa + kABytes;
+              const bool seg = FORM == DX && k + j >= a.steps;
+              const int kk = (seg ? k + j - a.steps : k + j) * BK;
+              const CUtensorMap *const A = (FORM == DX ? seg : FORM == DW ? second != 0 : false) ? &ma1 : &ma0;
+              const CUtensorMap *const B = FORM == DX && seg ? &mb1 : &mb0;
+              if constexpr (kAMn) {
+                ptx::tma_load_2d(sa, A, m0, kk, full);
+                ptx::tma_load_2d(sa + kABytes / 2, A, m0 + 64, kk, full);
+              } else {
+                ptx::tma_load_2d(sa, A, kk, m0, full);
+              }
+              if constexpr (FORM == FWD) {
+                ptx::tma_load_2d(sb, &mb0, kk, n0, full);
+                ptx::tma_load_2d(sb + kBBytes / 2, &mb1, kk, n0, full);
+              } else {
+#pragma unroll
+                for (int q = 0; q < BN / 64; ++q) ptx::tma_load_2d(sb + q * (64 * BK * 2), B, n0 + 64 * q, kk, full);
+              }
+            }
           }
           if (++s == kStages) {
             s = 0;
@@ -231,16 +243,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) break;
       ptx::tc_fence_after();
       const uint32_t d = tmem + acc * BN;
-      for (int k = 0; k < steps; ++k) {
+      for (int k = 0; k < steps; k += KS) {
         ok = warp_wait(full0 + 8 * s, par, a.status);
         if (!ok) break;
         ptx::tc_fence_after();
-        const uint32_t sa = sbase + s * kStageBytes, sb = sa + kABytes;
-        const uint64_t da = kAMn ? ptx::sw128_mnmajor_desc(sa, kABytes / 2) : ptx::sw128_kmajor_desc(sa);
-        const uint64_t db = kBMn ? ptx::sw128_mnmajor_desc(sb, 64 * BK * 2) : ptx::sw128_kmajor_desc(sb);
 #pragma unroll
-        for (int j = 0; j < BK / 16; ++j)
-          ptx::mma_f16(leader, d, da + j * kAStep, db + j * kBStep, idesc, k > 0 || j > 0);
+        for (int q = 0; q < KS; ++q) {
+          if (KS == 1 || k + q < steps) {
+            const uint32_t sa = sbase + s * kStageBytes + q * kStepBytes, sb = sa + kABytes;
+            const uint64_t da = kAMn ? ptx::sw128_mnmajor_desc(sa, kABytes / 2) : ptx::sw128_kmajor_desc(sa);
+            const uint64_t db = kBMn ? ptx::sw128_mnmajor_desc(sb, 64 * BK * 2) : ptx::sw128_kmajor_desc(sb);
+#pragma unroll
+            for (int j = 0; j < BK / 16; ++j)
+              ptx::mma_f16(leader, d, da + j * kAStep, db + j * kBStep, idesc, k > 0 || q > 0 || j > 0);
+          }
+        }
         ptx::mma_commit(leader, empty0 + 8 * s);
         if (++s == kStages) {
           s = 0;
