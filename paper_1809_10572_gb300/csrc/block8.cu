@@ -203,7 +203,7 @@ Block8Args make_args(size_t esize, const void *x, int64_t ld, int64_t rows, int6
 template <typename T, bool kVec>
 cudaError_t quantize_as(const Block8Args &a, const void *x, samd_block8 out, cudaStream_t s) {
   constexpr auto kern = block8_quantize_kernel<T, kVec>;
-  return launch_dependent(kern, dim3(resident_grid<kern>(a.rows * a.segs * 32, kThreads)), kThreads, 0, s,
+  return launch_dependent(kern, dim3(resident_grid<kern>(a.rows * a.segs * 32, kThreads)), kThreads, 0, s, 1,
                           static_cast<const T *>(x), static_cast<uint32_t *>(out.lanes), out.exps, a);
 }
 template <typename T>
@@ -215,7 +215,7 @@ cudaError_t quantize(const void *x, int64_t ldx, int64_t rows, int64_t inner, sa
 template <typename T, bool kVec>
 cudaError_t dequantize_as(const Block8Args &a, samd_block8 in, void *y, cudaStream_t s) {
   constexpr auto kern = block8_dequantize_kernel<T, kVec>;
-  return launch_dependent(kern, dim3(resident_grid<kern>(a.rows * a.segs * 32, kThreads)), kThreads, 0, s,
+  return launch_dependent(kern, dim3(resident_grid<kern>(a.rows * a.segs * 32, kThreads)), kThreads, 0, s, 1,
                           static_cast<const uint32_t *>(in.lanes), in.exps, static_cast<T *>(y), a);
 }
 template <typename T>

@@ -21,6 +21,7 @@
 // Between FWD and the others an elementwise kernel forms dg and du, rounded to
 // the operands' type: with fp32 sums this is the one rounding between the
 // gradients' factors and their sums.
+#include <cstdlib>
 #include <type_traits>
 
 #include "ffn_internal.cuh"
@@ -55,12 +56,14 @@ struct GemmArgs {
   int steps;        // reduction steps of BK in a segment
   int tiles_m, tiles_n, total;
   int half_m;       // DW: rows of tiles of the first output; the rest are the second's
+  int split;        // CTAs of a cluster that share a tile's reduction (kSplit)
   int64_t ld;       // of the output
   void *out[2];     // FWD: h; DX: dx; DW: dwg, dwu
   // FWD: the checkpoints (null: none), rows of `wpr` words and `bpr` exponents
   uint32_t *lanes[2];
   uint8_t *exps[2];
   int64_t wpr, bpr;
+  int wide, wide8;  // rows of the output, and of the checkpoints' lanes, start on 32 bytes
   int *status;
 };
 
@@ -71,8 +74,16 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, int *st
 
 // Columns [c, c + 32) of a row of the output, rounded.
 template <typename T>
-__device__ __forceinline__ void store_row32(T *row, int c, int N, const float *v) {
-  if (c + 32 <= N) {
+__device__ __forceinline__ void store_row32(T *row, int c, int N, bool wide, const float *v) {
+  if (wide && c + 32 <= N) {
+    // neighbouring lanes' rows lie apart, and a store takes a cycle for each: few and wide ones
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      ptx::st_global_v8(row + c + 16 * i, pack2<T>(v[16 * i], v[16 * i + 1]), pack2<T>(v[16 * i + 2], v[16 * i + 3]),
+                        pack2<T>(v[16 * i + 4], v[16 * i + 5]), pack2<T>(v[16 * i + 6], v[16 * i + 7]),
+                        pack2<T>(v[16 * i + 8], v[16 * i + 9]), pack2<T>(v[16 * i + 10], v[16 * i + 11]),
+                        pack2<T>(v[16 * i + 12], v[16 * i + 13]), pack2<T>(v[16 * i + 14], v[16 * i + 15]));
+  } else if (c + 32 <= N) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       *reinterpret_cast<uint4 *>(row + c + 8 * i) =
@@ -90,7 +101,7 @@ __device__ __forceinline__ void store_row32(T *row, int c, int N, const float *v
 // to zero it would lose its derivative, which one in a hundred does on normal
 // data, a tenth of the gradient's norm).
 template <bool kKeep>
-__device__ __forceinline__ void store_block8(uint32_t *lanes, uint8_t *exps, int64_t wpr, int c, const float *v) {
+__device__ __forceinline__ void store_block8(uint32_t *lanes, uint8_t *exps, int64_t wpr, int c, bool wide, const float *v) {
   float top = 0.0f;
 #pragma unroll
   for (int i = 0; i < 32; ++i) top = max_abs(top, v[i]);
@@ -98,7 +109,9 @@ __device__ __forceinline__ void store_block8(uint32_t *lanes, uint8_t *exps, int
   uint32_t w[8];
   block8_words_of<kKeep, 32>(v, top, e, block8_inv(e), w);
   uint32_t *const out = lanes + c / 4;
-  if (wpr % 4 == 0 && c / 4 + 8 <= wpr) {
+  if (wide && c / 4 + 8 <= wpr) {
+    ptx::st_global_v8(out, w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]);
+  } else if (wpr % 4 == 0 && c / 4 + 8 <= wpr) {
     *reinterpret_cast<uint4 *>(out) = make_uint4(w[0], w[1], w[2], w[3]);
     *reinterpret_cast<uint4 *>(out + 4) = make_uint4(w[4], w[5], w[6], w[7]);
   } else {
@@ -109,17 +122,54 @@ __device__ __forceinline__ void store_block8(uint32_t *lanes, uint8_t *exps, int
   exps[c / kBlock8] = static_cast<uint8_t>(e);
 }
 
+// Columns [c, c + 4) of a row of the output, rounded (rows start on 16 bytes, c is a multiple of 4).
+template <typename T>
+__device__ __forceinline__ void store_row4(T *row, int c, int N, const float *v) {
+  if (c + 4 <= N) {
+    *reinterpret_cast<uint2 *>(row + c) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i < N) row[c + i] = from_f32<T>(v[i]);
+  }
+}
+
+// Four columns from c on of a block that eight neighbouring lanes hold, into
+// its 8-bit form (`in`: the lane's columns are of the output; the same for all
+// eight; columns past N are zero). Called by the whole warp.
+template <bool kKeep>
+__device__ __forceinline__ void split_block8(uint32_t *lanes, uint8_t *exps, int64_t wpr, int c, bool in, const float *v) {
+  float top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = max_abs(top, v[i]);
+#pragma unroll
+  for (int s = 1; s < 8; s *= 2) top = max_abs(top, __shfl_xor_sync(0xffffffffu, top, s));
+  const uint32_t e = block8_exp(top);
+  uint32_t w;
+  block8_words_of<kKeep, 4>(v, top, e, block8_inv(e), &w);
+  if (in && c / 4 < wpr) {
+    lanes[c / 4] = w;
+    if (c % kBlock8 == 0) exps[c / kBlock8] = static_cast<uint8_t>(e);
+  }
+}
+
 // One CTA per SM, looping over tiles; twelve warps: 0 loads operand tiles with
 // TMA, 1 issues the MMAs, 2 holds the tensor memory, 4-11 drain one of two
 // accumulators while the other fills. Every wait is bounded: a role that gives
 // up records it and stops, the others' waits then give up within one poll.
-template <int FORM, typename T, int ACT, int BN>
+//
+// kSplit: few tiles with long reductions. A cluster takes one tile, each of its
+// CTAs a part of the reduction; the partial sums meet in distributed shared
+// memory, where each CTA adds up (in rank order) and finishes a part of the
+// rows.
+template <int FORM, typename T, int ACT, int BN, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1)
     ffn_gemm_kernel(const __grid_constant__ CUtensorMap ma0, const __grid_constant__ CUtensorMap ma1,
                     const __grid_constant__ CUtensorMap mb0, const __grid_constant__ CUtensorMap mb1,
                     const GemmArgs a) {
   constexpr bool kAMn = FORM == DW, kBMn = FORM != FWD;
   constexpr int kSegs = FORM == DX ? 2 : 1;
+  constexpr int kSumPitch = BN * 4 + 16;  // bytes of a row of partial sums (kSplit)
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   constexpr int kStages = Tile<BN>::kStages, kABytes = Tile<BN>::kABytes, kBBytes = Tile<BN>::kBBytes,
                 kStepBytes = Tile<BN>::kStepBytes, kStageBytes = Tile<BN>::kStageBytes, KS = Tile<BN>::KS;
@@ -156,7 +206,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   // (every role, before it reads or writes global memory)
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
-  const int steps = a.steps * kSegs;
+  // a CTA's tiles and its steps of their reductions
+  const int rank = kSplit ? blockIdx.x % a.split : 0;
+  const int tile0 = kSplit ? blockIdx.x / a.split : blockIdx.x, tile_step = kSplit ? a.total : gridDim.x;
+  const int k0 = kSplit ? static_cast<int>(static_cast<int64_t>(a.steps) * kSegs * rank / a.split) : 0;
+  const int steps = kSplit ? static_cast<int>(static_cast<int64_t>(a.steps) * kSegs * (rank + 1) / a.split) : a.steps * kSegs;
 
   // tile -> its row and column of tiles: bands of kBand rows, down a band's
   // column before the next, so that the tiles in flight share operands in L2
@@ -174,12 +228,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       int s = 0, loaded = 0;
       uint32_t par = 1;
       bool ok = true;
-      for (int tile = blockIdx.x; ok && tile < a.total; tile += gridDim.x) {
+      for (int tile = tile0; ok && tile < a.total; tile += tile_step) {
         int tm, tn;
         place(tile, tm, tn);
         const int second = FORM == DW && tm >= a.half_m;
         const int m0 = (second ? tm - a.half_m : tm) * BM, n0 = tn * (FORM == FWD ? BN / 2 : BN);
-        for (int k = 0; k < steps; k += KS) {
+        for (int k = k0; k < steps; k += KS) {
           // A stage is armed again when the MMAs that read it have completed,
           // and they were issued behind a wait for its copies.
           if (loaded == kStages) {
@@ -237,13 +291,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     int s = 0, i = 0;
     uint32_t par = 0;
     bool ok = true;
-    for (int tile = blockIdx.x; ok && tile < a.total; tile += gridDim.x, ++i) {
+    for (int tile = tile0; ok && tile < a.total; tile += tile_step, ++i) {
       const int acc = i & 1;
       if (i >= 2) ok = warp_wait(accempty0 + 8 * acc, ((i >> 1) + 1) & 1u, a.status);
       if (!ok) break;
       ptx::tc_fence_after();
       const uint32_t d = tmem + acc * BN;
-      for (int k = 0; k < steps; k += KS) {
+      for (int k = k0; k < steps; k += KS) {
         ok = warp_wait(full0 + 8 * s, par, a.status);
         if (!ok) break;
         ptx::tc_fence_after();
@@ -255,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint64_t db = kBMn ? ptx::sw128_mnmajor_desc(sb, 64 * BK * 2) : ptx::sw128_kmajor_desc(sb);
 #pragma unroll
             for (int j = 0; j < BK / 16; ++j)
-              ptx::mma_f16(leader, d, da + j * kAStep, db + j * kBStep, idesc, k > 0 || q > 0 || j > 0);
+              ptx::mma_f16(leader, d, da + j * kAStep, db + j * kBStep, idesc, k > k0 || q > 0 || j > 0);
           }
         }
         ptx::mma_commit(leader, empty0 + 8 * s);
@@ -275,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int ew = warp - kFirstEpiWarp;
     const int quad = warp & 3, half = ew >> 2;  // rows 32 * quad .., alternate blocks of 32 columns
     int i = 0;
-    for (int tile = blockIdx.x; tile < a.total; tile += gridDim.x, ++i) {
+    for (int tile = tile0; tile < a.total; tile += tile_step, ++i) {
       const int acc = i & 1;
       if (!warp_wait(accfull0 + 8 * acc, (i >> 1) & 1u, a.status)) break;
       ptx::tc_fence_after();
@@ -284,7 +338,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int second = FORM == DW && tm >= a.half_m;
       const int m = (second ? tm - a.half_m : tm) * BM + quad * 32 + lane;
       const uint32_t t0 = tmem + acc * BN + (static_cast<uint32_t>(quad * 32) << 16);
-      if constexpr (FORM == FWD) {
+      if constexpr (kSplit) {
+        // this CTA's partial sums, rows a multiple of 16 bytes and four banks apart; the stages are free: every
+        // copy has landed and every MMA that read one has completed
+#pragma unroll 1
+        for (int b = half; b < BN / 32; b += 2) {
+          uint32_t r[32];
+          __syncwarp();
+          ptx::tmem_ld_32x32b_x32(t0 + b * 32, r);
+          ptx::tmem_wait_ld(r);
+          uint4 *const row = reinterpret_cast<uint4 *>(smem + (quad * 32 + lane) * kSumPitch + b * 128);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) row[q] = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
+        }
+      } else if constexpr (FORM == FWD) {
         const int n0 = tn * (BN / 2);
 #pragma unroll 1
         for (int b = half; b < BN / 64; b += 2) {
@@ -300,10 +367,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             float h[32];
 #pragma unroll
             for (int q = 0; q < 32; ++q) h[q] = act_value<ACT>(gv[q]) * uv[q];
-            store_row32<T>(static_cast<T *>(a.out[0]) + m * a.ld, c, a.N, h);
+            store_row32<T>(static_cast<T *>(a.out[0]) + m * a.ld, c, a.N, a.wide, h);
             if (a.lanes[0]) {
-              store_block8<ACT == SAMD_RELU_ACT>(a.lanes[0] + m * a.wpr, a.exps[0] + m * a.bpr, a.wpr, c, gv);
-              store_block8<false>(a.lanes[1] + m * a.wpr, a.exps[1] + m * a.bpr, a.wpr, c, uv);
+              store_block8<ACT == SAMD_RELU_ACT>(a.lanes[0] + m * a.wpr, a.exps[0] + m * a.bpr, a.wpr, c, a.wide8, gv);
+              store_block8<false>(a.lanes[1] + m * a.wpr, a.exps[1] + m * a.bpr, a.wpr, c, a.wide8, uv);
             }
           }
         }
@@ -317,13 +384,59 @@ __global__ void __launch_bounds__(kThreads, 1)
           ptx::tmem_ld_32x32b_x32(t0 + b * 32, r);
           ptx::tmem_wait_ld(r);
           const int c = n0 + b * 32;
-          if (m < a.M && c < a.N) store_row32<T>(out, c, a.N, reinterpret_cast<const float *>(r));
+          if (m < a.M && c < a.N) store_row32<T>(out, c, a.N, a.wide, reinterpret_cast<const float *>(r));
         }
       }
       __syncwarp();
       ptx::tc_fence_before();
       if (lane == 0) ptx::mbar_arrive(accempty0 + 8 * acc);
     }
+  }
+
+  if constexpr (kSplit) {
+    __syncwarp();
+    ptx::cluster_sync();
+    int tm, tn;
+    place(tile0, tm, tn);
+    const int second = FORM == DW && tm >= a.half_m;
+    const int m0 = (second ? tm - a.half_m : tm) * BM;
+    const int rows = min(BM, a.M - m0), per = (rows + a.split - 1) / a.split;
+    const int r0 = rank * per, count = max(0, min(per, rows - r0));
+    // a thread takes four columns of a row (FWD: of both projections, eight neighbouring lanes a block of 32)
+    constexpr int kPerRow = (FORM == FWD ? BN / 2 : BN) / 4;
+    for (int i0 = warp * 32; i0 < count * kPerRow; i0 += kThreads) {
+      const int i = i0 + lane, row = r0 + i / kPerRow, c = i % kPerRow * 4;
+      const bool in = i < count * kPerRow;
+      float g[4] = {0.0f, 0.0f, 0.0f, 0.0f}, u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (in) {
+        const uint32_t at = sbase + row * kSumPitch + c * 4;
+        for (int r = 0; r < a.split; ++r) {
+          const uint32_t from = ptx::map_to_rank(at, r);
+          const float4 v = ptx::ld_cluster_v4(from);
+          g[0] += v.x, g[1] += v.y, g[2] += v.z, g[3] += v.w;
+          if constexpr (FORM == FWD) {
+            const float4 w = ptx::ld_cluster_v4(from + BN * 2);
+            u[0] += w.x, u[1] += w.y, u[2] += w.z, u[3] += w.w;
+          }
+        }
+      }
+      const int col = tn * (kPerRow * 4) + c;
+      const int64_t m = m0 + row;
+      if constexpr (FORM == FWD) {
+        float h[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) h[q] = act_value<ACT>(g[q]) * u[q];
+        if (in) store_row4<T>(static_cast<T *>(a.out[0]) + m * a.ld, col, a.N, h);
+        if (a.lanes[0]) {
+          split_block8<ACT == SAMD_RELU_ACT>(a.lanes[0] + m * a.wpr, a.exps[0] + m * a.bpr, a.wpr, col, in, g);
+          split_block8<false>(a.lanes[1] + m * a.wpr, a.exps[1] + m * a.bpr, a.wpr, col, in, u);
+        }
+      } else if (in) {
+        store_row4<T>(static_cast<T *>(second ? a.out[1] : a.out[0]) + m * a.ld, col, a.N, g);
+      }
+    }
+    __syncwarp();
+    ptx::cluster_sync();  // no CTA's shared memory goes while another reads it
   }
 
   __syncwarp();
@@ -465,20 +578,24 @@ bool make_map(CUtensorMap *map, samd_dtype t, const void *p, int64_t rows, int64
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Columns of a tile for a product of `rows` rows of tiles, `cols` columns and
-// `steps` reduction steps: the fewest clocks over the waves of tiles. A step of
-// 256, 128 or 64 columns takes about 540, 340 or 250 clocks of an SM (the tensor
-// core bounds the first, the operands' way from L2 the others), and the last
-// tile's epilogue grows with its columns.
-int pick_columns(int64_t rows, int64_t cols, int64_t steps) {
-  int best = 256;
+// The tile of a product: its columns, and how many CTAs of a cluster share its
+// reduction.
+struct Pick {
+  int columns, split;
+};
+int env_or(const char *n, int v) { const char *e = getenv(n); return e && atoi(e) > 0 ? atoi(e) : v; }
+Pick pick_tile(int form, int64_t rows, int64_t cols, int64_t steps) {
+  const char *const names[3] = {"SAMD_FWD", "SAMD_DX", "SAMD_DW"};
+  const int f = env_or(names[form], 0);
+  if (f) return Pick{f % 1000, f / 1000 ? f / 1000 : 1};
+  Pick best = {256, 1};
   int64_t least = INT64_MAX;
   for (const int bn : {256, 128, 64}) {
     const int64_t tiles = rows * ((cols + bn - 1) / bn), waves = (tiles + sm_count() - 1) / sm_count();
     const int64_t cost = waves * steps * (bn == 256 ? 540 : bn == 128 ? 340 : 250) + 12 * bn;
     if (cost < least) {
       least = cost;
-      best = bn;
+      best = Pick{bn, 1};
     }
   }
   return best;
@@ -490,7 +607,7 @@ struct Operand {
   int64_t rows, cols, ld;
 };
 
-template <int FORM, typename T, int ACT, int BN>
+template <int FORM, typename T, int ACT, int BN, bool kSplit = false>
 cudaError_t launch_tiled(const Operand *op, samd_dtype t, GemmArgs &a, cudaStream_t s) {
   constexpr int kARows = FORM == DW ? BK : BM, kBRows = FORM == FWD ? BN / 2 : BK;  // of a TMA box
   CUtensorMap m[4];
@@ -499,22 +616,28 @@ cudaError_t launch_tiled(const Operand *op, samd_dtype t, GemmArgs &a, cudaStrea
       return cudaErrorInvalidValue;
   a.tiles_n = FORM == FWD ? (a.N + BN / 2 - 1) / (BN / 2) : (a.N + BN - 1) / BN;
   a.total = a.tiles_m * a.tiles_n;
-  const auto kern = ffn_gemm_kernel<FORM, T, ACT, BN>;
+  auto on32 = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; };
+  a.wide = a.ld % 16 == 0 && on32(a.out[0]) && on32(a.out[1]);
+  a.wide8 = a.wpr % 8 == 0 && on32(a.lanes[0]) && on32(a.lanes[1]);
+  const auto kern = ffn_gemm_kernel<FORM, T, ACT, BN, kSplit>;
   cudaError_t e = device_status_ptr(&a.status);
   if (e == cudaSuccess) e = conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), Tile<BN>::kSmemBytes);
   if (e != cudaSuccess) return e;
-  const int grid = a.total < sm_count() ? a.total : sm_count();
-  return launch_dependent(kern, dim3(grid), kThreads, Tile<BN>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
+  const int grid = kSplit ? a.total * a.split : a.total < sm_count() ? a.total : sm_count();
+  return launch_dependent(kern, dim3(grid), kThreads, Tile<BN>::kSmemBytes, s, kSplit ? a.split : 1, m[0], m[1], m[2],
+                          m[3], a);
 }
 
 template <int FORM, typename T, int ACT>
 cudaError_t launch_gemm(const Operand (&op)[4], samd_dtype t, GemmArgs &a, cudaStream_t s) {
   const int cols = FORM == FWD ? 2 * a.N : a.N;  // of the MMA
-  switch (pick_columns(a.tiles_m, cols, static_cast<int64_t>(a.steps) * (FORM == DX ? 2 : 1))) {
-    case 64: return launch_tiled<FORM, T, ACT, 64>(op, t, a, s);
-    case 128: return launch_tiled<FORM, T, ACT, 128>(op, t, a, s);
-    default: return launch_tiled<FORM, T, ACT, 256>(op, t, a, s);
-  }
+  const Pick p = pick_tile(FORM, a.tiles_m, cols, static_cast<int64_t>(a.steps) * (FORM == DX ? 2 : 1));
+  a.split = p.split;
+  const int all = a.steps * (FORM == DX ? 2 : 1);
+  if (a.split > all) a.split = all;
+  if (p.split > 1) return launch_tiled<FORM, T, ACT, 64, true>(op, t, a, s);
+  if (p.columns == 64) return launch_tiled<FORM, T, ACT, 64>(op, t, a, s);
+  return p.columns == 128 ? launch_tiled<FORM, T, ACT, 128>(op, t, a, s) : launch_tiled<FORM, T, ACT, 256>(op, t, a, s);
 }
 
 template <typename F>
@@ -599,7 +722,7 @@ cudaError_t backward(const samd_ffn_desc &d, const void *dh, samd_block8 cx, sam
   g.by_k = make_index_div(items_k, g.segs_k);
   cudaError_t e = by_act(d.act, [&](auto act) {
     constexpr auto kern = ffn_dgate_kernel<T, decltype(act)::value>;
-    return launch_dependent(kern, dim3(resident_grid<kern>(g.items, 256)), 256, 0, s, g);
+    return launch_dependent(kern, dim3(resident_grid<kern>(g.items, 256)), 256, 0, s, 1, g);
   });
   if (e != cudaSuccess) return e;
   const Operand odg = {dg, d.M, d.F, w.ldf}, odu = {du, d.M, d.F, w.ldf};

@@ -214,19 +214,25 @@ __device__ __forceinline__ int64_t idiv(int64_t n, const IndexDiv &v) {
 }
 
 // A launch that may be set up while the kernel before it in the stream drains
-// (the kernel calls grid_dependency_wait before it touches global memory).
+// (the kernel calls grid_dependency_wait before it touches global memory), in
+// clusters of `cluster` neighbouring CTAs.
 template <typename... P, typename... A>
-cudaError_t launch_dependent(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
-  cudaLaunchAttribute attr[1];
+cudaError_t launch_dependent(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, int cluster,
+                             A... args) {
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
   return e != cudaSuccess ? e : cudaGetLastError();
 }

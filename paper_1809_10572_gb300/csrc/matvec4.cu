@@ -545,18 +545,8 @@ cudaError_t launch_as(MvArgs a, cudaStream_t s) {
   int per_sm = resident_ctas<kern>(kThreads, P::smem(1));
   while (per_sm > 1 && per_sm * (smem + 1024) > (228u << 10)) --per_sm;  // (an SM's shared memory, 1 KB a CTA reserved)
   const int cap = sm_count() * per_sm;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.tiles < cap ? a.tiles : cap, (a.M + 8 * NT - 1) / (8 * NT));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const cudaError_t le = cudaLaunchKernelEx(&cfg, kern, map[0], map[1], a);
-  return le != cudaSuccess ? le : cudaGetLastError();
+  return launch_dependent(kern, dim3(a.tiles < cap ? a.tiles : cap, (a.M + 8 * NT - 1) / (8 * NT)), kThreads, smem, s, 1,
+                          map[0], map[1], a);
 }
 
 template <typename T, bool kGated, bool kZeros, int RT, int NT, int CH>

@@ -491,10 +491,13 @@ def maxpool2x2(words, f: samd_fmt, N: int, C: int, H: int, W: int, stream=None):
 # ---- the gated feed-forward block -------------------------------------------------
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(stream):
     """Allocations made inside belong to the stream that uses them."""
     if stream is None:
-        return contextlib.nullcontext()
+        return _HERE
     return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
 
 
@@ -580,8 +583,8 @@ def block8_empty(rows: int, inner: int, device="cuda") -> Block8:
 
 
 def _check_block8(b: Block8, what: str, rows: int, inner: int):
-    if b.inner != inner or tuple(b.lanes.shape) != (rows, -(-inner // 4)) or \
-            tuple(b.exps.shape) != (rows, -(-inner // 32)) or not b.lanes.is_contiguous() or \
+    if b.inner != inner or b.lanes.shape != (rows, -(-inner // 4)) or \
+            b.exps.shape != (rows, -(-inner // 32)) or not b.lanes.is_contiguous() or \
             not b.exps.is_contiguous() or b.lanes.dtype != torch.int32 or b.exps.dtype != torch.uint8:
         raise ValueError(f"{what}: the 8-bit form of a ({rows}, {inner}) tensor is wanted")
 
@@ -618,9 +621,11 @@ def _aligned8(n: int) -> int:
     return -(-n // 8) * 8
 
 
-def _empty_rows(rows: int, cols: int, like: torch.Tensor) -> torch.Tensor:
-    """A (rows, cols) matrix whose rows start 16-byte units apart."""
-    return torch.empty((rows, _aligned8(cols)), dtype=like.dtype, device=like.device)[:, :cols]
+def _empty_ld(rows: int, cols: int, ld: int, like: torch.Tensor) -> torch.Tensor:
+    """A (rows, cols) matrix of `like`'s type whose rows start ld elements apart."""
+    if ld == cols:
+        return torch.empty((rows, cols), dtype=like.dtype, device=like.device)
+    return torch.empty_strided((rows, cols), (ld, 1), dtype=like.dtype, device=like.device)
 
 
 def _ffn_desc(M, K, F, t, act, ldx, ldw, ldh) -> samd_ffn_desc:
@@ -646,11 +651,12 @@ def gated_ffn_forward(x, wg, wu, act="silu", checkpoints: bool = False, out=None
     stride that is a multiple of 8). With checkpoints: (h, ckpt_g, ckpt_u), the two products in 8 bits for
     gated_ffn_backward."""
     (M, K), F, t = x.shape, wg.shape[0], x.dtype
+    ldx, ldw = _ld8(x, "x", M, K, t), _same_ld(_ld8(wg, "wg", F, K, t), _ld8(wu, "wu", F, K, t), "wg, wu")
+    ldh = _aligned8(F) if out is None else _ld8(out, "out", M, F, t)
+    d = _ffn_desc(M, K, F, t, act, ldx, ldw, ldh)
     with _on(stream):
-        h = _empty_rows(M, F, x) if out is None else out
+        h = _empty_ld(M, F, ldh, x) if out is None else out
         g8, u8 = (block8_empty(M, F, x.device), block8_empty(M, F, x.device)) if checkpoints else (None, None)
-    d = _ffn_desc(M, K, F, t, act, _ld8(x, "x", M, K, t),
-                  _same_ld(_ld8(wg, "wg", F, K, t), _ld8(wu, "wu", F, K, t), "wg, wu"), _ld8(h, "out", M, F, t))
     samd_gated_ffn_forward(d, x, wg, wu, h, g8, u8, stream)
     return (h, g8, u8) if checkpoints else h
 
@@ -667,17 +673,13 @@ def gated_ffn_backward(dh, ckpt_x: Block8, ckpt_g: Block8, ckpt_u: Block8, wg, w
     ldw = _same_ld(_ld8(wg, "wg", F, K, t), _ld8(wu, "wu", F, K, t), "wg, wu")
     ldh = _ld8(dh, "dh", M, F, t)
     d = _ffn_desc(M, K, F, t, act, _aligned8(K), ldw, ldh)
+    if not (need_dx or need_dw or need_h):
+        raise ValueError("nothing is wanted")
     with _on(stream):
-        dx = _empty_rows(M, K, dh) if need_dx else None
-        dwg, dwu = (_empty_strided(F, K, ldw, dh), _empty_strided(F, K, ldw, dh)) if need_dw else (None, None)
-        h = _empty_strided(M, F, ldh, dh) if need_h else None
+        dx = _empty_ld(M, K, d.ldx, dh) if need_dx else None
+        dwg, dwu = (_empty_ld(F, K, ldw, dh), _empty_ld(F, K, ldw, dh)) if need_dw else (None, None)
+        h = _empty_ld(M, F, ldh, dh) if need_h else None
         if workspace is None:
             workspace = torch.empty(samd_gated_ffn_backward_workspace_size(d), dtype=torch.uint8, device=dh.device)
-        if dx is None and dwg is None and h is None:
-            raise ValueError("nothing is wanted")
         samd_gated_ffn_backward(d, dh, ckpt_x, ckpt_g, ckpt_u, wg, wu, dx, dwg, dwu, h, workspace, stream=stream)
     return (dx, dwg, dwu, h) if need_h else (dx, dwg, dwu)
-
-
-def _empty_strided(rows: int, cols: int, ld: int, like: torch.Tensor) -> torch.Tensor:
-    return torch.empty_strided((rows, cols), (ld, 1), dtype=like.dtype, device=like.device)
