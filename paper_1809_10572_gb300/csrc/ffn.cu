@@ -224,64 +224,64 @@ __global__ void __launch_bounds__(kThreads, 1)
   };
 
   if (warp == 0) {
-    if (lane == 0) {
-      int s = 0, loaded = 0;
-      uint32_t par = 1;
-      bool ok = true;
-      for (int tile = tile0; ok && tile < a.total; tile += tile_step) {
-        int tm, tn;
-        place(tile, tm, tn);
-        const int second = FORM == DW && tm >= a.half_m;
-        const int m0 = (second ? tm - a.half_m : tm) * BM, n0 = tn * (FORM == FWD ? BN / 2 : BN);
-        for (int k = k0; k < steps; k += KS) {
-          // A stage is armed again when the MMAs that read it have completed,
-          // and they were issued behind a wait for its copies.
-          if (loaded == kStages) {
-            ok = ptx::mbar_wait(empty0 + 8 * s, par, a.status, SAMD_ETIMEOUT, kWaitLimitNs);
-            if (!ok) break;
-          } else {
-            ++loaded;
-          }
-          const int now = KS == 1 ? 1 : min(KS, steps - k);  // steps of this stage
-          const uint32_t full = full0 + 8 * s;
-          ptx::mbar_arrive_expect_tx(full, now * kStepBytes);
+    const uint32_t leader = ptx::elect_one() ? 1u : 0u;
+    int s = 0, loaded = 0;
+    uint32_t par = 1;
+    bool ok = true;
+    for (int tile = tile0; ok && tile < a.total; tile += tile_step) {
+      int tm, tn;
+      place(tile, tm, tn);
+      const int second = FORM == DW && tm >= a.half_m;
+      const int m0 = (second ? tm - a.half_m : tm) * BM, n0 = tn * (FORM == FWD ? BN / 2 : BN);
+      for (int k = k0; k < steps; k += KS) {
+        // A stage is armed again when the MMAs that read it have completed,
+        // and they were issued behind a wait for its copies.
+        if (loaded == kStages) {
+          ok = warp_wait(empty0 + 8 * s, par, a.status);
+          if (!ok) break;
+        } else {
+          ++loaded;
+        }
+        const int now = KS == 1 ? 1 : min(KS, steps - k);  // steps of this stage
+        const uint32_t full = full0 + 8 * s;
+        ptx::mbar_arrive_expect_tx_if(leader, full, now * kStepBytes);
 #pragma unroll
-          for (int j = 0; j < KS; ++j) {
-            if (j < now) {
-              const uint32_t sa = sbase + s * kStageBytes + j * kStepBytes, sb = sa + kABytes;
-              const bool seg = FORM == DX && k + j >= a.steps;
-              const int kk = (seg ? k + j - a.steps : k + j) * BK;
-              const CUtensorMap *const A = (FORM == DX ? seg : FORM == DW ? second != 0 : false) ? &ma1 : &ma0;
-              const CUtensorMap *const B = FORM == DX && seg ? &mb1 : &mb0;
-              if constexpr (kAMn) {
-                ptx::tma_load_2d(sa, A, m0, kk, full);
-                ptx::tma_load_2d(sa + kABytes / 2, A, m0 + 64, kk, full);
-              } else {
-                ptx::tma_load_2d(sa, A, kk, m0, full);
-              }
-              if constexpr (FORM == FWD) {
-                ptx::tma_load_2d(sb, &mb0, kk, n0, full);
-                ptx::tma_load_2d(sb + kBBytes / 2, &mb1, kk, n0, full);
-              } else {
+        for (int j = 0; j < KS; ++j) {
+          if (j < now) {
+            const uint32_t sa = sbase + s * kStageBytes + j * kStepBytes, sb = sa + kABytes;
+            const bool seg = FORM == DX && k + j >= a.steps;
+            const int kk = (seg ? k + j - a.steps : k + j) * BK;
+            const CUtensorMap *const A = (FORM == DX ? seg : FORM == DW ? second != 0 : false) ? &ma1 : &ma0;
+            const CUtensorMap *const B = FORM == DX && seg ? &mb1 : &mb0;
+            if constexpr (kAMn) {
+              ptx::tma_load_2d_if(leader, sa, A, m0, kk, full);
+              ptx::tma_load_2d_if(leader, sa + kABytes / 2, A, m0 + 64, kk, full);
+            } else {
+              ptx::tma_load_2d_if(leader, sa, A, kk, m0, full);
+            }
+            if constexpr (FORM == FWD) {
+              ptx::tma_load_2d_if(leader, sb, &mb0, kk, n0, full);
+              ptx::tma_load_2d_if(leader, sb + kBBytes / 2, &mb1, kk, n0, full);
+            } else {
 #pragma unroll
-                for (int q = 0; q < BN / 64; ++q) ptx::tma_load_2d(sb + q * (64 * BK * 2), B, n0 + 64 * q, kk, full);
-              }
+              for (int q = 0; q < BN / 64; ++q)
+                ptx::tma_load_2d_if(leader, sb + q * (64 * BK * 2), B, n0 + 64 * q, kk, full);
             }
           }
-          if (++s == kStages) {
-            s = 0;
-            par ^= 1;
-          }
+        }
+        if (++s == kStages) {
+          s = 0;
+          par ^= 1;
         }
       }
-      // the CTA does not exit with a copy in flight: the ring's last round,
-      // oldest first
-      int quiet = 0;
-      for (int k = 0; k < loaded; ++k) {
-        int q = loaded == kStages ? s + k : k;
-        if (q >= kStages) q -= kStages;
-        ptx::mbar_wait_bounded(full0 + 8 * q, q < s ? par ^ 1u : par, &quiet, kWaitLimitNs / 10);
-      }
+    }
+    // the CTA does not exit with a copy in flight: the ring's last round,
+    // oldest first
+    int quiet = 0;
+    for (int k = 0; k < loaded; ++k) {
+      int q = loaded == kStages ? s + k : k;
+      if (q >= kStages) q -= kStages;
+      ptx::mbar_wait_bounded(full0 + 8 * q, q < s ? par ^ 1u : par, &quiet, kWaitLimitNs / 10);
     }
   } else if (warp == 1) {
     const uint32_t leader = ptx::elect_one() ? 1u : 0u;
