@@ -21,7 +21,7 @@
 // Between FWD and the others an elementwise kernel forms dg and du, rounded to
 // the operands' type: with fp32 sums this is the one rounding between the
 // gradients' factors and their sums.
-#include <cstdlib>
+#include <mutex>
 #include <type_traits>
 
 #include "ffn_internal.cuh"
@@ -562,7 +562,7 @@ __global__ void __launch_bounds__(256) ffn_dgate_kernel(const DgateArgs a) {
 
 // ---- host side -------------------------------------------------------------------
 
-int64_t round_up8(int64_t v) { return (v + 7) / 8 * 8; }
+int64_t round_up64(int64_t v) { return (v + 63) / 64 * 64; }
 size_t round_up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // A tensor of `rows` rows of `cols` 16-bit elements, read in boxes of 64
@@ -583,22 +583,65 @@ bool make_map(CUtensorMap *map, samd_dtype t, const void *p, int64_t rows, int64
 struct Pick {
   int columns, split;
 };
-int env_or(const char *n, int v) { const char *e = getenv(n); return e && atoi(e) > 0 ? atoi(e) : v; }
-Pick pick_tile(int form, int64_t rows, int64_t cols, int64_t steps) {
-  const char *const names[3] = {"SAMD_FWD", "SAMD_DX", "SAMD_DW"};
-  const int f = env_or(names[form], 0);
-  if (f) return Pick{f % 1000, f / 1000 ? f / 1000 : 1};
+// The least estimate over the tiles, in ns, from times measured on one GB300: a
+// reduction step of a tile of 256, 128 or 64 columns takes 330, 215 or 150 (the
+// operands' way into the SM bounds the narrow ones); start and end of a launch
+// 1500 and five a column of the last tile (FWD: 6000, its epilogue hides less).
+// A tile whose reduction is split over a cluster: steps of 64 columns, 3300 for
+// start and meeting (FWD: 6000), and 2000 more for every further wave of
+// clusters. For 16 tokens by 1024 by 4096, dx: 23.3 us unsplit, 8.6 over four
+// CTAs.
+template <typename Clusters>
+Pick pick_tile(int form, int64_t rows, int64_t cols, int64_t steps, Clusters clusters) {
   Pick best = {256, 1};
   int64_t least = INT64_MAX;
-  for (const int bn : {256, 128, 64}) {
-    const int64_t tiles = rows * ((cols + bn - 1) / bn), waves = (tiles + sm_count() - 1) / sm_count();
-    const int64_t cost = waves * steps * (bn == 256 ? 540 : bn == 128 ? 340 : 250) + 12 * bn;
+  auto offer = [&](Pick p, int64_t cost) {
     if (cost < least) {
       least = cost;
-      best = Pick{bn, 1};
+      best = p;
     }
+  };
+  for (const int bn : {256, 128, 64}) {
+    const int64_t tiles = rows * ((cols + bn - 1) / bn), waves = (tiles + sm_count() - 1) / sm_count();
+    offer(Pick{bn, 1}, waves * steps * (bn == 256 ? 330 : bn == 128 ? 215 : 150) + (form == FWD ? 6000 : 1500 + 5 * bn));
+  }
+  const int64_t tiles = rows * ((cols + 63) / 64);
+  for (const int split : {2, 4, 8}) {
+    if (split > steps || 2 * tiles > sm_count()) break;
+    const int64_t fit = clusters(split);
+    if (fit < 1) break;
+    const int64_t waves = (tiles + fit - 1) / fit;
+    offer(Pick{64, split}, waves * ((steps + split - 1) / split * 150 + 2000) + (form == FWD ? 4000 : 1300));
   }
   return best;
+}
+
+// Clusters of `split` CTAs of the kernel that the GPU holds at once; asked once for each size.
+template <auto Kern>
+int resident_clusters(int split, size_t smem) {
+  static std::mutex mu;
+  static int known[9];  // 0: not asked yet, -1: none
+  std::lock_guard<std::mutex> lock(mu);
+  if (known[split] == 0) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = split;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(split * sm_count());
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, Kern, &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();  // the query's own error; the launch reports any other
+      n = 0;
+    }
+    known[split] = n > 0 ? n : -1;
+  }
+  return known[split];
 }
 
 // The operands of a product before its tile is picked.
@@ -631,10 +674,15 @@ cudaError_t launch_tiled(const Operand *op, samd_dtype t, GemmArgs &a, cudaStrea
 template <int FORM, typename T, int ACT>
 cudaError_t launch_gemm(const Operand (&op)[4], samd_dtype t, GemmArgs &a, cudaStream_t s) {
   const int cols = FORM == FWD ? 2 * a.N : a.N;  // of the MMA
-  const Pick p = pick_tile(FORM, a.tiles_m, cols, static_cast<int64_t>(a.steps) * (FORM == DX ? 2 : 1));
+  const int64_t steps = static_cast<int64_t>(a.steps) * (FORM == DX ? 2 : 1);
+  const Pick p = pick_tile(FORM, a.tiles_m, cols, steps, [](int split) {
+    constexpr auto kern = ffn_gemm_kernel<FORM, T, ACT, 64, true>;
+    const size_t smem = Tile<64>::kSmemBytes;
+    return conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), smem) == cudaSuccess
+               ? resident_clusters<kern>(split, smem)
+               : 0;
+  });
   a.split = p.split;
-  const int all = a.steps * (FORM == DX ? 2 : 1);
-  if (a.split > all) a.split = all;
   if (p.split > 1) return launch_tiled<FORM, T, ACT, 64, true>(op, t, a, s);
   if (p.columns == 64) return launch_tiled<FORM, T, ACT, 64>(op, t, a, s);
   return p.columns == 128 ? launch_tiled<FORM, T, ACT, 128>(op, t, a, s) : launch_tiled<FORM, T, ACT, 256>(op, t, a, s);
@@ -672,15 +720,15 @@ cudaError_t forward(const samd_ffn_desc &d, const void *x, const void *wg, const
 }
 
 // The workspace: dg and du (M rows of F) and x (M rows of K), each row a
-// multiple of eight elements.
+// multiple of 64 elements (whole 128-byte lines, what a row of a TMA box is).
 struct Workspace {
   size_t dg, du, x, bytes;
   int64_t ldf, ldk;
 };
 Workspace plan_workspace(const samd_ffn_desc &d) {
   Workspace w;
-  w.ldf = round_up8(d.F);
-  w.ldk = round_up8(d.K);
+  w.ldf = round_up64(d.F);
+  w.ldk = round_up64(d.K);
   const size_t f = round_up256(static_cast<size_t>(d.M) * w.ldf * 2), k = round_up256(static_cast<size_t>(d.M) * w.ldk * 2);
   w.dg = 0;
   w.du = f;

@@ -94,13 +94,12 @@ struct Offset;
 template <>
 struct Offset<__nv_bfloat16> {
   uint32_t a;
-  __device__ __forceinline__ void set(uint32_t z) { a = 0x43004300u | z | z << 16; }
+  __device__ __forceinline__ void set(uint32_t zz) { a = 0x43004300u | zz; }  // z in both halves
 };
 template <>
 struct Offset<__half> {
   uint32_t a, b;
-  __device__ __forceinline__ void set(uint32_t z) {
-    const uint32_t zz = z | z << 16;
+  __device__ __forceinline__ void set(uint32_t zz) {
     a = 0x64006400u | zz;
     b = 0x54005400u | zz << 4;
   }
@@ -266,15 +265,27 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
     }
     if constexpr (kZeros) {
       const int64_t tile_g = n0 * a.groups + ((static_cast<int64_t>(blk) * KB) >> a.group_shift);
-      constexpr int kWords = P::kGroups == 1 ? 1 : P::kGroups <= 4 ? 2 : 3;
+      if (P::kGroups >= 4 && a.s_vec) {
 #pragma unroll
-      for (int i = 0; i < (kRows * kWords + 31) / 32; ++i) {
-        const int idx = i * 32 + lane, row = idx / kWords, w = idx % kWords, mat = kGated && row >= 16 * RT;
-        if (kRows * kWords % 32 == 0 || row < kRows) {
-          const int64_t n = tile_g + min(row - mat * 16 * RT, last) * a.groups;
-          const int64_t at = (n & ~int64_t(3)) + w * 4, left = a.n_scales - at;
-          ptx::cp_async_4(ss + P::kZOff + row * P::kZPitch + w * 4, a.zeros[mat] + (left > 0 ? at : 0),
-                          left >= 4 ? 4u : left > 0 ? static_cast<uint32_t>(left) : 0u);
+        for (int i = 0; i < (kRows + 31) / 32; ++i) {
+          const int row = i * 32 + lane, mat = kGated && row >= 16 * RT;
+          if (kRows % 32 == 0 || row < kRows) {
+            const uint8_t *const src = a.zeros[mat] + tile_g + min(row - mat * 16 * RT, last) * a.groups;
+            if constexpr (P::kGroups == 8) ptx::cp_async_8(ss + P::kZOff + row * P::kZPitch, src, 8);
+            if constexpr (P::kGroups == 4) ptx::cp_async_4(ss + P::kZOff + row * P::kZPitch, src, 4);
+          }
+        }
+      } else {
+        constexpr int kWords = P::kGroups == 1 ? 1 : P::kGroups <= 4 ? 2 : 3;
+#pragma unroll
+        for (int i = 0; i < (kRows * kWords + 31) / 32; ++i) {
+          const int idx = i * 32 + lane, row = idx / kWords, w = idx % kWords, mat = kGated && row >= 16 * RT;
+          if (kRows * kWords % 32 == 0 || row < kRows) {
+            const int64_t n = tile_g + min(row - mat * 16 * RT, last) * a.groups;
+            const int64_t at = (n & ~int64_t(3)) + w * 4, left = a.n_scales - at;
+            ptx::cp_async_4(ss + P::kZOff + row * P::kZPitch + w * 4, a.zeros[mat] + (left > 0 ? at : 0),
+                            left >= 4 ? 4u : left > 0 ? static_cast<uint32_t>(left) : 0u);
+          }
         }
       }
     }
@@ -288,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
 
   const uint32_t flip = a.is_signed ? 0x00080008u : 0u;
   Offset<T> plain;  // without zero points: offset binary's 8 for signed lanes, else 0
-  plain.set(flip & 15u);
+  plain.set(flip);
 
   // the ring's next block to load, which runs ahead of the one in hand, over the CTA's tiles
   int l_tile = blockIdx.x, l_blk = warp, fill = 0, slot = 0, loaded = 0, used = 0;
@@ -340,10 +351,11 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
     for (int blk = warp; blk < a.nblk; blk += kWarps) {
       const int64_t k0 = static_cast<int64_t>(blk) * KB;
       // tokens first: their way through L1 overlaps the wait for the stage
+      const bool x_whole = a.x_vec && k0 + KB <= a.K;
       if constexpr (NT == 1) {
         if (g < tokens) {
           const T *const xr = x_lane + k0;
-          if (a.x_vec && k0 + KB <= a.K) {
+          if (x_whole) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) xq[c] = __ldg(reinterpret_cast<const uint4 *>(xr + c * 32));
           } else {
@@ -396,6 +408,31 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
             }
           }
         }
+      // and their zero points, four in a word
+      constexpr int kZW = (P::kGroups + 3) / 4;
+      uint32_t zraw[kTiles][2][kZW];
+      if constexpr (kZeros) {
+#pragma unroll
+        for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint8_t *const zp = st + P::kZOff + (r * 16 + g + 8 * h) * P::kZPitch;
+            if (P::kGroups >= 4 && a.s_vec) {
+#pragma unroll
+              for (int i = 0; i < kZW; ++i) zraw[r][h][i] = reinterpret_cast<const uint32_t *>(zp)[i];
+            } else {
+              const uint8_t *const zb = zp + ((first[r][h] + g0) & 3);
+#pragma unroll
+              for (int i = 0; i < kZW; ++i) {
+                zraw[r][h][i] = 0;
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                  if (4 * i + b < P::kGroups)
+                    zraw[r][h][i] |= static_cast<uint32_t>(zb[one_scale ? 0 : 4 * i + b]) << 8 * b;
+              }
+            }
+          }
+      }
       if (k0 + KB > a.K) {
         // The last block of a row: past the row's end lanes and tokens are zero
         // and add nothing, whatever their scale, unless that is not finite.
@@ -422,7 +459,8 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
               const uint32_t w = sraw[r][h][gi / 2];
               s[r][h] = f32_of_bits<T>(static_cast<uint16_t>(gi & 1 ? w >> 16 : w));
               if constexpr (kZeros)
-                o[r][h].set(st[P::kZOff + (r * 16 + g + 8 * h) * P::kZPitch + ((first[r][h] + g0) & 3) + (one_scale ? 0 : gi)] & 15u);
+                // byte gi % 4, low four bits, in both halves
+                o[r][h].set(__byte_perm(zraw[r][h][gi / 4], 0, 0x4040 | (gi & 3) | (gi & 3) << 8) & 0x000F000Fu);
               else
                 o[r][h] = plain;
             }
@@ -444,8 +482,13 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
                 if constexpr (NT == 1) {
                   q = xq[c];
                 } else {
-                  if (8 * j + g < tokens)
-                    q = load_x8<T>(x + (8 * j + g) * a.ldx, k0 + c * 32 + t * 8, a.K, a.x_vec);
+                  if (8 * j + g < tokens) {
+                    const T *const xr = x_lane + (8 * j) * a.ldx + k0 + c * 32;
+                    if (x_whole)
+                      q = __ldg(reinterpret_cast<const uint4 *>(xr));
+                    else
+                      q = load_x8<T>(x + (8 * j + g) * a.ldx, k0 + c * 32 + t * 8, a.K, a.x_vec);
+                  }
                 }
                 b[j][0] = __byte_perm(q.x, q.z, 0x5410);
                 b[j][1] = __byte_perm(q.x, q.z, 0x7632);
