@@ -132,11 +132,30 @@ __device__ __forceinline__ float f32_of_bits(uint16_t v) {
   return to_f32<T>(reinterpret_cast<const T &>(v));
 }
 
-// The lane's eight inputs k .. k + 7 of a token; those past K are zero and not read.
-template <typename T>
-__device__ __forceinline__ uint4 load_x8(const T *row, int64_t k, int K, bool vec) {
+// The lane's eight inputs k .. k + 7 of a token; those past K are zero and not read. Rows that are not 16-byte
+// aligned (kXVec false) are read by the 4-byte words that hold the inputs, shifted by half a word where those begin
+// in a word's middle (then with a ninth input of the row).
+template <typename T, bool kXVec>
+__device__ __forceinline__ uint4 load_x8(const T *row, int64_t k, int K) {
   const int64_t left = K - k;
-  if (vec && left >= 8) return __ldg(reinterpret_cast<const uint4 *>(row + k));
+  if constexpr (kXVec) {
+    if (left >= 8) return __ldg(reinterpret_cast<const uint4 *>(row + k));
+  } else {
+    if (left > 8) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(row + k);
+      const uint32_t *const p = reinterpret_cast<const uint32_t *>(at & ~uintptr_t(3));
+      const bool half = (at & 2) != 0;
+      uint32_t v[5];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __ldg(p + i);
+      v[4] = half ? __ldg(p + 4) : 0u;
+      if (half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(v[i], v[i + 1], 16);
+      }
+      return make_uint4(v[0], v[1], v[2], v[3]);
+    }
+  }
   uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -174,7 +193,7 @@ struct Mv {
   }
 };
 
-template <typename T, bool kGated, bool kZeros, int RT, int NT, int CH, int CPG>
+template <typename T, bool kGated, bool kZeros, bool kXVec, int RT, int NT, int CH, int CPG>
 __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_constant__ CUtensorMap map0,
                                                                 const __grid_constant__ CUtensorMap map1,
                                                                 const MvArgs a) {
@@ -351,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
     for (int blk = warp; blk < a.nblk; blk += kWarps) {
       const int64_t k0 = static_cast<int64_t>(blk) * KB;
       // tokens first: their way through L1 overlaps the wait for the stage
-      const bool x_whole = a.x_vec && k0 + KB <= a.K;
+      const bool x_whole = kXVec && k0 + KB <= a.K;
       if constexpr (NT == 1) {
         if (g < tokens) {
           const T *const xr = x_lane + k0;
@@ -360,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
             for (int c = 0; c < CH; ++c) xq[c] = __ldg(reinterpret_cast<const uint4 *>(xr + c * 32));
           } else {
 #pragma unroll
-            for (int c = 0; c < CH; ++c) xq[c] = load_x8<T>(x + g * a.ldx, k0 + c * 32 + t * 8, a.K, a.x_vec);
+            for (int c = 0; c < CH; ++c) xq[c] = load_x8<T, kXVec>(x + g * a.ldx, k0 + c * 32 + t * 8, a.K);
           }
         }
       }
@@ -487,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
                     if (x_whole)
                       q = __ldg(reinterpret_cast<const uint4 *>(xr));
                     else
-                      q = load_x8<T>(x + (8 * j + g) * a.ldx, k0 + c * 32 + t * 8, a.K, a.x_vec);
+                      q = load_x8<T, kXVec>(x + (8 * j + g) * a.ldx, k0 + c * 32 + t * 8, a.K);
                   }
                 }
                 b[j][0] = __byte_perm(q.x, q.z, 0x5410);
@@ -559,13 +578,13 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
   }
 }
 
-template <typename T, bool kGated, bool kZeros, int RT, int NT, int CH, int CPG>
+template <typename T, bool kGated, bool kZeros, bool kXVec, int RT, int NT, int CH, int CPG>
 cudaError_t launch_as(MvArgs a, cudaStream_t s) {
   using P = Mv<T, kGated, kZeros, RT, NT, CH, CPG>;
   a.nblk = (a.K + P::KB - 1) / P::KB;
   a.tiles = (a.N + 16 * RT - 1) / (16 * RT);
   a.s_vec = a.groups % P::kGroups == 0 && (1 << a.group_shift) * P::kGroups == P::KB;
-  constexpr auto kern = matvec4_kernel<T, kGated, kZeros, RT, NT, CH, CPG>;
+  constexpr auto kern = matvec4_kernel<T, kGated, kZeros, kXVec, RT, NT, CH, CPG>;
   CUtensorMap map[2] = {};
   if (a.tma) {
     // bytes of a row by rows, in boxes of one block of one tile, swizzled as the kernel's ldmatrix reads them
@@ -592,23 +611,35 @@ cudaError_t launch_as(MvArgs a, cudaStream_t s) {
                           map[0], map[1], a);
 }
 
-template <typename T, bool kGated, bool kZeros, int RT, int NT, int CH>
+template <typename T, bool kGated, bool kZeros, bool kXVec, int RT, int NT, int CH>
 cudaError_t launch_grouped(const MvArgs &a, cudaStream_t s) {
-  if (a.group_shift == 5) return launch_as<T, kGated, kZeros, RT, NT, CH, 1>(a, s);
-  if (a.group_shift == 6) return launch_as<T, kGated, kZeros, RT, NT, CH, 2>(a, s);
-  return launch_as<T, kGated, kZeros, RT, NT, CH, 4>(a, s);
+  if (a.group_shift == 5) return launch_as<T, kGated, kZeros, kXVec, RT, NT, CH, 1>(a, s);
+  if (a.group_shift == 6) return launch_as<T, kGated, kZeros, kXVec, RT, NT, CH, 2>(a, s);
+  return launch_as<T, kGated, kZeros, kXVec, RT, NT, CH, 4>(a, s);
 }
 
+// Which instance: 8, 16 or 32 tokens a pass. Up to eight: blocks of 256 inputs
+// where there are at least eight of them for the warps (K = 1024 leaves half
+// the warps idle with them), of 128 otherwise; two row tiles share a CTA's
+// tokens and its fixed work where that still gives every SM two CTAs' worth
+// (one token by 65536 x 4096: 45.7 us with one, 37.8 with two), with blocks of
+// 128 for more than two tokens, whose stages and sums would leave an SM one CTA.
 template <typename T, bool kGated, bool kZeros>
 cudaError_t launch_sized(const MvArgs &a, cudaStream_t s) {
   constexpr int kRT = kGated ? 1 : 2;
-  if (a.M > 16) return launch_grouped<T, kGated, kZeros, kRT, 4, 4>(a, s);
-  if (a.M > 8) return launch_grouped<T, kGated, kZeros, kRT, 2, 4>(a, s);
-  if (a.K < 2048) return launch_grouped<T, kGated, kZeros, 1, 1, 4>(a, s);
-  if (!kGated && a.N >= 9728)
-    return a.M <= 2 ? launch_grouped<T, kGated, kZeros, kRT, 1, 8>(a, s)
-                    : launch_grouped<T, kGated, kZeros, kRT, 1, 4>(a, s);
-  return launch_grouped<T, kGated, kZeros, 1, 1, 8>(a, s);
+  if (!a.x_vec) {
+    if (a.M > 16) return launch_grouped<T, kGated, kZeros, false, kRT, 4, 4>(a, s);
+    if (a.M > 8) return launch_grouped<T, kGated, kZeros, false, kRT, 2, 4>(a, s);
+    return launch_grouped<T, kGated, kZeros, false, 1, 1, 4>(a, s);
+  }
+  if (a.M > 16) return launch_grouped<T, kGated, kZeros, true, kRT, 4, 4>(a, s);
+  if (a.M > 8) return launch_grouped<T, kGated, kZeros, true, kRT, 2, 4>(a, s);
+  if (a.K < 2048) return launch_grouped<T, kGated, kZeros, true, 1, 1, 4>(a, s);
+  if constexpr (!kGated)
+    if (a.N >= 9728)
+      return a.M <= 2 ? launch_grouped<T, kGated, kZeros, true, 2, 1, 8>(a, s)
+                      : launch_grouped<T, kGated, kZeros, true, 2, 1, 4>(a, s);
+  return launch_grouped<T, kGated, kZeros, true, 1, 1, 8>(a, s);
 }
 
 template <typename T>

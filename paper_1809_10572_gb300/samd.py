@@ -16,7 +16,6 @@ import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
-from typing import NamedTuple
 
 import torch
 
@@ -292,7 +291,12 @@ def _weights4(lanes, scales, zeros) -> samd_weights4:
 
 def _block8(b) -> samd_block8:
     """Of a Block8, a pair (lanes, exps) of tensors or addresses, or None."""
-    return samd_block8(None, None) if b is None else samd_block8(_ptr(b[0]), _ptr(b[1]))
+    if b is None:
+        return samd_block8(None, None)
+    if isinstance(b, Block8) and b._buf is not None:
+        p = _ptr(b._buf)
+        return samd_block8(p, p + 4 * b._lane_words())
+    return samd_block8(_ptr(b[0]), _ptr(b[1]))
 
 
 def _act(act) -> int:
@@ -566,11 +570,38 @@ def _empty(like, rows: int, cols: int, stream) -> torch.Tensor:
         return torch.empty((rows, cols), dtype=like.dtype, device=like.device)
 
 
-class Block8(NamedTuple):
-    """An activation tensor in 8 bits (samd_block8): packed lanes (format block8_fmt()) and block exponents."""
-    lanes: torch.Tensor
-    exps: torch.Tensor
-    inner: int
+class Block8:
+    """An activation tensor of `rows` rows of `inner` elements in 8 bits (samd_block8): lanes, the packed rows (int32,
+    format block8_fmt()), and exps, the block exponents (uint8). block8_empty puts both into one allocation, of which
+    the two tensors are views that are made when they are asked for."""
+
+    __slots__ = ("rows", "inner", "_lanes", "_exps", "_buf")
+
+    def __init__(self, lanes: torch.Tensor | None, exps: torch.Tensor | None, inner: int, rows: int | None = None,
+                 buf: torch.Tensor | None = None):
+        self.rows, self.inner = lanes.shape[0] if rows is None else rows, inner
+        self._lanes, self._exps, self._buf = lanes, exps, buf
+
+    def _lane_words(self) -> int:
+        """Words of all rows, up to the exponents of a block8_empty (16-byte units)."""
+        return -(-self.rows * -(-self.inner // 4) // 4) * 4
+
+    @property
+    def lanes(self) -> torch.Tensor:
+        if self._lanes is None:
+            words = -(-self.inner // 4)
+            self._lanes = self._buf[:self.rows * words].view(self.rows, words)
+        return self._lanes
+
+    @property
+    def exps(self) -> torch.Tensor:
+        if self._exps is None:
+            n = -(-self.inner // 32)
+            self._exps = self._buf[self._lane_words():].view(torch.uint8)[:self.rows * n].view(self.rows, n)
+        return self._exps
+
+    def __getitem__(self, i):
+        return (self.lanes, self.exps)[i]
 
 
 def block8_fmt() -> samd_fmt:
@@ -578,15 +609,18 @@ def block8_fmt() -> samd_fmt:
 
 
 def block8_empty(rows: int, inner: int, device="cuda") -> Block8:
-    return Block8(torch.empty((rows, -(-inner // 4)), dtype=torch.int32, device=device),
-                  torch.empty((rows, -(-inner // 32)), dtype=torch.uint8, device=device), inner)
+    b = Block8(None, None, inner, rows)
+    b._buf = torch.empty(b._lane_words() + -(-rows * -(-inner // 32) // 4), dtype=torch.int32, device=device)
+    return b
 
 
 def _check_block8(b: Block8, what: str, rows: int, inner: int):
-    if b.inner != inner or b.lanes.shape != (rows, -(-inner // 4)) or \
-            b.exps.shape != (rows, -(-inner // 32)) or not b.lanes.is_contiguous() or \
-            not b.exps.is_contiguous() or b.lanes.dtype != torch.int32 or b.exps.dtype != torch.uint8:
-        raise ValueError(f"{what}: the 8-bit form of a ({rows}, {inner}) tensor is wanted")
+    if b.rows != rows or b.inner != inner:
+        raise ValueError(f"{what}: the 8-bit form of a ({rows}, {inner}) tensor is wanted, got ({b.rows}, {b.inner})")
+    if b._buf is None and (b.lanes.shape != (rows, -(-inner // 4)) or b.exps.shape != (rows, -(-inner // 32)) or
+                           not b.lanes.is_contiguous() or not b.exps.is_contiguous() or
+                           b.lanes.dtype != torch.int32 or b.exps.dtype != torch.uint8):
+        raise ValueError(f"{what}: contiguous int32 lanes and uint8 exponents of a ({rows}, {inner}) tensor are wanted")
 
 
 def block8_quantize(x: torch.Tensor, out: Block8 | None = None, stream=None) -> Block8:
@@ -608,12 +642,15 @@ def block8_dequantize(b: Block8, dtype: torch.dtype, out=None, stream=None) -> t
     """The values an 8-bit form stands for, as a matrix of `dtype`."""
     if dtype not in DTYPES:
         raise ValueError(f"dtype: {dtype}, wanted float16, bfloat16 or float32")
-    rows = b.lanes.shape[0]
-    _check_block8(b, "b", rows, b.inner)
+    rows, inner = b.rows, b.inner
+    _check_block8(b, "b", rows, inner)
     if out is None:
         with _on(stream):
-            out = torch.empty((rows, b.inner), dtype=dtype, device=b.lanes.device)
-    samd_block8_dequantize(dtype, b, rows, b.inner, out, _rows(out, "out", b.inner, rows, dtype), stream)
+            out = torch.empty((rows, inner), dtype=dtype, device=(b._lanes if b._buf is None else b._buf).device)
+        ldy = max(inner, 1)
+    else:
+        ldy = _rows(out, "out", inner, rows, dtype)
+    samd_block8_dequantize(dtype, b, rows, inner, out, ldy, stream)
     return out
 
 
