@@ -109,7 +109,8 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list[str] | N
             return obj
 
         # the slowest units (the kernel instantiations) first
-        todo = sorted(units(), key=lambda u: u[0] != INST_SRC)
+        slow = [os.path.join(CSRC, f) for f in ("matvec4_bf16.cu", "matvec4_f16.cu", "ffn.cu")] + [INST_SRC]
+        todo = sorted(units(), key=lambda u: slow.index(u[0]) if u[0] in slow else len(slow))
         with ThreadPoolExecutor(max_workers=max(1, min(len(todo), os.cpu_count() or 4))) as ex:
             objs = list(ex.map(compile_one, todo))
         out_tmp = os.path.join(tmp, "libsamd.so")

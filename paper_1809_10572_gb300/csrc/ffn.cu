@@ -47,6 +47,7 @@ struct Tile {
   static constexpr int kStageBytes = KS * kStepBytes;
   static constexpr int kStages = BN == 128 ? 3 : 4;
   static constexpr size_t kSmemBytes = 1024 + static_cast<size_t>(kStages) * kStageBytes + 256;
+  static_assert(kSmemBytes <= 227 * 1024 && 2 * BN <= 512, "shared and tensor memory of an SM");
 };
 constexpr uint64_t kWaitLimitNs = 1000000000ull;  // 1 s
 constexpr int kBand = 12;  // tiles along M that follow one another before the next along N
