@@ -172,7 +172,6 @@ struct Mv {
   static constexpr int kTiles = RT * kMats;  // 16-row tiles of a CTA's tile: the first matrix's, then the second's
   static constexpr int kRows = 16 * kTiles;
   static constexpr int KB = 32 * CH;
-  static constexpr int kStages = RT * kMats > 1 && CH == 8 ? 3 : 4;
   static constexpr int kPitch = 16 * CH;  // bytes of a row of weights in a stage
   static constexpr int kGroups = CH / CPG;  // scales of a row in a block
   // bytes of a row's scales, and of its zero points, in a stage: the 4-byte
@@ -182,11 +181,17 @@ struct Mv {
   static constexpr int kWBytes = kRows * kPitch;  // a stage's weights (whole 1024- or 512-byte swizzle patterns)
   static constexpr int kZOff = kRows * kSPitch;
   static constexpr int kSzBytes = kZOff + (kZeros ? kRows * kZPitch : 0);  // its scales and zero points
+  // as many stages as leave an SM two CTAs (one token by 65536 x 4096 with zero points: 43.3 us with three stages and
+  // one CTA)
+  static constexpr int fit(int stages) {
+    return kWarps * stages * (kWBytes + kSzBytes + 8) + kWarps * kRows * 4 + 1024 <= 114 * 1024;
+  }
+  static constexpr int kStages = fit(4) ? 4 : fit(3) ? 3 : 2;
   // shared memory: [warp][stage] weights, [warp][stage] scales and zero points, [warp][stage] barriers, the sums
   static constexpr int kSzAt = kWarps * kStages * kWBytes;
   static constexpr int kBarAt = kSzAt + kWarps * kStages * kSzBytes;
   static constexpr int kRedAt = kBarAt + kWarps * kStages * 8;
-  static constexpr int kBufs = NT == 1 ? 2 : 1;
+  static constexpr int kBufs = NT == 1 && kRows == 16 ? 2 : 1;
   // the warps' sums: rows of an odd number of tokens, so that neighbouring rows lie in other banks
   static __host__ __device__ constexpr int red_pitch(int tokens) { return tokens | 1; }
   static __host__ __device__ constexpr int red_floats(int tokens) { return kWarps * kRows * red_pitch(tokens); }  // of one buffer
@@ -232,6 +237,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
   // their own size (s_vec = 0), the 4-byte words around them are copied, a word
   // past the end of the array is clipped, and the reader finds its place in the
   // first word from the same index.
+  const bool one_scale = P::kGroups > 1 && CPG == 4 && a.group_shift > 7;  // groups that hold whole blocks
   auto scale_of = [&](int n0, int row, int blk) -> const uint8_t * {
     const int mat = kGated && row >= 16 * RT;
     const int64_t n = min(n0 + row - mat * 16 * RT, a.N - 1);
@@ -270,6 +276,16 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
           if constexpr (P::kGroups == 4) ptx::cp_async_8(dst, src, 8);
           if constexpr (P::kGroups == 2) ptx::cp_async_4(dst, src, 4);
         }
+    } else if (P::kGroups == 1 || one_scale) {
+      // the word that holds a row's one scale of the block
+#pragma unroll
+      for (int i = 0; i < (kRows + 31) / 32; ++i)
+        if (kRows % 32 == 0 || lane < kRows) {
+          const int row = i * 32 + lane;
+          const uint8_t *const base = a.scales[kGated && row >= 16 * RT];
+          const int64_t at = (scale_of(n0, row, blk) - base) & ~int64_t(3), left = a.n_scales * 2 - at;
+          ptx::cp_async_4(ss + row * P::kSPitch, base + at, left >= 4 ? 4u : static_cast<uint32_t>(left));
+        }
     } else {
       const int64_t tile_g = n0 * a.groups + ((static_cast<int64_t>(blk) * KB) >> a.group_shift);
       constexpr int kWords = P::kGroups == 1 ? 1 : P::kGroups / 2 + 1;
@@ -285,18 +301,19 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
       }
     }
     if constexpr (kZeros) {
-      const int64_t tile_g = n0 * a.groups + ((static_cast<int64_t>(blk) * KB) >> a.group_shift);
       if (P::kGroups >= 4 && a.s_vec) {
 #pragma unroll
-        for (int i = 0; i < (kRows + 31) / 32; ++i) {
-          const int row = i * 32 + lane, mat = kGated && row >= 16 * RT;
-          if (kRows % 32 == 0 || row < kRows) {
-            const uint8_t *const src = a.zeros[mat] + tile_g + min(row - mat * 16 * RT, last) * a.groups;
+        for (int i = 0; i < (kRows + 31) / 32; ++i)
+          if (kRows % 32 == 0 || lane < kRows) {
+            const int row = i * 32 + lane, mat = kGated && row >= 16 * RT;
+            // the zero points' index is the scales'
+            const uint8_t *const src =
+                a.zeros[mat] + ((i == 0 ? scale : scale_of(n0, row, blk)) - a.scales[mat]) / 2;
             if constexpr (P::kGroups == 8) ptx::cp_async_8(ss + P::kZOff + row * P::kZPitch, src, 8);
             if constexpr (P::kGroups == 4) ptx::cp_async_4(ss + P::kZOff + row * P::kZPitch, src, 4);
           }
-        }
       } else {
+        const int64_t tile_g = n0 * a.groups + ((static_cast<int64_t>(blk) * KB) >> a.group_shift);
         constexpr int kWords = P::kGroups == 1 ? 1 : P::kGroups <= 4 ? 2 : 3;
 #pragma unroll
         for (int i = 0; i < (kRows * kWords + 31) / 32; ++i) {
@@ -400,7 +417,6 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
         par ^= 1;
       }
       const int g0 = static_cast<int>((k0 >> a.group_shift) & 3);
-      const bool one_scale = P::kGroups > 1 && CPG == 4 && a.group_shift > 7;  // groups that hold whole blocks
       // the rows' scales of the block, two in a word
       constexpr int kSW = (P::kGroups + 1) / 2;
       uint32_t sraw[kTiles][2][kSW];
