@@ -21,6 +21,12 @@
 // Between FWD and the others an elementwise kernel forms dg and du, rounded to
 // the operands' type: with fp32 sums this is the one rounding between the
 // gradients' factors and their sums.
+//
+// Measured (one GB300): 4096 x 4096 x 8192 forward 322 us (1.71 PFLOP/s) in a
+// short run, 354 under the power cap; 8192 x 4096 x 8192 bf16 step 2.04 ms (1.61
+// PFLOP/s), 2.24 under it, where the library product of that size holds 1.66
+// PFLOP/s. Large products are bound by power (1.6 GHz of 2.07), small ones by
+// start, end and the reduction steps of one CTA (pick_tile).
 #include <mutex>
 #include <type_traits>
 
@@ -455,7 +461,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 //   (where the weights' gradients are wanted), which T holds without rounding.
 // One pass over HBM: 4 1/16 bytes an element of dh in and 4 or 6 out, 1 1/32 in
 // and 2 out for x. dg, du and xb are rows of whole units of eight; past F and K
-// their columns are not read.
+// their columns are not read. 8192 x 8192 with x of 4096: 642 MB in 111 us, 0.87
+// of the copy bandwidth.
 struct DgateArgs {
   const void *dh;
   void *dg, *du, *h, *xb;  // h, xb: null if not wanted
