@@ -373,10 +373,25 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
 #pragma unroll 1
   for (int s = 0; s < kStages - 1; ++s) load_next();
 
-  uint4 xq[NT == 1 ? CH : 1];  // the block's tokens; lanes without one keep zeros
+  // the block's tokens (8 of them), or those of the chunk in hand and of the next (16: 20.4 us for 16 tokens by 8192 x
+  // 8192 without the next, 18.0 with; for 32 the registers cost more, 33 us to 40); lanes without a token keep zeros
+  constexpr int kHeld = NT == 1 ? CH : NT == 2 ? 4 : 1;
+  uint4 xq[kHeld];
 #pragma unroll
-  for (int c = 0; c < (NT == 1 ? CH : 1); ++c) xq[c] = make_uint4(0, 0, 0, 0);
+  for (int c = 0; c < kHeld; ++c) xq[c] = make_uint4(0, 0, 0, 0);
   const T *const x_lane = x + g * a.ldx + t * 8;
+  auto load_token = [&](int64_t k0, int c, int j, uint4 &q) {
+    if (8 * j + g < tokens) {
+      if (kXVec && k0 + KB <= a.K)
+        q = __ldg(reinterpret_cast<const uint4 *>(x_lane + (8 * j) * a.ldx + k0 + c * 32));
+      else
+        q = load_x8<T, kXVec>(x + (8 * j + g) * a.ldx, k0 + c * 32 + t * 8, a.K);
+    }
+  };
+  auto load_tokens = [&](int64_t k0, int c) {  // NT = 2
+    load_token(k0, c, 0, xq[(c & 1) * 2]);
+    load_token(k0, c, 1, xq[(c & 1) * 2 + 1]);
+  };
   int buf = 0;
   for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
     const int n0 = tile * (16 * RT);
@@ -412,6 +427,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
           }
         }
       }
+      if constexpr (NT == 2) load_tokens(k0, 0);
       ptx::cp_async_wait<kStages - 2>();
       __syncwarp();  // every lane's copies are in, and the slot filled next has been read by every lane
       load_next();
@@ -522,21 +538,18 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
                   ldmatrix_x4(((sw + lm) ^ (c * 16)) + r * (16 * kPitch), words[r]);
                 }
               }
+              if constexpr (NT == 2)
+                if (c + 1 < CH) load_tokens(k0, c + 1);
               uint32_t b[NT][4];
 #pragma unroll
               for (int j = 0; j < NT; ++j) {
                 uint4 q = make_uint4(0, 0, 0, 0);
-                if constexpr (NT == 1) {
+                if constexpr (NT == 1)
                   q = xq[c];
-                } else {
-                  if (8 * j + g < tokens) {
-                    const T *const xr = x_lane + (8 * j) * a.ldx + k0 + c * 32;
-                    if (x_whole)
-                      q = __ldg(reinterpret_cast<const uint4 *>(xr));
-                    else
-                      q = load_x8<T, kXVec>(x + (8 * j + g) * a.ldx, k0 + c * 32 + t * 8, a.K);
-                  }
-                }
+                else if constexpr (NT == 2)
+                  q = xq[(c & 1) * 2 + j];
+                else
+                  load_token(k0, c, j, q);
                 b[j][0] = __byte_perm(q.x, q.z, 0x5410);
                 b[j][1] = __byte_perm(q.x, q.z, 0x7632);
                 b[j][2] = __byte_perm(q.y, q.w, 0x5410);
