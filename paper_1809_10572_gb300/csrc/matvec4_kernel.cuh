@@ -32,14 +32,14 @@
 // Tokens come through L1, which holds a CTA's x from tile to tile.
 //
 // Measured (one GB300, weights not in L2): one bf16 token by 65536 x 4096 with
-// scales for 64 inputs 33.9 us, 4.2 TB/s, 0.63 of the copy bandwidth (fp16 0.69,
+// scales for 64 inputs 34.4 us, 4.2 TB/s, 0.62 of the copy bandwidth (fp16 0.69,
 // scales for 32 inputs 0.64, zero points 0.57). About 42 instructions for 512
 // weights, half of them on the 64-lane integer pipe, which is busy 55% of the
 // time: issue and that pipe bound it, not memory. A CTA for each tile took 65
 // us (rings that start and drain for every tile); shifts on the multiplier
 // instead 40; tokens permuted once into shared memory 36. From nine tokens on
-// x's way from L2 (every tile reads all of it) bounds it: 16 tokens by 8192 x
-// 8192 20 us, 32 tokens 33.
+// x's way from L2 (every tile reads all of it) and its latency bound it: 16
+// tokens by 8192 x 8192 18 us, 32 tokens 33 (four row tiles a CTA: 24 and 32).
 #pragma once
 
 #include "ffn_internal.cuh"
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
   }
   __syncwarp();
 
-  // the tokens may come from the kernel before; the next one may be set up
+  // weights and tokens may come from the kernel before; the next one may be set up
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
 
@@ -240,19 +240,20 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
   const uint32_t sz_s = ptx::smem_addr(sz);
   const T *const x = static_cast<const T *>(a.x) + m0 * a.ldx;
 
-  // One block's weights, scales and zero points into a stage: the weights by
-  // one TMA tile where rows are whole 16-byte units (rows past N and bytes past
-  // a row's end are zero), else by 4-byte copies (rows past N repeat row N - 1;
-  // their sums are not stored). Where a row's scales of a block do not lie on
-  // their own size (s_vec = 0), the 4-byte words around them are copied, a word
-  // past the end of the array is clipped, and the reader finds its place in the
-  // first word from the same index.
   const bool one_scale = P::kGroups > 1 && CPG == 4 && a.group_shift > 7;  // groups that hold whole blocks
+  // the scales of a block in row `row` of a tile; past N, row N - 1 again (its sums are not stored)
   auto scale_of = [&](int n0, int row, int blk) -> const uint8_t * {
     const int mat = kGated && row >= 16 * RT;
     const int64_t n = min(n0 + row - mat * 16 * RT, a.N - 1);
     return a.scales[mat] + (n * a.groups + ((static_cast<int64_t>(blk) * KB) >> a.group_shift)) * 2;
   };
+  // One block's weights, scales and zero points into a stage: the weights by
+  // one TMA tile where rows are whole 16-byte units (rows past N and bytes past
+  // a row's end are zero), else by 4-byte copies. Where a row's scales of a
+  // block do not lie on their own size (s_vec = 0), the 4-byte words around them
+  // are copied, a word past the end of the array is clipped, and the reader
+  // finds its place in the first word from the same index. scale: scale_of for
+  // the lane's row.
   auto load = [&](int n0, int blk, int stage, const uint8_t *scale) {
     const int last = a.N - 1 - n0;  // of the tile's rows
     const uint32_t sw = w_s + stage * P::kWBytes, ss = sz_s + stage * P::kSzBytes;
