@@ -6,7 +6,8 @@
 //             dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x
 //
 // Four large products (2 M K F multiply-adds forward, 4 M K F backward) on
-// tcgen05 with fp32 accumulators, through one persistent kernel in three forms:
+// tcgen05 with fp32 accumulators, through one persistent kernel in three forms
+// (BWD: DX and DW in one launch, where their tiles fill the GPU together):
 //   FWD  tile 128 tokens x 128 hidden columns of both projections: the B
 //        operand stacks 128 rows of Wg on 128 rows of Wu, so one MMA of N = 256
 //        fills g and u side by side in tensor memory, and the epilogue forms
@@ -23,10 +24,12 @@
 // gradients' factors and their sums.
 //
 // Measured (one GB300): 4096 x 4096 x 8192 forward 322 us (1.71 PFLOP/s) in a
-// short run, 354 under the power cap; 8192 x 4096 x 8192 bf16 step 2.04 ms (1.61
+// short run, 354 under the power cap; 8192 x 4096 x 8192 bf16 step 2.00 ms (1.65
 // PFLOP/s), 2.24 under it, where the library product of that size holds 1.66
 // PFLOP/s. Large products are bound by power (1.6 GHz of 2.07), small ones by
-// start, end and the reduction steps of one CTA (pick_tile).
+// start, end and the reduction steps of one CTA (pick_tile). DX and DW in one
+// launch: the step of 2048 x 2048 x 4096 167 -> 153 us, of 777 x 1000 x 2736
+// 65 -> 57.
 #include <mutex>
 #include <type_traits>
 
@@ -36,7 +39,7 @@
 namespace samd {
 namespace {
 
-enum Form { FWD = 0, DX = 1, DW = 2 };
+enum Form { FWD = 0, DX = 1, DW = 2, BWD = 3 };
 
 constexpr int BM = 128, BK = 64;
 constexpr int kEpiWarps = 8, kFirstEpiWarp = 4;
@@ -58,20 +61,35 @@ struct Tile {
 constexpr uint64_t kWaitLimitNs = 1000000000ull;  // 1 s
 constexpr int kBand = 12;  // tiles along M that follow one another before the next along N
 
-struct GemmArgs {
+// One product: its tiles, and where its result goes.
+struct Job {
   int M, N;         // of an output: rows and columns
   int steps;        // reduction steps of BK in a segment
-  int tiles_m, tiles_n, total;
+  int tiles_m, tiles_n;
   int half_m;       // DW: rows of tiles of the first output; the rest are the second's
-  int split;        // CTAs of a cluster that share a tile's reduction (kSplit)
+  int wide;         // rows of the output start on 32 bytes
   int64_t ld;       // of the output
   void *out[2];     // FWD: h; DX: dx; DW: dwg, dwu
+};
+
+struct GemmArgs {
+  Job job[2];       // BWD: that of DX and that of DW; else the one
+  int first, total; // tiles of job[0]; of both
+  int fill;         // BWD: DW tiles that last as long as one of DX
+  int split;        // CTAs of a cluster that share a tile's reduction (kSplit)
   // FWD: the checkpoints (null: none), rows of `wpr` words and `bpr` exponents
   uint32_t *lanes[2];
   uint8_t *exps[2];
   int64_t wpr, bpr;
-  int wide, wide8;  // rows of the output, and of the checkpoints' lanes, start on 32 bytes
+  int wide8;        // rows of the checkpoints' lanes start on 32 bytes
   int *status;
+};
+
+// The operands' tensor maps: A of the first and the second segment (DX) or
+// output (DW), B of the first and the second segment (DX) or projection (FWD);
+// BWD: those of DX, then dg, du and x as DW reads them.
+struct Maps {
+  CUtensorMap m[7];
 };
 
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, int *status) {
@@ -171,11 +189,8 @@ __device__ __forceinline__ void split_block8(uint32_t *lanes, uint8_t *exps, int
 // rows.
 template <int FORM, typename T, int ACT, int BN, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1)
-    ffn_gemm_kernel(const __grid_constant__ CUtensorMap ma0, const __grid_constant__ CUtensorMap ma1,
-                    const __grid_constant__ CUtensorMap mb0, const __grid_constant__ CUtensorMap mb1,
-                    const GemmArgs a) {
-  constexpr bool kAMn = FORM == DW, kBMn = FORM != FWD;
-  constexpr int kSegs = FORM == DX ? 2 : 1;
+    ffn_gemm_kernel(const __grid_constant__ Maps maps, const __grid_constant__ GemmArgs a) {
+  static_assert(FORM != BWD || !kSplit, "a split takes one product");
   constexpr int kSumPitch = BN * 4 + 16;  // bytes of a row of partial sums (kSplit)
   constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
   constexpr int kStages = Tile<BN>::kStages, kABytes = Tile<BN>::kABytes, kBBytes = Tile<BN>::kBBytes,
@@ -216,16 +231,47 @@ __global__ void __launch_bounds__(kThreads, 1)
   // a CTA's tiles and its steps of their reductions
   const int rank = kSplit ? blockIdx.x % a.split : 0;
   const int tile0 = kSplit ? blockIdx.x / a.split : blockIdx.x, tile_step = kSplit ? a.total : gridDim.x;
-  const int k0 = kSplit ? static_cast<int>(static_cast<int64_t>(a.steps) * kSegs * rank / a.split) : 0;
-  const int steps = kSplit ? static_cast<int>(static_cast<int64_t>(a.steps) * kSegs * (rank + 1) / a.split) : a.steps * kSegs;
+  // The CTA's next tile. BWD: the tiles of DX in turn over the CTAs; those that
+  // have none in the last, partial turn take a.fill rounds of DW's tiles
+  // meanwhile (as many as a DX tile lasts); then DW's in turn over all.
+  auto next_tile = [&](int tile) {
+    if constexpr (FORM != BWD) {
+      return tile + tile_step;
+    } else {
+      const int P = gridDim.x, c = blockIdx.x, rest = a.first % P, spare = P - rest;
+      const int base = a.first + (rest ? spare * a.fill : 0);  // the first tile that is dealt to all
+      const bool free = rest != 0 && c >= rest;
+      if (tile < a.first) {
+        if (tile + P < a.first) return tile + P;
+        return free && a.fill ? a.first + (c - rest) : base + c;
+      }
+      if (tile < base) return tile + spare < base ? tile + spare : base + c;
+      return tile + P;
+    }
+  };
+  const int tile_1 = FORM == BWD && tile0 >= a.first ? next_tile(tile0 - static_cast<int>(gridDim.x)) : tile0;
+  // calls f with a tile's form, its job and its number there
+  auto on_tile = [&](int tile, auto f) {
+    if constexpr (FORM == BWD) {
+      if (tile < a.first)
+        f(std::integral_constant<int, DX>(), a.job[0], tile);
+      else
+        f(std::integral_constant<int, DW>(), a.job[1], tile - a.first);
+    } else {
+      f(std::integral_constant<int, FORM>(), a.job[0], tile);
+    }
+  };
+  // a CTA's reduction steps [k0, k1) of a job
+  auto k_begin = [&](int all) { return kSplit ? static_cast<int>(static_cast<int64_t>(all) * rank / a.split) : 0; };
+  auto k_end = [&](int all) { return kSplit ? static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / a.split) : all; };
 
   // tile -> its row and column of tiles: bands of kBand rows, down a band's
   // column before the next, so that the tiles in flight share operands in L2
-  auto place = [&](int tile, int &tm, int &tn) {
-    const int band = tile / (kBand * a.tiles_n);
+  auto place = [](const Job &job, int tile, int &tm, int &tn) {
+    const int band = tile / (kBand * job.tiles_n);
     const int first = band * kBand;
-    const int rows = min(kBand, a.tiles_m - first);
-    const int r = tile - band * kBand * a.tiles_n;
+    const int rows = min(kBand, job.tiles_m - first);
+    const int r = tile - band * kBand * job.tiles_n;
     tn = r / rows;
     tm = first + (r - tn * rows);
   };
@@ -235,53 +281,56 @@ __global__ void __launch_bounds__(kThreads, 1)
     int s = 0, loaded = 0;
     uint32_t par = 1;
     bool ok = true;
-    for (int tile = tile0; ok && tile < a.total; tile += tile_step) {
-      int tm, tn;
-      place(tile, tm, tn);
-      const int second = FORM == DW && tm >= a.half_m;
-      const int m0 = (second ? tm - a.half_m : tm) * BM, n0 = tn * (FORM == FWD ? BN / 2 : BN);
-      for (int k = k0; k < steps; k += KS) {
-        // A stage is armed again when the MMAs that read it have completed,
-        // and they were issued behind a wait for its copies.
-        if (loaded == kStages) {
-          ok = warp_wait(empty0 + 8 * s, par, a.status);
-          if (!ok) break;
-        } else {
-          ++loaded;
-        }
-        const int now = KS == 1 ? 1 : min(KS, steps - k);  // steps of this stage
-        const uint32_t full = full0 + 8 * s;
-        ptx::mbar_arrive_expect_tx_if(leader, full, now * kStepBytes);
+    for (int tile = tile_1; ok && tile < a.total; tile = next_tile(tile))
+      on_tile(tile, [&](auto form, const Job &job, int at) {
+        constexpr int F = decltype(form)::value, kMap = FORM == BWD && F == DW ? 4 : 0;
+        int tm, tn;
+        place(job, at, tm, tn);
+        const int second = F == DW && tm >= job.half_m;
+        const int m0 = (second ? tm - job.half_m : tm) * BM, n0 = tn * (F == FWD ? BN / 2 : BN);
+        const int all = job.steps * (F == DX ? 2 : 1), k1 = k_end(all);
+        for (int k = k_begin(all); k < k1; k += KS) {
+          // A stage is armed again when the MMAs that read it have completed,
+          // and they were issued behind a wait for its copies.
+          if (loaded == kStages) {
+            ok = warp_wait(empty0 + 8 * s, par, a.status);
+            if (!ok) break;
+          } else {
+            ++loaded;
+          }
+          const int now = KS == 1 ? 1 : min(KS, k1 - k);  // steps of this stage
+          const uint32_t full = full0 + 8 * s;
+          ptx::mbar_arrive_expect_tx_if(leader, full, now * kStepBytes);
 #pragma unroll
-        for (int j = 0; j < KS; ++j) {
-          if (j < now) {
-            const uint32_t sa = sbase + s * kStageBytes + j * kStepBytes, sb = sa + kABytes;
-            const bool seg = FORM == DX && k + j >= a.steps;
-            const int kk = (seg ? k + j - a.steps : k + j) * BK;
-            const CUtensorMap *const A = (FORM == DX ? seg : FORM == DW ? second != 0 : false) ? &ma1 : &ma0;
-            const CUtensorMap *const B = FORM == DX && seg ? &mb1 : &mb0;
-            if constexpr (kAMn) {
-              ptx::tma_load_2d_if(leader, sa, A, m0, kk, full);
-              ptx::tma_load_2d_if(leader, sa + kABytes / 2, A, m0 + 64, kk, full);
-            } else {
-              ptx::tma_load_2d_if(leader, sa, A, kk, m0, full);
-            }
-            if constexpr (FORM == FWD) {
-              ptx::tma_load_2d_if(leader, sb, &mb0, kk, n0, full);
-              ptx::tma_load_2d_if(leader, sb + kBBytes / 2, &mb1, kk, n0, full);
-            } else {
+          for (int j = 0; j < KS; ++j) {
+            if (j < now) {
+              const uint32_t sa = sbase + s * kStageBytes + j * kStepBytes, sb = sa + kABytes;
+              const bool seg = F == DX && k + j >= job.steps;
+              const int kk = (seg ? k + j - job.steps : k + j) * BK;
+              const CUtensorMap *const A = &maps.m[kMap + ((F == DX && seg) || second ? 1 : 0)];
+              if constexpr (F == DW) {
+                ptx::tma_load_2d_if(leader, sa, A, m0, kk, full);
+                ptx::tma_load_2d_if(leader, sa + kABytes / 2, A, m0 + 64, kk, full);
+              } else {
+                ptx::tma_load_2d_if(leader, sa, A, kk, m0, full);
+              }
+              if constexpr (F == FWD) {
+                ptx::tma_load_2d_if(leader, sb, &maps.m[2], kk, n0, full);
+                ptx::tma_load_2d_if(leader, sb + kBBytes / 2, &maps.m[3], kk, n0, full);
+              } else {
+                const CUtensorMap *const B = &maps.m[kMap + 2 + (seg ? 1 : 0)];
 #pragma unroll
-              for (int q = 0; q < BN / 64; ++q)
-                ptx::tma_load_2d_if(leader, sb + q * (64 * BK * 2), B, n0 + 64 * q, kk, full);
+                for (int q = 0; q < BN / 64; ++q)
+                  ptx::tma_load_2d_if(leader, sb + q * (64 * BK * 2), B, n0 + 64 * q, kk, full);
+              }
             }
           }
+          if (++s == kStages) {
+            s = 0;
+            par ^= 1;
+          }
         }
-        if (++s == kStages) {
-          s = 0;
-          par ^= 1;
-        }
-      }
-    }
+      });
     // the CTA does not exit with a copy in flight: the ring's last round,
     // oldest first
     int quiet = 0;
@@ -292,41 +341,45 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == 1) {
     const uint32_t leader = ptx::elect_one() ? 1u : 0u;
-    constexpr uint32_t idesc = ptx::idesc_16_f32(kBf16, kAMn, kBMn, BM, BN);
-    // 16 reduction positions further: 32 bytes along a row, or 16 rows down
-    constexpr uint64_t kAStep = kAMn ? 2048 >> 4 : 32 >> 4, kBStep = kBMn ? 2048 >> 4 : 32 >> 4;
     int s = 0, i = 0;
     uint32_t par = 0;
     bool ok = true;
-    for (int tile = tile0; ok && tile < a.total; tile += tile_step, ++i) {
-      const int acc = i & 1;
-      if (i >= 2) ok = warp_wait(accempty0 + 8 * acc, ((i >> 1) + 1) & 1u, a.status);
-      if (!ok) break;
-      ptx::tc_fence_after();
-      const uint32_t d = tmem + acc * BN;
-      for (int k = k0; k < steps; k += KS) {
-        ok = warp_wait(full0 + 8 * s, par, a.status);
-        if (!ok) break;
+    for (int tile = tile_1; ok && tile < a.total; tile = next_tile(tile), ++i)
+      on_tile(tile, [&](auto form, const Job &job, int) {
+        constexpr int F = decltype(form)::value;
+        constexpr bool kAMn = F == DW, kBMn = F != FWD;
+        constexpr uint32_t idesc = ptx::idesc_16_f32(kBf16, kAMn, kBMn, BM, BN);
+        // 16 reduction positions further: 32 bytes along a row, or 16 rows down
+        constexpr uint64_t kAStep = kAMn ? 2048 >> 4 : 32 >> 4, kBStep = kBMn ? 2048 >> 4 : 32 >> 4;
+        const int acc = i & 1;
+        if (i >= 2) ok = warp_wait(accempty0 + 8 * acc, ((i >> 1) + 1) & 1u, a.status);
+        if (!ok) return;
         ptx::tc_fence_after();
+        const uint32_t d = tmem + acc * BN;
+        const int all = job.steps * (F == DX ? 2 : 1), k0 = k_begin(all), k1 = k_end(all);
+        for (int k = k0; k < k1; k += KS) {
+          ok = warp_wait(full0 + 8 * s, par, a.status);
+          if (!ok) break;
+          ptx::tc_fence_after();
 #pragma unroll
-        for (int q = 0; q < KS; ++q) {
-          if (KS == 1 || k + q < steps) {
-            const uint32_t sa = sbase + s * kStageBytes + q * kStepBytes, sb = sa + kABytes;
-            const uint64_t da = kAMn ? ptx::sw128_mnmajor_desc(sa, kABytes / 2) : ptx::sw128_kmajor_desc(sa);
-            const uint64_t db = kBMn ? ptx::sw128_mnmajor_desc(sb, 64 * BK * 2) : ptx::sw128_kmajor_desc(sb);
+          for (int q = 0; q < KS; ++q) {
+            if (KS == 1 || k + q < k1) {
+              const uint32_t sa = sbase + s * kStageBytes + q * kStepBytes, sb = sa + kABytes;
+              const uint64_t da = kAMn ? ptx::sw128_mnmajor_desc(sa, kABytes / 2) : ptx::sw128_kmajor_desc(sa);
+              const uint64_t db = kBMn ? ptx::sw128_mnmajor_desc(sb, 64 * BK * 2) : ptx::sw128_kmajor_desc(sb);
 #pragma unroll
-            for (int j = 0; j < BK / 16; ++j)
-              ptx::mma_f16(leader, d, da + j * kAStep, db + j * kBStep, idesc, k > k0 || q > 0 || j > 0);
+              for (int j = 0; j < BK / 16; ++j)
+                ptx::mma_f16(leader, d, da + j * kAStep, db + j * kBStep, idesc, k > k0 || q > 0 || j > 0);
+            }
+          }
+          ptx::mma_commit(leader, empty0 + 8 * s);
+          if (++s == kStages) {
+            s = 0;
+            par ^= 1;
           }
         }
-        ptx::mma_commit(leader, empty0 + 8 * s);
-        if (++s == kStages) {
-          s = 0;
-          par ^= 1;
-        }
-      }
-      if (ok) ptx::mma_commit(leader, accfull0 + 8 * acc);
-    }
+        if (ok) ptx::mma_commit(leader, accfull0 + 8 * acc);
+      });
     // nothing of this CTA's reads shared memory or writes tensor memory after
     // this: every MMA issued has completed
     ptx::mma_commit(leader, drain);
@@ -336,14 +389,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int ew = warp - kFirstEpiWarp;
     const int quad = warp & 3, half = ew >> 2;  // rows 32 * quad .., alternate blocks of 32 columns
     int i = 0;
-    for (int tile = tile0; tile < a.total; tile += tile_step, ++i) {
+    for (int tile = tile_1; tile < a.total; tile = next_tile(tile), ++i) {
       const int acc = i & 1;
       if (!warp_wait(accfull0 + 8 * acc, (i >> 1) & 1u, a.status)) break;
       ptx::tc_fence_after();
+      // (DX and DW end alike; a DX has one output)
+      const bool other = FORM == BWD && tile >= a.first;
+      const Job &job = other ? a.job[1] : a.job[0];
       int tm, tn;
-      place(tile, tm, tn);
-      const int second = FORM == DW && tm >= a.half_m;
-      const int m = (second ? tm - a.half_m : tm) * BM + quad * 32 + lane;
+      place(job, other ? tile - a.first : tile, tm, tn);
+      const int second = tm >= job.half_m;
+      const int m = (second ? tm - job.half_m : tm) * BM + quad * 32 + lane;
       const uint32_t t0 = tmem + acc * BN + (static_cast<uint32_t>(quad * 32) << 16);
       if constexpr (kSplit) {
         // this CTA's partial sums, rows a multiple of 16 bytes and four banks apart; the stages are free: every
@@ -370,11 +426,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           ptx::tmem_wait_ld(ru);
           const float *const gv = reinterpret_cast<const float *>(rg), *const uv = reinterpret_cast<const float *>(ru);
           const int c = n0 + b * 32;
-          if (m < a.M && c < a.N) {
+          if (m < job.M && c < job.N) {
             float h[32];
 #pragma unroll
             for (int q = 0; q < 32; ++q) h[q] = act_value<ACT>(gv[q]) * uv[q];
-            store_row32<T>(static_cast<T *>(a.out[0]) + m * a.ld, c, a.N, a.wide, h);
+            store_row32<T>(static_cast<T *>(job.out[0]) + m * job.ld, c, job.N, job.wide, h);
             if (a.lanes[0]) {
               store_block8<ACT == SAMD_RELU_ACT>(a.lanes[0] + m * a.wpr, a.exps[0] + m * a.bpr, a.wpr, c, a.wide8, gv);
               store_block8<false>(a.lanes[1] + m * a.wpr, a.exps[1] + m * a.bpr, a.wpr, c, a.wide8, uv);
@@ -383,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       } else {
         const int n0 = tn * BN;
-        T *const out = static_cast<T *>(second ? a.out[1] : a.out[0]) + m * a.ld;
+        T *const out = static_cast<T *>(second ? job.out[1] : job.out[0]) + m * job.ld;
 #pragma unroll 1
         for (int b = half; b < BN / 32; b += 2) {
           uint32_t r[32];
@@ -391,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           ptx::tmem_ld_32x32b_x32(t0 + b * 32, r);
           ptx::tmem_wait_ld(r);
           const int c = n0 + b * 32;
-          if (m < a.M && c < a.N) store_row32<T>(out, c, a.N, a.wide, reinterpret_cast<const float *>(r));
+          if (m < job.M && c < job.N) store_row32<T>(out, c, job.N, job.wide, reinterpret_cast<const float *>(r));
         }
       }
       __syncwarp();
@@ -403,11 +459,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   if constexpr (kSplit) {
     __syncwarp();
     ptx::cluster_sync();
+    const Job &job = a.job[0];
     int tm, tn;
-    place(tile0, tm, tn);
-    const int second = FORM == DW && tm >= a.half_m;
-    const int m0 = (second ? tm - a.half_m : tm) * BM;
-    const int rows = min(BM, a.M - m0), per = (rows + a.split - 1) / a.split;
+    place(job, tile0, tm, tn);
+    const int second = tm >= job.half_m;
+    const int m0 = (second ? tm - job.half_m : tm) * BM;
+    const int rows = min(BM, job.M - m0), per = (rows + a.split - 1) / a.split;
     const int r0 = rank * per, count = max(0, min(per, rows - r0));
     // a thread takes four columns of a row (FWD: of both projections, eight neighbouring lanes a block of 32)
     constexpr int kPerRow = (FORM == FWD ? BN / 2 : BN) / 4;
@@ -433,13 +490,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         float h[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) h[q] = act_value<ACT>(g[q]) * u[q];
-        if (in) store_row4<T>(static_cast<T *>(a.out[0]) + m * a.ld, col, a.N, h);
+        if (in) store_row4<T>(static_cast<T *>(job.out[0]) + m * job.ld, col, job.N, h);
         if (a.lanes[0]) {
           split_block8<ACT == SAMD_RELU_ACT>(a.lanes[0] + m * a.wpr, a.exps[0] + m * a.bpr, a.wpr, col, in, g);
           split_block8<false>(a.lanes[1] + m * a.wpr, a.exps[1] + m * a.bpr, a.wpr, col, in, u);
         }
       } else if (in) {
-        store_row4<T>(static_cast<T *>(second ? a.out[1] : a.out[0]) + m * a.ld, col, a.N, g);
+        store_row4<T>(static_cast<T *>(second ? job.out[1] : job.out[0]) + m * job.ld, col, job.N, g);
       }
     }
     __syncwarp();
@@ -586,40 +643,55 @@ bool make_map(CUtensorMap *map, samd_dtype t, const void *p, int64_t rows, int64
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The tile of a product: its columns, and how many CTAs of a cluster share its
-// reduction.
+// The tile of a product: its columns, how many CTAs of a cluster share its
+// reduction, and the estimated time in ns.
 struct Pick {
   int columns, split;
+  int64_t cost;
 };
-// The least estimate over the tiles, in ns, from times measured on one GB300: a
-// reduction step of a tile of 256, 128 or 64 columns takes 330, 215 or 150 (the
-// operands' way into the SM bounds the narrow ones); start and end of a launch
-// 1500 and five a column of the last tile (FWD: 6000, its epilogue hides less).
-// A tile whose reduction is split over a cluster: steps of 64 columns, 3300 for
-// start and meeting (FWD: 6000), and 2000 more for every further wave of
-// clusters. For 16 tokens by 1024 by 4096, dx: 23.3 us unsplit, 8.6 over four
-// CTAs.
+// Times measured on one GB300: a reduction step of a tile of 256, 128 or 64
+// columns takes 330, 215 or 150 ns (the operands' way into the SM bounds the
+// narrow ones); start and end of a launch 1500 and five a column of the last
+// tile (FWD: 6000, its epilogue hides less). A tile whose reduction is split
+// over a cluster: steps of 64 columns, 3300 for start and meeting (FWD: 6000),
+// and 2000 more for every further wave of clusters. For 16 tokens by 1024 by
+// 4096, dx: 23.3 us unsplit, 8.6 over four CTAs.
+int64_t step_ns(int columns) { return columns == 256 ? 330 : columns == 128 ? 215 : 150; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 template <typename Clusters>
 Pick pick_tile(int form, int64_t rows, int64_t cols, int64_t steps, Clusters clusters) {
-  Pick best = {256, 1};
-  int64_t least = INT64_MAX;
-  auto offer = [&](Pick p, int64_t cost) {
-    if (cost < least) {
-      least = cost;
-      best = p;
-    }
+  Pick best = {256, 1, INT64_MAX};
+  auto offer = [&](int columns, int split, int64_t cost) {
+    if (cost < best.cost) best = Pick{columns, split, cost};
   };
-  for (const int bn : {256, 128, 64}) {
-    const int64_t tiles = rows * ((cols + bn - 1) / bn), waves = (tiles + sm_count() - 1) / sm_count();
-    offer(Pick{bn, 1}, waves * steps * (bn == 256 ? 330 : bn == 128 ? 215 : 150) + (form == FWD ? 6000 : 1500 + 5 * bn));
-  }
-  const int64_t tiles = rows * ((cols + 63) / 64);
+  for (const int bn : {256, 128, 64})
+    offer(bn, 1, ceil_div(rows * ceil_div(cols, bn), sm_count()) * steps * step_ns(bn) +
+                     (form == FWD ? 6000 : 1500 + 5 * bn));
+  const int64_t tiles = rows * ceil_div(cols, 64);
   for (const int split : {2, 4, 8}) {
     if (split > steps || 2 * tiles > sm_count()) break;
     const int64_t fit = clusters(split);
     if (fit < 1) break;
-    const int64_t waves = (tiles + fit - 1) / fit;
-    offer(Pick{64, split}, waves * ((steps + split - 1) / split * 150 + 2000) + (form == FWD ? 4000 : 1300));
+    offer(64, split, ceil_div(tiles, fit) * (ceil_div(steps, split) * step_ns(64) + 2000) + (form == FWD ? 4000 : 1300));
+  }
+  return best;
+}
+
+// DW's tiles that a CTA does in the time of one of DX's.
+int fill_of(int64_t steps_x, int64_t steps_w) { return static_cast<int>((2 * steps_x + steps_w) / (2 * steps_w)); }
+
+// DX and DW in one launch: its columns, and the time.
+Pick pick_both(int64_t rows_x, int64_t steps_x, int64_t rows_w, int64_t steps_w, int64_t cols) {
+  Pick best = {256, 1, INT64_MAX};
+  const int64_t P = sm_count();
+  for (const int bn : {256, 128, 64}) {
+    const int64_t x = rows_x * ceil_div(cols, bn), w = rows_w * ceil_div(cols, bn), rest = x % P;
+    if (x + w < P) continue;  // the GPU is not full: a launch each
+    const int64_t early = rest ? (P - rest) * fill_of(steps_x, steps_w) : 0;
+    const int64_t steps = ceil_div(x, P) * steps_x + (w > early ? ceil_div(w - early, P) * steps_w : 0);
+    const int64_t cost = steps * step_ns(bn) + 1500 + 5 * bn;
+    if (cost < best.cost) best = Pick{bn, 1, cost};
   }
   return best;
 }
@@ -658,42 +730,65 @@ struct Operand {
   int64_t rows, cols, ld;
 };
 
-template <int FORM, typename T, int ACT, int BN, bool kSplit = false>
-cudaError_t launch_tiled(const Operand *op, samd_dtype t, GemmArgs &a, cudaStream_t s) {
-  constexpr int kARows = FORM == DW ? BK : BM, kBRows = FORM == FWD ? BN / 2 : BK;  // of a TMA box
-  CUtensorMap m[4];
-  for (int i = 0; i < 4; ++i)
-    if (!make_map(&m[i], t, op[i].p, op[i].rows, op[i].cols, op[i].ld, i < 2 ? kARows : kBRows))
-      return cudaErrorInvalidValue;
-  a.tiles_n = FORM == FWD ? (a.N + BN / 2 - 1) / (BN / 2) : (a.N + BN - 1) / BN;
-  a.total = a.tiles_m * a.tiles_n;
+// Maps at .. at + n - 1 from a product's operands, the first two those of A.
+bool make_maps(Maps &maps, int at, int form, int columns, const Operand *op, int n, samd_dtype t) {
+  const int a_rows = form == DW ? BK : BM, b_rows = form == FWD ? columns / 2 : BK;  // of a TMA box
+  for (int i = 0; i < n; ++i)
+    if (!make_map(&maps.m[at + i], t, op[i].p, op[i].rows, op[i].cols, op[i].ld, i < 2 ? a_rows : b_rows)) return false;
+  return true;
+}
+
+// A job's tiles for a tile width; the number of them.
+int set_tiles(Job &job, int form, int columns, bool two) {
   auto on32 = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 31u) == 0; };
-  a.wide = a.ld % 16 == 0 && on32(a.out[0]) && on32(a.out[1]);
-  a.wide8 = a.wpr % 8 == 0 && on32(a.lanes[0]) && on32(a.lanes[1]);
-  const auto kern = ffn_gemm_kernel<FORM, T, ACT, BN, kSplit>;
+  const int cols = form == FWD ? columns / 2 : columns;
+  job.half_m = (job.M + BM - 1) / BM;
+  job.tiles_m = two ? 2 * job.half_m : job.half_m;
+  job.tiles_n = (job.N + cols - 1) / cols;
+  job.wide = job.ld % 16 == 0 && on32(job.out[0]) && on32(job.out[1]);
+  return job.tiles_m * job.tiles_n;
+}
+
+template <int FORM, typename T, int ACT, int BN, bool kSplit = false>
+cudaError_t launch_tiled(const Maps &maps, GemmArgs &a, cudaStream_t s) {
+  constexpr auto kern = ffn_gemm_kernel<FORM, T, ACT, BN, kSplit>;
   cudaError_t e = device_status_ptr(&a.status);
   if (e == cudaSuccess) e = conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), Tile<BN>::kSmemBytes);
   if (e != cudaSuccess) return e;
   const int grid = kSplit ? a.total * a.split : a.total < sm_count() ? a.total : sm_count();
-  return launch_dependent(kern, dim3(grid), kThreads, Tile<BN>::kSmemBytes, s, kSplit ? a.split : 1, m[0], m[1], m[2],
-                          m[3], a);
+  return launch_dependent(kern, dim3(grid), kThreads, Tile<BN>::kSmemBytes, s, kSplit ? a.split : 1, maps, a);
 }
 
 template <int FORM, typename T, int ACT>
-cudaError_t launch_gemm(const Operand (&op)[4], samd_dtype t, GemmArgs &a, cudaStream_t s) {
-  const int cols = FORM == FWD ? 2 * a.N : a.N;  // of the MMA
-  const int64_t steps = static_cast<int64_t>(a.steps) * (FORM == DX ? 2 : 1);
-  const Pick p = pick_tile(FORM, a.tiles_m, cols, steps, [](int split) {
+cudaError_t launch_columns(int columns, const Maps &maps, GemmArgs &a, cudaStream_t s) {
+  if (columns == 64) return launch_tiled<FORM, T, ACT, 64>(maps, a, s);
+  return columns == 128 ? launch_tiled<FORM, T, ACT, 128>(maps, a, s) : launch_tiled<FORM, T, ACT, 256>(maps, a, s);
+}
+
+int64_t all_steps(int form, const Job &job) { return static_cast<int64_t>(job.steps) * (form == DX ? 2 : 1); }
+
+template <int FORM, typename T, int ACT>
+Pick pick_for(const Job &job, bool two) {
+  const int64_t rows = static_cast<int64_t>(job.M + BM - 1) / BM * (two ? 2 : 1);
+  const int64_t cols = FORM == FWD ? 2 * static_cast<int64_t>(job.N) : job.N;  // of the MMA
+  return pick_tile(FORM, rows, cols, all_steps(FORM, job), [](int split) {
     constexpr auto kern = ffn_gemm_kernel<FORM, T, ACT, 64, true>;
     const size_t smem = Tile<64>::kSmemBytes;
     return conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), smem) == cudaSuccess
                ? resident_clusters<kern>(split, smem)
                : 0;
   });
+}
+
+// One product, whose job is a.job[0] (two: a DW with both outputs).
+template <int FORM, typename T, int ACT>
+cudaError_t launch_gemm(const Pick &p, const Operand (&op)[4], samd_dtype t, bool two, GemmArgs &a, cudaStream_t s) {
+  Maps maps = {};
+  if (!make_maps(maps, 0, FORM, p.columns, op, 4, t)) return cudaErrorInvalidValue;
+  a.first = a.total = set_tiles(a.job[0], FORM, p.columns, two);
   a.split = p.split;
-  if (p.split > 1) return launch_tiled<FORM, T, ACT, 64, true>(op, t, a, s);
-  if (p.columns == 64) return launch_tiled<FORM, T, ACT, 64>(op, t, a, s);
-  return p.columns == 128 ? launch_tiled<FORM, T, ACT, 128>(op, t, a, s) : launch_tiled<FORM, T, ACT, 256>(op, t, a, s);
+  return p.split > 1 ? launch_tiled<FORM, T, ACT, 64, true>(maps, a, s)
+                     : launch_columns<FORM, T, ACT>(p.columns, maps, a, s);
 }
 
 template <typename F>
@@ -712,19 +807,24 @@ cudaError_t forward(const samd_ffn_desc &d, const void *x, const void *wg, const
   const Operand op[4] = {
       {x, d.M, d.K, d.ldx}, {x, d.M, d.K, d.ldx}, {wg, d.F, d.K, d.ldw}, {wu, d.F, d.K, d.ldw}};
   GemmArgs a = {};
-  a.M = d.M;
-  a.N = d.F;
-  a.steps = (d.K + BK - 1) / BK;
-  a.tiles_m = (d.M + BM - 1) / BM;
-  a.ld = d.ldh;
-  a.out[0] = h;
+  Job &job = a.job[0];
+  job.M = d.M;
+  job.N = d.F;
+  job.steps = (d.K + BK - 1) / BK;
+  job.ld = d.ldh;
+  job.out[0] = h;
   a.lanes[0] = static_cast<uint32_t *>(cg.lanes);
   a.lanes[1] = static_cast<uint32_t *>(cu.lanes);
   a.exps[0] = cg.exps;
   a.exps[1] = cu.exps;
   a.wpr = block8_words(d.F);
   a.bpr = block8_blocks(d.F);
-  return by_act(d.act, [&](auto act) { return launch_gemm<FWD, T, decltype(act)::value>(op, d.type, a, s); });
+  a.wide8 = a.wpr % 8 == 0 && (reinterpret_cast<uintptr_t>(cg.lanes) & 31u) == 0 &&
+            (reinterpret_cast<uintptr_t>(cu.lanes) & 31u) == 0;
+  return by_act(d.act, [&](auto act) {
+    constexpr int kAct = decltype(act)::value;
+    return launch_gemm<FWD, T, kAct>(pick_for<FWD, T, kAct>(job, false), op, d.type, false, a, s);
+  });
 }
 
 // The workspace: dg and du (M rows of F) and x (M rows of K), each row a
@@ -781,31 +881,50 @@ cudaError_t backward(const samd_ffn_desc &d, const void *dh, samd_block8 cx, sam
     return launch_dependent(kern, dim3(resident_grid<kern>(g.items, 256)), 256, 0, s, 1, g);
   });
   if (e != cudaSuccess) return e;
-  const Operand odg = {dg, d.M, d.F, w.ldf}, odu = {du, d.M, d.F, w.ldf};
+  const Operand odg = {dg, d.M, d.F, w.ldf}, odu = {du, d.M, d.F, w.ldf}, ox = {xb, d.M, d.K, w.ldk};
+  const Operand opx[4] = {odg, odu, {wg, d.F, d.K, d.ldw}, {wu, d.F, d.K, d.ldw}};
+  const Operand opw[4] = {dwg ? odg : odu, odu, ox, ox};
+  const bool two = dwg && dwu;
+  Job jx = {}, jw = {};
+  jx.M = d.M;
+  jx.N = d.K;
+  jx.steps = (d.F + BK - 1) / BK;
+  jx.ld = d.ldx;
+  jx.out[0] = dx;
+  jw.M = d.F;
+  jw.N = d.K;
+  jw.steps = (d.M + BK - 1) / BK;
+  jw.ld = d.ldw;
+  jw.out[0] = dwg ? dwg : dwu;
+  jw.out[1] = two ? dwu : nullptr;
+  GemmArgs a = {};
+  const Pick px = dx ? pick_for<DX, T, 0>(jx, false) : Pick{}, pw = weights ? pick_for<DW, T, 0>(jw, two) : Pick{};
+  if (dx && weights) {
+    // both in one launch where that is the shorter, a launch's start (2 us) counted
+    const int64_t sx = all_steps(DX, jx), sw = all_steps(DW, jw);
+    const Pick pb = pick_both(ceil_div(jx.M, BM), sx, ceil_div(jw.M, BM) * (two ? 2 : 1), sw, d.K);
+    if (pb.cost < px.cost + pw.cost + 2000) {
+      Maps maps = {};
+      const Operand opd[3] = {opw[0], opw[1], ox};
+      if (!make_maps(maps, 0, DX, pb.columns, opx, 4, d.type) || !make_maps(maps, 4, DW, pb.columns, opd, 3, d.type))
+        return cudaErrorInvalidValue;
+      a.job[0] = jx;
+      a.job[1] = jw;
+      a.first = set_tiles(a.job[0], DX, pb.columns, false);
+      a.total = a.first + set_tiles(a.job[1], DW, pb.columns, two);
+      a.fill = fill_of(sx, sw);
+      a.split = 1;
+      return launch_columns<BWD, T, 0>(pb.columns, maps, a, s);
+    }
+  }
   if (dx) {
-    const Operand op[4] = {odg, odu, {wg, d.F, d.K, d.ldw}, {wu, d.F, d.K, d.ldw}};
-    GemmArgs a = {};
-    a.M = d.M;
-    a.N = d.K;
-    a.steps = (d.F + BK - 1) / BK;
-    a.tiles_m = (d.M + BM - 1) / BM;
-    a.ld = d.ldx;
-    a.out[0] = dx;
-    e = launch_gemm<DX, T, 0>(op, d.type, a, s);
+    a.job[0] = jx;
+    e = launch_gemm<DX, T, 0>(px, opx, d.type, false, a, s);
     if (e != cudaSuccess) return e;
   }
   if (weights) {
-    const Operand ox = {xb, d.M, d.K, w.ldk}, op[4] = {dwg ? odg : odu, odu, ox, ox};
-    GemmArgs a = {};
-    a.M = d.F;
-    a.N = d.K;
-    a.steps = (d.M + BK - 1) / BK;
-    a.half_m = (d.F + BM - 1) / BM;
-    a.tiles_m = dwg && dwu ? 2 * a.half_m : a.half_m;
-    a.ld = d.ldw;
-    a.out[0] = dwg ? dwg : dwu;
-    a.out[1] = dwu;
-    e = launch_gemm<DW, T, 0>(op, d.type, a, s);
+    a.job[0] = jw;
+    e = launch_gemm<DW, T, 0>(pw, opw, d.type, two, a, s);
   }
   return e;
 }

@@ -270,3 +270,31 @@ def test_many_tiles(samd_lib):
     assert torch.equal(dx, (dg @ wg.double() + du @ wu.double()).to(t))
     assert torch.equal(dwg, (dg.t() @ X).to(t)) and torch.equal(dwu, (du.t() @ X).to(t))
     assert_status_clean()
+
+
+@pytest.mark.parametrize("shape", [(700, 1096, 900), (200, 4104, 1300), (1500, 2600, 1200), (3000, 600, 3100), (2600, 3000, 2200)])
+def test_gradients_of_x_and_of_the_weights_in_one_launch(samd_lib, shape):
+    """Sizes whose dx and weight gradients fill the GPU together, with tiles of each width: bit for bit on integers, all
+    outputs, and dx with one weight's gradient."""
+    M, K, F = shape
+    t = BF16
+    x, g, u = ref.ints(1, (M, K), -9, 9), ref.ints(2, (M, F), -9, 9), ref.ints(3, (M, F), -3, 3)
+    dh, wg, wu = ref.ints(4, (M, F), -2, 2, t), ref.ints(5, (F, K), -3, 3, t), ref.ints(6, (F, K), -3, 3, t)
+    dh, wg, wu = (ref.wide(v) for v in (dh, wg, wu))
+    D = dh.double()
+    dg, du = D * u * (g > 0), D * torch.clamp(g, min=0)
+    want = ((dg @ wg.double() + du @ wu.double()).to(t), (dg.t() @ x).to(t), (du.t() @ x).to(t))
+    forms = form8(x), form8(g), form8(u)
+    got = samd.gated_ffn_backward(dh, *forms, wg, wu, "relu")
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    d = samd.samd_ffn_desc(M, K, F, K, wg.stride(0), dh.stride(0), samd.SAMD_BF16, samd.SAMD_RELU_ACT)
+    ws = torch.empty(samd.samd_gated_ffn_backward_workspace_size(d), dtype=torch.uint8, device="cuda")
+    for i in (1, 2):
+        dx = torch.full((M + 1, K), 5.0, dtype=t, device="cuda")
+        dw = torch.full((F + 1, wg.stride(0)), 5.0, dtype=t, device="cuda")
+        samd.samd_gated_ffn_backward(d, dh, *forms, wg, wu, dx, dw if i == 1 else None, dw if i == 2 else None, None, ws)
+        assert torch.equal(dx[:M], want[0]) and torch.equal(dw[:F, :K], want[i])
+        dx[:M] = 5.0
+        dw[:F, :K] = 5.0
+        assert (dx == 5.0).all() and (dw == 5.0).all()
+    assert_status_clean()
