@@ -322,7 +322,9 @@ typedef enum {
  * M tokens of K inputs and N outputs: x is M rows of K elements (stride ldx),
  * y M rows of N (stride ldy), both of `type` (SAMD_F16 or SAMD_BF16). `group`,
  * a power of two of at least 32, is the number of neighbouring inputs that
- * share a scale (at least K: one scale a row).
+ * share a scale (at least K: one scale a row). SAMD_EINVAL: another type or
+ * group; SAMD_ESHAPE: K < 1, a negative size, a stride below its row's length;
+ * SAMD_EUNSUP: a size above 2^30. M = 0 or N = 0 launches nothing.
  */
 typedef struct {
   int M, N, K, group;
@@ -389,7 +391,9 @@ SAMD_API samd_status samd_block8_dequantize(samd_dtype type, samd_block8 in, int
  * The gated block of M tokens, K inputs and F hidden columns. x (and dx): M
  * rows of K, stride ldx; wg, wu (and dwg, dwu): F rows of K, stride ldw; h (and
  * dh): M rows of F, stride ldh; all of `type` (SAMD_F16 or SAMD_BF16). The
- * strides are multiples of 8 (16-byte rows, else SAMD_EALIGN).
+ * strides are multiples of 8 (16-byte rows, else SAMD_EALIGN). SAMD_ESHAPE:
+ * K < 1, F < 1, M < 0, a stride below its row's length; SAMD_EUNSUP: a size
+ * above 2^30, or an output of 2^30 tiles of 128 x 128.
  */
 typedef struct {
   int M, K, F;
@@ -418,7 +422,8 @@ SAMD_API size_t samd_gated_ffn_backward_workspace_size(const samd_ffn_desc *desc
  *   dx = dg wg + du wu,  dwg = dg^T x,  dwu = du^T x,  h = act(g) * u.
  * Each output may be NULL if it is not wanted; those given are overwritten.
  * ckpt_x is read for dwg and dwu only, wg and wu for dx only. With M = 0 the
- * weights' gradients are zero. workspace: caller-owned device scratch.
+ * weights' gradients are zero. workspace: caller-owned device scratch of at
+ * least samd_gated_ffn_backward_workspace_size bytes (else SAMD_ESHAPE).
  * As with the convolution, a kernel that gives up on a bounded wait leaves its
  * outputs undefined and records SAMD_ETIMEOUT for samd_device_status.
  */
