@@ -508,6 +508,8 @@ def _on(stream):
 def _rows(t: torch.Tensor, what: str, cols: int | None = None, rows: int | None = None, dtype=None) -> int:
     """Checks a matrix whose rows lie contiguous in memory and returns its row stride in elements."""
     shape = t.shape
+    if cols is None and len(shape) == 2 and t.is_contiguous():
+        return max(shape[1], 1)
     if len(shape) != 2 or (shape[1] > 1 and t.stride(1) != 1):
         raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(shape)}, "
                          f"strides {t.stride()}")
@@ -673,6 +675,8 @@ def _ffn_desc(M, K, F, t, act, ldx, ldw, ldh) -> samd_ffn_desc:
 
 def _ld8(t: torch.Tensor, what: str, rows: int, cols: int, dtype) -> int:
     """The row stride of a matrix of the block, rounded up where a single row leaves it open."""
+    if cols % 8 == 0 and t.dtype is dtype and t.shape == (rows, cols) and t.is_contiguous():
+        return cols
     ld = _rows(t, what, cols, rows, dtype)
     return ld if rows > 1 else _aligned8(ld)
 
@@ -693,9 +697,12 @@ def gated_ffn_forward(x, wg, wu, act="silu", checkpoints: bool = False, out=None
     d = _ffn_desc(M, K, F, t, act, ldx, ldw, ldh)
     with _on(stream):
         h = _empty_ld(M, F, ldh, x) if out is None else out
-        g8, u8 = (block8_empty(M, F, x.device), block8_empty(M, F, x.device)) if checkpoints else (None, None)
-    samd_gated_ffn_forward(d, x, wg, wu, h, g8, u8, stream)
-    return (h, g8, u8) if checkpoints else h
+        if not checkpoints:
+            samd_gated_ffn_forward(d, x, wg, wu, h, None, None, stream)
+            return h
+        g8, u8 = block8_empty(M, F, x.device), block8_empty(M, F, x.device)
+        samd_gated_ffn_forward(d, x, wg, wu, h, g8, u8, stream)
+        return h, g8, u8
 
 
 def gated_ffn_backward(dh, ckpt_x: Block8, ckpt_g: Block8, ckpt_u: Block8, wg, wu, act="silu", need_dx: bool = True,
