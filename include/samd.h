@@ -420,10 +420,11 @@ SAMD_API size_t samd_gated_ffn_backward_workspace_size(const samd_ffn_desc *desc
  * 8-bit forms stand for, dg = dh * u * act'(g) and du = dh * act(g) (fp32,
  * rounded once to `type`, the operands of the products),
  *   dx = dg wg + du wu,  dwg = dg^T x,  dwu = du^T x,  h = act(g) * u.
- * Each output may be NULL if it is not wanted; those given are overwritten.
- * ckpt_x is read for dwg and dwu only, wg and wu for dx only. With M = 0 the
- * weights' gradients are zero. workspace: caller-owned device scratch of at
- * least samd_gated_ffn_backward_workspace_size bytes (else SAMD_ESHAPE).
+ * Each output may be NULL if it is not wanted (all of them: SAMD_EINVAL, unless
+ * M = 0); those given are overwritten. ckpt_x is read for dwg and dwu only, wg
+ * and wu for dx only. With M = 0 the weights' gradients are zero. workspace:
+ * caller-owned device scratch of at least
+ * samd_gated_ffn_backward_workspace_size bytes (else SAMD_ESHAPE).
  * As with the convolution, a kernel that gives up on a bounded wait leaves its
  * outputs undefined and records SAMD_ETIMEOUT for samd_device_status.
  */

@@ -330,16 +330,16 @@ samd_status samd_gated_ffn_backward(const samd_ffn_desc *d, const void *dh, samd
   const samd_status st = ffn_shape_checks(d);
   if (st != SAMD_OK) return st;
   const bool weights = dwg || dwu;
-  if (!dx && !weights && !h) return SAMD_EINVAL;
   if (!aligned16(dx) || !aligned16(dwg) || !aligned16(dwu) || !aligned16(h)) return SAMD_EALIGN;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (d->M == 0) {  // a sum over no tokens
+  if (d->M == 0) {  // a sum over no tokens; dx and h have no rows, and may have no address
     for (void *w : {dwg, dwu})
       if (w && cudaMemset2DAsync(w, static_cast<size_t>(d->ldw) * 2, 0, static_cast<size_t>(d->K) * 2, d->F, s) !=
                    cudaSuccess)
         return SAMD_ECUDA;
     return SAMD_OK;
   }
+  if (!dx && !weights && !h) return SAMD_EINVAL;
   if (!dh || !cg.lanes || !cg.exps || !cu.lanes || !cu.exps || !workspace) return SAMD_EINVAL;
   if ((dx && (!wg || !wu)) || (weights && (!cx.lanes || !cx.exps))) return SAMD_EINVAL;
   if (!aligned16(dh) || !aligned16(cx.lanes) || !aligned16(cx.exps) || !aligned16(cg.lanes) || !aligned16(cg.exps) ||

@@ -131,6 +131,18 @@ def test_backward_refusals(lib):
     assert call(d, cg=samd.samd_block8(16, 4)) == EALIGN
 
 
+def test_backward_of_no_tokens(lib):
+    """An empty tensor has no address: with M = 0 a dx or an h alone looks like no output, and there is nothing to do."""
+    n = samd.samd_block8(None, None)
+
+    def call(d, dx=None, h=None):
+        return lib.samd_gated_ffn_backward(ctypes.byref(d), None, n, n, n, None, None, dx, None, None, h, None, 0, None)
+
+    assert call(ffn(M=0)) == OK
+    assert call(ffn(M=0), dx=16) == OK and call(ffn(M=0), h=16) == OK
+    assert call(ffn(M=0), dx=8) == EALIGN and call(ffn(M=0, K=0)) == ESHAPE
+
+
 def test_the_binding_checks_its_tensors():
     """Shapes, types and strides that the C side cannot see (raised before the library is called)."""
     x = torch.zeros((2, 64), dtype=torch.bfloat16)

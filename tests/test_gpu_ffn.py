@@ -224,6 +224,21 @@ def test_no_tokens(samd_lib):
     assert dx.shape == (0, K) and not dwg.any() and not dwu.any()
 
 
+@pytest.mark.parametrize("want", [dict(need_dw=False), dict(need_dx=False, need_dw=False, need_h=True),
+                                  dict(need_dw=False, need_h=True), dict(need_h=True)])
+def test_no_tokens_and_some_outputs(samd_lib, want):
+    K, F, t = 24, 40, BF16
+    _, wg, wu = make((1, K, F), t, exact=False)
+    empty = torch.empty((0, F), dtype=t, device="cuda")
+    b8, f8 = samd.block8_empty(0, K), samd.block8_empty(0, F)
+    got = samd.gated_ffn_backward(empty, b8, f8, f8, wg, wu, **want)
+    torch.cuda.synchronize()
+    assert [g is not None for g in got[:3]] == [want.get("need_dx", True)] + [want.get("need_dw", True)] * 2
+    assert all(g.shape == (0, K) for g in got[:1] if g is not None) and all(not g.any() for g in got[1:3] if g is not None)
+    if want.get("need_h"):
+        assert got[3].shape == (0, F)
+
+
 def test_streams_graphs_and_repeats(samd_lib):
     shape = (300, 264, 520)
     x, wg, wu = make(shape, BF16, exact=False)
