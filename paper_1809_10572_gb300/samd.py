@@ -531,6 +531,12 @@ def _check_weights4(lanes, scales, zeros, N, K, group, f, dtype):
         raise ValueError(f"zeros: a contiguous {shape} uint8 tensor is wanted")
 
 
+def _int_sizes(*sizes: int) -> None:
+    """The descriptors' sizes are C ints, and ctypes cuts what does not fit one."""
+    if max(sizes) > 0x7FFFFFFF:
+        raise ValueError(f"a size of {max(sizes)}: the library's matrix products take sizes below 2^31 at most")
+
+
 def _matvec_desc(x, scales, group, out):
     t = x.dtype
     if t is not torch.float16 and t is not torch.bfloat16:
@@ -539,6 +545,7 @@ def _matvec_desc(x, scales, group, out):
         raise ValueError(f"group: {group}, wanted a power of two of at least 32")
     ldx = _rows(x, "x")
     (M, K), N = x.shape, scales.shape[0]
+    _int_sizes(M, K, N)
     return samd_matvec_desc(M, N, K, group, ldx, N if out is None else _rows(out, "out", N, M, t), DTYPES[t])
 
 
@@ -670,6 +677,7 @@ def _empty_ld(rows: int, cols: int, ld: int, like: torch.Tensor) -> torch.Tensor
 def _ffn_desc(M, K, F, t, act, ldx, ldw, ldh) -> samd_ffn_desc:
     if t not in (torch.float16, torch.bfloat16):
         raise ValueError(f"{t}: float16 or bfloat16 is wanted")
+    _int_sizes(M, K, F)
     return samd_ffn_desc(M, K, F, ldx, ldw, ldh, DTYPES[t], _act(act))
 
 

@@ -174,3 +174,30 @@ def test_the_binding_checks_its_tensors():
             samd.gated_ffn_backward(*args)
     with pytest.raises(ValueError):  # host tensors
         samd.matvec4(x, lanes, s, 32, f)
+
+
+def test_the_binding_refuses_sizes_past_an_int():
+    """The descriptors hold sizes in 32 bits: 2^32 + 5 rows are not 5 (tensors without memory: only shapes are read)."""
+    t, far = torch.bfloat16, (1 << 32) + 5
+
+    def empty(*shape, dtype=t):
+        return torch.empty(shape, dtype=dtype, device="meta")
+
+    f = samd.fmt(4, True)
+    lanes, s = empty(8, 1, dtype=torch.int32), empty(8, 1)
+    with pytest.raises(ValueError, match="size"):
+        samd.matvec4(empty(far, 8), lanes, s, 32, f)
+    with pytest.raises(ValueError, match="size"):
+        samd.matvec4(empty(1, 8), empty(far, 1, dtype=torch.int32), empty(far, 1), 32, f)
+    with pytest.raises(ValueError, match="size"):
+        samd.matvec4(empty(1, far), empty(1, -(-far // 8), dtype=torch.int32), empty(1, -(-far // 32)), 32, f)
+    with pytest.raises(ValueError, match="size"):
+        samd.gated_matvec4(empty(far, 8), lanes, s, lanes, s, 32, f)
+    for M, K, F in ((far, 8, 8), (1, far - 5, 8), (1, 8, far - 5)):
+        with pytest.raises(ValueError, match="size"):
+            samd.gated_ffn_forward(empty(M, K), empty(F, K), empty(F, K))
+        x8, f8 = samd.block8_empty(M, K, "meta"), samd.block8_empty(M, F, "meta")
+        with pytest.raises(ValueError, match="size"):
+            samd.gated_ffn_backward(empty(M, F), x8, f8, f8, empty(F, K), empty(F, K))
+    # what fits is answered by the library's own limit, or by the tensors' kind
+    assert samd._matvec_desc(empty((1 << 31) - 1, 8), s, 32, None).M == (1 << 31) - 1
