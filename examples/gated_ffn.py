@@ -25,7 +25,9 @@ def pack_weights(w: torch.Tensor, group: int):
     """(packed signed 4-bit lanes, scales) of a weight matrix (N, K), scaled by each group's largest magnitude."""
     N, K = w.shape
     pad = torch.nn.functional.pad(w.float(), (0, -K % group)).view(N, -1, group)
-    scales = (pad.abs().amax(-1) / 7).clamp(min=1e-8).to(w.dtype)
+    # a group of zeros has a scale too: of the type's smallest step, where that is above 1e-8 (which fp16 rounds to zero)
+    least = max(1e-8, torch.finfo(w.dtype).smallest_normal * torch.finfo(w.dtype).eps)
+    scales = (pad.abs().amax(-1) / 7).clamp(min=least).to(w.dtype)
     q = (pad / scales.float().unsqueeze(-1)).round().clamp(-8, 7).view(N, -1)[:, :K].to(torch.int8)
     return samd.pack(q, samd.fmt(4, True)).view(N, -1), scales
 

@@ -39,3 +39,19 @@ def test_packed_weights_are_the_librarys_lanes(samd_lib, example):
     want = x.double() @ stands.t()
     got = samd_lib.matvec4(x, lanes, scales, 32, samd_lib.fmt(4, True))
     assert float((got.double() - want).norm() / want.norm()) < 2.0 ** -11
+
+
+@pytest.mark.parametrize("t", [torch.float16, torch.bfloat16])
+def test_a_group_of_zeros(samd_lib, example, t):
+    """Its scale is not zero, its lanes are, and it adds nothing."""
+    torch.manual_seed(1)
+    w = torch.randn((40, 96), device="cuda").to(t)
+    w[3, 32:64] = 0
+    w[9] = 0
+    lanes, scales = example.pack_weights(w, 32)
+    assert (scales > 0).all() and torch.isfinite(scales).all()
+    q = samd_lib.unpack(lanes, samd_lib.fmt(4, True), 40, 96).view(40, 96)
+    assert not q[3, 32:64].any() and not q[9].any() and q[3, :32].any()
+    x = torch.randn((1, 96), device="cuda").to(t)
+    got = samd_lib.matvec4(x, lanes, scales, 32, samd_lib.fmt(4, True))
+    assert torch.isfinite(got).all() and got[0, 9] == 0
