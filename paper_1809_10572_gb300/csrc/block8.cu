@@ -107,9 +107,12 @@ __device__ __forceinline__ void store_staged(T *p, int64_t left, float *stage, i
   __syncwarp();
 }
 
+// (No const __restrict__ parameters: they allow loads by the read-only path,
+// which is for data that nothing writes while a kernel lives, and these are
+// set up while their input may still be written.)
 template <typename T, bool kVec>
-__global__ void __launch_bounds__(kThreads) block8_quantize_kernel(const T *__restrict__ x, uint32_t *__restrict__ lanes,
-                                                                   uint8_t *__restrict__ exps, const Block8Args a) {
+__global__ void __launch_bounds__(kThreads) block8_quantize_kernel(const T *x, uint32_t *lanes, uint8_t *exps,
+                                                                   const Block8Args a) {
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
   __shared__ float stage[kVec ? 1 : kThreads / 32][kVec ? 1 : kStageWords];
@@ -149,8 +152,7 @@ __global__ void __launch_bounds__(kThreads) block8_quantize_kernel(const T *__re
 
 template <typename T, bool kVec>
 __global__ void __launch_bounds__(kThreads)
-    block8_dequantize_kernel(const uint32_t *__restrict__ lanes, const uint8_t *__restrict__ exps, T *__restrict__ y,
-                             const Block8Args a) {
+    block8_dequantize_kernel(const uint32_t *lanes, const uint8_t *exps, T *y, const Block8Args a) {
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
   __shared__ float stage[kVec ? 1 : kThreads / 32][kVec ? 1 : kStageWords];

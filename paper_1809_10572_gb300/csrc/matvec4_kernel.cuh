@@ -146,12 +146,13 @@ __device__ __forceinline__ float f32_of_bits(uint16_t v) {
 
 // The lane's eight inputs k .. k + 7 of a token; those past K are zero and not read. Rows that are not 16-byte
 // aligned (kXVec false) are read by the 4-byte words that hold the inputs, shifted by half a word where those begin
-// in a word's middle (then with a ninth input of the row).
+// in a word's middle (then with a ninth input of the row). Plain loads: the read-only path is for data that nothing
+// writes while a kernel lives, and this one is set up while x may still be written.
 template <typename T, bool kXVec>
 __device__ __forceinline__ uint4 load_x8(const T *row, int64_t k, int K) {
   const int64_t left = K - k;
   if constexpr (kXVec) {
-    if (left >= 8) return __ldg(reinterpret_cast<const uint4 *>(row + k));
+    if (left >= 8) return *reinterpret_cast<const uint4 *>(row + k);
   } else {
     if (left > 8) {
       const uintptr_t at = reinterpret_cast<uintptr_t>(row + k);
@@ -159,8 +160,8 @@ __device__ __forceinline__ uint4 load_x8(const T *row, int64_t k, int K) {
       const bool half = (at & 2) != 0;
       uint32_t v[5];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = __ldg(p + i);
-      v[4] = half ? __ldg(p + 4) : 0u;
+      for (int i = 0; i < 4; ++i) v[i] = p[i];
+      v[4] = half ? p[4] : 0u;
       if (half) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(v[i], v[i + 1], 16);
@@ -171,7 +172,7 @@ __device__ __forceinline__ uint4 load_x8(const T *row, int64_t k, int K) {
   uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (i < left) w[i / 2] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t *>(row) + k + i)) << 16 * (i & 1);
+    if (i < left) w[i / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(row)[k + i]) << 16 * (i & 1);
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
   auto load_token = [&](int64_t k0, int c, int j, uint4 &q) {
     if (8 * j + g < tokens) {
       if (kXVec && k0 + KB <= a.K)
-        q = __ldg(reinterpret_cast<const uint4 *>(x_lane + (8 * j) * a.ldx + k0 + c * 32));
+        q = *reinterpret_cast<const uint4 *>(x_lane + (8 * j) * a.ldx + k0 + c * 32);
       else
         q = load_x8<T, kXVec>(x + (8 * j + g) * a.ldx, k0 + c * 32 + t * 8, a.K);
     }
@@ -421,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, 2) matvec4_kernel(const __grid_const
           const T *const xr = x_lane + k0;
           if (x_whole) {
 #pragma unroll
-            for (int c = 0; c < CH; ++c) xq[c] = __ldg(reinterpret_cast<const uint4 *>(xr + c * 32));
+            for (int c = 0; c < CH; ++c) xq[c] = *reinterpret_cast<const uint4 *>(xr + c * 32);
           } else {
 #pragma unroll
             for (int c = 0; c < CH; ++c) xq[c] = load_x8<T, kXVec>(x + g * a.ldx, k0 + c * 32 + t * 8, a.K);
