@@ -696,13 +696,18 @@ Pick pick_both(int64_t rows_x, int64_t steps_x, int64_t rows_w, int64_t steps_w,
   return best;
 }
 
-// Clusters of `split` CTAs of the kernel that the GPU holds at once; asked once for each size.
+// Clusters of `split` CTAs of the kernel that the current device holds at once
+// (0: none, or the query failed); asked once for each device and size.
 template <auto Kern>
 int resident_clusters(int split, size_t smem) {
+  constexpr int kDevices = 64;
   static std::mutex mu;
-  static int known[9];  // 0: not asked yet, -1: none
+  static int known[kDevices][9];  // 0: not asked yet, -1: none fit
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return 0;
   std::lock_guard<std::mutex> lock(mu);
-  if (known[split] == 0) {
+  int &held = known[dev][split];
+  if (held == 0) {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = split;
@@ -717,11 +722,11 @@ int resident_clusters(int split, size_t smem) {
     int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, Kern, &cfg) != cudaSuccess) {
       (void)cudaGetLastError();  // the query's own error; the launch reports any other
-      n = 0;
+      return 0;                  // (asked again by the next call)
     }
-    known[split] = n > 0 ? n : -1;
+    held = n > 0 ? n : -1;
   }
-  return known[split];
+  return held > 0 ? held : 0;
 }
 
 // The operands of a product before its tile is picked.

@@ -1,0 +1,12 @@
+"""The gated block's planning on the host (no GPU)."""
+from test_plan_cpu import run_host_program
+
+
+def test_resident_clusters_are_a_devices_and_failures_are_not_kept():
+    r = run_host_program("ffn_clusters")
+    assert r.returncode == 0, r.stderr[-2000:]
+    got = r.stdout.split()
+    said = {k: int(v) for k, v in zip(got[::2], got[1::2])}
+    assert said["failed"] < 1  # no clusters are counted on then
+    assert (said["first"], said["again"], said["other"], said["back"]) == (10, 10, 11, 10)
+    assert said["asked"] == 3  # the failure, and once a device
