@@ -97,6 +97,22 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, int *st
                     ptx::mbar_wait(bar, parity, status, static_cast<int>(SAMD_ETIMEOUT), kWaitLimitNs));
 }
 
+// BWD: CTA c's tile after `tile`, of P CTAs. The `first` tiles of DX go in turn
+// over the CTAs; those that have none in the last, partial turn take `fill`
+// rounds of DW's tiles meanwhile (as many as a DX tile lasts); then DW's go in
+// turn over all.
+__host__ __device__ inline int dealt_next(int tile, int c, int P, int first, int fill) {
+  const int rest = first % P, spare = P - rest;
+  const int base = first + (rest ? spare * fill : 0);  // the first tile that is dealt to all
+  const bool free = rest != 0 && c >= rest;
+  if (tile < first) {
+    if (tile + P < first) return tile + P;
+    return free && fill ? first + (c - rest) : base + c;
+  }
+  if (tile < base) return tile + spare < base ? tile + spare : base + c;
+  return tile + P;
+}
+
 // Columns [c, c + 32) of a row of the output, rounded.
 template <typename T>
 __device__ __forceinline__ void store_row32(T *row, int c, int N, bool wide, const float *v) {
@@ -231,23 +247,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   // a CTA's tiles and its steps of their reductions
   const int rank = kSplit ? blockIdx.x % a.split : 0;
   const int tile0 = kSplit ? blockIdx.x / a.split : blockIdx.x, tile_step = kSplit ? a.total : gridDim.x;
-  // The CTA's next tile. BWD: the tiles of DX in turn over the CTAs; those that
-  // have none in the last, partial turn take a.fill rounds of DW's tiles
-  // meanwhile (as many as a DX tile lasts); then DW's in turn over all.
+  // The CTA's next tile.
   auto next_tile = [&](int tile) {
-    if constexpr (FORM != BWD) {
+    if constexpr (FORM != BWD)
       return tile + tile_step;
-    } else {
-      const int P = gridDim.x, c = blockIdx.x, rest = a.first % P, spare = P - rest;
-      const int base = a.first + (rest ? spare * a.fill : 0);  // the first tile that is dealt to all
-      const bool free = rest != 0 && c >= rest;
-      if (tile < a.first) {
-        if (tile + P < a.first) return tile + P;
-        return free && a.fill ? a.first + (c - rest) : base + c;
-      }
-      if (tile < base) return tile + spare < base ? tile + spare : base + c;
-      return tile + P;
-    }
+    else
+      return dealt_next(tile, blockIdx.x, gridDim.x, a.first, a.fill);
   };
   const int tile_1 = FORM == BWD && tile0 >= a.first ? next_tile(tile0 - static_cast<int>(gridDim.x)) : tile0;
   // calls f with a tile's form, its job and its number there
@@ -681,6 +686,15 @@ Pick pick_tile(int form, int64_t rows, int64_t cols, int64_t steps, Clusters clu
 // DW's tiles that a CTA does in the time of one of DX's.
 int fill_of(int64_t steps_x, int64_t steps_w) { return static_cast<int>((2 * steps_x + steps_w) / (2 * steps_w)); }
 
+// The rounds of DW's tiles that a joint launch's spare CTAs are dealt: as many
+// as they have time for, and no more than there are (a dx of 2^24 reduction
+// steps beside weight gradients of one would count tiles past an int).
+int deal_fill(int first, int total, int fill) {
+  const int P = total < sm_count() ? total : sm_count(), spare = P - first % P;
+  const int most = (total - first + spare - 1) / spare;
+  return fill < most ? fill : most;
+}
+
 // DX and DW in one launch: its columns, and the time.
 Pick pick_both(int64_t rows_x, int64_t steps_x, int64_t rows_w, int64_t steps_w, int64_t cols) {
   Pick best = {256, 1, INT64_MAX};
@@ -917,7 +931,7 @@ cudaError_t backward(const samd_ffn_desc &d, const void *dh, samd_block8 cx, sam
       a.job[1] = jw;
       a.first = set_tiles(a.job[0], DX, pb.columns, false);
       a.total = a.first + set_tiles(a.job[1], DW, pb.columns, two);
-      a.fill = fill_of(sx, sw);
+      a.fill = deal_fill(a.first, a.total, fill_of(sx, sw));
       a.split = 1;
       return launch_columns<BWD, T, 0>(pb.columns, maps, a, s);
     }

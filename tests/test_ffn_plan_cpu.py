@@ -10,3 +10,9 @@ def test_resident_clusters_are_a_devices_and_failures_are_not_kept():
     assert said["failed"] < 1  # no clusters are counted on then
     assert (said["first"], said["again"], said["other"], said["back"]) == (10, 10, 11, 10)
     assert said["asked"] == 3  # the failure, and once a device
+
+
+def test_a_joint_launch_deals_every_tile_once():
+    r = run_host_program("ffn_deal")
+    assert r.returncode == 0 and "bad 0" in r.stdout, r.stdout[-2000:]
+    assert int(r.stdout.split("dealt ")[1].split(",")[0]) > 20000
