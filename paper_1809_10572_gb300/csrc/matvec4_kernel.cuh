@@ -662,6 +662,9 @@ cudaError_t launch_grouped(const MvArgs &a, cudaStream_t s) {
   return launch_as<T, kGated, kZeros, kXVec, RT, NT, CH, 4>(a, s);
 }
 
+// Whether tiles of 32 rows still give every SM two CTAs.
+inline bool two_row_tiles(int N) { return N >= 2 * 32 * sm_count(); }
+
 // Which instance: 8, 16 or 32 tokens a pass. Up to eight: blocks of 256 inputs
 // where there are at least eight of them for the warps (K = 1024 leaves half
 // the warps idle with them), of 128 otherwise; two row tiles share a CTA's
@@ -680,7 +683,7 @@ cudaError_t launch_sized(const MvArgs &a, cudaStream_t s) {
   if (a.M > 8) return launch_grouped<T, kGated, kZeros, true, kRT, 2, 4>(a, s);
   if (a.K < 2048) return launch_grouped<T, kGated, kZeros, true, 1, 1, 4>(a, s);
   if constexpr (!kGated)
-    if (a.N >= 9728)
+    if (two_row_tiles(a.N))
       return a.M <= 2 ? launch_grouped<T, kGated, kZeros, true, 2, 1, 8>(a, s)
                       : launch_grouped<T, kGated, kZeros, true, 2, 1, 4>(a, s);
   return launch_grouped<T, kGated, kZeros, true, 1, 1, 8>(a, s);

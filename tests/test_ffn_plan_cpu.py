@@ -16,3 +16,10 @@ def test_a_joint_launch_deals_every_tile_once():
     r = run_host_program("ffn_deal")
     assert r.returncode == 0 and "bad 0" in r.stdout, r.stdout[-2000:]
     assert int(r.stdout.split("dealt ")[1].split(",")[0]) > 20000
+
+
+def test_two_row_tiles_where_they_leave_every_sm_two_ctas():
+    r = run_host_program("matvec_rows")
+    assert r.returncode == 0, r.stderr[-2000:]
+    got = [tuple(map(int, line.split())) for line in r.stdout.splitlines()]
+    assert got == [(s, 2 * 32 * s) for s in (100, 148, 152, 160)]
