@@ -307,6 +307,13 @@ SAMD_API samd_status samd_maxpool2x2(samd_fmt f, const void *in, void *out, int 
  * allocation, checks on the host before any launch. Strides ld* are in
  * elements, from one row to the next. Inputs may overlap one another; no output
  * may overlap an input or another output.
+ *
+ * The waits in the matrix products' kernels (samd_matvec4, samd_gated_matvec4,
+ * samd_gated_ffn_*) are bounded as the convolution's are. One that runs out
+ * records SAMD_ETIMEOUT for samd_device_status and leaves the call's outputs
+ * undefined. So does a failure on record: after one of any call on the device,
+ * a convolution too, and until samd_device_status resets it, these calls may
+ * give up at their first wait, although they return SAMD_OK.
  */
 typedef enum { SAMD_F16 = 0, SAMD_BF16 = 1, SAMD_F32 = 2 } samd_dtype;
 
@@ -348,9 +355,10 @@ typedef struct {
  * samd_matvec4: y[m][n] = sum_k x[m][k] * weight[n][k], summed in fp32 and
  * rounded once. fw: 4-bit lanes without spacers, 32- or 64-bit words; signed
  * lanes take no zero points (SAMD_EINVAL). Made for few tokens (it reads the
- * weights once for every 32 of them); any M >= 0 is right. Each output depends
- * on its row of x and its row of weights alone, and the same inputs give the
- * same bits.
+ * weights once for every 32 of them); any M >= 0 is right. An output is its own
+ * row of x by its own row of weights. The same call gives the same bits; the
+ * order of a sum, and so its last bits, may change with the sizes, the group and
+ * ldx: a token's outputs need not be the same bits beside other tokens.
  */
 SAMD_API samd_status samd_matvec4(const samd_matvec_desc *desc, samd_fmt fw, const void *x, samd_weights4 w, void *y,
                                   samd_stream_t stream);
@@ -425,8 +433,6 @@ SAMD_API size_t samd_gated_ffn_backward_workspace_size(const samd_ffn_desc *desc
  * and wu for dx only. With M = 0 the weights' gradients are zero. workspace:
  * caller-owned device scratch of at least
  * samd_gated_ffn_backward_workspace_size bytes (else SAMD_ESHAPE).
- * As with the convolution, a kernel that gives up on a bounded wait leaves its
- * outputs undefined and records SAMD_ETIMEOUT for samd_device_status.
  */
 SAMD_API samd_status samd_gated_ffn_backward(const samd_ffn_desc *desc, const void *dh, samd_block8 ckpt_x,
                                              samd_block8 ckpt_g, samd_block8 ckpt_u, const void *wg, const void *wu,

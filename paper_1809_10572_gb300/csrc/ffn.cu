@@ -24,9 +24,9 @@
 // gradients' factors and their sums.
 //
 // Measured (one GB300): 4096 x 4096 x 8192 forward 322 us (1.71 PFLOP/s) in a
-// short run, 354 under the power cap; 8192 x 4096 x 8192 bf16 step 2.00 ms (1.65
-// PFLOP/s), 2.24 under it, where the library product of that size holds 1.66
-// PFLOP/s. Large products are bound by power (1.6 GHz of 2.07), small ones by
+// short run, 354 to 366 under the power cap; 8192 x 4096 x 8192 bf16 step 2.01 ms
+// (1.64 PFLOP/s), 2.24 to 2.29 under it, where the library product of that size
+// holds 1.66 PFLOP/s. Large products are bound by power (1.6 GHz of 2.07), small ones by
 // start, end and the reduction steps of one CTA (pick_tile). DX and DW in one
 // launch: the step of 2048 x 2048 x 4096 167 -> 153 us, of 777 x 1000 x 2736
 // 65 -> 57.

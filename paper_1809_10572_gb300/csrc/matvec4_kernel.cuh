@@ -32,14 +32,17 @@
 // Tokens come through L1, which holds a CTA's x from tile to tile.
 //
 // Measured (one GB300, weights not in L2): one bf16 token by 65536 x 4096 with
-// scales for 64 inputs 34.4 us, 4.2 TB/s, 0.62 of the copy bandwidth (fp16 0.69,
+// scales for 64 inputs 34.5 us, 4.1 TB/s, 0.62 of the copy bandwidth (fp16 0.69,
 // scales for 32 inputs 0.64, zero points 0.57). About 42 instructions for 512
-// weights, half of them on the 64-lane integer pipe, which is busy 55% of the
-// time: issue and that pipe bound it, not memory. A CTA for each tile took 65
-// us (rings that start and drain for every tile); shifts on the multiplier
-// instead 40; tokens permuted once into shared memory 36. From nine tokens on
-// x's way from L2 (every tile reads all of it) and its latency bound it: 16
-// tokens by 8192 x 8192 18 us, 32 tokens 33 (four row tiles a CTA: 24 and 32).
+// weights, half of them on the 64-lane integer pipe. No unit is full: issue
+// slots are 58% busy, that pipe 55%. Sixteen warps an SM do not hide what an
+// instruction waits for: of the 6.3 clocks from one of a warp's to its next, 1.1
+// go to others' turns, 1.1 to the pipe, 1.0 to fixed latencies, 0.7 to tokens. A
+// CTA for each tile took 65 us (rings that start and drain for every tile);
+// shifts on the multiplier instead 40; tokens permuted once into shared memory
+// 36. From nine tokens on x's way from L2 (every tile reads all of it) and its
+// latency bound it: 16 tokens by 8192 x 8192 18 us, 32 tokens 34 (four row tiles
+// a CTA: 24 and 32).
 #pragma once
 
 #include "ffn_internal.cuh"
@@ -192,8 +195,9 @@ struct Mv {
   static constexpr int kWBytes = kRows * kPitch;  // a stage's weights (whole 1024- or 512-byte swizzle patterns)
   static constexpr int kZOff = kRows * kSPitch;
   static constexpr int kSzBytes = kZOff + (kZeros ? kRows * kZPitch : 0);  // its scales and zero points
-  // as many stages as leave an SM two CTAs (one token by 65536 x 4096 with zero points: 43.3 us with three stages and
-  // one CTA)
+  // as many stages as leave an SM two CTAs of one token (one by 65536 x 4096 with zero points: 43.3 us with three stages
+  // and one CTA). The sums of more tokens are not counted: with scales for 32 inputs 32 tokens leave one CTA an SM, with
+  // zero points 24 of them, and 32 with zero points and scales for 64.
   static constexpr int fit(int stages) {
     return kWarps * stages * (kWBytes + kSzBytes + 8) + kWarps * kRows * 4 + 1024 <= 114 * 1024;
   }
@@ -669,8 +673,9 @@ inline bool two_row_tiles(int N) { return N >= 2 * 32 * sm_count(); }
 // where there are at least eight of them for the warps (K = 1024 leaves half
 // the warps idle with them), of 128 otherwise; two row tiles share a CTA's
 // tokens and its fixed work where that still gives every SM two CTAs' worth
-// (one token by 65536 x 4096: 45.7 us with one, 37.8 with two), with blocks of
-// 128 for more than two tokens, whose stages and sums would leave an SM one CTA.
+// (one token by 65536 x 4096 took 45.7 us with one and 37.8 with two, before
+// the weights came by TMA), with blocks of 128 for more than two tokens, whose
+// stages and sums would leave an SM one CTA.
 template <typename T, bool kGated, bool kZeros>
 cudaError_t launch_sized(const MvArgs &a, cudaStream_t s) {
   constexpr int kRT = kGated ? 1 : 2;
