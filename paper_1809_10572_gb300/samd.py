@@ -531,10 +531,9 @@ def _check_weights4(lanes, scales, zeros, N, K, group, f, dtype):
         raise ValueError(f"zeros: a contiguous {shape} uint8 tensor is wanted")
 
 
-def _int_sizes(*sizes: int) -> None:
+def _past_int(*sizes: int):
     """The descriptors' sizes are C ints, and ctypes cuts what does not fit one."""
-    if max(sizes) > 0x7FFFFFFF:
-        raise ValueError(f"a size of {max(sizes)}: the library's matrix products take sizes below 2^31 at most")
+    raise ValueError(f"a size of {max(sizes)}: the library's matrix products take sizes below 2^31 at most")
 
 
 def _matvec_desc(x, scales, group, out):
@@ -545,7 +544,8 @@ def _matvec_desc(x, scales, group, out):
         raise ValueError(f"group: {group}, wanted a power of two of at least 32")
     ldx = _rows(x, "x")
     (M, K), N = x.shape, scales.shape[0]
-    _int_sizes(M, K, N)
+    if (M | K | N) >> 31:
+        _past_int(M, K, N)
     return samd_matvec_desc(M, N, K, group, ldx, N if out is None else _rows(out, "out", N, M, t), DTYPES[t])
 
 
@@ -677,7 +677,8 @@ def _empty_ld(rows: int, cols: int, ld: int, like: torch.Tensor) -> torch.Tensor
 def _ffn_desc(M, K, F, t, act, ldx, ldw, ldh) -> samd_ffn_desc:
     if t not in (torch.float16, torch.bfloat16):
         raise ValueError(f"{t}: float16 or bfloat16 is wanted")
-    _int_sizes(M, K, F)
+    if (M | K | F) >> 31:
+        _past_int(M, K, F)
     return samd_ffn_desc(M, K, F, ldx, ldw, ldh, DTYPES[t], _act(act))
 
 
