@@ -440,6 +440,88 @@ SAMD_API samd_status samd_gated_ffn_backward(const samd_ffn_desc *desc, const vo
                                              size_t workspace_bytes, samd_stream_t stream);
 
 /*
+ * ---- A key-value cache in packed lanes: writing, reading, attention of one
+ * ---- new token, eviction; and a layer of experts on 4-bit weights.
+ *
+ * What serving the block above needs next to it. The conventions of the top of
+ * this file and of the gated block hold.
+ *
+ * A cache is `pages` pages of `page` tokens (a power of two, 16 or more) for
+ * `heads` key heads of `dim` elements (a multiple of 32, 32 .. 256). A row is
+ * one token's key or value of one head: its lanes as samd_pack writes them
+ * (signed, 4 or 8 bits, 32-bit words, no spacers), and a scale of `type`
+ * (SAMD_F16 or SAMD_BF16) for every 32 of them. All four arrays hold their rows
+ * as [pages][heads][page]. The value of lane q is scale * q. samd_cache_append
+ * writes, with L = 2^(bits - 1) - 1,
+ *   scale = max |v| / L rounded to `type`; q = v / scale rounded to even and
+ *   clamped to -L .. L (0 where the scale is 0); a block with an infinity or a
+ *   NaN has a NaN for its scale and zero lanes, and stands for NaNs.
+ */
+typedef struct {
+  int pages, page, heads, dim;
+  samd_fmt fmt;
+  samd_dtype type;
+  void *k_lanes, *k_scales, *v_lanes, *v_scales;
+} samd_cache;
+
+/*
+ * `seqs` sequences in a cache: token t of sequence b lies in slot t mod page of
+ * page table[b * ld + t / page]; lengths[b] is how many tokens it has (device
+ * memory both). A length below 0 counts as 0, one above max_pages * page as
+ * that. An entry of the table that names none of the cache's pages holds no
+ * tokens. Sequences may share pages that none of them writes.
+ */
+typedef struct {
+  int seqs, max_pages;
+  int64_t ld;
+  const int32_t *table, *lengths;
+} samd_cache_seqs;
+
+/*
+ * samd_cache_append: k and v hold `tokens` new tokens, rows of heads * dim
+ * elements of the cache's type (strides ldk, ldv, multiples of 8, else
+ * SAMD_EALIGN). starts[b] .. starts[b + 1] - 1 are those of sequence b (device
+ * memory, seqs + 1 entries, rising); NULL: tokens = seqs (else SAMD_ESHAPE) and
+ * row b is sequence b's. lengths counts the new tokens already: sequence b's
+ * are its last ones. A token whose place would lie before the sequence's start
+ * (a padded batch: length 0), behind its pages or in no page is left out, and so
+ * are rows of no sequence. Rows that are written have to be in pages of that
+ * sequence alone.
+ */
+SAMD_API samd_status samd_cache_append(const samd_cache *cache, const samd_cache_seqs *seqs, const int32_t *starts,
+                                       int tokens, const void *k, int64_t ldk, const void *v, int64_t ldv,
+                                       samd_stream_t stream);
+/*
+ * samd_cache_read: the values of the same rows, rounded to the type, into k and
+ * v: what samd_cache_append with these arguments wrote. A token without a place
+ * gives zeros; rows of no sequence are left as they are.
+ */
+SAMD_API samd_status samd_cache_read(const samd_cache *cache, const samd_cache_seqs *seqs, const int32_t *starts,
+                                     int tokens, void *k, int64_t ldk, void *v, int64_t ldv, samd_stream_t stream);
+
+/* Bytes of workspace samd_paged_attention needs on the current device (0 on
+ * error, or where it needs none); `scores` tells whether it gets them. */
+SAMD_API size_t samd_paged_attention_workspace_size(const samd_cache *cache, const samd_cache_seqs *seqs, int q_heads,
+                                                    int scores);
+/*
+ * samd_paged_attention: one query token for each sequence; q and out are rows
+ * of q_heads * dim elements of the cache's type (strides ldq, ldo, multiples of
+ * 8); q_heads is a multiple of the cache's heads, up to 256 times them, and key head h serves
+ * query heads h * G .. h * G + G - 1.
+ *   p = softmax over the sequence's tokens t of scale * sum_d q_d K_td,
+ *   out_d = sum_t p_t V_td, rounded once; a sequence without tokens gives 0.
+ * scores, or NULL: fp32 [seqs][heads][ld_scores]; to each token's place
+ * (t < ld_scores) the sum of p_t over the G query heads is added: the weight
+ * that samd_cache_evict goes by. The same call gives the same bits; the order
+ * of sums changes with the batch's lengths. q, key and value of infinity or NaN
+ * give NaNs in their own head only. |scale| has to be finite (SAMD_EINVAL).
+ */
+SAMD_API samd_status samd_paged_attention(const samd_cache *cache, const samd_cache_seqs *seqs, int q_heads,
+                                          const void *q, int64_t ldq, float scale, void *out, int64_t ldo,
+                                          float *scores, int64_t ld_scores, void *workspace, size_t workspace_bytes,
+                                          samd_stream_t stream);
+
+/*
  * samd_device_status: reads (and with reset=1 clears) the sticky status the
  * kernels of the current device record when a bounded wait runs out.
  * Synchronises `stream`. *status is SAMD_OK or SAMD_ETIMEOUT.

@@ -1,0 +1,207 @@
+// kv_cache.cu -- rows of keys and values into the packed cache, and back.
+//
+//   scale = round16(max |v| / L), lane = round(v / scale) clamped to -L .. L,
+//   L = 2^(bits - 1) - 1, for every 32 neighbouring elements of a row.
+//
+// Both are one pass: 2 bytes an element on the wide side, bits / 8 + 1/16 in
+// the cache. Two neighbouring lanes hold a block, sixteen elements each, and
+// find its largest magnitude with a shuffle.
+//
+// The lane is the rounded quotient, without a division: v and the scale have
+// at most 11 significant bits each, so a quotient that is not half way between
+// two integers is at least 2^-12 away from there, and v * (1 / scale), whose
+// error is below 2^-15, rounds to the same integer; a quotient that is half way
+// is told by the remainder v - lane * scale, which is exact.
+#include "cache_internal.cuh"
+#include "tc_ptx.cuh"
+
+namespace samd {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPer = 16;  // elements a thread handles
+
+struct RowArgs {
+  kv::Seqs s;
+  const int32_t *starts;
+  uint8_t *lanes[2], *scales[2];  // of keys and of values
+  uint8_t *x[2];
+  int64_t ld[2];                  // of x, in bytes
+  int64_t items;                  // tokens x 2 x heads x dim / kPer
+  IndexDiv by_token, by_matrix, by_head;
+  int heads, dim;
+};
+
+struct Item {
+  int64_t token, x_at, row;  // x_at: bytes from x; row: of the cache, or below 0
+  int m, e;                  // 0: keys, 1: values; first element
+};
+
+__device__ __forceinline__ Item item_of(const RowArgs &a, int64_t n) {
+  Item it;
+  it.token = idiv(n, a.by_token);
+  int64_t left = n - it.token * a.by_token.d;
+  it.m = static_cast<int>(idiv(left, a.by_matrix));
+  left -= it.m * a.by_matrix.d;
+  const int h = static_cast<int>(idiv(left, a.by_head));
+  it.e = static_cast<int>(left - h * a.by_head.d) * kPer;
+  it.x_at = it.token * a.ld[it.m] + (static_cast<int64_t>(h) * a.dim + it.e) * 2;
+  const int64_t p = kv::place_of(a.s, a.starts, static_cast<int>(it.token));
+  it.row = p < 0 ? p : kv::row_of(a.s, p, a.heads, h);
+  return it;
+}
+
+template <typename T>
+__device__ __forceinline__ uint16_t bits_of(float v) {
+  const T t = from_f32<T>(v);
+  return reinterpret_cast<const uint16_t &>(t);
+}
+
+template <typename T, int BITS>
+__global__ void __launch_bounds__(kThreads) cache_append_kernel(const RowArgs a) {
+  ptx::grid_dependency_wait();
+  ptx::grid_dependents_launch();
+  constexpr float kMost = BITS == 8 ? 127.0f : 7.0f;
+  constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: adding it rounds to an integer, which its low bits then hold
+  for (int64_t n = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;; n += static_cast<int64_t>(gridDim.x) * kThreads) {
+    // (a block's two threads, an even lane and the next, are both in or both out)
+    const bool on = n < a.items;
+    if (!__any_sync(0xffffffffu, on)) break;
+    Item it = {};
+    it.row = -1;
+    float v[kPer], top = 0.0f;
+    if (on) {
+      it = item_of(a, n);
+      const uint4 *const p = reinterpret_cast<const uint4 *>(a.x[it.m] + it.x_at);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint4 q = p[i];
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 f = unpack2<T>(w[k]);
+          v[8 * i + 2 * k] = f.x;
+          v[8 * i + 2 * k + 1] = f.y;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) top = max_abs(top, v[i]);
+    }
+    top = max_abs(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    if (!on || it.row < 0) continue;
+    const bool fine = top <= 3.402823466e38f;  // no infinity, no NaN
+    const uint16_t raw = fine ? bits_of<T>(__fdiv_rn(top, kMost)) : static_cast<uint16_t>(0x7FFF);
+    const float s = fine ? to_f32<T>(reinterpret_cast<const T &>(raw)) : 0.0f;
+    uint32_t w[BITS / 2] = {};  // of sixteen lanes
+    if (s > 0.0f) {
+      const float inv = __fdiv_rn(1.0f, s);
+      if (inv <= 3.402823466e38f) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          float k = __fadd_rn(__fmul_rn(v[i], inv), kMagic) - kMagic;
+          const float left = fmaf(-k, s, v[i]);
+          if (fabsf(left) + fabsf(left) == s && (static_cast<int>(k) & 1)) k += copysignf(1.0f, left);
+          k = fminf(fmaxf(k, -kMost), kMost);
+          const uint32_t q = __float_as_uint(k + kMagic) & ((1u << BITS) - 1);
+          w[i * BITS / 32] |= q << (i * BITS % 32);
+        }
+      } else {  // a scale of bfloat16 below 2^-127
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const float k = fminf(fmaxf(rintf(__fdiv_rn(v[i], s)), -kMost), kMost);
+          w[i * BITS / 32] |= (static_cast<uint32_t>(static_cast<int>(k)) & ((1u << BITS) - 1)) << (i * BITS % 32);
+        }
+      }
+    }
+    uint8_t *const to = a.lanes[it.m] + (it.row * a.dim + it.e) / 8 * BITS;
+    if constexpr (BITS == 8)
+      *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    else
+      *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+    if ((it.e & 16) == 0)
+      *reinterpret_cast<uint16_t *>(a.scales[it.m] + (it.row * a.dim + it.e) / 16) = raw;
+  }
+}
+
+template <typename T, int BITS>
+__global__ void __launch_bounds__(kThreads) cache_read_kernel(const RowArgs a) {
+  ptx::grid_dependency_wait();
+  ptx::grid_dependents_launch();
+  for (int64_t n = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; n < a.items;
+       n += static_cast<int64_t>(gridDim.x) * kThreads) {
+    const Item it = item_of(a, n);
+    if (it.row == -2) continue;
+    uint32_t w[BITS / 2] = {};
+    float s = 0.0f;
+    if (it.row >= 0) {
+      const uint8_t *const from = a.lanes[it.m] + (it.row * a.dim + it.e) / 8 * BITS;
+      if constexpr (BITS == 8) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(from);
+        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+      } else {
+        const uint2 q = *reinterpret_cast<const uint2 *>(from);
+        w[0] = q.x, w[1] = q.y;
+      }
+      s = to_f32<T>(*reinterpret_cast<const T *>(a.scales[it.m] + (it.row * a.dim + it.e) / 32 * 2));
+    }
+    uint32_t out[kPer / 2];
+#pragma unroll
+    for (int i = 0; i < kPer / 2; ++i) {
+      float f[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int at = (2 * i + j) * BITS;
+        const int q = static_cast<int>(w[at / 32] << (32 - BITS - at % 32)) >> (32 - BITS);
+        f[j] = static_cast<float>(q) * s;
+      }
+      out[i] = pack2<T>(f[0], f[1]);
+    }
+    uint4 *const p = reinterpret_cast<uint4 *>(a.x[it.m] + it.x_at);
+    p[0] = make_uint4(out[0], out[1], out[2], out[3]);
+    p[1] = make_uint4(out[4], out[5], out[6], out[7]);
+  }
+}
+
+RowArgs make_args(const samd_cache &c, const samd_cache_seqs &s, const int32_t *starts, int tokens, const void *k,
+                  int64_t ldk, const void *v, int64_t ldv) {
+  RowArgs a = {};
+  a.s = kv::make_seqs(c, s);
+  a.starts = starts;
+  a.lanes[0] = static_cast<uint8_t *>(c.k_lanes), a.lanes[1] = static_cast<uint8_t *>(c.v_lanes);
+  a.scales[0] = static_cast<uint8_t *>(c.k_scales), a.scales[1] = static_cast<uint8_t *>(c.v_scales);
+  a.x[0] = static_cast<uint8_t *>(const_cast<void *>(k)), a.x[1] = static_cast<uint8_t *>(const_cast<void *>(v));
+  a.ld[0] = ldk * 2, a.ld[1] = ldv * 2;
+  a.heads = c.heads, a.dim = c.dim;
+  const int64_t head = c.dim / kPer, matrix = head * c.heads;
+  a.items = 2 * matrix * tokens;
+  a.by_token = make_index_div(a.items, 2 * matrix);
+  a.by_matrix = make_index_div(2 * matrix, matrix);
+  a.by_head = make_index_div(matrix, head);
+  return a;
+}
+
+template <typename T, int BITS, bool kAppend>
+cudaError_t launch_as(const RowArgs &a, cudaStream_t s) {
+  constexpr auto kern = kAppend ? cache_append_kernel<T, BITS> : cache_read_kernel<T, BITS>;
+  return launch_dependent(kern, dim3(resident_grid<kern>(a.items, kThreads)), kThreads, 0, s, 1, a);
+}
+template <bool kAppend>
+cudaError_t launch(const samd_cache &c, const RowArgs &a, cudaStream_t s) {
+  if (c.type == SAMD_BF16)
+    return c.fmt.bits == 8 ? launch_as<__nv_bfloat16, 8, kAppend>(a, s) : launch_as<__nv_bfloat16, 4, kAppend>(a, s);
+  return c.fmt.bits == 8 ? launch_as<__half, 8, kAppend>(a, s) : launch_as<__half, 4, kAppend>(a, s);
+}
+
+}  // namespace
+
+cudaError_t launch_cache_append(const samd_cache &c, const samd_cache_seqs &s, const int32_t *starts, int tokens,
+                                const void *k, int64_t ldk, const void *v, int64_t ldv, cudaStream_t stream) {
+  return launch<true>(c, make_args(c, s, starts, tokens, k, ldk, v, ldv), stream);
+}
+
+cudaError_t launch_cache_read(const samd_cache &c, const samd_cache_seqs &s, const int32_t *starts, int tokens, void *k,
+                              int64_t ldk, void *v, int64_t ldv, cudaStream_t stream) {
+  return launch<false>(c, make_args(c, s, starts, tokens, k, ldk, v, ldv), stream);
+}
+
+}  // namespace samd

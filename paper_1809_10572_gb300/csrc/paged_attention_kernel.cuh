@@ -1,0 +1,663 @@
+// paged_attention_kernel.cuh -- attention of one new token of each sequence
+// over a paged cache of packed lanes.
+//
+//   x_t = scale log2(e) sum_d q_d K_td,  out_d = sum_t 2^x_t V_td / sum_t 2^x_t
+//
+// Bound by its reads: a cached token of a key head comes once, 2 dim bits / 8
+// bytes and a scale of 16 bits for 32 lanes. Every lane has to be widened to a
+// 16-bit float and multiplied with up to eight query heads, which is more than
+// the CUDA cores can do at that rate, so the products go through mma.sync
+// (m16n8k16): 16 tokens by the 8 heads for the logits, 16 elements by the 8
+// heads for the sums. tcgen05 would want the widened lanes in shared memory, at
+// two to four times the bytes that come from HBM.
+//
+// Numbers: a lane over the mantissa of a power of two is that power plus the
+// lane, subtracting both is exact in fp16, so the products are those of the
+// integers. q is brought into fp16's range by a power of two of its head (its
+// largest magnitude to 2^13 .. 2^14: bfloat16's eight and fp16's eleven bits are
+// kept, what lies 2^-27 below the largest is rounded at 2^-38 of it). The sums
+// of 32 elements are scaled in fp32. For the second product the weight of a
+// token and the scale of its 32 values go together, p = 2^(x - ref) s, rounded
+// once to fp16 (2^-11, as a result in fp16 is). ref is a running
+// reference of each head: the largest x + log2 s seen, less 6; it moves only
+// when a weight passes 2^15 (nine doublings later), so that a step's common
+// path has no reduction over tokens. Weights below 2^-30 of the largest seen
+// are rounded at 2^-31 of it. Logits, weights' sums and outputs are in fp32.
+// (Scales outside 2^-90 .. 2^110 are taken for the nearer bound in ref: values
+// that small are lost, values that large may come out infinite.)
+//
+// Layout: a warp takes 16 tokens (one step, never more than one page) through a
+// ring of its own in shared memory, filled by cp.async of 16 bytes a lane; rows
+// an odd number of 16-byte units apart, so that ldmatrix reads eight rows
+// without conflicts. ldmatrix deals a token's word to the thread that has it
+// in the MMA's operand (keys), and transposed two tokens' lanes of one element
+// (values). The weights change operand layout by movmatrix.
+//
+// Split: all steps of all sequences and key heads lie in one line, of which
+// every CTA takes an equal part, whatever the lengths; its warps take steps in
+// turn. A CTA's parts of two heads are finished one after the other (the ring
+// runs on); where a head's steps lie in several CTAs, each leaves its sums and
+// references in the workspace for paged_attention_join (fixed order: the same
+// call gives the same bits). Head groups of more than eight query heads are
+// neighbouring CTAs that read the same pages at the same time.
+#pragma once
+
+#include "cache_internal.cuh"
+#include "tc_ptx.cuh"
+
+namespace samd {
+namespace kv {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kHeads = 8;     // query heads of a CTA: the MMA's columns
+constexpr int kMinSteps = 8;  // a CTA is not used for fewer
+
+struct AttArgs {
+  Seqs s;
+  const uint8_t *k, *v, *ks, *vs;
+  const uint8_t *q;
+  uint8_t *out;
+  int64_t ldq, ldo;  // bytes
+  float scale;       // with log2(e)
+  int heads;         // of keys
+  int group;         // query heads of a key head
+  int parts;         // CTAs that share a key head's pages: ceil(group / per)
+  int per;           // query heads of a CTA
+  int slots;         // CTAs of a part
+  int whole;         // CTAs take whole heads: nothing is split
+  // the workspace
+  float *sums;       // [CTA][2][kHeads][dim]
+  float2 *stat;      // [CTA][kHeads]: reference and sum of weights, of the part of a head that it goes on with
+  float2 *head_stat; // [unit][part][kHeads]: of a head's first part; or null, where nothing is split or counted
+  int2 *span;        // [unit][part]: first and last slot
+  float *logits;     // [unit][part][tokens of max_pages][kHeads]; or null
+};
+
+// ---- where the steps lie ---------------------------------------------------------
+
+__host__ __device__ __forceinline__ int steps_of(const Seqs &s, int b) {
+  return static_cast<int>((length_of(s, b) + kStep - 1) / kStep);
+}
+
+// CTAs that are used for so many steps, and the steps of one of them.
+__host__ __device__ __forceinline__ int64_t used_of(int64_t all, int slots) {
+  const int64_t most = (all + kMinSteps - 1) / kMinSteps;
+  return most < slots ? most : slots;
+}
+__host__ __device__ __forceinline__ int64_t begin_of(int64_t slot, int64_t all, int64_t used) { return slot * all / used; }
+
+// By the whole CTA: its steps [begin, end), the sequence that the first lies in, and the step's place from that
+// sequence's first, *rem. Returns the number of all steps. tmp: kWarps + 2.
+__device__ __forceinline__ int64_t locate(const Seqs &s, int heads, int slot, int slots, int64_t *tmp, int *b_out,
+                                          int64_t *begin, int64_t *end, int64_t *rem) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int chunk = (s.seqs + kThreads - 1) / kThreads, b0 = tid * chunk;
+  int64_t mine = 0;
+  for (int b = b0; b < min(b0 + chunk, s.seqs); ++b) mine += steps_of(s, b);
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) tmp[warp] = incl;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) before += tmp[w];
+    all += tmp[w];
+  }
+  all *= heads;
+  const int64_t used = used_of(all, slots);
+  *begin = *end = 0;
+  if (slot < used) {
+    *begin = begin_of(slot, all, used);
+    *end = begin_of(slot + 1, all, used);
+    int64_t first = (before + incl - mine) * heads;
+    if (*begin >= first && *begin < first + mine * heads) {
+      int b = b0;
+      for (;; ++b) {
+        const int64_t n = static_cast<int64_t>(steps_of(s, b)) * heads;
+        if (*begin < first + n) break;
+        first += n;
+      }
+      tmp[kWarps] = b;
+      tmp[kWarps + 1] = *begin - first;
+    }
+  }
+  __syncthreads();
+  *b_out = static_cast<int>(tmp[kWarps]);
+  *rem = tmp[kWarps + 1];
+  __syncthreads();
+  return all;
+}
+
+// The slot that step x of all `all` lies in, of `used`: the last one whose begin, floor(slot all / used), is at most x.
+__host__ __device__ __forceinline__ int slot_of(int64_t x, int64_t all, int64_t used) {
+  return static_cast<int>(((x + 1) * used - 1) / all);
+}
+
+// A walk over the parts of heads that a CTA has: sequence, key head, steps [first, last) of it.
+struct Walk {
+  int64_t left;  // steps of the CTA behind this part (whole: units behind this one count as 1)
+  int b, h, steps, first, last;
+
+  __host__ __device__ __forceinline__ bool on() const { return first < last; }
+  __host__ __device__ __forceinline__ void take(const AttArgs &a, int from) {
+    first = from;
+    last = steps - from < left ? steps : from + static_cast<int>(left);
+    left -= last - first;
+  }
+  __host__ __device__ __forceinline__ void start(const AttArgs &a, int b_, int64_t rem, int64_t n) {
+    b = b_, h = 0, first = last = 0, steps = 0, left = n;
+    if (n <= 0) return;
+    steps = steps_of(a.s, b);
+    h = static_cast<int>(rem / steps);
+    take(a, static_cast<int>(rem - static_cast<int64_t>(h) * steps));
+  }
+  __host__ __device__ __forceinline__ void start_whole(const AttArgs &a, int unit) {
+    left = 0, first = 0;
+    b = unit / a.heads, h = unit - b * a.heads;
+    last = steps = unit < a.s.seqs * a.heads ? steps_of(a.s, b) : 0;
+  }
+  // The next part (or, where nothing is split, the next unit, which may have no steps); steps of none at the end.
+  __host__ __device__ __forceinline__ void next(const AttArgs &a) {
+    if (a.whole) return start_whole(a, b * a.heads + h + a.slots);
+    if (left <= 0) {
+      first = last = 0;
+      return;
+    }
+    if (++h == a.heads) {
+      h = 0;
+      do steps = steps_of(a.s, ++b);
+      while (steps == 0 && b + 1 < a.s.seqs);
+    }
+    take(a, 0);
+  }
+};
+
+// ---- operands --------------------------------------------------------------------
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm4_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
+      "%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_of(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t sub_h2(uint32_t a, uint32_t b) {
+  const __half2 d = __hsub2(reinterpret_cast<const __half2 &>(a), reinterpret_cast<const __half2 &>(b));
+  return reinterpret_cast<const uint32_t &>(d);
+}
+
+// Signed lanes of a word, or of two tokens' halves of words, as pairs in fp16: lane i of the low half with lane i of
+// the high half. 8 bits: 1024 + 128 + lane over a byte; 4 bits: 1024 + 8 + lane, or 64 + 8 + lane four bits up.
+template <int BITS>
+__device__ __forceinline__ void widen(uint32_t w, uint32_t (&p)[16 / BITS]) {
+  if constexpr (BITS == 8) {
+    p[0] = sub_h2((w & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
+    p[1] = sub_h2(((w >> 8) & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t v = w >> 8 * i;
+      p[2 * i] = sub_h2((v & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
+      p[2 * i + 1] = sub_h2((v & 0x00F000F0u) ^ 0x54805480u, 0x54805480u);
+    }
+  }
+}
+
+// ---- sizes -------------------------------------------------------------------------
+
+// NB: blocks of 32 elements in a row.
+template <int NB, int BITS>
+struct Att {
+  static constexpr int kDim = 32 * NB;
+  static constexpr int kRow = 4 * NB * BITS;        // bytes of a row of lanes
+  static constexpr int kUnits = kRow / 16;
+  static constexpr int kPitch = 16 * (kUnits | 1);  // of a row in a stage
+  static constexpr int kScales = kStep * NB * 2;    // bytes of a step's scales, of keys or values
+  static constexpr int kStage = 2 * kStep * kPitch + 2 * kScales;
+  static constexpr int kRed = kWarps * (kHeads * kDim + 2 * kHeads) * 4;  // the warps' sums, references, weights
+  static constexpr int bytes(int stages) { return kWarps * stages * kStage + kRed; }
+  static constexpr bool fits(int stages, int ctas) { return ctas * (bytes(stages) + 1024 + 128) <= 228 * 1024; }
+  // a CTA has four stages a warp where three CTAs fit with them, else as many as fit
+  static constexpr int kCtas = fits(2, 3) ? 3 : 2;
+  static constexpr int kStages = fits(4, kCtas) ? 4 : fits(3, kCtas) ? 3 : 2;
+  static_assert(fits(kStages, kCtas), "shared memory");
+};
+
+// The scales of a row, two in a word, from shared memory.
+template <int NB>
+__device__ __forceinline__ void load_scales(const uint8_t *p, uint32_t (&w)[(NB + 1) / 2]) {
+  if constexpr (NB % 8 == 0) {
+    const uint4 v = *reinterpret_cast<const uint4 *>(p);
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  } else if constexpr (NB % 4 == 0) {
+    const uint2 v = *reinterpret_cast<const uint2 *>(p);
+    w[0] = v.x, w[1] = v.y;
+  } else if constexpr (NB % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < NB / 2; ++i) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+  } else {
+    const uint16_t *const h = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+    for (int i = 0; i < (NB + 1) / 2; ++i) w[i] = h[2 * i] | (2 * i + 1 < NB ? static_cast<uint32_t>(h[2 * i + 1]) << 16 : 0u);
+  }
+}
+template <typename T>
+__device__ __forceinline__ float scale_at(const uint32_t *w, int g) {
+  const float2 f = unpack2<T>(w[g / 2]);
+  return g & 1 ? f.y : f.x;
+}
+
+// log2 of a scale's magnitude, rounded down, within -90 .. 110.
+__device__ __forceinline__ float log2_down(float s) {
+  const int e = static_cast<int>((__float_as_uint(s) & 0x7FFFFFFFu) >> 23) - 127;
+  return static_cast<float>(e < -90 ? -90 : e > 110 ? 110 : e);
+}
+
+template <typename T, int NB, int BITS>
+__global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attention_kernel(const AttArgs a) {
+  using P = Att<NB, BITS>;
+  constexpr int kDim = P::kDim, kUnits = P::kUnits, kPitch = P::kPitch, kStages = P::kStages;
+  constexpr int kTiles = kDim / 16;  // of 16 elements
+  constexpr float kLow = -3e38f;     // a reference before any token
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int64_t tmp[kWarps + 2];
+  float *const red = reinterpret_cast<float *>(smem + kWarps * kStages * P::kStage);
+  float *const red_stat = red + kWarps * kHeads * kDim;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+
+  // the cache, the lengths and q may come from the kernel before; the next one may be set up
+  ptx::grid_dependency_wait();
+  ptx::grid_dependents_launch();
+
+  const int slot = blockIdx.x / a.parts, part = blockIdx.x - slot * a.parts;
+  const int64_t span_tokens = static_cast<int64_t>(a.s.max_pages) << a.s.page_shift;
+  int64_t all = 0, used = 1;
+  Walk have;
+  if (a.whole) {
+    have.start_whole(a, slot);
+  } else {
+    int b;
+    int64_t begin, end, rem;
+    all = locate(a.s, a.heads, slot, a.slots, tmp, &b, &begin, &end, &rem);
+    used = used_of(all, a.slots);
+    if (begin >= end) return;
+    have.start(a, b, rem, end - begin);
+  }
+  int64_t unit_begin = 0;  // of all steps, the first of the head in hand
+  if (!a.whole) unit_begin = begin_of(slot, all, used) - have.first;
+
+  // ---- the ring: this warp's steps, one after the other, over the CTA's parts
+  const uint32_t ring = ptx::smem_addr(smem) + warp * kStages * P::kStage;
+  Walk ahead = have;
+  int l_step = ahead.first + warp, fill = 0, slot_used = 0;
+  uint32_t missing = 0;  // bit of a stage: its page is none of the cache's
+  int l_page = -1;
+  // brings `ahead` and l_step to the next step of this warp, and its page
+  auto seek = [&]() {
+    while (l_step >= ahead.last) {
+      const int was = ahead.b * a.heads + ahead.h;
+      ahead.next(a);
+      if (a.whole ? was + a.slots >= a.s.seqs * a.heads : !ahead.on()) {
+        ahead.last = ahead.first = 0;
+        l_step = -1;
+        return;
+      }
+      l_step = ahead.first + warp;
+    }
+    l_page = page_of(a.s, ahead.b, static_cast<int64_t>(l_step) * kStep);
+  };
+  auto load_next = [&]() {
+    if (l_step >= 0) {
+      const uint32_t st = ring + fill * P::kStage;
+      const bool in = l_page >= 0;
+      missing = in ? missing & ~(1u << fill) : missing | 1u << fill;
+      const int64_t pos = (static_cast<int64_t>(l_step) * kStep) & ((1 << a.s.page_shift) - 1);
+      const int64_t row = in ? (((static_cast<int64_t>(l_page) * a.heads + ahead.h) << a.s.page_shift) + pos) : 0;
+      const uint32_t n = in ? 16u : 0u;
+      const uint8_t *const kp = a.k + row * P::kRow + lane * 16, *const vp = a.v + row * P::kRow + lane * 16;
+#pragma unroll
+      for (int i = 0; i < (kStep * kUnits + 31) / 32; ++i) {
+        const int idx = i * 32 + lane, r = idx / kUnits, c = idx - r * kUnits;
+        if (kStep * kUnits % 32 == 0 || idx < kStep * kUnits) {
+          ptx::cp_async_16(st + r * kPitch + c * 16, kp + i * 512, n);
+          ptx::cp_async_16(st + kStep * kPitch + r * kPitch + c * 16, vp + i * 512, n);
+        }
+      }
+      if (lane < 4 * NB) {
+        const int of_v = lane >= 2 * NB, u = of_v ? lane - 2 * NB : lane;
+        ptx::cp_async_16(st + 2 * kStep * kPitch + lane * 16, (of_v ? a.vs : a.ks) + row * (2 * NB) + u * 16, n);
+      }
+      l_step += kWarps;
+      seek();
+    }
+    ptx::cp_async_commit();
+    fill = fill + 1 == kStages ? 0 : fill + 1;
+  };
+  seek();
+#pragma unroll 1
+  for (int i = 0; i < kStages - 1; ++i) load_next();
+
+  // ldmatrix: keys: matrices (rows 0-7, unit c), (rows 8-15, c), (rows 0-7, c + 1), (rows 8-15, c + 1); values the
+  // same, transposed: (tokens 0-7), (tokens 8-15) of a unit
+  const uint32_t lm = ((lane >> 3 & 1) * 8 + (lane & 7)) * kPitch + (lane >> 4) * 16;
+
+  const int total_units = a.s.seqs * a.heads;
+  while (a.whole ? have.b * a.heads + have.h < total_units : have.on()) {
+    const int unit = have.b * a.heads + have.h;
+    const int head0 = have.h * a.group + part * a.per;  // the CTA's first query head
+    const int n_heads = min(a.per, a.group - part * a.per);
+    const int len = static_cast<int>(length_of(a.s, have.b));
+
+    // q of head g in the MMA's order, in fp16 under a power of two
+    uint32_t qb[kUnits][16 / BITS];  // pairs of a unit of 16 bytes: 2 (8 bits) or 4 (4 bits) words
+    float mult[2];
+    {
+      constexpr int kPer = 32 / BITS;  // elements of a thread's word
+      float top = 0.0f;
+      const T *const qrow = reinterpret_cast<const T *>(a.q + have.b * a.ldq) + static_cast<int64_t>(head0 + g) * kDim;
+      float f[kUnits][kPer];
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        uint32_t w[kPer / 2] = {};
+        if (g < n_heads) {
+          if constexpr (BITS == 8) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(qrow + u * 16 + t * 4);
+            w[0] = v.x, w[1] = v.y;
+          } else {
+            const uint4 v = *reinterpret_cast<const uint4 *>(qrow + u * 32 + t * 8);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kPer / 2; ++i) {
+          const float2 e = unpack2<T>(w[i]);
+          f[u][2 * i] = e.x, f[u][2 * i + 1] = e.y;
+          top = fmaxf(top, fmaxf(fabsf(e.x), fabsf(e.y)));
+        }
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // to 2^13 .. 2^14; powers of two in two halves, each within fp32's range
+      const int e = 13 - (static_cast<int>(__float_as_uint(top) >> 23) - 127);
+      const int e0 = e / 2, e1 = e - e0;
+      const float up0 = __int_as_float((127 + e0) << 23), up1 = __int_as_float((127 + e1) << 23);
+      const float down = __int_as_float((127 - e0) << 23), down1 = __int_as_float((127 - e1) << 23);
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+        for (int i = 0; i < kPer / 2; ++i) {
+          // the word's pairs: lanes (i, i + half of them)
+          qb[u][i] = pack2<__half>(f[u][i] * up0 * up1, f[u][i + kPer / 2] * up0 * up1);
+        }
+      const float m = a.scale * down * down1;
+      mult[0] = __shfl_sync(0xffffffffu, m, 8 * t);
+      mult[1] = __shfl_sync(0xffffffffu, m, 8 * t + 4);
+    }
+
+    float o[kTiles][4], ref[2] = {kLow, kLow}, sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
+
+#pragma unroll 1
+    for (int step = have.first + warp; step < have.last; step += kWarps) {
+      ptx::cp_async_wait<kStages - 2>();
+      __syncwarp();  // every lane's copies are in, and the stage filled next has been read by every lane
+      const bool gone = (missing >> slot_used & 1) != 0;
+      load_next();
+      const uint32_t st = ring + slot_used * P::kStage;
+      const uint8_t *const sc = smem + (st - ptx::smem_addr(smem)) + 2 * kStep * kPitch;
+      slot_used = slot_used + 1 == kStages ? 0 : slot_used + 1;
+
+      // logits
+      uint32_t kw[2][(NB + 1) / 2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) load_scales<NB>(sc + (g + 8 * r) * (2 * NB), kw[r]);
+      float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      // the products of a unit pair: 8 bits: both halves of block u / 2; 4 bits: blocks u and u + 1
+#pragma unroll
+      for (int u = 0; u < kUnits; u += 2) {
+        uint32_t r[4];
+        ldsm4(st + lm + u * 16, r);  // (past the last unit of an odd row: the row's padding, not used)
+        if constexpr (BITS == 8) {
+          float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t lo[2], hi[2];
+            widen<8>(r[2 * i], lo);
+            widen<8>(r[2 * i + 1], hi);
+            mma_f16(d, lo[0], hi[0], lo[1], hi[1], qb[u + i][0], qb[u + i][1]);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = fmaf(scale_at<T>(kw[j >> 1], u / 2), d[j], x[j]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (u + i < kUnits) {
+              float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+              uint32_t lo[4], hi[4];
+              widen<4>(r[2 * i], lo);
+              widen<4>(r[2 * i + 1], hi);
+              mma_f16(d, lo[0], hi[0], lo[1], hi[1], qb[u + i][0], qb[u + i][1]);
+              mma_f16(d, lo[2], hi[2], lo[3], hi[3], qb[u + i][2], qb[u + i][3]);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x[j] = fmaf(scale_at<T>(kw[j >> 1], u + i), d[j], x[j]);
+            }
+        }
+      }
+
+      // the values' scales; a token that is not there has none, and no weight
+      const int tok = step * kStep + g;
+      const bool in[2] = {!gone && tok < len, !gone && tok + 8 < len};
+      uint32_t vw[2][(NB + 1) / 2];
+      float vmax[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        load_scales<NB>(sc + P::kScales + (g + 8 * r) * (2 * NB), vw[r]);
+#pragma unroll
+        for (int i = 0; i < (NB + 1) / 2; ++i) vw[r][i] = in[r] ? vw[r][i] : 0u;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) vmax[r] = fmaxf(vmax[r], fabsf(scale_at<T>(vw[r], i)));
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = in[j >> 1] ? x[j] * mult[j & 1] : -INFINITY;
+      if (a.logits) {
+        float *const lp = a.logits + ((static_cast<int64_t>(unit) * a.parts + part) * span_tokens + tok) * kHeads + 2 * t;
+        *reinterpret_cast<float2 *>(lp) = make_float2(x[0], x[1]);
+        *reinterpret_cast<float2 *>(lp + 8 * kHeads) = make_float2(x[2], x[3]);
+      }
+
+      float e[4];
+      bool over[2] = {false, false};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        e[j] = exp2_of(x[j] - ref[j & 1]);
+        over[j & 1] |= !(e[j] * vmax[j >> 1] <= 32768.0f);
+      }
+      if (__any_sync(0xffffffffu, over[0] | over[1])) {
+        float top[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          top[c] = fmaxf(x[c] + log2_down(vmax[0]), x[2 + c] + log2_down(vmax[1])) - 6.0f;
+          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 4));
+          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 8));
+          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 16));
+          // (of this head's column alone: a head's bits do not depend on its neighbours)
+          const bool moves = (__ballot_sync(0xffffffffu, over[c]) & 0x11111111u << t) != 0;
+          top[c] = moves ? fmaxf(top[c], ref[c]) : ref[c];
+          const float f = exp2_of(ref[c] - top[c]);
+          ref[c] = top[c];
+          sum[c] *= f;
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) o[i][c] *= f, o[i][2 + c] *= f;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) e[j] = exp2_of(x[j] - ref[j & 1]);
+      }
+      sum[0] += e[0] + e[2];
+      sum[1] += e[1] + e[3];
+
+      // outputs
+#pragma unroll
+      for (int u = 0; u < kUnits; u += 2) {
+        uint32_t r[4];
+        ldsm4_trans(st + kStep * kPitch + lm + u * 16, r);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (u + i < kUnits) {
+            const int blk = BITS == 8 ? u / 2 : u + i;
+            static_assert(BITS == 8 || BITS == 4, "");
+            const float s0 = scale_at<T>(vw[0], blk), s1 = scale_at<T>(vw[1], blk);
+            const uint32_t b0 = transpose8x8(pack2<__half>(e[0] * s0, e[1] * s0));
+            const uint32_t b1 = transpose8x8(pack2<__half>(e[2] * s1, e[3] * s1));
+            uint32_t lo[16 / BITS], hi[16 / BITS];
+            widen<BITS>(r[2 * i], lo);
+            widen<BITS>(r[2 * i + 1], hi);
+            if constexpr (BITS == 8) {
+              mma_f16(o[u + i], lo[0], lo[1], hi[0], hi[1], b0, b1);
+            } else {
+              mma_f16(o[2 * (u + i)], lo[0], lo[1], hi[0], hi[1], b0, b1);
+              mma_f16(o[2 * (u + i) + 1], lo[2], lo[3], hi[2], hi[3], b0, b1);
+            }
+          }
+      }
+    }
+
+    // ---- join the warps: sums [warp][head][element], references and weights [warp][head]
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 4);
+      sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 8);
+      sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 16);
+    }
+    if (g == 0) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        red_stat[(warp * kHeads + 2 * t + c) * 2] = ref[c];
+        red_stat[(warp * kHeads + 2 * t + c) * 2 + 1] = sum[c];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // row g (and g + 8) of tile i is this element
+        const int d = BITS == 8 ? 16 * i + 2 * g + (j >> 1) : 32 * (i / 2) + 4 * g + 2 * (i & 1) + (j >> 1);
+        red[(warp * kHeads + 2 * t + (j & 1)) * kDim + d] = o[i][j];
+      }
+    __syncthreads();
+    const bool first_part = have.first == 0, last_part = have.last == have.steps;
+    for (int idx = tid; idx < n_heads * (kDim / 2); idx += kThreads) {
+      const int h = idx / (kDim / 2), d = (idx - h * (kDim / 2)) * 2;
+      float top = kLow;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, red_stat[(w * kHeads + h) * 2]);
+      float2 v = make_float2(0.0f, 0.0f);
+      float weight = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = exp2_of(red_stat[(w * kHeads + h) * 2] - top);
+        const float2 p = *reinterpret_cast<const float2 *>(red + (w * kHeads + h) * kDim + d);
+        v.x = fmaf(f, p.x, v.x);
+        v.y = fmaf(f, p.y, v.y);
+        weight = fmaf(f, red_stat[(w * kHeads + h) * 2 + 1], weight);
+      }
+      if (d == 0 && a.head_stat) {
+        float2 *const to = first_part ? a.head_stat + (static_cast<int64_t>(unit) * a.parts + part) * kHeads
+                                      : a.stat + static_cast<int64_t>(blockIdx.x) * kHeads;
+        to[h] = make_float2(top, weight);
+      }
+      if (first_part && last_part) {
+        const float inv = weight == 0.0f ? 0.0f : 1.0f / weight;  // no tokens: zeros
+        *reinterpret_cast<uint32_t *>(a.out + have.b * a.ldo + (static_cast<int64_t>(head0 + h) * kDim + d) * 2) =
+            pack2<T>(v.x * inv, v.y * inv);
+      } else {
+        float *const to = a.sums + ((static_cast<int64_t>(blockIdx.x) * 2 + first_part) * kHeads + h) * kDim + d;
+        *reinterpret_cast<float2 *>(to) = v;
+      }
+    }
+    if (!a.whole && first_part && tid == 0)
+      a.span[static_cast<int64_t>(unit) * a.parts + part] =
+          make_int2(slot, slot_of(unit_begin + have.steps - 1, all, used));
+    __syncthreads();
+    unit_begin += have.steps;
+    have.next(a);
+  }
+  ptx::cp_async_wait<0>();
+}
+
+// ---- host ----------------------------------------------------------------------------
+
+template <typename T, int NB, int BITS>
+cudaError_t launch_att(const AttArgs &a, int grid, cudaStream_t s) {
+  using P = Att<NB, BITS>;
+  constexpr auto kern = paged_attention_kernel<T, NB, BITS>;
+  const cudaError_t e = conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), P::bytes(P::kStages));
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kern, dim3(grid), kThreads, P::bytes(P::kStages), s, 1, a);
+}
+
+// CTAs on an SM of the instance for rows of nb blocks.
+template <int BITS>
+constexpr int ctas_of(int nb) {
+  return nb == 1   ? Att<1, BITS>::kCtas
+         : nb == 2 ? Att<2, BITS>::kCtas
+         : nb == 3 ? Att<3, BITS>::kCtas
+         : nb == 4 ? Att<4, BITS>::kCtas
+         : nb == 5 ? Att<5, BITS>::kCtas
+         : nb == 6 ? Att<6, BITS>::kCtas
+         : nb == 7 ? Att<7, BITS>::kCtas
+                   : Att<8, BITS>::kCtas;
+}
+
+// One launcher a type and lane width, each compiled in its own unit.
+template <typename T, int BITS>
+cudaError_t launch_dims(const AttArgs &a, int nb, int grid, cudaStream_t s) {
+  switch (nb) {
+    case 1: return launch_att<T, 1, BITS>(a, grid, s);
+    case 2: return launch_att<T, 2, BITS>(a, grid, s);
+    case 3: return launch_att<T, 3, BITS>(a, grid, s);
+    case 4: return launch_att<T, 4, BITS>(a, grid, s);
+    case 5: return launch_att<T, 5, BITS>(a, grid, s);
+    case 6: return launch_att<T, 6, BITS>(a, grid, s);
+    case 7: return launch_att<T, 7, BITS>(a, grid, s);
+    default: return launch_att<T, 8, BITS>(a, grid, s);
+  }
+}
+cudaError_t launch_att_bf16_8(const AttArgs &a, int nb, int grid, cudaStream_t s);
+cudaError_t launch_att_bf16_4(const AttArgs &a, int nb, int grid, cudaStream_t s);
+cudaError_t launch_att_f16_8(const AttArgs &a, int nb, int grid, cudaStream_t s);
+cudaError_t launch_att_f16_4(const AttArgs &a, int nb, int grid, cudaStream_t s);
+
+}  // namespace kv
+}  // namespace samd

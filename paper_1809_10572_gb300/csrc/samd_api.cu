@@ -3,6 +3,7 @@
 // stream. See include/samd.h for the contract of each call.
 #include <mutex>
 
+#include "cache_internal.cuh"
 #include "ffn_internal.cuh"
 #include "samd_internal.cuh"
 
@@ -347,6 +348,103 @@ samd_status samd_gated_ffn_backward(const samd_ffn_desc *d, const void *dh, samd
     return SAMD_EALIGN;
   if (workspace_bytes < ffn_backward_workspace(*d)) return SAMD_ESHAPE;
   return from_cuda(launch_ffn_backward(*d, dh, cx, cg, cu, wg, wu, dx, dwg, dwu, h, workspace, s));
+}
+
+namespace {
+// A cache and the sequences in it, without the addresses.
+samd_status cache_shape_checks(const samd_cache *c, const samd_cache_seqs *s) {
+  if (!c || !s || !type16(c->type) || !fmt_valid(c->fmt)) return SAMD_EINVAL;
+  if ((c->fmt.bits != 4 && c->fmt.bits != 8) || !c->fmt.is_signed || c->fmt.spacer != 0 || c->fmt.word_bits != 32)
+    return SAMD_EUNSUP;
+  if (c->pages < 0 || c->page < 1 || c->heads < 1 || c->dim < 1 || s->seqs < 0 || s->max_pages < 0 ||
+      s->ld < s->max_pages)
+    return SAMD_ESHAPE;
+  if (c->page < 16 || c->page > 65536 || (c->page & (c->page - 1)) != 0 || c->dim % 32 != 0 || c->dim > 256 ||
+      c->heads > 65536)
+    return SAMD_EUNSUP;
+  // rows are counted in an int64, tokens of a sequence and pairs of a sequence and a head in an int
+  if (static_cast<int64_t>(s->max_pages) * c->page > kMaxDim || static_cast<int64_t>(s->seqs) * c->heads > kMaxDim)
+    return SAMD_EUNSUP;
+  return SAMD_OK;
+}
+
+samd_status cache_address_checks(const samd_cache *c, const samd_cache_seqs *s) {
+  if (!c->k_lanes || !c->k_scales || !c->v_lanes || !c->v_scales || !s->lengths || (!s->table && s->max_pages > 0))
+    return SAMD_EINVAL;
+  if (!aligned16(c->k_lanes) || !aligned16(c->k_scales) || !aligned16(c->v_lanes) || !aligned16(c->v_scales) ||
+      !aligned16(s->table) || !aligned16(s->lengths))
+    return SAMD_EALIGN;
+  return SAMD_OK;
+}
+
+// samd_cache_append and samd_cache_read; *empty: there is nothing to do.
+samd_status cache_rows_checks(const samd_cache *c, const samd_cache_seqs *s, const int32_t *starts, int tokens,
+                              const void *k, int64_t ldk, const void *v, int64_t ldv, bool *empty) {
+  *empty = false;
+  samd_status st = cache_shape_checks(c, s);
+  if (st != SAMD_OK) return st;
+  const int64_t row = static_cast<int64_t>(c->heads) * c->dim;
+  if (tokens < 0 || ldk < row || ldv < row || (!starts && tokens != s->seqs)) return SAMD_ESHAPE;
+  if (ldk % 8 != 0 || ldv % 8 != 0) return SAMD_EALIGN;
+  if (tokens > 0 && (ldk > INT64_MAX / 8 / tokens || ldv > INT64_MAX / 8 / tokens)) return SAMD_ESHAPE;
+  *empty = tokens == 0 || s->seqs == 0;
+  if (*empty) return SAMD_OK;
+  if (!k || !v) return SAMD_EINVAL;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(starts)) return SAMD_EALIGN;
+  return cache_address_checks(c, s);
+}
+
+samd_status attention_shape_checks(const samd_cache *c, const samd_cache_seqs *s, int q_heads) {
+  const samd_status st = cache_shape_checks(c, s);
+  if (st != SAMD_OK) return st;
+  if (q_heads < 1 || q_heads % c->heads != 0) return SAMD_ESHAPE;
+  if (q_heads / c->heads > 256 || static_cast<int64_t>(s->seqs) * q_heads > kMaxDim) return SAMD_EUNSUP;
+  return SAMD_OK;
+}
+}  // namespace
+
+samd_status samd_cache_append(const samd_cache *c, const samd_cache_seqs *s, const int32_t *starts, int tokens,
+                              const void *k, int64_t ldk, const void *v, int64_t ldv, samd_stream_t stream) {
+  bool empty;
+  const samd_status st = cache_rows_checks(c, s, starts, tokens, k, ldk, v, ldv, &empty);
+  if (st != SAMD_OK || empty) return st;
+  return from_cuda(launch_cache_append(*c, *s, starts, tokens, k, ldk, v, ldv, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+samd_status samd_cache_read(const samd_cache *c, const samd_cache_seqs *s, const int32_t *starts, int tokens, void *k,
+                            int64_t ldk, void *v, int64_t ldv, samd_stream_t stream) {
+  bool empty;
+  const samd_status st = cache_rows_checks(c, s, starts, tokens, k, ldk, v, ldv, &empty);
+  if (st != SAMD_OK || empty) return st;
+  return from_cuda(launch_cache_read(*c, *s, starts, tokens, k, ldk, v, ldv, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+size_t samd_paged_attention_workspace_size(const samd_cache *c, const samd_cache_seqs *s, int q_heads, int scores) {
+  if (attention_shape_checks(c, s, q_heads) != SAMD_OK || s->seqs == 0) return 0;
+  return paged_attention_workspace(*c, *s, q_heads, scores != 0);
+}
+
+samd_status samd_paged_attention(const samd_cache *c, const samd_cache_seqs *s, int q_heads, const void *q,
+                                 int64_t ldq, float scale, void *out, int64_t ldo, float *scores, int64_t ld_scores,
+                                 void *workspace, size_t workspace_bytes, samd_stream_t stream) {
+  samd_status st = attention_shape_checks(c, s, q_heads);
+  if (st != SAMD_OK) return st;
+  if (!(scale - scale == 0.0f)) return SAMD_EINVAL;
+  const int64_t row = static_cast<int64_t>(q_heads) * c->dim;
+  if (ldq < row || ldo < row || (scores && ld_scores < 0)) return SAMD_ESHAPE;
+  if (ldq % 8 != 0 || ldo % 8 != 0) return SAMD_EALIGN;
+  if (s->seqs > 0 && (ldq > INT64_MAX / 8 / s->seqs || ldo > INT64_MAX / 8 / s->seqs)) return SAMD_ESHAPE;
+  if (scores && s->seqs > 0 && ld_scores > INT64_MAX / 8 / s->seqs / c->heads) return SAMD_ESHAPE;
+  if (s->seqs == 0) return SAMD_OK;
+  if (!q || !out) return SAMD_EINVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(scores) || !aligned16(workspace)) return SAMD_EALIGN;
+  st = cache_address_checks(c, s);
+  if (st != SAMD_OK) return st;
+  const size_t need = paged_attention_workspace(*c, *s, q_heads, scores != nullptr);
+  if (need > 0 && !workspace) return SAMD_EINVAL;
+  if (workspace_bytes < need) return SAMD_ESHAPE;
+  return from_cuda(launch_paged_attention(*c, *s, q_heads, q, ldq, scale, out, ldo, scores, ld_scores, workspace,
+                                          reinterpret_cast<cudaStream_t>(stream)));
 }
 
 samd_status samd_device_status(int *status, int reset, samd_stream_t stream) {

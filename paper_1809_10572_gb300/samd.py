@@ -56,6 +56,17 @@ class samd_ffn_desc(ctypes.Structure):
                 ("ldw", ctypes.c_int64), ("ldh", ctypes.c_int64), ("type", ctypes.c_int), ("act", ctypes.c_int)]
 
 
+class samd_cache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int), ("page", ctypes.c_int), ("heads", ctypes.c_int), ("dim", ctypes.c_int),
+                ("fmt", samd_fmt), ("type", ctypes.c_int), ("k_lanes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_lanes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class samd_cache_seqs(ctypes.Structure):
+    _fields_ = [("seqs", ctypes.c_int), ("max_pages", ctypes.c_int), ("ld", ctypes.c_int64), ("table", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p)]
+
+
 SAMD_OK, SAMD_EINVAL, SAMD_EALIGN, SAMD_ESHAPE, SAMD_EUNSUP, SAMD_ECUDA, SAMD_ETIMEOUT = range(7)
 SAMD_ADD, SAMD_SUB, SAMD_MUL, SAMD_RELU, SAMD_REQUANT = range(5)
 SAMD_NCHW, SAMD_NHWC = 0, 1
@@ -70,6 +81,7 @@ EXPORTED = ["samd_lanes_per_word", "samd_packed_words", "samd_pack", "samd_unpac
             "samd_conv2d_noalloc", "samd_conv2d_prepared_pool2x2", "samd_conv2d_pool2x2_supported",
             "samd_matvec4", "samd_gated_matvec4", "samd_block8_quantize", "samd_block8_dequantize",
             "samd_gated_ffn_forward", "samd_gated_ffn_backward", "samd_gated_ffn_backward_workspace_size",
+            "samd_cache_append", "samd_cache_read", "samd_paged_attention", "samd_paged_attention_workspace_size",
             "samd_maxpool2x2", "samd_device_status", "samd_selftest_wait_timeout", "samd_status_str", "samd_version"]
 FMT_NONE = (0, 0, 0, 0)
 
@@ -141,6 +153,13 @@ def load(build_if_missing: bool = True):
     lib.samd_gated_ffn_backward.restype = i32
     lib.samd_gated_ffn_backward_workspace_size.argtypes = [fdp]
     lib.samd_gated_ffn_backward_workspace_size.restype = sz
+    cp, sp, f32 = c.POINTER(samd_cache), c.POINTER(samd_cache_seqs), c.c_float
+    lib.samd_cache_append.argtypes, lib.samd_cache_append.restype = [cp, sp, vp, i32, vp, i64, vp, i64, vp], i32
+    lib.samd_cache_read.argtypes, lib.samd_cache_read.restype = [cp, sp, vp, i32, vp, i64, vp, i64, vp], i32
+    lib.samd_paged_attention.argtypes = [cp, sp, i32, vp, i64, f32, vp, i64, vp, i64, vp, sz, vp]
+    lib.samd_paged_attention.restype = i32
+    lib.samd_paged_attention_workspace_size.argtypes = [cp, sp, i32, i32]
+    lib.samd_paged_attention_workspace_size.restype = sz
     lib.samd_device_status.argtypes, lib.samd_device_status.restype = [c.POINTER(c.c_int), i32, vp], i32
     lib.samd_selftest_wait_timeout.argtypes, lib.samd_selftest_wait_timeout.restype = [c.c_uint64, vp], i32
     lib.samd_status_str.argtypes, lib.samd_status_str.restype = [i32], c.c_char_p
@@ -339,6 +358,28 @@ def samd_gated_ffn_backward(desc: samd_ffn_desc, dh, ckpt_x, ckpt_g, ckpt_u, wg,
     _check(load().samd_gated_ffn_backward(ctypes.byref(desc), _ptr(dh), _block8(ckpt_x), _block8(ckpt_g),
                                           _block8(ckpt_u), _ptr(wg), _ptr(wu), _ptr(dx), _ptr(dwg), _ptr(dwu), _ptr(h),
                                           _ptr(workspace), nb, _stream(stream)), "samd_gated_ffn_backward")
+
+
+def samd_cache_append(cache: samd_cache, seqs: samd_cache_seqs, starts, tokens, k, ldk, v, ldv, stream=None):
+    _check(load().samd_cache_append(ctypes.byref(cache), ctypes.byref(seqs), _ptr(starts), tokens, _ptr(k), ldk, _ptr(v),
+                                    ldv, _stream(stream)), "samd_cache_append")
+
+
+def samd_cache_read(cache: samd_cache, seqs: samd_cache_seqs, starts, tokens, k, ldk, v, ldv, stream=None):
+    _check(load().samd_cache_read(ctypes.byref(cache), ctypes.byref(seqs), _ptr(starts), tokens, _ptr(k), ldk, _ptr(v),
+                                  ldv, _stream(stream)), "samd_cache_read")
+
+
+def samd_paged_attention_workspace_size(cache: samd_cache, seqs: samd_cache_seqs, q_heads: int, scores: bool) -> int:
+    return int(load().samd_paged_attention_workspace_size(ctypes.byref(cache), ctypes.byref(seqs), q_heads, int(scores)))
+
+
+def samd_paged_attention(cache: samd_cache, seqs: samd_cache_seqs, q_heads, q, ldq, scale, out, ldo, scores, ld_scores,
+                         workspace, workspace_bytes=None, stream=None):
+    nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(load().samd_paged_attention(ctypes.byref(cache), ctypes.byref(seqs), q_heads, _ptr(q), ldq, scale, _ptr(out),
+                                       ldo, _ptr(scores), ld_scores, _ptr(workspace), nb, _stream(stream)),
+           "samd_paged_attention")
 
 
 def samd_device_status(reset: bool = False, stream=None) -> int:
@@ -736,3 +777,156 @@ def gated_ffn_backward(dh, ckpt_x: Block8, ckpt_g: Block8, ckpt_u: Block8, wg, w
             workspace = torch.empty(samd_gated_ffn_backward_workspace_size(d), dtype=torch.uint8, device=dh.device)
         samd_gated_ffn_backward(d, dh, ckpt_x, ckpt_g, ckpt_u, wg, wu, dx, dwg, dwu, h, workspace, stream=stream)
     return (dx, dwg, dwu, h) if need_h else (dx, dwg, dwu)
+
+
+# ---- the packed key-value cache ----------------------------------------------------
+
+
+class PagedCache:
+    """Keys and values of tokens in packed lanes, in pages (samd_cache): k_lanes and v_lanes (pages, heads, page, words)
+    int32, the rows as samd_pack writes them in the format cache_fmt(bits); k_scales and v_scales (pages, heads, page,
+    dim // 32) float16 or bfloat16. The lane width follows from the shapes."""
+
+    __slots__ = ("k_lanes", "k_scales", "v_lanes", "v_scales", "bits", "dim", "_desc")
+
+    def __init__(self, k_lanes, k_scales, v_lanes, v_scales):
+        rows, words, blocks = k_lanes.shape[:-1], k_lanes.shape[-1], k_scales.shape[-1]
+        if len(rows) != 3 or blocks < 1 or words not in (4 * blocks, 8 * blocks):
+            raise ValueError(f"lanes (pages, heads, page, words) and scales (pages, heads, page, dim // 32) of 4 or 8 bits "
+                             f"are wanted, got {tuple(k_lanes.shape)} and {tuple(k_scales.shape)}")
+        t = k_scales.dtype
+        if t is not torch.float16 and t is not torch.bfloat16:
+            raise ValueError(f"scales: {t}, wanted float16 or bfloat16")
+        for lanes, scales in ((k_lanes, k_scales), (v_lanes, v_scales)):
+            if lanes.dtype is not torch.int32 or lanes.shape != (*rows, words) or not lanes.is_contiguous():
+                raise ValueError(f"lanes: a contiguous {(*rows, words)} int32 tensor is wanted")
+            if scales.dtype is not t or scales.shape != (*rows, blocks) or not scales.is_contiguous():
+                raise ValueError(f"scales: a contiguous {(*rows, blocks)} {t} tensor is wanted")
+        if max(rows) >> 31:
+            _past_int(*rows)
+        self.k_lanes, self.k_scales, self.v_lanes, self.v_scales = k_lanes, k_scales, v_lanes, v_scales
+        self.bits, self.dim = words // blocks, 32 * blocks
+        pages, heads, page = rows
+        self._desc = samd_cache(pages, page, heads, self.dim, cache_fmt(self.bits), DTYPES[t], _ptr(k_lanes), _ptr(k_scales),
+                                _ptr(v_lanes), _ptr(v_scales))
+
+    @property
+    def heads(self) -> int:
+        return self._desc.heads
+
+    @property
+    def page(self) -> int:
+        return self._desc.page
+
+    @property
+    def dtype(self) -> torch.dtype:
+        return self.k_scales.dtype
+
+
+def cache_fmt(bits: int) -> samd_fmt:
+    return fmt(bits, True, 0, 32)
+
+
+def cache_empty(pages: int, page: int, heads: int, dim: int, bits: int, dtype: torch.dtype, device="cuda") -> PagedCache:
+    """A cache of `pages` pages of `page` tokens (a power of two, 16 or more) for `heads` key heads of `dim` elements (a
+    multiple of 32 up to 256), in lanes of `bits` (4 or 8). Its rows are not initialised: none is read that was not
+    written, as long as the sequences' lengths count what was."""
+    if bits not in (4, 8) or dim % 32 or not 32 <= dim <= 256 or page < 16 or page & (page - 1):
+        raise ValueError(f"page {page}, dim {dim}, bits {bits}: a power of two of at least 16, a multiple of 32 up to 256, "
+                         "and 4 or 8 are wanted")
+    def lanes():
+        return torch.empty((pages, heads, page, dim * bits // 32), dtype=torch.int32, device=device)
+    def scales():
+        return torch.empty((pages, heads, page, dim // 32), dtype=dtype, device=device)
+    return PagedCache(lanes(), scales(), lanes(), scales())
+
+
+def _cache_seqs(table, lengths) -> samd_cache_seqs:
+    """table (sequences, pages of one) int32 with contiguous rows, lengths (sequences) int32."""
+    if table.dtype is not torch.int32 or lengths.dtype is not torch.int32:
+        raise ValueError(f"table, lengths: {table.dtype}, {lengths.dtype}, wanted int32")
+    ld = _rows(table, "table")
+    seqs, width = table.shape
+    if lengths.shape != (seqs,) or not lengths.is_contiguous():
+        raise ValueError(f"lengths: a contiguous ({seqs},) tensor is wanted, got {tuple(lengths.shape)}")
+    if (seqs | width) >> 31:
+        _past_int(seqs, width)
+    return samd_cache_seqs(seqs, width, ld, _ptr(table), _ptr(lengths))
+
+
+def _token_rows(x, what: str, heads: int, dim: int, dtype, tokens: int | None = None) -> int:
+    """Checks a (tokens, heads, dim) tensor whose tokens lie whole in memory, and returns the stride of a token."""
+    shape = x.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or (tokens is not None and shape[0] != tokens):
+        raise ValueError(f"{what}: shape {tuple(shape)}, wanted ({tokens if tokens is not None else 'any'}, {heads}, {dim})")
+    if x.dtype is not dtype:
+        raise ValueError(f"{what}: {x.dtype}, wanted {dtype}")
+    if x.is_contiguous():
+        return heads * dim
+    if x.stride(2) != 1 or (heads > 1 and x.stride(1) != dim):
+        raise ValueError(f"{what}: the heads of a token one behind the other are wanted, got strides {x.stride()}")
+    return x.stride(0) if shape[0] > 1 else heads * dim
+
+
+def _starts(starts, seqs: int):
+    if starts is not None and (starts.dtype is not torch.int32 or starts.shape != (seqs + 1,) or not starts.is_contiguous()):
+        raise ValueError(f"starts: a contiguous ({seqs + 1},) int32 tensor is wanted")
+    return starts
+
+
+def cache_append(cache: PagedCache, k, v, table, lengths, starts=None, stream=None) -> None:
+    """Writes new tokens' keys and values (tokens, heads, dim) into the cache. lengths counts them already: rows
+    starts[b] .. starts[b + 1] - 1 are the last tokens of sequence b; without starts every sequence has one, row b."""
+    ldk = _token_rows(k, "k", cache.heads, cache.dim, cache.dtype)
+    tokens = k.shape[0]
+    ldv = _token_rows(v, "v", cache.heads, cache.dim, cache.dtype, tokens)
+    s = _cache_seqs(table, lengths)
+    if tokens >> 31:
+        _past_int(tokens)
+    samd_cache_append(cache._desc, s, _starts(starts, s.seqs), tokens, k, ldk, v, ldv, stream)
+
+
+def cache_read(cache: PagedCache, tokens: int, table, lengths, starts=None, k=None, v=None, stream=None):
+    """(k, v): the values (tokens, heads, dim) of the rows that cache_append with the same table, lengths and starts
+    wrote, in the scales' type. Rows of no sequence are left as they are in k and v."""
+    s = _cache_seqs(table, lengths)
+    if not 0 <= tokens < 1 << 31:
+        _past_int(tokens)
+    with _on(stream):
+        k, v = (torch.empty((tokens, cache.heads, cache.dim), dtype=cache.dtype, device=table.device) if x is None else x
+                for x in (k, v))
+    ldk, ldv = (_token_rows(x, n, cache.heads, cache.dim, cache.dtype, tokens) for x, n in ((k, "k"), (v, "v")))
+    samd_cache_read(cache._desc, s, _starts(starts, s.seqs), tokens, k, ldk, v, ldv, stream)
+    return k, v
+
+
+def paged_attention(q, cache: PagedCache, table, lengths, scale: float | None = None, scores=None, out=None,
+                    workspace=None, stream=None):
+    """One query token for each sequence over the cache: q and out (sequences, query heads, dim), key head h for a run of
+    query heads; scale defaults to dim ** -0.5. scores (sequences, heads, any) float32: each token's weight is added to
+    it, for cache_evict."""
+    s = _cache_seqs(table, lengths)
+    q_heads = q.shape[1] if q.dim() == 3 else 0
+    ldq = _token_rows(q, "q", q_heads, cache.dim, cache.dtype, s.seqs)
+    if q_heads < 1 or q_heads % cache.heads or q_heads >> 31:
+        raise ValueError(f"q: {q_heads} heads, wanted a multiple of the cache's {cache.heads}")
+    ld_scores = 0
+    if scores is not None:
+        if (scores.dtype is not torch.float32 or scores.dim() != 3 or scores.shape[:2] != (s.seqs, cache.heads) or
+                not scores.is_contiguous()):
+            raise ValueError(f"scores: a contiguous ({s.seqs}, {cache.heads}, any) float32 tensor is wanted")
+        ld_scores = scores.shape[2]
+    if scale is None:
+        scale = cache.dim ** -0.5
+    with _on(stream):
+        if out is None:
+            out = torch.empty((s.seqs, q_heads, cache.dim), dtype=q.dtype, device=q.device)
+            ldo = q_heads * cache.dim
+        else:
+            ldo = _token_rows(out, "out", q_heads, cache.dim, q.dtype, s.seqs)
+        if workspace is None:
+            n = samd_paged_attention_workspace_size(cache._desc, s, q_heads, scores is not None)
+            workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    samd_paged_attention(cache._desc, s, q_heads, q, ldq, scale, out, ldo, scores if ld_scores else None, ld_scores,
+                         workspace, stream=stream)
+    return out
