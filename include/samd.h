@@ -444,7 +444,9 @@ SAMD_API samd_status samd_gated_ffn_backward(const samd_ffn_desc *desc, const vo
  * ---- new token, eviction; and a layer of experts on 4-bit weights.
  *
  * What serving the block above needs next to it. The conventions of the top of
- * this file and of the gated block hold.
+ * this file and of the gated block hold, except that arrays of int32 and fp32
+ * (tables, lengths, starts, scores, kept places) need no more than the 4-byte
+ * alignment of their elements.
  *
  * A cache is `pages` pages of `page` tokens (a power of two, 16 or more) for
  * `heads` key heads of `dim` elements (a multiple of 32, 32 .. 256). A row is
@@ -520,6 +522,25 @@ SAMD_API samd_status samd_paged_attention(const samd_cache *cache, const samd_ca
                                           const void *q, int64_t ldq, float scale, void *out, int64_t ldo,
                                           float *scores, int64_t ld_scores, void *workspace, size_t workspace_bytes,
                                           samd_stream_t stream);
+
+/*
+ * samd_cache_evict: cuts every head of every sequence down to `keep` tokens (1
+ * or more): its last `recent` ones (0 .. keep) and of the others those with the
+ * largest scores (fp32 [seqs][heads][ld_scores], which samd_paged_attention adds
+ * to; a tie goes to the earlier token, a NaN is below everything, a token past
+ * ld_scores has 0). A sequence of `keep` tokens or fewer keeps them all. The
+ * kept rows are copied, in order, into the pages that dst_table names
+ * (dst_table[b * ld_dst + i / page] for the i-th; ceil(keep / page) entries a
+ * sequence), which have to be other pages than those of any sequence, or other
+ * slots of them than tokens lie in (SAMD_EINVAL if dst_table is seqs->table);
+ * a row whose old or new page is none of the cache's is not copied.
+ *   kept         int32 [seqs][heads][keep]: the kept tokens' places, then -1
+ *   new_lengths  int32 [seqs]: min(length, keep)
+ *   new_scores   fp32 [seqs][heads][keep] or NULL: their scores, then 0
+ */
+SAMD_API samd_status samd_cache_evict(const samd_cache *cache, const samd_cache_seqs *seqs, const float *scores,
+                                      int64_t ld_scores, int keep, int recent, const int32_t *dst_table, int64_t ld_dst,
+                                      int32_t *kept, int32_t *new_lengths, float *new_scores, samd_stream_t stream);
 
 /*
  * samd_device_status: reads (and with reset=1 clears) the sticky status the

@@ -75,5 +75,8 @@ size_t paged_attention_workspace(const samd_cache &c, const samd_cache_seqs &s, 
 cudaError_t launch_paged_attention(const samd_cache &c, const samd_cache_seqs &s, int q_heads, const void *q,
                                    int64_t ldq, float scale, void *out, int64_t ldo, float *scores, int64_t ld_scores,
                                    void *workspace, cudaStream_t stream);
+cudaError_t launch_cache_evict(const samd_cache &c, const samd_cache_seqs &s, const samd_cache_seqs &dst,
+                               const float *scores, int64_t ld_scores, int keep, int recent, int32_t *kept,
+                               int32_t *new_lengths, float *new_scores, cudaStream_t stream);
 
 }  // namespace samd

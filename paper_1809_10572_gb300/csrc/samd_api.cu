@@ -351,6 +351,9 @@ samd_status samd_gated_ffn_backward(const samd_ffn_desc *d, const void *dh, samd
 }
 
 namespace {
+// Tables, lengths, scores: arrays of 4-byte elements that callers cut out of larger ones.
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
 // A cache and the sequences in it, without the addresses.
 samd_status cache_shape_checks(const samd_cache *c, const samd_cache_seqs *s) {
   if (!c || !s || !type16(c->type) || !fmt_valid(c->fmt)) return SAMD_EINVAL;
@@ -372,7 +375,7 @@ samd_status cache_address_checks(const samd_cache *c, const samd_cache_seqs *s) 
   if (!c->k_lanes || !c->k_scales || !c->v_lanes || !c->v_scales || !s->lengths || (!s->table && s->max_pages > 0))
     return SAMD_EINVAL;
   if (!aligned16(c->k_lanes) || !aligned16(c->k_scales) || !aligned16(c->v_lanes) || !aligned16(c->v_scales) ||
-      !aligned16(s->table) || !aligned16(s->lengths))
+      !aligned4(s->table) || !aligned4(s->lengths))
     return SAMD_EALIGN;
   return SAMD_OK;
 }
@@ -390,7 +393,7 @@ samd_status cache_rows_checks(const samd_cache *c, const samd_cache_seqs *s, con
   *empty = tokens == 0 || s->seqs == 0;
   if (*empty) return SAMD_OK;
   if (!k || !v) return SAMD_EINVAL;
-  if (!aligned16(k) || !aligned16(v) || !aligned16(starts)) return SAMD_EALIGN;
+  if (!aligned16(k) || !aligned16(v) || !aligned4(starts)) return SAMD_EALIGN;
   return cache_address_checks(c, s);
 }
 
@@ -437,7 +440,7 @@ samd_status samd_paged_attention(const samd_cache *c, const samd_cache_seqs *s, 
   if (scores && s->seqs > 0 && ld_scores > INT64_MAX / 8 / s->seqs / c->heads) return SAMD_ESHAPE;
   if (s->seqs == 0) return SAMD_OK;
   if (!q || !out) return SAMD_EINVAL;
-  if (!aligned16(q) || !aligned16(out) || !aligned16(scores) || !aligned16(workspace)) return SAMD_EALIGN;
+  if (!aligned16(q) || !aligned16(out) || !aligned4(scores) || !aligned16(workspace)) return SAMD_EALIGN;
   st = cache_address_checks(c, s);
   if (st != SAMD_OK) return st;
   const size_t need = paged_attention_workspace(*c, *s, q_heads, scores != nullptr);
@@ -445,6 +448,29 @@ samd_status samd_paged_attention(const samd_cache *c, const samd_cache_seqs *s, 
   if (workspace_bytes < need) return SAMD_ESHAPE;
   return from_cuda(launch_paged_attention(*c, *s, q_heads, q, ldq, scale, out, ldo, scores, ld_scores, workspace,
                                           reinterpret_cast<cudaStream_t>(stream)));
+}
+
+samd_status samd_cache_evict(const samd_cache *c, const samd_cache_seqs *s, const float *scores, int64_t ld_scores,
+                             int keep, int recent, const int32_t *dst_table, int64_t ld_dst, int32_t *kept,
+                             int32_t *new_lengths, float *new_scores, samd_stream_t stream) {
+  samd_status st = cache_shape_checks(c, s);
+  if (st != SAMD_OK) return st;
+  if (recent < 0 || recent > keep) return SAMD_EINVAL;
+  if (keep < 1 || ld_scores < 0) return SAMD_ESHAPE;
+  if (keep > kMaxDim) return SAMD_EUNSUP;
+  const int dst_pages = (keep + c->page - 1) / c->page;
+  if (ld_dst < dst_pages || (s->seqs > 0 && ld_scores > INT64_MAX / 8 / s->seqs / c->heads)) return SAMD_ESHAPE;
+  // a launch's CTAs (a cluster a row) and the index of a row's unit
+  if (static_cast<int64_t>(s->seqs) * c->heads > kMaxDim / 8) return SAMD_EUNSUP;
+  if (s->seqs == 0) return SAMD_OK;
+  if ((!scores && ld_scores > 0) || !dst_table || !kept || !new_lengths || dst_table == s->table) return SAMD_EINVAL;
+  if (!aligned4(scores) || !aligned4(dst_table) || !aligned4(kept) || !aligned4(new_lengths) || !aligned4(new_scores))
+    return SAMD_EALIGN;
+  st = cache_address_checks(c, s);
+  if (st != SAMD_OK) return st;
+  const samd_cache_seqs dst = {s->seqs, dst_pages, ld_dst, dst_table, new_lengths};
+  return from_cuda(launch_cache_evict(*c, *s, dst, scores, ld_scores, keep, recent, kept, new_lengths, new_scores,
+                                      reinterpret_cast<cudaStream_t>(stream)));
 }
 
 samd_status samd_device_status(int *status, int reset, samd_stream_t stream) {

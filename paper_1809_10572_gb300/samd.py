@@ -82,6 +82,7 @@ EXPORTED = ["samd_lanes_per_word", "samd_packed_words", "samd_pack", "samd_unpac
             "samd_matvec4", "samd_gated_matvec4", "samd_block8_quantize", "samd_block8_dequantize",
             "samd_gated_ffn_forward", "samd_gated_ffn_backward", "samd_gated_ffn_backward_workspace_size",
             "samd_cache_append", "samd_cache_read", "samd_paged_attention", "samd_paged_attention_workspace_size",
+            "samd_cache_evict",
             "samd_maxpool2x2", "samd_device_status", "samd_selftest_wait_timeout", "samd_status_str", "samd_version"]
 FMT_NONE = (0, 0, 0, 0)
 
@@ -160,6 +161,8 @@ def load(build_if_missing: bool = True):
     lib.samd_paged_attention.restype = i32
     lib.samd_paged_attention_workspace_size.argtypes = [cp, sp, i32, i32]
     lib.samd_paged_attention_workspace_size.restype = sz
+    lib.samd_cache_evict.argtypes = [cp, sp, vp, i64, i32, i32, vp, i64, vp, vp, vp, vp]
+    lib.samd_cache_evict.restype = i32
     lib.samd_device_status.argtypes, lib.samd_device_status.restype = [c.POINTER(c.c_int), i32, vp], i32
     lib.samd_selftest_wait_timeout.argtypes, lib.samd_selftest_wait_timeout.restype = [c.c_uint64, vp], i32
     lib.samd_status_str.argtypes, lib.samd_status_str.restype = [i32], c.c_char_p
@@ -380,6 +383,13 @@ def samd_paged_attention(cache: samd_cache, seqs: samd_cache_seqs, q_heads, q, l
     _check(load().samd_paged_attention(ctypes.byref(cache), ctypes.byref(seqs), q_heads, _ptr(q), ldq, scale, _ptr(out),
                                        ldo, _ptr(scores), ld_scores, _ptr(workspace), nb, _stream(stream)),
            "samd_paged_attention")
+
+
+def samd_cache_evict(cache: samd_cache, seqs: samd_cache_seqs, scores, ld_scores, keep, recent, dst_table, ld_dst, kept,
+                     new_lengths, new_scores, stream=None):
+    _check(load().samd_cache_evict(ctypes.byref(cache), ctypes.byref(seqs), _ptr(scores), ld_scores, keep, recent,
+                                   _ptr(dst_table), ld_dst, _ptr(kept), _ptr(new_lengths), _ptr(new_scores),
+                                   _stream(stream)), "samd_cache_evict")
 
 
 def samd_device_status(reset: bool = False, stream=None) -> int:
@@ -874,6 +884,13 @@ def _starts(starts, seqs: int):
     return starts
 
 
+def _scores_ld(scores, seqs: int, heads: int) -> int:
+    if (scores.dtype is not torch.float32 or scores.dim() != 3 or scores.shape[0] != seqs or scores.shape[1] != heads or
+            not scores.is_contiguous()):
+        raise ValueError(f"scores: a contiguous ({seqs}, {heads}, any) float32 tensor is wanted")
+    return scores.shape[2]
+
+
 def cache_append(cache: PagedCache, k, v, table, lengths, starts=None, stream=None) -> None:
     """Writes new tokens' keys and values (tokens, heads, dim) into the cache. lengths counts them already: rows
     starts[b] .. starts[b + 1] - 1 are the last tokens of sequence b; without starts every sequence has one, row b."""
@@ -910,12 +927,7 @@ def paged_attention(q, cache: PagedCache, table, lengths, scale: float | None = 
     ldq = _token_rows(q, "q", q_heads, cache.dim, cache.dtype, s.seqs)
     if q_heads < 1 or q_heads % cache.heads or q_heads >> 31:
         raise ValueError(f"q: {q_heads} heads, wanted a multiple of the cache's {cache.heads}")
-    ld_scores = 0
-    if scores is not None:
-        if (scores.dtype is not torch.float32 or scores.dim() != 3 or scores.shape[:2] != (s.seqs, cache.heads) or
-                not scores.is_contiguous()):
-            raise ValueError(f"scores: a contiguous ({s.seqs}, {cache.heads}, any) float32 tensor is wanted")
-        ld_scores = scores.shape[2]
+    ld_scores = 0 if scores is None else _scores_ld(scores, s.seqs, cache.heads)
     if scale is None:
         scale = cache.dim ** -0.5
     with _on(stream):
@@ -930,3 +942,25 @@ def paged_attention(q, cache: PagedCache, table, lengths, scale: float | None = 
     samd_paged_attention(cache._desc, s, q_heads, q, ldq, scale, out, ldo, scores if ld_scores else None, ld_scores,
                          workspace, stream=stream)
     return out
+
+
+def cache_evict(cache: PagedCache, table, lengths, scores, dst_table, keep: int, recent: int = 0, stream=None):
+    """Cuts every head of every sequence down to `keep` tokens, its last `recent` ones and those with the largest scores
+    (sequences, heads, any), by copying the kept rows, in order, into the pages of dst_table (other ones than the
+    sequences'). (kept, new lengths, new scores): the kept tokens' places (sequences, heads, keep), -1 behind the last,
+    and their scores, 0 behind it; dst_table with the new lengths and scores is the cache to go on with."""
+    s = _cache_seqs(table, lengths)
+    ld_scores = _scores_ld(scores, s.seqs, cache.heads)
+    if not 0 <= recent <= keep or keep < 1:
+        raise ValueError(f"keep {keep}, recent {recent}: 0 <= recent <= keep, and a keep of 1 or more, are wanted")
+    if keep >> 31:
+        _past_int(keep)
+    if dst_table.dtype is not torch.int32 or dst_table.shape[0] != s.seqs or dst_table.shape[1] * cache.page < keep:
+        raise ValueError(f"dst_table: ({s.seqs}, {-(-keep // cache.page)}) int32 pages are wanted")
+    ld_dst = _rows(dst_table, "dst_table")
+    with _on(stream):
+        kept = torch.empty((s.seqs, cache.heads, keep), dtype=torch.int32, device=scores.device)
+        new_lengths = torch.empty(s.seqs, dtype=torch.int32, device=scores.device)
+        new_scores = torch.empty((s.seqs, cache.heads, keep), dtype=torch.float32, device=scores.device)
+    samd_cache_evict(cache._desc, s, scores, ld_scores, keep, recent, dst_table, ld_dst, kept, new_lengths, new_scores, stream)
+    return kept, new_lengths, new_scores

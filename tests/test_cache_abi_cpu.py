@@ -33,8 +33,8 @@ BAD_CACHES = [(dict(type=samd.SAMD_F32), EINVAL), (dict(type=9), EINVAL), (dict(
 BAD_SEQS = [(dict(seqs=-1), ESHAPE), (dict(max_pages=-1), ESHAPE), (dict(ld=1), ESHAPE),
             (dict(max_pages=1 << 27, ld=1 << 27), EUNSUP), (dict(seqs=1 << 30), EUNSUP)]
 BAD_ADDRESSES = [(dict(kl=None), {}, EINVAL), (dict(vs=None), {}, EINVAL), (dict(ks=8), {}, EALIGN), (dict(vl=4), {}, EALIGN),
-                 ({}, dict(table=None), EINVAL), ({}, dict(lengths=None), EINVAL), ({}, dict(table=4), EALIGN),
-                 ({}, dict(lengths=8), EALIGN)]
+                 ({}, dict(table=None), EINVAL), ({}, dict(lengths=None), EINVAL), ({}, dict(table=6), EALIGN),
+                 ({}, dict(lengths=9), EALIGN)]
 
 
 def check_both(call):
@@ -60,7 +60,7 @@ def test_rows_refusals(lib, name):
     assert call(tokens=0, k=None, v=None) == OK and call(s=seqs(seqs=0), tokens=0, k=None, v=None, starts=None) == OK
     for kw in (dict(k=None), dict(v=None)):
         assert call(**kw) == EINVAL
-    for kw in (dict(k=8), dict(v=4), dict(starts=4)):
+    for kw in (dict(k=8), dict(v=4), dict(starts=2)):
         assert call(**kw) == EALIGN
 
 
@@ -80,7 +80,7 @@ def test_attention_refusals(lib):
     assert call(ldq=260) == EALIGN and call(ldo=257) == EALIGN
     for kw in (dict(q=None), dict(out=None)):
         assert call(**kw) == EINVAL
-    for kw in (dict(q=2), dict(out=8), dict(scores=4, lds=1), dict(ws=8)):
+    for kw in (dict(q=2), dict(out=8), dict(scores=2, lds=1), dict(ws=8)):
         assert call(**kw) == EALIGN
     assert call(s=seqs(seqs=0), q=None, out=None) == OK
     long = seqs(max_pages=1000, ld=1000)
@@ -92,6 +92,23 @@ def test_attention_refusals(lib):
     assert samd.samd_paged_attention_workspace_size(cache(dim=48), long, 4, False) == 0
     assert samd.samd_paged_attention_workspace_size(cache(), long, 3, False) == 0
     assert samd.samd_paged_attention_workspace_size(cache(), seqs(), 4, False) == 0  # 32 tokens: nothing is split
+
+
+def test_evict_refusals(lib):
+    def call(c=None, s=None, scores=16, lds=32, keep=20, recent=5, dst=32, ldd=2, kept=16, new=16, out=16, null=False):
+        return lib.samd_cache_evict(None if null else ctypes.byref(c or cache()), ctypes.byref(s or seqs()), scores, lds, keep,
+                                    recent, dst, ldd, kept, new, out, None)
+
+    check_both(call)
+    assert call(recent=-1) == EINVAL and call(recent=21) == EINVAL and call(keep=0, recent=0) == ESHAPE
+    assert call(keep=(1 << 30) + 1, ldd=1 << 40) == EUNSUP and call(s=seqs(seqs=1 << 27)) == EUNSUP
+    for kw in (dict(lds=-1), dict(lds=1 << 61), dict(ldd=1), dict(keep=33)):
+        assert call(**kw) == ESHAPE, kw
+    for kw in (dict(scores=None), dict(dst=None), dict(kept=None), dict(new=None), dict(dst=16)):  # 16: the sequences' own
+        assert call(**kw) == EINVAL, kw
+    for kw in (dict(scores=5), dict(dst=18), dict(kept=7), dict(new=2), dict(out=1)):
+        assert call(**kw) == EALIGN, kw
+    assert call(s=seqs(seqs=0), scores=None, kept=None) == OK
 
 
 def meta(*shape, dtype=torch.int32):
@@ -140,6 +157,13 @@ def test_the_binding_checks_its_tensors(monkeypatch):
         a = dict(q=q, cache=c, table=table, lengths=lengths) | kw
         with pytest.raises(ValueError):
             samd.paged_attention(**a)
+    w, dst = meta(3, 2, 32, dtype=torch.float32), meta(3, 2)
+    for kw in (dict(keep=0), dict(recent=21), dict(recent=-1), dict(dst_table=meta(3, 1)), dict(dst_table=meta(2, 2)),
+               dict(dst_table=dst.long()), dict(scores=w.half()), dict(scores=meta(2, 2, 32, dtype=torch.float32)),
+               dict(keep=1 << 31, dst_table=meta(3, 1 << 28))):
+        a = dict(cache=c, table=table, lengths=lengths, scores=w, dst_table=dst, keep=20, recent=4) | kw
+        with pytest.raises(ValueError):
+            samd.cache_evict(**a)
     with pytest.raises(ValueError, match="size"):
         samd._cache_seqs(meta((1 << 32) + 5, 1), meta((1 << 32) + 5))
 
