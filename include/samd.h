@@ -543,6 +543,50 @@ SAMD_API samd_status samd_cache_evict(const samd_cache *cache, const samd_cache_
                                       int32_t *kept, int32_t *new_lengths, float *new_scores, samd_stream_t stream);
 
 /*
+ * A layer of E experts, each a gated block with a down projection, of which
+ * every token goes through `topk`: M tokens of K elements (rows of stride ldx;
+ * y: ldy; multiples of 8, else SAMD_EALIGN), F hidden columns; all of `type`
+ * (SAMD_F16 or SAMD_BF16). `group` as in samd_matvec_desc. SAMD_EINVAL: another
+ * type, act or group; SAMD_ESHAPE: M < 0, E < 1, topk < 1 (or above E, for
+ * samd_moe_route), K or F < 1, a stride below its row's length; SAMD_EUNSUP: K or F not a multiple of 32 or
+ * above 2^20, E above 1024, topk above 32.
+ */
+typedef struct {
+  int M, K, F, E, topk, group;
+  int64_t ldx, ldy;
+  samd_dtype type;
+  samd_act act;
+} samd_moe_desc;
+
+/*
+ * samd_moe_route: which experts a token goes to. logits[e] = sum_k x[m][k] *
+ * router[e][k] in fp32 (router: E rows of K of `type`); ids[m][0 .. topk - 1]
+ * are the largest, in falling order (a tie: the lower expert first; a NaN is
+ * below everything); weights[m][..] their softmax, over the chosen ones
+ * (normalize = 1) or over all E (0). F, group, act and ldy are not read.
+ */
+SAMD_API samd_status samd_moe_route(const samd_moe_desc *desc, int normalize, const void *x, const void *router,
+                                    int32_t *ids, float *weights, samd_stream_t stream);
+
+/* Bytes of workspace samd_moe4 needs for this desc (0 on error, or for M = 0). */
+SAMD_API size_t samd_moe4_workspace_size(const samd_moe_desc *desc);
+/*
+ * samd_moe4: y[m] = sum_j weights[m][j] * Wd (act(Wg x[m]) * (Wu x[m])) over the
+ * experts ids[m][j], an id below 0 or from E on counting nothing (a token of
+ * none gives 0), the same one twice counting twice. gate and up are E times F
+ * rows of K weights, down E times K rows of F, one expert behind the other, as
+ * samd_matvec4 takes them (fw: 4-bit lanes without spacers, 32- or 64-bit words);
+ * all three have zero points or none has. weights * act * up is rounded to
+ * `type` before the last product, everything else is in fp32 and rounded once.
+ * Made for few tokens (an expert's weights are read once for every eight tokens
+ * that chose it); any M is right. The same call gives the same bits. A token
+ * with an infinity or a NaN gives NaNs, in its own row only.
+ */
+SAMD_API samd_status samd_moe4(const samd_moe_desc *desc, samd_fmt fw, const void *x, const int32_t *ids,
+                               const float *weights, samd_weights4 gate, samd_weights4 up, samd_weights4 down, void *y,
+                               void *workspace, size_t workspace_bytes, samd_stream_t stream);
+
+/*
  * samd_device_status: reads (and with reset=1 clears) the sticky status the
  * kernels of the current device record when a bounded wait runs out.
  * Synchronises `stream`. *status is SAMD_OK or SAMD_ETIMEOUT.

@@ -110,7 +110,8 @@ def build(force: bool = False, verbose: bool = False, extra_flags: list[str] | N
 
         # the slowest units (the kernel instantiations) first
         slow = [os.path.join(CSRC, f) for f in ("paged_attention_bf16_8.cu", "paged_attention_f16_8.cu",
-                                               "paged_attention_bf16_4.cu", "paged_attention_f16_4.cu", "matvec4_bf16.cu",
+                                               "paged_attention_bf16_4.cu", "paged_attention_f16_4.cu", "moe4_bf16.cu",
+                                               "moe4_f16.cu", "matvec4_bf16.cu",
                                                "matvec4_f16.cu", "ffn.cu")] + [INST_SRC]
         todo = sorted(units(), key=lambda u: slow.index(u[0]) if u[0] in slow else len(slow))
         with ThreadPoolExecutor(max_workers=max(1, min(len(todo), os.cpu_count() or 4))) as ex:

@@ -5,6 +5,7 @@
 
 #include "cache_internal.cuh"
 #include "ffn_internal.cuh"
+#include "moe4_kernel.cuh"
 #include "samd_internal.cuh"
 
 namespace samd {
@@ -471,6 +472,59 @@ samd_status samd_cache_evict(const samd_cache *c, const samd_cache_seqs *s, cons
   const samd_cache_seqs dst = {s->seqs, dst_pages, ld_dst, dst_table, new_lengths};
   return from_cuda(launch_cache_evict(*c, *s, dst, scores, ld_scores, keep, recent, kept, new_lengths, new_scores,
                                       reinterpret_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+// Sizes of a layer of experts; route: those that samd_moe_route reads.
+samd_status moe_shape_checks(const samd_moe_desc *d, bool route) {
+  if (!d || !type16(d->type)) return SAMD_EINVAL;
+  if (!route && (!act_ok(d->act) || d->group < 32 || (d->group & (d->group - 1)) != 0)) return SAMD_EINVAL;
+  if (d->M < 0 || d->K < 1 || d->E < 1 || d->topk < 1 || d->ldx < d->K) return SAMD_ESHAPE;
+  if (route && d->topk > d->E) return SAMD_ESHAPE;
+  if (!route && (d->F < 1 || d->ldy < d->K)) return SAMD_ESHAPE;
+  if (d->ldx % 8 != 0 || (!route && d->ldy % 8 != 0)) return SAMD_EALIGN;
+  constexpr int kMost = 1 << 20;
+  if (d->K % 32 != 0 || d->K > kMost || d->E > 1024 || d->topk > 32 || d->M > kMaxDim) return SAMD_EUNSUP;
+  if (!route && (d->F % 32 != 0 || d->F > kMost)) return SAMD_EUNSUP;
+  if (d->M > 0 && (d->ldx > INT64_MAX / 8 / d->M || (!route && d->ldy > INT64_MAX / 8 / d->M))) return SAMD_ESHAPE;
+  return SAMD_OK;
+}
+}  // namespace
+
+samd_status samd_moe_route(const samd_moe_desc *d, int normalize, const void *x, const void *router, int32_t *ids,
+                           float *weights, samd_stream_t stream) {
+  const samd_status st = moe_shape_checks(d, true);
+  if (st != SAMD_OK) return st;
+  if (normalize != 0 && normalize != 1) return SAMD_EINVAL;
+  if (d->M == 0) return SAMD_OK;
+  if (!x || !router || !ids || !weights) return SAMD_EINVAL;
+  if (!aligned16(x) || !aligned16(router) || !aligned4(ids) || !aligned4(weights)) return SAMD_EALIGN;
+  return from_cuda(launch_moe_route(*d, normalize != 0, x, router, ids, weights, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+size_t samd_moe4_workspace_size(const samd_moe_desc *d) {
+  return moe_shape_checks(d, false) == SAMD_OK ? moe4_workspace(*d) : 0;
+}
+
+samd_status samd_moe4(const samd_moe_desc *d, samd_fmt fw, const void *x, const int32_t *ids, const float *weights,
+                      samd_weights4 gate, samd_weights4 up, samd_weights4 down, void *y, void *workspace,
+                      size_t workspace_bytes, samd_stream_t stream) {
+  if (!fmt_valid(fw)) return SAMD_EINVAL;
+  const samd_status st = moe_shape_checks(d, false);
+  if (st != SAMD_OK) return st;
+  if (fw.bits != 4 || fw.spacer != 0) return SAMD_EUNSUP;
+  if (d->M == 0) return SAMD_OK;
+  if (!x || !ids || !weights || !y || !workspace) return SAMD_EINVAL;
+  const samd_weights4 *const w[3] = {&gate, &up, &down};
+  for (const samd_weights4 *m : w) {
+    if (!m->lanes || !m->scales || (m->zeros && fw.is_signed) || !m->zeros != !gate.zeros) return SAMD_EINVAL;
+  }
+  for (const samd_weights4 *m : w)
+    if (!aligned16(m->lanes) || !aligned16(m->scales) || !aligned16(m->zeros)) return SAMD_EALIGN;
+  if (!aligned16(x) || !aligned16(y) || !aligned16(workspace) || !aligned4(ids) || !aligned4(weights)) return SAMD_EALIGN;
+  if (workspace_bytes < moe4_workspace(*d)) return SAMD_ESHAPE;
+  return from_cuda(launch_moe4(*d, fw, x, ids, weights, gate, up, down, y, workspace,
+                               reinterpret_cast<cudaStream_t>(stream)));
 }
 
 samd_status samd_device_status(int *status, int reset, samd_stream_t stream) {

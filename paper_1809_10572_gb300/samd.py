@@ -67,6 +67,12 @@ class samd_cache_seqs(ctypes.Structure):
                 ("lengths", ctypes.c_void_p)]
 
 
+class samd_moe_desc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int), ("K", ctypes.c_int), ("F", ctypes.c_int), ("E", ctypes.c_int), ("topk", ctypes.c_int),
+                ("group", ctypes.c_int), ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64), ("type", ctypes.c_int),
+                ("act", ctypes.c_int)]
+
+
 SAMD_OK, SAMD_EINVAL, SAMD_EALIGN, SAMD_ESHAPE, SAMD_EUNSUP, SAMD_ECUDA, SAMD_ETIMEOUT = range(7)
 SAMD_ADD, SAMD_SUB, SAMD_MUL, SAMD_RELU, SAMD_REQUANT = range(5)
 SAMD_NCHW, SAMD_NHWC = 0, 1
@@ -82,7 +88,7 @@ EXPORTED = ["samd_lanes_per_word", "samd_packed_words", "samd_pack", "samd_unpac
             "samd_matvec4", "samd_gated_matvec4", "samd_block8_quantize", "samd_block8_dequantize",
             "samd_gated_ffn_forward", "samd_gated_ffn_backward", "samd_gated_ffn_backward_workspace_size",
             "samd_cache_append", "samd_cache_read", "samd_paged_attention", "samd_paged_attention_workspace_size",
-            "samd_cache_evict",
+            "samd_cache_evict", "samd_moe_route", "samd_moe4", "samd_moe4_workspace_size",
             "samd_maxpool2x2", "samd_device_status", "samd_selftest_wait_timeout", "samd_status_str", "samd_version"]
 FMT_NONE = (0, 0, 0, 0)
 
@@ -163,6 +169,10 @@ def load(build_if_missing: bool = True):
     lib.samd_paged_attention_workspace_size.restype = sz
     lib.samd_cache_evict.argtypes = [cp, sp, vp, i64, i32, i32, vp, i64, vp, vp, vp, vp]
     lib.samd_cache_evict.restype = i32
+    xdp = c.POINTER(samd_moe_desc)
+    lib.samd_moe_route.argtypes, lib.samd_moe_route.restype = [xdp, i32, vp, vp, vp, vp, vp], i32
+    lib.samd_moe4.argtypes, lib.samd_moe4.restype = [xdp, samd_fmt, vp, vp, vp, w4, w4, w4, vp, vp, sz, vp], i32
+    lib.samd_moe4_workspace_size.argtypes, lib.samd_moe4_workspace_size.restype = [xdp], sz
     lib.samd_device_status.argtypes, lib.samd_device_status.restype = [c.POINTER(c.c_int), i32, vp], i32
     lib.samd_selftest_wait_timeout.argtypes, lib.samd_selftest_wait_timeout.restype = [c.c_uint64, vp], i32
     lib.samd_status_str.argtypes, lib.samd_status_str.restype = [i32], c.c_char_p
@@ -390,6 +400,22 @@ def samd_cache_evict(cache: samd_cache, seqs: samd_cache_seqs, scores, ld_scores
     _check(load().samd_cache_evict(ctypes.byref(cache), ctypes.byref(seqs), _ptr(scores), ld_scores, keep, recent,
                                    _ptr(dst_table), ld_dst, _ptr(kept), _ptr(new_lengths), _ptr(new_scores),
                                    _stream(stream)), "samd_cache_evict")
+
+
+def samd_moe_route(desc: samd_moe_desc, normalize, x, router, ids, weights, stream=None):
+    _check(load().samd_moe_route(ctypes.byref(desc), int(normalize), _ptr(x), _ptr(router), _ptr(ids), _ptr(weights),
+                                 _stream(stream)), "samd_moe_route")
+
+
+def samd_moe4_workspace_size(desc: samd_moe_desc) -> int:
+    return int(load().samd_moe4_workspace_size(ctypes.byref(desc)))
+
+
+def samd_moe4(desc: samd_moe_desc, fw, x, ids, weights, gate, up, down, y, workspace, workspace_bytes=None, stream=None):
+    """gate, up, down: (lanes, scales, zeros or None)."""
+    nb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(load().samd_moe4(ctypes.byref(desc), fw, _ptr(x), _ptr(ids), _ptr(weights), _weights4(*gate), _weights4(*up),
+                            _weights4(*down), _ptr(y), _ptr(workspace), nb, _stream(stream)), "samd_moe4")
 
 
 def samd_device_status(reset: bool = False, stream=None) -> int:
@@ -964,3 +990,84 @@ def cache_evict(cache: PagedCache, table, lengths, scores, dst_table, keep: int,
         new_scores = torch.empty((s.seqs, cache.heads, keep), dtype=torch.float32, device=scores.device)
     samd_cache_evict(cache._desc, s, scores, ld_scores, keep, recent, dst_table, ld_dst, kept, new_lengths, new_scores, stream)
     return kept, new_lengths, new_scores
+
+
+# ---- a layer of experts ----------------------------------------------------------------
+
+
+def _moe_desc(x, E: int, topk: int, F: int = 32, group: int = 32, ldy: int = 0, act="silu") -> samd_moe_desc:
+    t = x.dtype
+    if t is not torch.float16 and t is not torch.bfloat16:
+        raise ValueError(f"x: {t}, wanted float16 or bfloat16")
+    if not 1 <= topk <= 32:
+        raise ValueError(f"{topk} experts of a token: 1 .. 32 are wanted")
+    if group < 32 or group & (group - 1):
+        raise ValueError(f"group: {group}, wanted a power of two of at least 32")
+    M, K = x.shape
+    ldx = _ld8(x, "x", M, K, t)
+    if (M | K | E | F | group) >> 31:
+        _past_int(M, K, E, F, group)
+    return samd_moe_desc(M, K, F, E, topk, group, ldx, ldy or K, DTYPES[t], _act(act))
+
+
+def moe_route(x, router, topk: int, normalize: bool = True, ids=None, weights=None, stream=None):
+    """(ids, weights), (M, topk) int32 and float32: the experts with the largest logits of x (M, K) by router (E, K), the
+    largest first, and the softmax of their logits, over themselves (normalize) or over all experts."""
+    if router.dtype is not x.dtype or router.dim() != 2 or router.shape[1] != x.shape[-1] or not router.is_contiguous():
+        raise ValueError(f"router: a contiguous (experts, {x.shape[-1]}) {x.dtype} tensor is wanted")
+    if topk > router.shape[0]:
+        raise ValueError(f"{topk} experts of {router.shape[0]} are wanted")
+    d = _moe_desc(x, router.shape[0], topk)
+    for o, what, t in ((ids, "ids", torch.int32), (weights, "weights", torch.float32)):
+        if o is not None and (o.dtype is not t or o.shape != (d.M, topk) or not o.is_contiguous()):
+            raise ValueError(f"{what}: a contiguous ({d.M}, {topk}) {t} tensor is wanted")
+    with _on(stream):
+        if ids is None:
+            ids = torch.empty((d.M, topk), dtype=torch.int32, device=x.device)
+        if weights is None:
+            weights = torch.empty((d.M, topk), dtype=torch.float32, device=x.device)
+    samd_moe_route(d, normalize, x, router, ids, weights, stream)
+    return ids, weights
+
+
+def _experts4(gate, up, down, K: int, group: int, f: samd_fmt, dtype) -> tuple[int, int]:
+    """Checks the matrices of a layer of experts, and returns how many experts there are and their hidden columns. The
+    scales (rows of all experts, groups of a row) say how many rows there are."""
+    rows, n = gate[1].shape[0], down[1].shape[0]
+    E = n // K if K else 0
+    if E < 1 or n != E * K or rows % E:
+        raise ValueError(f"gate, down: scales of {rows} and {n} rows, wanted a multiple of the experts, and {K} times them")
+    F = rows // E
+    for w, r, k in ((gate, E * F, K), (up, E * F, K), (down, E * K, F)):
+        _check_weights4(w[0], w[1], w[2] if len(w) > 2 else None, r, k, group, f, dtype)
+    return E, F
+
+
+def moe4(x, ids, weights, gate, up, down, group: int, f: samd_fmt, act="silu", out=None, workspace=None, stream=None):
+    """y (M, K) = sum over j of weights[:, j] * (act(x @ Wg.T) * (x @ Wu.T)) @ Wd.T with the matrices of expert ids[:, j]
+    (an id that is no expert's counts nothing). gate, up and down are (lanes, scales) or (lanes, scales, zeros), as matvec4
+    takes them: E * F, E * F and E * K packed rows, one expert behind the other."""
+    M, K = x.shape
+    E, F = _experts4(gate, up, down, K, group, f, x.dtype)
+    topk = ids.shape[1] if ids.dim() == 2 else 0
+    if ids.dtype is not torch.int32 or ids.shape != (M, topk) or not ids.is_contiguous():
+        raise ValueError(f"ids: a contiguous ({M}, any) int32 tensor is wanted")
+    if weights.dtype is not torch.float32 or weights.shape != ids.shape or not weights.is_contiguous():
+        raise ValueError(f"weights: a contiguous {tuple(ids.shape)} float32 tensor is wanted")
+    ldy = K if out is None else _ld8(out, "out", M, K, x.dtype)
+    d = _moe_desc(x, E, topk, F, group, ldy, act)
+    with _on(stream):
+        if out is None:
+            out = torch.empty((M, K), dtype=x.dtype, device=x.device)
+        if workspace is None:
+            workspace = torch.empty(samd_moe4_workspace_size(d), dtype=torch.uint8, device=x.device)
+    gate, up, down = (w if len(w) > 2 else (*w, None) for w in (gate, up, down))
+    samd_moe4(d, f, x, ids, weights, gate, up, down, out, workspace, stream=stream)
+    return out
+
+
+def moe_layer4(x, router, topk: int, gate, up, down, group: int, f: samd_fmt, act="silu", normalize: bool = True, out=None,
+               workspace=None, stream=None):
+    """A whole layer of experts: moe_route, and moe4 on its choice."""
+    ids, weights = moe_route(x, router, topk, normalize, stream=stream)
+    return moe4(x, ids, weights, gate, up, down, group, f, act, out, workspace, stream)
