@@ -99,16 +99,17 @@ __global__ void __launch_bounds__(kThreads) cache_choose_kernel(const EvictArgs 
     return;
   }
   const int old = n - a.recent;  // tokens behind these stay
-  auto key_at = [&](int64_t i) { return i >= old ? 0xFFFFFFFFu : order_of(score_at(i)); };
+  auto key_of = [&](int64_t i, float f) { return i >= old ? 0xFFFFFFFFu : order_of(f); };
+  auto key_at = [&](int64_t i) { return key_of(i, score_at(i)); };
   // this CTA's tokens: [first, last), a run of the row
   const int64_t per = kHeld ? kChunk : (static_cast<int64_t>((n + cluster - 1) / cluster) + kChunk - 1) / kChunk * kChunk;
   const int64_t first = rank * per, last = first + per < n ? first + per : n;
-  uint32_t key[kKeys];
+  float score[kKeys];
   if constexpr (kHeld) {
 #pragma unroll
     for (int i = 0; i < kKeys; ++i) {
       const int64_t at = first + i * kThreads + tid;
-      key[i] = at < last ? key_at(at) : 0u;
+      score[i] = at < last ? score_at(at) : 0.0f;
     }
   }
   __syncthreads();  // the histograms are zero
@@ -118,13 +119,13 @@ __global__ void __launch_bounds__(kThreads) cache_choose_kernel(const EvictArgs 
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
     auto count = [&](uint32_t k) {
-      if (pass == 0 || k >> (shift + bits) == prefix >> (shift + bits))
+      if (pass == 0 || k >> ((shift + bits) & 31) == prefix >> ((shift + bits) & 31))
         atomicAdd(&hist[pass][(k >> shift) & ((1u << bits) - 1)], 1u);
     };
     if constexpr (kHeld) {
 #pragma unroll
       for (int i = 0; i < kKeys; ++i)
-        if (first + i * kThreads + tid < last) count(key[i]);
+        if (first + i * kThreads + tid < last) count(key_of(first + i * kThreads + tid, score[i]));
     } else {
       for (int64_t at = first + tid; at < last; at += kThreads) count(key_at(at));
     }
@@ -163,8 +164,9 @@ __global__ void __launch_bounds__(kThreads) cache_choose_kernel(const EvictArgs 
   if constexpr (kHeld) {
 #pragma unroll
     for (int i = 0; i < kKeys; ++i) {
-      const bool in = first + i * kThreads + tid < last;
-      const uint32_t gt = __ballot_sync(0xffffffffu, in && key[i] > prefix), eq = __ballot_sync(0xffffffffu, in && key[i] == prefix);
+      const int64_t at = first + i * kThreads + tid;
+      const uint32_t k = key_of(at, score[i]);
+      const uint32_t gt = __ballot_sync(0xffffffffu, at < last && k > prefix), eq = __ballot_sync(0xffffffffu, at < last && k == prefix);
       if (lane == 0) range[0][i * kWarps + warp] = __popc(gt), range[1][i * kWarps + warp] = __popc(eq);
     }
     __syncthreads();
@@ -191,11 +193,11 @@ __global__ void __launch_bounds__(kThreads) cache_choose_kernel(const EvictArgs 
     }
   }
   __syncthreads();
-  auto put = [&](int64_t at, bool gt, bool eq, uint32_t gts, uint32_t eqs) {
+  auto put = [&](int64_t at, float f, bool gt, bool eq, uint32_t gts, uint32_t eqs) {
     if (gt || (eq && eqs < want)) {
       const uint32_t to = gts + (eqs < want ? eqs : want);
       a.kept[out + to] = static_cast<int>(at);
-      if (a.new_scores) a.new_scores[out + to] = score_at(at);
+      if (a.new_scores) a.new_scores[out + to] = f;
     }
   };
   const uint32_t below = (1u << lane) - 1;
@@ -203,18 +205,20 @@ __global__ void __launch_bounds__(kThreads) cache_choose_kernel(const EvictArgs 
 #pragma unroll
     for (int i = 0; i < kKeys; ++i) {
       const int64_t at = first + i * kThreads + tid;
-      const bool in = at < last, gt = in && key[i] > prefix, eq = in && key[i] == prefix;
+      const uint32_t k = key_of(at, score[i]);
+      const bool gt = at < last && k > prefix, eq = at < last && k == prefix;
       const uint32_t g = __ballot_sync(0xffffffffu, gt), e = __ballot_sync(0xffffffffu, eq);
-      put(at, gt, eq, gt0 + range[0][i * kWarps + warp] + __popc(g & below), eq0 + range[1][i * kWarps + warp] + __popc(e & below));
+      put(at, score[i], gt, eq, gt0 + range[0][i * kWarps + warp] + __popc(g & below), eq0 + range[1][i * kWarps + warp] + __popc(e & below));
     }
   } else {
     for (int64_t base = first; base < last; base += kThreads) {
       const int64_t at = base + tid;
-      const uint32_t k = at < last ? key_at(at) : 0u;
+      const float f = at < last ? score_at(at) : 0.0f;
+      const uint32_t k = key_of(at, f);
       const bool gt = at < last && k > prefix, eq = at < last && k == prefix;
       uint32_t all_gt, all_eq;
       const uint32_t g = sum_before(gt, tmp, &all_gt), e = sum_before(eq, tmp, &all_eq);
-      put(at, gt, eq, gt0 + g, eq0 + e);
+      put(at, f, gt, eq, gt0 + g, eq0 + e);
       gt0 += all_gt, eq0 += all_eq;
     }
   }
@@ -226,41 +230,71 @@ struct CopyArgs {
   kv::Seqs s, dst;
   const int32_t *kept;
   uint8_t *lanes[2], *scales[2];
-  int heads, keep, units, blocks;  // 16-byte units of a row of lanes, scales of a row
-  int64_t rows;
-  IndexDiv by_row, by_keep, by_heads;
+  int heads, keep;
+  int units, parts;      // 16-byte units of a row of lanes; pieces of a row of scales
+  int unit_mul, part_mul;  // 2^16 / them, and one more: a division of less than 32 * 16
+  int64_t rows, chunks;  // pairs of a sequence and a head; runs of 32 kept rows of one
+  IndexDiv by_chunks, by_heads;
 };
 
-// An item: a unit of a row of keys and of the same row of values; the first one of a row takes the scales along.
+// A warp copies 32 kept rows of one head: lane r finds out where row r comes from and goes to, then all lanes copy units
+// of all rows, four of keys and four of values in flight. Part: two bytes of scales, or four where a row has an even number.
+template <typename Part>
 __global__ void __launch_bounds__(256) cache_copy_kernel(const CopyArgs a) {
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
-  const int64_t items = a.rows * a.units;
-  for (int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; n < items; n += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t row = idiv(n, a.by_row);
-    const int u = static_cast<int>(n - row * a.units);
-    const int from = a.kept[row];
-    if (from < 0) continue;
-    const int64_t bh = idiv(row, a.by_keep);
-    const int r = static_cast<int>(row - bh * a.keep);
+  const int lane = threadIdx.x & 31;
+  const int64_t tasks = a.rows * a.chunks;
+  for (int64_t task = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5); task < tasks; task += static_cast<int64_t>(gridDim.x) * 8) {
+    const int64_t bh = idiv(task, a.by_chunks);
+    const int r = static_cast<int>(task - bh * a.chunks) * 32 + lane;
     const int b = static_cast<int>(idiv(bh, a.by_heads)), h = static_cast<int>(bh - static_cast<int64_t>(b) * a.heads);
-    const int sp = kv::page_of(a.s, b, from), dp = kv::page_of(a.dst, b, r);
-    if (sp < 0 || dp < 0) continue;
+    const int from = r < a.keep ? a.kept[bh * a.keep + r] : -1;
+    const int sp = from < 0 ? -1 : kv::page_of(a.s, b, from), dp = from < 0 ? -1 : kv::page_of(a.dst, b, r);
     const int mask = (1 << a.s.page_shift) - 1;
-    const int64_t src = ((static_cast<int64_t>(sp) * a.heads + h) << a.s.page_shift) + (from & mask);
-    const int64_t dst = ((static_cast<int64_t>(dp) * a.heads + h) << a.s.page_shift) + (r & mask);
-    uint4 v[2];
+    const bool on = sp >= 0 && dp >= 0;
+    const int64_t src = on ? ((static_cast<int64_t>(sp) * a.heads + h) << a.s.page_shift) + (from & mask) : -1;
+    const int64_t dst = on ? ((static_cast<int64_t>(dp) * a.heads + h) << a.s.page_shift) + (r & mask) : 0;
+    for (int i0 = 0; i0 < a.units; i0 += 4) {
+      uint4 v[4][2];
+      int64_t to[4];
 #pragma unroll
-    for (int m = 0; m < 2; ++m) v[m] = *reinterpret_cast<const uint4 *>(a.lanes[m] + (src * a.units + u) * 16);
+      for (int i = 0; i < 4; ++i) {
+        const int idx = (i0 + i) * 32 + lane, row = (idx * a.unit_mul) >> 16, u = idx - row * a.units;
+        const int64_t s = __shfl_sync(0xffffffffu, src, row & 31);
+        to[i] = __shfl_sync(0xffffffffu, dst, row & 31) * a.units + u;
+        if (row > 31 || s < 0) {
+          to[i] = -1;
+        } else {
 #pragma unroll
-    for (int m = 0; m < 2; ++m) *reinterpret_cast<uint4 *>(a.lanes[m] + (dst * a.units + u) * 16) = v[m];
-    for (int i = u; i < a.blocks; i += a.units)
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        uint16_t *const p = reinterpret_cast<uint16_t *>(a.scales[m]);
-        p[dst * a.blocks + i] = p[src * a.blocks + i];
+          for (int m = 0; m < 2; ++m) v[i][m] = *reinterpret_cast<const uint4 *>(a.lanes[m] + (s * a.units + u) * 16);
+        }
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (to[i] >= 0)
+#pragma unroll
+          for (int m = 0; m < 2; ++m) *reinterpret_cast<uint4 *>(a.lanes[m] + to[i] * 16) = v[i][m];
+    }
+    for (int i = 0; i < a.parts; ++i) {
+      const int idx = i * 32 + lane, row = (idx * a.part_mul) >> 16, u = idx - row * a.parts;
+      const int64_t s = __shfl_sync(0xffffffffu, src, row), d = __shfl_sync(0xffffffffu, dst, row);
+      if (s >= 0)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          Part *const p = reinterpret_cast<Part *>(a.scales[m]);
+          p[d * a.parts + u] = p[s * a.parts + u];
+        }
+    }
   }
+}
+
+template <typename Part>
+cudaError_t launch_copy(CopyArgs a, int blocks, cudaStream_t stream) {
+  constexpr auto kern = cache_copy_kernel<Part>;
+  a.parts = blocks * 2 / static_cast<int>(sizeof(Part));
+  a.part_mul = 65536 / a.parts + 1;
+  return launch_dependent(kern, dim3(resident_grid<kern>(a.rows * a.chunks * 32, 256)), 256, 0, stream, 1, a);
 }
 
 }  // namespace
@@ -281,12 +315,13 @@ cudaError_t launch_cache_evict(const samd_cache &c, const samd_cache_seqs &s, co
   a.s = e.s, a.dst = kv::make_seqs(c, dst), a.kept = kept;
   a.lanes[0] = static_cast<uint8_t *>(c.k_lanes), a.lanes[1] = static_cast<uint8_t *>(c.v_lanes);
   a.scales[0] = static_cast<uint8_t *>(c.k_scales), a.scales[1] = static_cast<uint8_t *>(c.v_scales);
-  a.heads = c.heads, a.keep = keep, a.units = c.dim * c.fmt.bits / 128, a.blocks = c.dim / 32;
-  a.rows = rows * keep;
-  a.by_row = make_index_div(a.rows * a.units, a.units);
-  a.by_keep = make_index_div(a.rows, keep);
+  a.heads = c.heads, a.keep = keep;
+  a.units = c.dim * c.fmt.bits / 128, a.unit_mul = 65536 / a.units + 1;
+  a.rows = rows, a.chunks = (keep + 31) / 32;
+  a.by_chunks = make_index_div(rows * a.chunks, a.chunks);
   a.by_heads = make_index_div(rows, c.heads);
-  return launch_dependent(cache_copy_kernel, dim3(resident_grid<cache_copy_kernel>(a.rows * a.units, 256)), 256, 0, stream, 1, a);
+  const int blocks = c.dim / 32;
+  return blocks % 2 == 0 ? launch_copy<uint32_t>(a, blocks, stream) : launch_copy<uint16_t>(a, blocks, stream);
 }
 
 }  // namespace samd

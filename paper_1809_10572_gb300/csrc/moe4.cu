@@ -2,10 +2,10 @@
 // experts; the layer's kernels are in moe4_kernel.cuh.
 //
 // Routing: a cluster of one to eight CTAs a token; every warp takes experts in
-// turn (16 bytes a lane of the router's row and of the token, products and sums
-// in fp32), the logits meet in the first CTA, where one warp takes the largest,
-// topk times. Bound by latency: the router's matrix comes from L2 for every
-// token.
+// turn, or slices of the inputs of few ones (16 bytes a lane of the router's row
+// and of the token, products and sums in fp32); the logits meet in the first
+// CTA, where one warp takes the largest, topk times. Bound by latency: the
+// router's matrix comes from L2 for every token.
 #include "moe4_kernel.cuh"
 
 namespace samd {
@@ -13,6 +13,7 @@ namespace {
 
 constexpr int kRouteThreads = 256;
 constexpr int kRouteWarps = kRouteThreads / 32;
+constexpr int kMaxCluster = 8;
 
 struct RouteArgs {
   const uint8_t *x, *router;
@@ -20,6 +21,7 @@ struct RouteArgs {
   int32_t *ids;
   float *weights;
   int K, E, topk, normalize, cluster;
+  int slices, per;  // warps that share an expert, and the inputs of one (a multiple of 256, or all)
 };
 
 __device__ __forceinline__ uint32_t order_of(float f) {
@@ -43,6 +45,7 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b, float s) {
 template <typename T>
 __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const RouteArgs a) {
   __shared__ float logits[moe::kMaxExperts];
+  __shared__ float parts[kRouteWarps * kMaxCluster];  // [expert][slice], where an expert has several
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int64_t token = blockIdx.x / a.cluster;
   const int rank = blockIdx.x % a.cluster;
@@ -50,11 +53,13 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const RouteArg
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
   const uint8_t *const x = a.x + token * a.ldx;
-  for (int e = rank * kRouteWarps + warp; e < a.E; e += a.cluster * kRouteWarps) {
+  float *const out = a.slices > 1 ? parts : logits;
+  for (int task = rank * kRouteWarps + warp; task < a.E * a.slices; task += a.cluster * kRouteWarps) {
+    const int e = task / a.slices, end = min(a.K, (task - e * a.slices + 1) * a.per);
     const uint8_t *const r = a.router + static_cast<int64_t>(e) * a.K * 2;
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    int k = lane * 8;
-    for (; k + 3 * 256 < a.K; k += 4 * 256) {
+    int k = (task - e * a.slices) * a.per + lane * 8;
+    for (; k + 3 * 256 < end; k += 4 * 256) {
       uint4 u[4], v[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -64,20 +69,29 @@ __global__ void __launch_bounds__(kRouteThreads) moe_route_kernel(const RouteArg
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[i] = dot8<T>(u[i], v[i], s[i]);
     }
-    for (; k < a.K; k += 256)
+#pragma unroll 2
+    for (; k < end; k += 256)
       s[0] = dot8<T>(*reinterpret_cast<const uint4 *>(r + k * 2), *reinterpret_cast<const uint4 *>(x + k * 2), s[0]);
     float v = (s[0] + s[1]) + (s[2] + s[3]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     if (lane == 0) {
       if (a.cluster == 1)
-        logits[e] = v;
+        out[task] = v;
       else
-        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(ptx::map_to_rank(ptx::smem_addr(&logits[e]), 0)), "f"(v) : "memory");
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(ptx::map_to_rank(ptx::smem_addr(out + task), 0)), "f"(v) : "memory");
     }
   }
   __syncthreads();
   if (a.cluster > 1) ptx::cluster_sync();
+  if (rank == 0 && warp == 0 && a.slices > 1) {
+    for (int e = lane; e < a.E; e += 32) {
+      float v = 0.0f;
+      for (int i = 0; i < a.slices; ++i) v += parts[e * a.slices + i];
+      logits[e] = v;
+    }
+    __syncwarp();
+  }
   if (rank != 0 || warp != 0) return;
 
   float all_top = -INFINITY, all_sum = 0.0f;
@@ -126,13 +140,16 @@ int chunk_tokens(const samd_moe_desc &d) {
 
 cudaError_t launch_moe_route(const samd_moe_desc &d, bool normalize, const void *x, const void *router, int32_t *ids,
                              float *weights, cudaStream_t s) {
-  int cluster = 1;
-  while (cluster < 8 && cluster * kRouteWarps < d.E) cluster *= 2;
+  // few experts: their inputs in slices of 512 or more, while the cluster has warps for them
+  int slices = 1, cluster = 1;
+  while (d.E * slices * 2 <= kMaxCluster * kRouteWarps && d.K >= 1024 * slices) slices *= 2;
+  const int per = slices == 1 ? d.K : (d.K + slices * 256 - 1) / (slices * 256) * 256;
+  while (cluster < kMaxCluster && cluster * kRouteWarps < d.E * slices) cluster *= 2;
   constexpr int kMost = 1 << 27;  // tokens of a launch: its CTAs are counted in 31 bits
   for (int64_t m = 0; m < d.M; m += kMost) {
     const int n = d.M - m < kMost ? static_cast<int>(d.M - m) : kMost;
     const RouteArgs a = {static_cast<const uint8_t *>(x) + m * d.ldx * 2, static_cast<const uint8_t *>(router), d.ldx * 2,
-                         ids + m * d.topk, weights + m * d.topk, d.K, d.E, d.topk, normalize, cluster};
+                         ids + m * d.topk, weights + m * d.topk, d.K, d.E, d.topk, normalize, cluster, slices, per};
     const cudaError_t e = d.type == SAMD_BF16
                               ? launch_dependent(moe_route_kernel<__nv_bfloat16>, dim3(n * cluster), kRouteThreads, 0, s, cluster, a)
                               : launch_dependent(moe_route_kernel<__half>, dim3(n * cluster), kRouteThreads, 0, s, cluster, a);

@@ -112,6 +112,22 @@ __device__ __forceinline__ void make_lists(const int32_t *ids, int pairs, int E,
   }
 }
 
+// d = a b, or d += a b; without side effects, so that the compiler may place it.
+template <typename T>
+__device__ __forceinline__ void mma_pure(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool add) {
+  const float c0 = add ? d[0] : 0.0f, c1 = add ? d[1] : 0.0f, c2 = add ? d[2] : 0.0f, c3 = add ? d[3] : 0.0f;
+  if constexpr (std::is_same<T, __half>::value)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, "
+        "%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, "
+        "%12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+
 // Minus the power and the zero point z (in both halves), for the nibbles at bit 0 (lo) and bit 4 (hi).
 template <typename T>
 __device__ __forceinline__ void minus(uint32_t zz, uint32_t &lo, uint32_t &hi) {
@@ -137,156 +153,177 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t flip, uint32_t (&p)[4
   }
 }
 
-// CH: chunks of 32 inputs in a block; CPG: chunks of a block that share a scale.
-template <int CH, int CPG>
+// RT: row tiles of 16 rows in a tile; CH: chunks of 32 inputs in a block; CPG: chunks of a block that share a scale.
+template <int RT, int CH, int CPG>
 struct Moe {
   static constexpr int KB = 32 * CH;
+  static constexpr int kRows = 16 * RT;
   static constexpr int kPitch = 16 * CH;
-  static constexpr int kStage = 16 * kPitch;
+  static constexpr int kStage = kRows * kPitch;
   static constexpr int kStages = 4;
   static constexpr int kGroups = CH / CPG;  // scales of a row in a block
   static constexpr int kRing = kWarps * kStages * kStage;
   // first kernel: two buffers of [warp][row][pair]; second: [warp][row][token], then the joined [row][token]
   static constexpr int kRedPitch = kCols + 1;
   static constexpr int red_bytes(bool gated, int tokens) {
-    return gated ? 2 * kWarps * 16 * kRedPitch * 4 : (kWarps + 1) * 16 * (tokens | 1) * 4;
+    return gated ? 2 * kWarps * kRows * kRedPitch * 4 : (kWarps + 1) * kRows * (tokens | 1) * 4;
   }
   static constexpr size_t smem(bool gated, int tokens) { return static_cast<size_t>(kRing) + red_bytes(gated, tokens); }
 };
 
-template <typename T, bool kGated, bool kZeros, int CH, int CPG>
+template <typename T, bool kGated, bool kZeros, int RT, int CH, int CPG>
 __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
-  using P = Moe<CH, CPG>;
-  constexpr int KB = P::KB, kPitch = P::kPitch, kStages = P::kStages, kG = P::kGroups;
-  constexpr int kSwz = CH >= 8 ? 0 : 1;  // rows that share a 128-byte line: 2^kSwz
+  using P = Moe<RT, CH, CPG>;
+  constexpr int KB = P::KB, kRows = P::kRows, kPitch = P::kPitch, kStages = P::kStages, kG = P::kGroups;
+  constexpr int kSwz = CH >= 8 ? 0 : 1;            // rows that share a 128-byte line: 2^kSwz
+  constexpr int kOut = kGated ? kRows / 2 : kRows; // rows of a matrix in a tile
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Lists lists;
-  __shared__ int count[kMaxExperts];
   float *const red = reinterpret_cast<float *>(smem + P::kRing);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
 
   // everything read may come from the kernel before; the next one may be set up
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
-  if (warp == 0) make_lists(a.ids, a.M * a.topk, a.E, &lists, count, reinterpret_cast<uint16_t *>(smem), lane);
+  if (warp == 0)  // (the ring is not in use yet)
+    make_lists(a.ids, a.M * a.topk, a.E, &lists, reinterpret_cast<int *>(smem), reinterpret_cast<uint16_t *>(smem + kMaxExperts * 4), lane);
   if constexpr (!kGated)
-    for (int i = tid; i < kWarps * 16 * (a.M | 1); i += kThreads) red[i] = 0.0f;
+    for (int i = tid; i < kWarps * kRows * (a.M | 1); i += kThreads) red[i] = 0.0f;
   __syncthreads();
 
+  // A warp's blocks, one after the other. First kernel: the CTA's items (pass and tile) in turn, every eighth block of
+  // each; second: the CTA's tile, the warp's share of the blocks of all passes.
   const int rank = kGated ? 0 : blockIdx.x % a.splits;
-  const int tile0 = kGated ? 0 : blockIdx.x / a.splits;  // the CTA's only tile
-  const uint32_t ring = ptx::smem_addr(smem) + warp * kStages * P::kStage;
-  // A walk over this warp's blocks: gated: items (pass, tile) of the CTA, and the warp's blocks of each; else the
-  // warp's share of the blocks of all passes.
+  const int stride = kGated ? kWarps : kWarps * a.splits;
+  const int passes = lists.passes, items = passes * a.tiles;
   struct At {
     int item, pass, tile, blk;
   };
-  const int items = lists.passes * a.tiles;
-  auto settle = [&](At &w) {  // pass and tile of an item, the pass behind the last at the end
+  auto settle = [&](At &w) {  // true where the pass or the tile is another one
+    if (w.blk < a.nblk) return false;
     if constexpr (kGated) {
+      w.blk = warp;
+      w.item += gridDim.x;
       if (w.item >= items) {
-        w.pass = lists.passes;
+        w.pass = passes;
       } else {
         w.pass = w.item / a.tiles;
         w.tile = w.item - w.pass * a.tiles;
       }
     } else {
-      while (w.blk >= a.nblk) w.blk -= a.nblk, ++w.pass;
+      do w.blk -= a.nblk, ++w.pass;
+      while (w.blk >= a.nblk);
     }
+    return true;
   };
-  auto begin = [&]() {
-    At w = {static_cast<int>(blockIdx.x), 0, tile0, kGated ? warp : rank * kWarps + warp};
-    settle(w);
-    if (kGated && warp >= a.nblk) w.pass = lists.passes;  // no block is this warp's
-    return w;
-  };
-  auto next = [&](At &w) {
-    if constexpr (kGated) {
-      w.blk += kWarps;
-      if (w.blk >= a.nblk) {
-        w.blk = warp;
-        w.item += gridDim.x;
-        settle(w);
-      }
-    } else {
-      w.blk += kWarps * a.splits;
-      settle(w);
-    }
-  };
+  At have = {static_cast<int>(blockIdx.x), 0, kGated ? 0 : static_cast<int>(blockIdx.x) / a.splits, kGated ? warp : rank * kWarps + warp};
+  if constexpr (kGated) {
+    have.pass = have.item / a.tiles, have.tile = have.item - have.pass * a.tiles;
+    if (have.item >= items || warp >= a.nblk) have.pass = passes;  // nothing is this warp's
+  } else {
+    settle(have);
+  }
 
-  // ---- loading: row r of a tile is row n of matrix m
-  auto row_index = [&](const At &w, int r) -> int64_t {
-    const int n = kGated ? w.tile * 8 + (r & 7) : w.tile * 16 + r;
-    return static_cast<int64_t>(lists.expert[w.pass]) * a.N + n;
+  // ---- loading. Row r of a tile: 16-row tiles of eight rows of each matrix, or of sixteen of the one.
+  const int64_t expert_bytes = a.N * a.row_bytes, expert_scales = a.N * a.groups;
+  const int lc = (lane % CH) * 16, lr = lane / CH;  // a copy: the lane's bytes of a row, and row
+  const uint32_t ring = ptx::smem_addr(smem) + warp * kStages * P::kStage;
+  const uint32_t copy_at = lr * kPitch + ((lc / 16) ^ ((lr >> kSwz) & (CH - 1))) * 16;
+  At ahead = have;
+  const uint8_t *w_row[kGated ? 2 : 1];
+  auto seek = [&]() {
+    if (ahead.pass < passes) {
+      const int64_t off = lists.expert[ahead.pass] * expert_bytes + static_cast<int64_t>(ahead.tile * kOut + lr) * a.row_bytes + lc;
+      w_row[0] = a.lanes[0] + off;
+      if constexpr (kGated) w_row[1] = a.lanes[1] + off;
+    }
   };
-  At ahead = begin();
+  seek();
   int fill = 0;
   auto load_next = [&]() {
-    if (ahead.pass < lists.passes) {
+    if (ahead.pass < passes) {
       const uint32_t st = ring + fill * P::kStage;
-      constexpr int kLanes = CH, kStep = 32 / kLanes;  // lanes of a row, rows of a warp's copy
-      const int c = lane % kLanes, r0 = lane / kLanes;
-      const int64_t at = static_cast<int64_t>(ahead.blk) * (KB / 2) + c * 16;
-      const uint32_t n = at < a.row_bytes ? 16u : 0u;
-      const int64_t off = row_index(ahead, r0) * a.row_bytes + (n ? at : 0);
+      const int at = ahead.blk * (KB / 2);
+      if (at + lc < a.row_bytes) {  // (behind a row's end the stage keeps what it holds: any lanes, times inputs of zero)
+        constexpr int kStep = 32 / CH;  // rows of a warp's copy
 #pragma unroll
-      for (int i = 0; i < 16 / kStep; ++i) {
-        const int r = i * kStep + r0;
-        const uint8_t *const m = a.lanes[kGated && i * kStep >= 8];
-        const int up = kGated ? (i * kStep) & 7 : i * kStep;  // rows further than r0
-        ptx::cp_async_16(st + r * kPitch + ((c ^ ((r >> kSwz) & (CH - 1))) * 16), m + off + up * a.row_bytes, n);
+        for (int i = 0; i < kRows / kStep; ++i) {
+          constexpr int kEight = 8 / kStep;  // copies of eight rows
+          const int r = i * kStep;           // and lr: of the stage
+          const int m = kGated ? (i / kEight) & 1 : 0;
+          const int n = kGated ? (i / (2 * kEight)) * 8 + (i % kEight) * kStep : r;  // of the matrix
+          // (lr is below kStep, so row lr + r is swizzled by the exclusive or of both)
+          ptx::cp_async_16(st + (copy_at ^ ((r >> kSwz) & (CH - 1)) * 16) + r * kPitch, w_row[m] + n * a.row_bytes + at);
+        }
       }
-      next(ahead);
+      ahead.blk += stride;
+      if (settle(ahead)) seek();
     }
     ptx::cp_async_commit();
     fill = fill + 1 == kStages ? 0 : fill + 1;
   };
   // lane r's row's scales and zero points of a block; those behind the row's end are zero
   constexpr int kSW = (kG + 1) / 2, kZW = (kG + 3) / 4;
+  const bool scale_lane = kRows >= 32 || lane < kRows;
+  int64_t s_row = 0;  // of the item in hand: the row's first scale
+  const uint16_t *s_base = reinterpret_cast<const uint16_t *>(a.scales[0]);
+  const uint8_t *z_base = a.zeros[0];
+  if (kGated && (lane & 8)) s_base = reinterpret_cast<const uint16_t *>(a.scales[1]), z_base = a.zeros[1];
+  auto seek_scales = [&](const At &w) {
+    const int n = kGated ? w.tile * kOut + (lane >> 4) * 8 + (lane & 7) : w.tile * kOut + lane;
+    if (w.pass < passes && scale_lane) s_row = lists.expert[w.pass] * expert_scales + n * a.groups;
+  };
   auto load_scales = [&](const At &w, uint32_t (&s)[kSW], uint32_t (&z)[kZW]) {
-#pragma unroll
-    for (int i = 0; i < kSW; ++i) s[i] = 0;
-#pragma unroll
-    for (int i = 0; i < kZW; ++i) z[i] = 0;
-    if (lane < 16 && w.pass < lists.passes) {
-      const int m = kGated && lane >= 8;
-      const int64_t grp = (static_cast<int64_t>(w.blk) * KB) >> a.group_shift;
-      const int64_t at = row_index(w, lane) * a.groups + grp;
-      const uint16_t *const sp = reinterpret_cast<const uint16_t *>(a.scales[m]) + at;
-      const uint8_t *const zp = a.zeros[m] + at;
-      if (kG > 1 && a.s_vec) {
-        if constexpr (kG == 8) {
-          const uint4 v = *reinterpret_cast<const uint4 *>(sp);
-          s[0] = v.x, s[1] = v.y, s[2] = v.z, s[3] = v.w;
-          if constexpr (kZeros) {
-            const uint2 q = *reinterpret_cast<const uint2 *>(zp);
-            z[0] = q.x, z[1] = q.y;
-          }
-        } else if constexpr (kG == 4) {
-          const uint2 v = *reinterpret_cast<const uint2 *>(sp);
-          s[0] = v.x, s[1] = v.y;
-          if constexpr (kZeros) z[0] = *reinterpret_cast<const uint32_t *>(zp);
-        } else if constexpr (kG == 2) {
-          s[0] = *reinterpret_cast<const uint32_t *>(sp);
-          if constexpr (kZeros) z[0] = *reinterpret_cast<const uint16_t *>(zp);
+    if (!scale_lane || w.pass >= passes) return;
+    const int64_t grp = (static_cast<int64_t>(w.blk) * KB) >> a.group_shift;
+    const uint16_t *const sp = s_base + s_row + grp;
+    const uint8_t *const zp = z_base + s_row + grp;
+    if (kG > 1 && a.s_vec) {
+      if constexpr (kG == 8) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(sp);
+        s[0] = v.x, s[1] = v.y, s[2] = v.z, s[3] = v.w;
+        if constexpr (kZeros) {
+          const uint2 q = *reinterpret_cast<const uint2 *>(zp);
+          z[0] = q.x, z[1] = q.y;
         }
-      } else {
+      } else if constexpr (kG == 4) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(sp);
+        s[0] = v.x, s[1] = v.y;
+        if constexpr (kZeros) z[0] = *reinterpret_cast<const uint32_t *>(zp);
+      } else if constexpr (kG == 2) {
+        s[0] = *reinterpret_cast<const uint32_t *>(sp);
+        if constexpr (kZeros) z[0] = *reinterpret_cast<const uint16_t *>(zp);
+      }
+    } else {
 #pragma unroll
-        for (int i = 0; i < kG; ++i) {
-          // groups of more than a block: the same one for all of it
-          const int j = CPG == 4 && a.group_shift > 7 ? static_cast<int>(((static_cast<int64_t>(w.blk) * KB + i * 128) >> a.group_shift) - grp) : i;
-          if (grp + j < a.groups) {
-            s[i / 2] |= static_cast<uint32_t>(sp[j]) << 16 * (i & 1);
-            if constexpr (kZeros) z[i / 4] |= static_cast<uint32_t>(zp[j]) << 8 * (i & 3);
-          }
+      for (int i = 0; i < kSW; ++i) s[i] = 0;
+#pragma unroll
+      for (int i = 0; i < kZW; ++i) z[i] = 0;
+#pragma unroll
+      for (int i = 0; i < kG; ++i) {
+        // groups of more than a block: the same one for all of it
+        const int j = CPG == 4 && a.group_shift > 7 ? static_cast<int>(((static_cast<int64_t>(w.blk) * KB + i * 128) >> a.group_shift) - grp) : i;
+        if (grp + j < a.groups) {
+          s[i / 2] |= static_cast<uint32_t>(sp[j]) << 16 * (i & 1);
+          if constexpr (kZeros) z[i / 4] |= static_cast<uint32_t>(zp[j]) << 8 * (i & 3);
         }
       }
     }
   };
 
-  At have = begin();
-  uint32_t s_next[kSW], z_next[kZW];
+  uint32_t s_next[kSW] = {}, z_next[kZW] = {};
+  seek_scales(have);
   load_scales(have, s_next, z_next);
+  const uint8_t *x_row = nullptr;
+  // the lane's column of a pass: its inputs; lanes without a pair read the first one's, and their sums are not used
+  auto seek_inputs = [&](int pass) {
+    if (pass < passes) {
+      const int first = lists.first[pass], n = min(static_cast<int>(lists.first[pass + 1]) - first, kCols);
+      const int pair = lists.order[first + (g < n ? g : 0)];
+      x_row = a.x + (kGated ? pair / a.topk : pair) * a.ldx + t * 16;
+    }
+  };
+  seek_inputs(have.pass);
 #pragma unroll 1
   for (int i = 0; i < kStages - 1; ++i) load_next();
 
@@ -295,137 +332,155 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
   uint32_t plain_lo, plain_hi;
   minus<T>(flip, plain_lo, plain_hi);
 
-  float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  float acc[RT][4] = {};
   int slot = 0;
-  // one block: its products into acc
+  // one block: its products into acc; true where the next one is of another pass or tile
   auto block = [&]() {
-    const int first = lists.first[have.pass], n = min(static_cast<int>(lists.first[have.pass + 1]) - first, kCols);
-    const int64_t k0 = static_cast<int64_t>(have.blk) * KB;
     uint4 xq[CH];
+    const int k0 = have.blk * KB;
+    if (k0 + KB <= a.K) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) xq[c] = make_uint4(0, 0, 0, 0);
-    if (g < n) {
-      const int pair = lists.order[first + g];
-      const uint8_t *const xr = a.x + (kGated ? pair / a.topk : pair) * a.ldx + (k0 + t * 8) * 2;
+      for (int c = 0; c < CH; ++c) xq[c] = *reinterpret_cast<const uint4 *>(x_row + k0 * 2 + c * 64);
+    } else {
 #pragma unroll
       for (int c = 0; c < CH; ++c)
-        if (k0 + c * 32 < a.K) xq[c] = *reinterpret_cast<const uint4 *>(xr + c * 64);
+        xq[c] = k0 + c * 32 < a.K ? *reinterpret_cast<const uint4 *>(x_row + k0 * 2 + c * 64) : make_uint4(0, 0, 0, 0);
     }
     uint32_t s[kSW], z[kZW];
 #pragma unroll
     for (int i = 0; i < kSW; ++i) s[i] = s_next[i];
 #pragma unroll
     for (int i = 0; i < kZW; ++i) z[i] = z_next[i];
-    At then = have;
-    next(then);
-    load_scales(then, s_next, z_next);
+    have.blk += stride;
+    const bool other = settle(have);
+    if (other) {
+      seek_scales(have);
+      seek_inputs(have.pass);
+    }
+    load_scales(have, s_next, z_next);
     ptx::cp_async_wait<kStages - 2>();
     __syncwarp();  // every lane's copies are in, and the stage filled next has been read by every lane
     load_next();
     const uint32_t sw = ring + slot * P::kStage;
     slot = slot + 1 == kStages ? 0 : slot + 1;
-    uint32_t words[4], s0 = 0, s1 = 0, z0 = 0, z1 = 0;
+    uint32_t words[RT][4], sc[RT][2] = {}, zc[RT][2] = {};
 #pragma unroll
     for (int gi = 0; gi < kG; ++gi) {
-      if ((gi & 1) == 0) {
-        s0 = __shfl_sync(0xffffffffu, s[gi / 2], g);
-        s1 = __shfl_sync(0xffffffffu, s[gi / 2], g + 8);
-      }
-      uint32_t lo0 = plain_lo, lo1 = plain_lo, hi0 = plain_hi, hi1 = plain_hi;
-      if constexpr (kZeros) {
-        if ((gi & 3) == 0) {
-          z0 = __shfl_sync(0xffffffffu, z[gi / 4], g);
-          z1 = __shfl_sync(0xffffffffu, z[gi / 4], g + 8);
+      uint32_t less[RT][4];
+#pragma unroll
+      for (int q = 0; q < RT; ++q) {
+        if ((gi & 1) == 0) {
+          sc[q][0] = __shfl_sync(0xffffffffu, s[gi / 2], 16 * q + g);
+          sc[q][1] = __shfl_sync(0xffffffffu, s[gi / 2], 16 * q + g + 8);
         }
-        constexpr uint32_t kLow = 0x000F000Fu;
-        minus<T>(__byte_perm(z0, 0, 0x4040 | (gi & 3) | (gi & 3) << 8) & kLow, lo0, hi0);
-        minus<T>(__byte_perm(z1, 0, 0x4040 | (gi & 3) | (gi & 3) << 8) & kLow, lo1, hi1);
+        less[q][0] = less[q][1] = plain_lo, less[q][2] = less[q][3] = plain_hi;
+        if constexpr (kZeros) {
+          if ((gi & 3) == 0) {
+            zc[q][0] = __shfl_sync(0xffffffffu, z[gi / 4], 16 * q + g);
+            zc[q][1] = __shfl_sync(0xffffffffu, z[gi / 4], 16 * q + g + 8);
+          }
+          const int sel = 0x4040 | (gi & 3) | (gi & 3) << 8;
+          minus<T>(__byte_perm(zc[q][0], 0, sel) & 0x000F000Fu, less[q][0], less[q][2]);
+          minus<T>(__byte_perm(zc[q][1], 0, sel) & 0x000F000Fu, less[q][1], less[q][3]);
+        }
       }
-      const uint32_t less[4] = {lo0, lo1, hi0, hi1};
-      float d[4];
+      float d[RT][4];
 #pragma unroll
       for (int cc = 0; cc < CPG; ++cc) {
         const int c = gi * CPG + cc;
-        if ((c & 1) == 0) mv::ldmatrix_x4((sw + lm) ^ (c * 16), words);
-        const uint4 q = xq[c];
-        const uint32_t b0 = __byte_perm(q.x, q.z, 0x5410), b1 = __byte_perm(q.x, q.z, 0x7632);
-        const uint32_t b2 = __byte_perm(q.y, q.w, 0x5410), b3 = __byte_perm(q.y, q.w, 0x7632);
-        uint32_t lo[4], hi[4];
-        widen<T>(words[2 * (c & 1)], flip, lo);
-        widen<T>(words[2 * (c & 1) + 1], flip, hi);
-        const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
-        if (cc == 0)
-          mv::mma16816<T, false>(d, less, b0, b1);
-        else
-          mv::mma16816<T, true>(d, less, b0, b1);
-        mv::mma16816<T, true>(d, less, b2, b3);
-        mv::mma16816<T, true>(d, a0, b0, b1);
-        mv::mma16816<T, true>(d, a1, b2, b3);
+        if ((c & 1) == 0)
+#pragma unroll
+          for (int q = 0; q < RT; ++q) mv::ldmatrix_x4(((sw + lm) ^ (c * 16)) + q * (16 * kPitch), words[q]);
+        const uint4 v = xq[c];
+        const uint32_t b0 = __byte_perm(v.x, v.z, 0x5410), b1 = __byte_perm(v.x, v.z, 0x7632);
+        const uint32_t b2 = __byte_perm(v.y, v.w, 0x5410), b3 = __byte_perm(v.y, v.w, 0x7632);
+#pragma unroll
+        for (int q = 0; q < RT; ++q) {
+          uint32_t lo[4], hi[4];
+          widen<T>(words[q][2 * (c & 1)], flip, lo);
+          widen<T>(words[q][2 * (c & 1) + 1], flip, hi);
+          mma_pure<T>(d[q], less[q], b0, b1, cc > 0);
+          mma_pure<T>(d[q], less[q], b2, b3, true);
+          const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+          mma_pure<T>(d[q], a0, b0, b1, true);
+          mma_pure<T>(d[q], a1, b2, b3, true);
+        }
       }
-      const float f0 = mv::f32_of_bits<T>(static_cast<uint16_t>(gi & 1 ? s0 >> 16 : s0));
-      const float f1 = mv::f32_of_bits<T>(static_cast<uint16_t>(gi & 1 ? s1 >> 16 : s1));
-      acc[0] = fmaf(f0, d[0], acc[0]), acc[1] = fmaf(f0, d[1], acc[1]);
-      acc[2] = fmaf(f1, d[2], acc[2]), acc[3] = fmaf(f1, d[3], acc[3]);
+#pragma unroll
+      for (int q = 0; q < RT; ++q) {
+        const float f0 = mv::f32_of_bits<T>(static_cast<uint16_t>(gi & 1 ? sc[q][0] >> 16 : sc[q][0]));
+        const float f1 = mv::f32_of_bits<T>(static_cast<uint16_t>(gi & 1 ? sc[q][1] >> 16 : sc[q][1]));
+        acc[q][0] = fmaf(f0, d[q][0], acc[q][0]), acc[q][1] = fmaf(f0, d[q][1], acc[q][1]);
+        acc[q][2] = fmaf(f1, d[q][2], acc[q][2]), acc[q][3] = fmaf(f1, d[q][3], acc[q][3]);
+      }
     }
-    have = then;
+    return other;
   };
 
   if constexpr (kGated) {
     int buf = 0;
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
-      while (have.pass < lists.passes && have.item == item) block();
-      const int pass = item / a.tiles, n0 = (item - pass * a.tiles) * 8;
+      const int pass = item / a.tiles, n0 = (item - pass * a.tiles) * kOut;
+      if (have.pass < passes && have.item == item)
+        while (!block()) {
+        }
       const int first = lists.first[pass], n = min(static_cast<int>(lists.first[pass + 1]) - first, kCols);
-      float *const rb = red + buf * (kWarps * 16 * P::kRedPitch);
+      float *const rb = red + buf * (kWarps * kRows * P::kRedPitch);
       buf ^= 1;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        rb[(warp * 16 + g + (i >> 1) * 8) * P::kRedPitch + 2 * t + (i & 1)] = acc[i];
-        acc[i] = 0.0f;
-      }
+      for (int q = 0; q < RT; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          rb[(warp * kRows + q * 16 + g + (i >> 1) * 8) * P::kRedPitch + 2 * t + (i & 1)] = acc[q][i];
+          acc[q][i] = 0.0f;
+        }
       __syncthreads();
       // (the other buffer is written next, and this one only behind another barrier)
-      if (tid < 8 * n) {
-        const int r = tid & 7, c = tid >> 3, pair = lists.order[first + c];
+      if (tid < kOut * n) {
+        const int r = tid % kOut, c = tid / kOut, pair = lists.order[first + c], row = (r >> 3) * 16 + (r & 7);
         float gate = 0.0f, up = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-          gate += rb[(w * 16 + r) * P::kRedPitch + c];
-          up += rb[(w * 16 + 8 + r) * P::kRedPitch + c];
+          gate += rb[(w * kRows + row) * P::kRedPitch + c];
+          up += rb[(w * kRows + row + 8) * P::kRedPitch + c];
         }
         reinterpret_cast<T *>(a.y + pair * a.ldy)[n0 + r] = from_f32<T>(a.weights[pair] * (act_of(a.act, gate) * up));
       }
     }
   } else {
-    const int pitch = a.M | 1;
-    float *const mine = red + warp * 16 * pitch;
-    while (have.pass < lists.passes) {
+    const int pitch = a.M | 1, n0 = have.tile * kOut;
+    float *const mine = red + warp * kRows * pitch;
+    while (have.pass < passes) {
       const int pass = have.pass;
-      block();
-      if (have.pass != pass) {
+      if (block()) {
         // into the tokens' sums, column by column: a token may have the same expert twice
         const int first = lists.first[pass], n = min(static_cast<int>(lists.first[pass + 1]) - first, kCols);
         for (int c = 0; c < n; ++c) {
           if (t == c >> 1) {
             const int m = lists.order[first + c] / a.topk;
-            mine[g * pitch + m] += c & 1 ? acc[1] : acc[0];
-            mine[(g + 8) * pitch + m] += c & 1 ? acc[3] : acc[2];
+#pragma unroll
+            for (int q = 0; q < RT; ++q) {
+              mine[(16 * q + g) * pitch + m] += c & 1 ? acc[q][1] : acc[q][0];
+              mine[(16 * q + g + 8) * pitch + m] += c & 1 ? acc[q][3] : acc[q][2];
+            }
           }
           __syncwarp();
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = 0.0f;
+        for (int q = 0; q < RT; ++q)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[q][i] = 0.0f;
       }
     }
     __syncthreads();
-    float *const sum = red + kWarps * 16 * pitch;
-    for (int i = tid; i < 16 * a.M; i += kThreads) {
-      const int m = i >> 4, r = i & 15;
+    float *const sum = red + kWarps * kRows * pitch;
+    for (int i = tid; i < kRows * a.M; i += kThreads) {
+      const int m = i / kRows, r = i % kRows;
       float v = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) v += red[(w * 16 + r) * pitch + m];
+      for (int w = 0; w < kWarps; ++w) v += red[(w * kRows + r) * pitch + m];
       if (a.splits == 1)
-        reinterpret_cast<T *>(a.y + m * a.ldy)[tile0 * 16 + r] = from_f32<T>(v);
+        reinterpret_cast<T *>(a.y + m * a.ldy)[n0 + r] = from_f32<T>(v);
       else
         sum[r * pitch + m] = v;
     }
@@ -433,8 +488,8 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
       __syncthreads();
       ptx::cluster_sync();
       if (rank == 0)
-        for (int i = tid; i < 16 * a.M; i += kThreads) {
-          const int m = i >> 4, r = i & 15;
+        for (int i = tid; i < kRows * a.M; i += kThreads) {
+          const int m = i / kRows, r = i % kRows;
           float v = 0.0f;
           for (int k = 0; k < a.splits; ++k) {
             float p;
@@ -444,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
                          : "memory");
             v += p;
           }
-          reinterpret_cast<T *>(a.y + m * a.ldy)[tile0 * 16 + r] = from_f32<T>(v);
+          reinterpret_cast<T *>(a.y + m * a.ldy)[n0 + r] = from_f32<T>(v);
         }
       __syncthreads();
       ptx::cluster_sync();  // no CTA ends while its sums are read
@@ -453,41 +508,44 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
   ptx::cp_async_wait<0>();
 }
 
-template <typename T, bool kGated, bool kZeros, int CH, int CPG>
+template <typename T, bool kGated, bool kZeros, int RT, int CH, int CPG>
 cudaError_t launch_as(MoeArgs a, cudaStream_t s) {
-  using P = Moe<CH, CPG>;
+  using P = Moe<RT, CH, CPG>;
   a.nblk = (a.K + P::KB - 1) / P::KB;
-  a.tiles = a.N / (kGated ? 8 : 16);
+  a.tiles = a.N / (kGated ? 8 * RT : 16 * RT);
   a.s_vec = a.groups % P::kGroups == 0 && (1 << a.group_shift) * P::kGroups == P::KB;
-  constexpr auto kern = moe4_kernel<T, kGated, kZeros, CH, CPG>;
+  constexpr auto kern = moe4_kernel<T, kGated, kZeros, RT, CH, CPG>;
   const size_t smem = P::smem(kGated, a.M);
   const cudaError_t e = conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), smem);
   if (e != cudaSuccess) return e;
   const int64_t pairs = static_cast<int64_t>(a.M) * a.topk;
   const int slots = 2 * sm_count();
+  a.splits = 1;
   if (kGated) {
     const int64_t most = pairs * a.tiles;
-    a.splits = 1;
     return launch_dependent(kern, dim3(static_cast<unsigned>(most < slots ? most : slots)), kThreads, smem, s, 1, a);
   }
   // a tile's blocks over as many CTAs as fill the GPU, while each warp still has a block
   const int64_t blocks = (pairs < a.E ? pairs : a.E) * a.nblk;
-  a.splits = 1;
   while (a.splits < 8 && static_cast<int64_t>(a.tiles) * a.splits * 2 <= slots && blocks >= 2 * kWarps * a.splits) a.splits *= 2;
   return launch_dependent(kern, dim3(a.tiles * a.splits), kThreads, smem, s, a.splits, a);
 }
 
-template <typename T, bool kGated, bool kZeros, int CH>
+template <typename T, bool kGated, bool kZeros, int RT, int CH>
 cudaError_t launch_grouped(const MoeArgs &a, cudaStream_t s) {
-  if (a.group_shift == 5) return launch_as<T, kGated, kZeros, CH, 1>(a, s);
-  if (a.group_shift == 6) return launch_as<T, kGated, kZeros, CH, 2>(a, s);
-  return launch_as<T, kGated, kZeros, CH, 4>(a, s);
+  if (a.group_shift == 5) return launch_as<T, kGated, kZeros, RT, CH, 1>(a, s);
+  if (a.group_shift == 6) return launch_as<T, kGated, kZeros, RT, CH, 2>(a, s);
+  return launch_as<T, kGated, kZeros, RT, CH, 4>(a, s);
 }
 
-// Blocks of 256 inputs where every warp gets one, else of 128.
+// Tiles of 32 rows where there are two for each place of a CTA (second kernel: where the warps of that many get a block),
+// else of 16: inputs are put in order and looked up for twice the weights.
 template <typename T, bool kGated, bool kZeros>
 cudaError_t launch_sized(const MoeArgs &a, cudaStream_t s) {
-  return a.K >= 256 * kWarps ? launch_grouped<T, kGated, kZeros, 8>(a, s) : launch_grouped<T, kGated, kZeros, 4>(a, s);
+  const int64_t pairs = static_cast<int64_t>(a.M) * a.topk, experts = pairs < a.E ? pairs : a.E;
+  const int64_t work = kGated ? experts * (a.N / 16) : experts * (a.N / 32) * ((a.K + 127) / 128) / kWarps;
+  return work >= 4 * sm_count() ? launch_grouped<T, kGated, kZeros, 2, 4>(a, s)
+                                : launch_grouped<T, kGated, kZeros, 1, 4>(a, s);
 }
 
 template <typename T>

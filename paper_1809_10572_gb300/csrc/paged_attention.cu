@@ -40,19 +40,33 @@ __device__ __forceinline__ float2 stat_of(const AttArgs &a, int64_t unit_part, i
 __device__ __forceinline__ float2 stat_all(const AttArgs &a, int64_t unit_part, int part, int2 span, int h, int lane) {
   const int n = span.y - span.x + 1;
   float top = -3e38f, weight = 0.0f;
-  for (int i = lane; i < n; i += 32) top = fmaxf(top, stat_of(a, unit_part, part, span.x, i, h).x);
-  top = warp_max(top);
   for (int i = lane; i < n; i += 32) {
     const float2 s = stat_of(a, unit_part, part, span.x, i, h);
-    weight = fmaf(exp2_of(s.x - top), s.y, weight);
+    const float now = fmaxf(top, s.x);
+    weight = fmaf(weight, exp2_of(top - now), s.y * exp2_of(s.x - now));
+    top = now;
   }
-  return make_float2(top, warp_sum(weight));
+  const float all = warp_max(top);
+  return make_float2(all, warp_sum(weight * exp2_of(top - all)));
 }
+
+// What a thread has of a head: four elements' sums and the sum of weights, under a reference.
+struct Joined {
+  float4 v;
+  float top, weight;
+
+  __device__ __forceinline__ void add(const float4 &p, float2 s) {
+    const float now = fmaxf(top, s.x), mine = exp2_of(top - now), its = exp2_of(s.x - now);
+    v.x = fmaf(v.x, mine, p.x * its), v.y = fmaf(v.y, mine, p.y * its);
+    v.z = fmaf(v.z, mine, p.z * its), v.w = fmaf(v.w, mine, p.w * its);
+    weight = fmaf(weight, mine, s.y * its);
+    top = now;
+  }
+};
 
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) paged_attention_join(const JoinArgs j) {
-  __shared__ float factor[kMaxSlots];
-  __shared__ float4 red[kJoinThreads];
+  __shared__ Joined red[kJoinThreads];
   extern __shared__ float2 head[];  // with scores: reference and 1 / sum of weights of the unit's query heads
   const AttArgs &a = j.a;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -66,40 +80,36 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join(const JoinA
   const int len = static_cast<int>(length_of(a.s, b));
 
   if (!a.whole) {
+    const int2 span = a.span[unit_part];  // (not yet written where there are no tokens)
     if (len == 0) {
       uint32_t *const out = reinterpret_cast<uint32_t *>(a.out + b * a.ldo + static_cast<int64_t>(head0) * j.dim * 2);
       if (blockIdx.y == 0)
         for (int i = tid; i < n_heads * j.dim / 2; i += kJoinThreads) out[i] = 0;
       return;
     }
-    const int2 span = a.span[unit_part];
     const int n = span.y - span.x + 1;
     if (n > 1) {
+      // columns of four elements by groups of threads that take parts in turn
       const int cols = j.dim / 4, groups = kJoinThreads / cols, col = tid % cols, grp = tid / cols;
       for (int h = blockIdx.y; h < n_heads; h += gridDim.y) {
-        const float2 all = stat_all(a, unit_part, part, span, h, lane);
-        const float inv = all.y == 0.0f ? 0.0f : 1.0f / all.y;
-        for (int i = tid; i < n; i += kJoinThreads)
-          factor[i] = exp2_of(stat_of(a, unit_part, part, span.x, i, h).x - all.x);
-        __syncthreads();
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        Joined mine = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), -3e38f, 0.0f};
         if (grp < groups)
 #pragma unroll 4
           for (int i = grp; i < n; i += groups) {
             const int64_t cta = static_cast<int64_t>(span.x + i) * a.parts + part;
-            const float4 p = *reinterpret_cast<const float4 *>(a.sums + ((cta * 2 + (i == 0)) * kHeads + h) * j.dim + col * 4);
-            const float f = factor[i];
-            v.x = fmaf(f, p.x, v.x), v.y = fmaf(f, p.y, v.y), v.z = fmaf(f, p.z, v.z), v.w = fmaf(f, p.w, v.w);
+            mine.add(*reinterpret_cast<const float4 *>(a.sums + ((cta * 2 + (i == 0)) * kHeads + h) * j.dim + col * 4),
+                     stat_of(a, unit_part, part, span.x, i, h));
           }
-        red[tid] = v;
+        red[tid] = mine;
         __syncthreads();
         if (grp == 0) {
-          for (int i = 1; i < groups; ++i) {
-            const float4 p = red[i * cols + col];
-            v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
+          for (int i = 1; i < groups && i < n; ++i) {
+            const Joined p = red[i * cols + col];
+            mine.add(p.v, make_float2(p.top, p.weight));
           }
+          const float inv = mine.weight == 0.0f ? 0.0f : 1.0f / mine.weight;
           *reinterpret_cast<uint2 *>(a.out + b * a.ldo + (static_cast<int64_t>(head0 + h) * j.dim + col * 4) * 2) =
-              make_uint2(pack2<T>(v.x * inv, v.y * inv), pack2<T>(v.z * inv, v.w * inv));
+              make_uint2(pack2<T>(mine.v.x * inv, mine.v.y * inv), pack2<T>(mine.v.z * inv, mine.v.w * inv));
         }
         __syncthreads();
       }

@@ -194,16 +194,21 @@ __device__ __forceinline__ void ldsm4_trans(uint32_t addr, uint32_t (&r)[4]) {
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, "
-      "%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                              uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, "
+      "%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ float exp2_of(float x) {
   float r;
@@ -215,19 +220,40 @@ __device__ __forceinline__ uint32_t sub_h2(uint32_t a, uint32_t b) {
   return reinterpret_cast<const uint32_t &>(d);
 }
 
-// Signed lanes of a word, or of two tokens' halves of words, as pairs in fp16: lane i of the low half with lane i of
-// the high half. 8 bits: 1024 + 128 + lane over a byte; 4 bits: 1024 + 8 + lane, or 64 + 8 + lane four bits up.
+// The powers of two with a signed lane's zero, in both halves: 1024 + 128 (8 bits), 1024 + 8 and 64 + 8 (4 bits, at bit 0
+// and at bit 4). Held in registers that the compiler does not know the values of: it would spend an instruction more on
+// every (w & mask) ^ power of two constants.
 template <int BITS>
-__device__ __forceinline__ void widen(uint32_t w, uint32_t (&p)[16 / BITS]) {
+struct Powers {
+  uint32_t v[BITS == 8 ? 1 : 2];
+  __device__ __forceinline__ Powers() {
+    if constexpr (BITS == 8) {
+      asm volatile("mov.u32 %0, 0x64806480;" : "=r"(v[0]));
+    } else {
+      asm volatile("mov.u32 %0, 0x64086408;" : "=r"(v[0]));
+      asm volatile("mov.u32 %0, 0x54805480;" : "=r"(v[1]));
+    }
+  }
+};
+__device__ __forceinline__ uint32_t and_xor(uint32_t w, uint32_t mask, uint32_t x) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(r) : "r"(w), "r"(mask), "r"(x));
+  return r;
+}
+
+// Signed lanes of a word, or of two tokens' halves of words, as pairs in fp16: lane i of the low half with lane i of
+// the high half.
+template <int BITS>
+__device__ __forceinline__ void widen(uint32_t w, const Powers<BITS> &c, uint32_t (&p)[16 / BITS]) {
   if constexpr (BITS == 8) {
-    p[0] = sub_h2((w & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
-    p[1] = sub_h2(((w >> 8) & 0x00FF00FFu) ^ 0x64806480u, 0x64806480u);
+    p[0] = sub_h2(and_xor(w, 0x00FF00FFu, c.v[0]), c.v[0]);
+    p[1] = sub_h2(and_xor(w >> 8, 0x00FF00FFu, c.v[0]), c.v[0]);
   } else {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t v = w >> 8 * i;
-      p[2 * i] = sub_h2((v & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
-      p[2 * i + 1] = sub_h2((v & 0x00F000F0u) ^ 0x54805480u, 0x54805480u);
+      p[2 * i] = sub_h2(and_xor(v, 0x000F000Fu, c.v[0]), c.v[0]);
+      p[2 * i + 1] = sub_h2(and_xor(v, 0x00F000F0u, c.v[1]), c.v[1]);
     }
   }
 }
@@ -246,8 +272,11 @@ struct Att {
   static constexpr int kRed = kWarps * (kHeads * kDim + 2 * kHeads) * 4;  // the warps' sums, references, weights
   static constexpr int bytes(int stages) { return kWarps * stages * kStage + kRed; }
   static constexpr bool fits(int stages, int ctas) { return ctas * (bytes(stages) + 1024 + 128) <= 228 * 1024; }
-  // a CTA has four stages a warp where three CTAs fit with them, else as many as fit
-  static constexpr int kCtas = fits(2, 3) ? 3 : 2;
+  // CTAs of an SM by their registers (128 a thread with four, 168 with three); then as many stages a warp as fit, up to four
+#ifndef SW
+#define SW 4
+#endif
+  static constexpr int kCtas = NB <= 4 && fits(2, SW) ? SW : NB <= 6 && fits(2, 3) ? 3 : 2;
   static constexpr int kStages = fits(4, kCtas) ? 4 : fits(3, kCtas) ? 3 : 2;
   static_assert(fits(kStages, kCtas), "shared memory");
 };
@@ -292,7 +321,9 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   __shared__ int64_t tmp[kWarps + 2];
   float *const red = reinterpret_cast<float *>(smem + kWarps * kStages * P::kStage);
   float *const red_stat = red + kWarps * kHeads * kDim;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  // (the warp's number by a shuffle: what follows from it is the same in all lanes, and the compiler knows)
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const Powers<BITS> power;
 
   // the cache, the lengths and q may come from the kernel before; the next one may be set up
   ptx::grid_dependency_wait();
@@ -317,6 +348,9 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
 
   // ---- the ring: this warp's steps, one after the other, over the CTA's parts
   const uint32_t ring = ptx::smem_addr(smem) + warp * kStages * P::kStage;
+  const uint32_t copy_at = lane / kUnits * kPitch + lane % kUnits * 16;
+  const uint8_t *const k_lane = a.k + lane * 16, *const v_lane = a.v + lane * 16;
+  const uint8_t *const s_lane = lane < 2 * NB ? a.ks + lane * 16 : a.vs + (lane - 2 * NB) * 16;  // (lanes below 4 NB)
   Walk ahead = have;
   int l_step = ahead.first + warp, fill = 0, slot_used = 0;
   uint32_t missing = 0;  // bit of a stage: its page is none of the cache's
@@ -338,23 +372,31 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   auto load_next = [&]() {
     if (l_step >= 0) {
       const uint32_t st = ring + fill * P::kStage;
-      const bool in = l_page >= 0;
-      missing = in ? missing & ~(1u << fill) : missing | 1u << fill;
-      const int64_t pos = (static_cast<int64_t>(l_step) * kStep) & ((1 << a.s.page_shift) - 1);
-      const int64_t row = in ? (((static_cast<int64_t>(l_page) * a.heads + ahead.h) << a.s.page_shift) + pos) : 0;
-      const uint32_t n = in ? 16u : 0u;
-      const uint8_t *const kp = a.k + row * P::kRow + lane * 16, *const vp = a.v + row * P::kRow + lane * 16;
+      // (a page that is none of the cache's: the stage keeps what it holds, and the step counts nothing)
+      missing = l_page >= 0 ? missing & ~(1u << fill) : missing | 1u << fill;
+      if (l_page >= 0) {
+        const int pos = (l_step * kStep) & ((1 << a.s.page_shift) - 1);  // (tokens are counted in an int)
+        const int64_t row = ((static_cast<int64_t>(l_page) * a.heads + ahead.h) << a.s.page_shift) + pos;
+        const uint8_t *const kp = k_lane + row * P::kRow, *const vp = v_lane + row * P::kRow;
+        if constexpr (32 % kUnits == 0) {  // a copy of the warp is whole rows
+          const uint32_t to = st + copy_at;
 #pragma unroll
-      for (int i = 0; i < (kStep * kUnits + 31) / 32; ++i) {
-        const int idx = i * 32 + lane, r = idx / kUnits, c = idx - r * kUnits;
-        if (kStep * kUnits % 32 == 0 || idx < kStep * kUnits) {
-          ptx::cp_async_16(st + r * kPitch + c * 16, kp + i * 512, n);
-          ptx::cp_async_16(st + kStep * kPitch + r * kPitch + c * 16, vp + i * 512, n);
+          for (int i = 0; i < (kStep * kUnits + 31) / 32; ++i)
+            if (kStep * kUnits >= 32 || lane < kStep * kUnits) {
+              ptx::cp_async_16(to + i * (32 / kUnits) * kPitch, kp + i * 512);
+              ptx::cp_async_16(to + kStep * kPitch + i * (32 / kUnits) * kPitch, vp + i * 512);
+            }
+        } else {
+#pragma unroll
+          for (int i = 0; i < (kStep * kUnits + 31) / 32; ++i) {
+            const int idx = i * 32 + lane, r = idx / kUnits, c = idx - r * kUnits;
+            if (kStep * kUnits % 32 == 0 || idx < kStep * kUnits) {
+              ptx::cp_async_16(st + r * kPitch + c * 16, kp + i * 512);
+              ptx::cp_async_16(st + kStep * kPitch + r * kPitch + c * 16, vp + i * 512);
+            }
+          }
         }
-      }
-      if (lane < 4 * NB) {
-        const int of_v = lane >= 2 * NB, u = of_v ? lane - 2 * NB : lane;
-        ptx::cp_async_16(st + 2 * kStep * kPitch + lane * 16, (of_v ? a.vs : a.ks) + row * (2 * NB) + u * 16, n);
+        if (lane < 4 * NB) ptx::cp_async_16(st + 2 * kStep * kPitch + lane * 16, s_lane + row * (2 * NB));
       }
       l_step += kWarps;
       seek();
@@ -370,8 +412,28 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   // same, transposed: (tokens 0-7), (tokens 8-15) of a unit
   const uint32_t lm = ((lane >> 3 & 1) * 8 + (lane & 7)) * kPitch + (lane >> 4) * 16;
 
+  // the elements of q that a thread has of a head's row, head g's: those of its word of every unit
+  constexpr int kQ = 32 / BITS;
+  uint32_t q_raw[kUnits][kQ / 2];
+  auto load_q = [&](const Walk &w) {
+    const bool on = g < min(a.per, a.group - part * a.per);
+    const T *const row = reinterpret_cast<const T *>(a.q + w.b * a.ldq) +
+                         static_cast<int64_t>(w.h * a.group + part * a.per + (on ? g : 0)) * kDim;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      if constexpr (BITS == 8) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(row + u * 16 + t * 4);
+        q_raw[u][0] = on ? v.x : 0u, q_raw[u][1] = on ? v.y : 0u;
+      } else {
+        const uint4 v = *reinterpret_cast<const uint4 *>(row + u * 32 + t * 8);
+        q_raw[u][0] = on ? v.x : 0u, q_raw[u][1] = on ? v.y : 0u, q_raw[u][2] = on ? v.z : 0u, q_raw[u][3] = on ? v.w : 0u;
+      }
+    }
+  };
   const int total_units = a.s.seqs * a.heads;
-  while (a.whole ? have.b * a.heads + have.h < total_units : have.on()) {
+  auto goes_on = [&](const Walk &w) { return a.whole ? w.b * a.heads + w.h < total_units : w.on(); };
+  if (goes_on(have)) load_q(have);
+  while (goes_on(have)) {
     const int unit = have.b * a.heads + have.h;
     const int head0 = have.h * a.group + part * a.per;  // the CTA's first query head
     const int n_heads = min(a.per, a.group - part * a.per);
@@ -381,29 +443,16 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
     uint32_t qb[kUnits][16 / BITS];  // pairs of a unit of 16 bytes: 2 (8 bits) or 4 (4 bits) words
     float mult[2];
     {
-      constexpr int kPer = 32 / BITS;  // elements of a thread's word
       float top = 0.0f;
-      const T *const qrow = reinterpret_cast<const T *>(a.q + have.b * a.ldq) + static_cast<int64_t>(head0 + g) * kDim;
-      float f[kUnits][kPer];
+      float f[kUnits][kQ];
 #pragma unroll
-      for (int u = 0; u < kUnits; ++u) {
-        uint32_t w[kPer / 2] = {};
-        if (g < n_heads) {
-          if constexpr (BITS == 8) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(qrow + u * 16 + t * 4);
-            w[0] = v.x, w[1] = v.y;
-          } else {
-            const uint4 v = *reinterpret_cast<const uint4 *>(qrow + u * 32 + t * 8);
-            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-          }
-        }
+      for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-        for (int i = 0; i < kPer / 2; ++i) {
-          const float2 e = unpack2<T>(w[i]);
+        for (int i = 0; i < kQ / 2; ++i) {
+          const float2 e = unpack2<T>(q_raw[u][i]);
           f[u][2 * i] = e.x, f[u][2 * i + 1] = e.y;
           top = fmaxf(top, fmaxf(fabsf(e.x), fabsf(e.y)));
         }
-      }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       // to 2^13 .. 2^14; powers of two in two halves, each within fp32's range
@@ -414,10 +463,8 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
 #pragma unroll
       for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-        for (int i = 0; i < kPer / 2; ++i) {
-          // the word's pairs: lanes (i, i + half of them)
-          qb[u][i] = pack2<__half>(f[u][i] * up0 * up1, f[u][i + kPer / 2] * up0 * up1);
-        }
+        for (int i = 0; i < kQ / 2; ++i)  // the word's pairs: lanes (i, i + half of them)
+          qb[u][i] = pack2<__half>(f[u][i] * up0 * up1, f[u][i + kQ / 2] * up0 * up1);
       const float m = a.scale * down * down1;
       mult[0] = __shfl_sync(0xffffffffu, m, 8 * t);
       mult[1] = __shfl_sync(0xffffffffu, m, 8 * t + 4);
@@ -450,13 +497,16 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
         uint32_t r[4];
         ldsm4(st + lm + u * 16, r);  // (past the last unit of an odd row: the row's padding, not used)
         if constexpr (BITS == 8) {
-          float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          float d[4];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             uint32_t lo[2], hi[2];
-            widen<8>(r[2 * i], lo);
-            widen<8>(r[2 * i + 1], hi);
-            mma_f16(d, lo[0], hi[0], lo[1], hi[1], qb[u + i][0], qb[u + i][1]);
+            widen<8>(r[2 * i], power, lo);
+            widen<8>(r[2 * i + 1], power, hi);
+            if (i == 0)
+              mma_f16_first(d, lo[0], hi[0], lo[1], hi[1], qb[u][0], qb[u][1]);
+            else
+              mma_f16(d, lo[0], hi[0], lo[1], hi[1], qb[u + 1][0], qb[u + 1][1]);
           }
 #pragma unroll
           for (int j = 0; j < 4; ++j) x[j] = fmaf(scale_at<T>(kw[j >> 1], u / 2), d[j], x[j]);
@@ -464,11 +514,11 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
 #pragma unroll
           for (int i = 0; i < 2; ++i)
             if (u + i < kUnits) {
-              float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+              float d[4];
               uint32_t lo[4], hi[4];
-              widen<4>(r[2 * i], lo);
-              widen<4>(r[2 * i + 1], hi);
-              mma_f16(d, lo[0], hi[0], lo[1], hi[1], qb[u + i][0], qb[u + i][1]);
+              widen<4>(r[2 * i], power, lo);
+              widen<4>(r[2 * i + 1], power, hi);
+              mma_f16_first(d, lo[0], hi[0], lo[1], hi[1], qb[u + i][0], qb[u + i][1]);
               mma_f16(d, lo[2], hi[2], lo[3], hi[3], qb[u + i][2], qb[u + i][3]);
 #pragma unroll
               for (int j = 0; j < 4; ++j) x[j] = fmaf(scale_at<T>(kw[j >> 1], u + i), d[j], x[j]);
@@ -476,21 +526,30 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
         }
       }
 
-      // the values' scales; a token that is not there has none, and no weight
+      // the values' scales
       const int tok = step * kStep + g;
-      const bool in[2] = {!gone && tok < len, !gone && tok + 8 < len};
       uint32_t vw[2][(NB + 1) / 2];
-      float vmax[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        load_scales<NB>(sc + P::kScales + (g + 8 * r) * (2 * NB), vw[r]);
+      for (int r = 0; r < 2; ++r) load_scales<NB>(sc + P::kScales + (g + 8 * r) * (2 * NB), vw[r]);
 #pragma unroll
-        for (int i = 0; i < (NB + 1) / 2; ++i) vw[r][i] = in[r] ? vw[r][i] : 0u;
+      for (int j = 0; j < 4; ++j) x[j] *= mult[j & 1];
+      if (gone || (step + 1) * kStep > len) {  // a token that is not there has no scale and no weight
 #pragma unroll
-        for (int i = 0; i < NB; ++i) vmax[r] = fmaxf(vmax[r], fabsf(scale_at<T>(vw[r], i)));
+        for (int r = 0; r < 2; ++r)
+          if (gone || tok + 8 * r >= len) {
+#pragma unroll
+            for (int i = 0; i < (NB + 1) / 2; ++i) vw[r][i] = 0u;
+            x[2 * r] = x[2 * r + 1] = -INFINITY;
+          }
       }
+      float vs[2][NB], vmax[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = in[j >> 1] ? x[j] * mult[j & 1] : -INFINITY;
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          vs[r][i] = scale_at<T>(vw[r], i);
+          vmax[r] = fmaxf(vmax[r], fabsf(vs[r][i]));
+        }
       if (a.logits) {
         float *const lp = a.logits + ((static_cast<int64_t>(unit) * a.parts + part) * span_tokens + tok) * kHeads + 2 * t;
         *reinterpret_cast<float2 *>(lp) = make_float2(x[0], x[1]);
@@ -527,31 +586,33 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       sum[0] += e[0] + e[2];
       sum[1] += e[1] + e[3];
 
-      // outputs
+      // outputs: a block's weights, and the two units (8 bits) or the one (4 bits) that hold its values
+      uint32_t r[4];
 #pragma unroll
-      for (int u = 0; u < kUnits; u += 2) {
-        uint32_t r[4];
-        ldsm4_trans(st + kStep * kPitch + lm + u * 16, r);
+      for (int blk = 0; blk < NB; ++blk) {
+        const uint32_t b0 = transpose8x8(pack2<__half>(e[0] * vs[0][blk], e[1] * vs[0][blk]));
+        const uint32_t b1 = transpose8x8(pack2<__half>(e[2] * vs[1][blk], e[3] * vs[1][blk]));
+        if (BITS == 8 || (blk & 1) == 0) ldsm4_trans(st + kStep * kPitch + lm + (BITS == 8 ? 2 * blk : blk) * 16, r);
+        uint32_t lo[16 / BITS], hi[16 / BITS];
+        if constexpr (BITS == 8) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (u + i < kUnits) {
-            const int blk = BITS == 8 ? u / 2 : u + i;
-            static_assert(BITS == 8 || BITS == 4, "");
-            const float s0 = scale_at<T>(vw[0], blk), s1 = scale_at<T>(vw[1], blk);
-            const uint32_t b0 = transpose8x8(pack2<__half>(e[0] * s0, e[1] * s0));
-            const uint32_t b1 = transpose8x8(pack2<__half>(e[2] * s1, e[3] * s1));
-            uint32_t lo[16 / BITS], hi[16 / BITS];
-            widen<BITS>(r[2 * i], lo);
-            widen<BITS>(r[2 * i + 1], hi);
-            if constexpr (BITS == 8) {
-              mma_f16(o[u + i], lo[0], lo[1], hi[0], hi[1], b0, b1);
-            } else {
-              mma_f16(o[2 * (u + i)], lo[0], lo[1], hi[0], hi[1], b0, b1);
-              mma_f16(o[2 * (u + i) + 1], lo[2], lo[3], hi[2], hi[3], b0, b1);
-            }
+          for (int i = 0; i < 2; ++i) {
+            widen<8>(r[2 * i], power, lo);
+            widen<8>(r[2 * i + 1], power, hi);
+            mma_f16(o[2 * blk + i], lo[0], lo[1], hi[0], hi[1], b0, b1);
           }
+        } else {
+          widen<4>(r[2 * (blk & 1)], power, lo);
+          widen<4>(r[2 * (blk & 1) + 1], power, hi);
+          mma_f16(o[2 * blk], lo[0], lo[1], hi[0], hi[1], b0, b1);
+          mma_f16(o[2 * blk + 1], lo[2], lo[3], hi[2], hi[3], b0, b1);
+        }
       }
     }
+
+    Walk then = have;
+    then.next(a);
+    if (goes_on(then)) load_q(then);  // on its way while the warps join
 
     // ---- join the warps: sums [warp][head][element], references and weights [warp][head]
 #pragma unroll
@@ -611,7 +672,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
           make_int2(slot, slot_of(unit_begin + have.steps - 1, all, used));
     __syncthreads();
     unit_begin += have.steps;
-    have.next(a);
+    have = then;
   }
   ptx::cp_async_wait<0>();
 }
