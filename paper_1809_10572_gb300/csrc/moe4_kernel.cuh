@@ -65,11 +65,13 @@ struct Lists {
   uint16_t order[kMaxPairs];   // pairs, expert by expert, rising within one
   uint16_t expert[kMaxPairs];  // of a pass
   uint16_t first[kMaxPairs + 1];  // of a pass in `order`
+  float weight[kMaxPairs];     // of the pairs in `order`
   int passes;
 };
 
 // By one warp. count: E words. Pairs whose expert is none are in no list.
-__device__ __forceinline__ void make_lists(const int32_t *ids, int pairs, int E, Lists *l, int *count, uint16_t *place, int lane) {
+__device__ __forceinline__ void make_lists(const int32_t *ids, const float *weights, int pairs, int E, Lists *l, int *count,
+                                           uint16_t *place, int lane) {
   for (int e = lane; e < E; e += 32) count[e] = 0;
   __syncwarp();
   for (int p0 = 0; p0 < pairs; p0 += 32) {
@@ -108,7 +110,10 @@ __device__ __forceinline__ void make_lists(const int32_t *ids, int pairs, int E,
   __syncwarp();
   for (int p = lane; p < pairs; p += 32) {
     const int e = ids[p];
-    if (e >= 0 && e < E) l->order[count[e] + place[p]] = static_cast<uint16_t>(p);
+    if (e >= 0 && e < E) {
+      l->order[count[e] + place[p]] = static_cast<uint16_t>(p);
+      l->weight[count[e] + place[p]] = weights[p];
+    }
   }
 }
 
@@ -186,7 +191,8 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
   ptx::grid_dependency_wait();
   ptx::grid_dependents_launch();
   if (warp == 0)  // (the ring is not in use yet)
-    make_lists(a.ids, a.M * a.topk, a.E, &lists, reinterpret_cast<int *>(smem), reinterpret_cast<uint16_t *>(smem + kMaxExperts * 4), lane);
+    make_lists(a.ids, a.weights, a.M * a.topk, a.E, &lists, reinterpret_cast<int *>(smem),
+               reinterpret_cast<uint16_t *>(smem + kMaxExperts * 4), lane);
   if constexpr (!kGated)
     for (int i = tid; i < kWarps * kRows * (a.M | 1); i += kThreads) red[i] = 0.0f;
   __syncthreads();
@@ -418,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
   };
 
   if constexpr (kGated) {
-    int buf = 0;
+    int buf = 0, turn = 0;
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
       const int pass = item / a.tiles, n0 = (item - pass * a.tiles) * kOut;
       if (have.pass < passes && have.item == item)
@@ -436,15 +442,16 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
         }
       __syncthreads();
       // (the other buffer is written next, and this one only behind another barrier)
-      if (tid < kOut * n) {
-        const int r = tid % kOut, c = tid / kOut, pair = lists.order[first + c], row = (r >> 3) * 16 + (r & 7);
+      const int mine = (tid + 32 * turn++) % kThreads;  // warps in turn
+      if (mine < kOut * n) {
+        const int r = mine % kOut, c = mine / kOut, pair = lists.order[first + c], row = (r >> 3) * 16 + (r & 7);
         float gate = 0.0f, up = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
           gate += rb[(w * kRows + row) * P::kRedPitch + c];
           up += rb[(w * kRows + row + 8) * P::kRedPitch + c];
         }
-        reinterpret_cast<T *>(a.y + pair * a.ldy)[n0 + r] = from_f32<T>(a.weights[pair] * (act_of(a.act, gate) * up));
+        reinterpret_cast<T *>(a.y + pair * a.ldy)[n0 + r] = from_f32<T>(lists.weight[first + c] * (act_of(a.act, gate) * up));
       }
     }
   } else {

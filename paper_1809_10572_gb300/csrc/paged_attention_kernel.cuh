@@ -266,19 +266,27 @@ struct Att {
   static constexpr int kDim = 32 * NB;
   static constexpr int kRow = 4 * NB * BITS;        // bytes of a row of lanes
   static constexpr int kUnits = kRow / 16;
-  static constexpr int kPitch = 16 * (kUnits | 1);  // of a row in a stage
+  // Rows in a stage: a power of two of units, swizzled (unit u of row r at u ^ (r >> kShift)), or an odd number of them.
+  static constexpr bool kSwizzled = (kUnits & (kUnits - 1)) == 0;
+  static constexpr int kShift = kUnits >= 8 ? 0 : kUnits == 4 ? 1 : 2;
+  static constexpr int kMask = kUnits >= 8 ? 7 : kUnits - 1;
+  static constexpr int kPitch = 16 * (kSwizzled ? kUnits : kUnits | 1);
   static constexpr int kScales = kStep * NB * 2;    // bytes of a step's scales, of keys or values
-  static constexpr int kStage = 2 * kStep * kPitch + 2 * kScales;
-  static constexpr int kRed = kWarps * (kHeads * kDim + 2 * kHeads) * 4;  // the warps' sums, references, weights
-  static constexpr int bytes(int stages) { return kWarps * stages * kStage + kRed; }
-  static constexpr bool fits(int stages, int ctas) { return ctas * (bytes(stages) + 1024 + 128) <= 228 * 1024; }
+  // (whole swizzle patterns: a unit's place in a stage is an exclusive or of its address)
+  static constexpr int kStage = (2 * kStep * kPitch + 2 * kScales + 255) / 256 * 256;
+  // The warps' sums when they are joined, [head][element]: in the stage that each of them fills next, where that holds them
+  static constexpr int kSums = kHeads * kDim * 4;
+  static constexpr bool kInStage = kStage >= kSums;
+  static constexpr int bytes(int stages) { return kWarps * (stages * kStage + (kInStage ? 0 : kSums)); }
+  static constexpr bool fits(int stages, int ctas) { return ctas * (bytes(stages) + 1024 + 512) <= 228 * 1024; }
   // CTAs of an SM by their registers (128 a thread with four, 168 with three); then as many stages a warp as fit, up to four
-#ifndef SW
-#define SW 4
-#endif
-  static constexpr int kCtas = NB <= 4 && fits(2, SW) ? SW : NB <= 6 && fits(2, 3) ? 3 : 2;
+  static constexpr int kCtas = NB <= 4 && fits(2, 4) ? 4 : NB <= 6 && fits(2, 3) ? 3 : 2;
   static constexpr int kStages = fits(4, kCtas) ? 4 : fits(3, kCtas) ? 3 : 2;
   static_assert(fits(kStages, kCtas), "shared memory");
+  // where unit u of row r of a stage begins
+  static __device__ __forceinline__ int at(int r, int u) {
+    return r * kPitch + (kSwizzled ? u ^ ((r >> kShift) & kMask) : u) * 16;
+  }
 };
 
 // The scales of a row, two in a word, from shared memory.
@@ -317,10 +325,10 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   constexpr int kDim = P::kDim, kUnits = P::kUnits, kPitch = P::kPitch, kStages = P::kStages;
   constexpr int kTiles = kDim / 16;  // of 16 elements
   constexpr float kLow = -3e38f;     // a reference before any token
-  extern __shared__ __align__(128) uint8_t smem[];
+  extern __shared__ __align__(256) uint8_t smem[];
   __shared__ int64_t tmp[kWarps + 2];
-  float *const red = reinterpret_cast<float *>(smem + kWarps * kStages * P::kStage);
-  float *const red_stat = red + kWarps * kHeads * kDim;
+  __shared__ float2 red_stat[kWarps][kHeads];  // references and sums of weights
+  __shared__ float *red_at[kWarps];            // the warps' sums
   // (the warp's number by a shuffle: what follows from it is the same in all lanes, and the compiler knows)
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t = lane & 3;
   const Powers<BITS> power;
@@ -348,7 +356,10 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
 
   // ---- the ring: this warp's steps, one after the other, over the CTA's parts
   const uint32_t ring = ptx::smem_addr(smem) + warp * kStages * P::kStage;
-  const uint32_t copy_at = lane / kUnits * kPitch + lane % kUnits * 16;
+  constexpr int kCopies = (kStep * kUnits + 31) / 32;
+  uint32_t copy_at[kCopies];  // where the lane's units of a step's rows go in a stage
+#pragma unroll
+  for (int i = 0; i < kCopies; ++i) copy_at[i] = P::at((i * 32 + lane) / kUnits, (i * 32 + lane) % kUnits);
   const uint8_t *const k_lane = a.k + lane * 16, *const v_lane = a.v + lane * 16;
   const uint8_t *const s_lane = lane < 2 * NB ? a.ks + lane * 16 : a.vs + (lane - 2 * NB) * 16;  // (lanes below 4 NB)
   Walk ahead = have;
@@ -378,24 +389,12 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
         const int pos = (l_step * kStep) & ((1 << a.s.page_shift) - 1);  // (tokens are counted in an int)
         const int64_t row = ((static_cast<int64_t>(l_page) * a.heads + ahead.h) << a.s.page_shift) + pos;
         const uint8_t *const kp = k_lane + row * P::kRow, *const vp = v_lane + row * P::kRow;
-        if constexpr (32 % kUnits == 0) {  // a copy of the warp is whole rows
-          const uint32_t to = st + copy_at;
 #pragma unroll
-          for (int i = 0; i < (kStep * kUnits + 31) / 32; ++i)
-            if (kStep * kUnits >= 32 || lane < kStep * kUnits) {
-              ptx::cp_async_16(to + i * (32 / kUnits) * kPitch, kp + i * 512);
-              ptx::cp_async_16(to + kStep * kPitch + i * (32 / kUnits) * kPitch, vp + i * 512);
-            }
-        } else {
-#pragma unroll
-          for (int i = 0; i < (kStep * kUnits + 31) / 32; ++i) {
-            const int idx = i * 32 + lane, r = idx / kUnits, c = idx - r * kUnits;
-            if (kStep * kUnits % 32 == 0 || idx < kStep * kUnits) {
-              ptx::cp_async_16(st + r * kPitch + c * 16, kp + i * 512);
-              ptx::cp_async_16(st + kStep * kPitch + r * kPitch + c * 16, vp + i * 512);
-            }
+        for (int i = 0; i < kCopies; ++i)
+          if (kStep * kUnits % 32 == 0 || i * 32 + lane < kStep * kUnits) {
+            ptx::cp_async_16(st + copy_at[i], kp + i * 512);
+            ptx::cp_async_16(st + copy_at[i] + kStep * kPitch, vp + i * 512);
           }
-        }
         if (lane < 4 * NB) ptx::cp_async_16(st + 2 * kStep * kPitch + lane * 16, s_lane + row * (2 * NB));
       }
       l_step += kWarps;
@@ -410,7 +409,11 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
 
   // ldmatrix: keys: matrices (rows 0-7, unit c), (rows 8-15, c), (rows 0-7, c + 1), (rows 8-15, c + 1); values the
   // same, transposed: (tokens 0-7), (tokens 8-15) of a unit
-  const uint32_t lm = ((lane >> 3 & 1) * 8 + (lane & 7)) * kPitch + (lane >> 4) * 16;
+  const uint32_t lm = P::at((lane >> 3 & 1) * 8 + (lane & 7), kUnits > 1 ? lane >> 4 : 0);
+  // units 2 i and 2 i + 1 of the rows of keys (0) or values (1) of a stage
+  auto pair_at = [&](uint32_t st, int v, int i) {
+    return P::kSwizzled ? (st + v * kStep * kPitch + lm) ^ (i * 32) : st + v * kStep * kPitch + lm + i * 32;
+  };
 
   // the elements of q that a thread has of a head's row, head g's: those of its word of every unit
   constexpr int kQ = 32 / BITS;
@@ -495,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
 #pragma unroll
       for (int u = 0; u < kUnits; u += 2) {
         uint32_t r[4];
-        ldsm4(st + lm + u * 16, r);  // (past the last unit of an odd row: the row's padding, not used)
+        ldsm4(pair_at(st, 0, u / 2), r);  // (one unit, or past the last of an odd number: the second half is not used)
         if constexpr (BITS == 8) {
           float d[4];
 #pragma unroll
@@ -592,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       for (int blk = 0; blk < NB; ++blk) {
         const uint32_t b0 = transpose8x8(pack2<__half>(e[0] * vs[0][blk], e[1] * vs[0][blk]));
         const uint32_t b1 = transpose8x8(pack2<__half>(e[2] * vs[1][blk], e[3] * vs[1][blk]));
-        if (BITS == 8 || (blk & 1) == 0) ldsm4_trans(st + kStep * kPitch + lm + (BITS == 8 ? 2 * blk : blk) * 16, r);
+        if (BITS == 8 || (blk & 1) == 0) ldsm4_trans(pair_at(st, 1, BITS == 8 ? blk : blk / 2), r);
         uint32_t lo[16 / BITS], hi[16 / BITS];
         if constexpr (BITS == 8) {
 #pragma unroll
@@ -623,18 +626,20 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
     }
     if (g == 0) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        red_stat[(warp * kHeads + 2 * t + c) * 2] = ref[c];
-        red_stat[(warp * kHeads + 2 * t + c) * 2 + 1] = sum[c];
-      }
+      for (int c = 0; c < 2; ++c) red_stat[warp][2 * t + c] = make_float2(ref[c], sum[c]);
     }
+    // (the stage filled next holds nothing that is still wanted)
+    float *const red = reinterpret_cast<float *>(P::kInStage ? smem + (warp * kStages + fill) * P::kStage
+                                                             : smem + kWarps * kStages * P::kStage + warp * P::kSums);
+    if (lane == 0) red_at[warp] = red;
+    __syncwarp();  // every lane has read the last stage
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         // row g (and g + 8) of tile i is this element
         const int d = BITS == 8 ? 16 * i + 2 * g + (j >> 1) : 32 * (i / 2) + 4 * g + 2 * (i & 1) + (j >> 1);
-        red[(warp * kHeads + 2 * t + (j & 1)) * kDim + d] = o[i][j];
+        red[(2 * t + (j & 1)) * kDim + d] = o[i][j];
       }
     __syncthreads();
     const bool first_part = have.first == 0, last_part = have.last == have.steps;
@@ -642,16 +647,16 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       const int h = idx / (kDim / 2), d = (idx - h * (kDim / 2)) * 2;
       float top = kLow;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, red_stat[(w * kHeads + h) * 2]);
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, red_stat[w][h].x);
       float2 v = make_float2(0.0f, 0.0f);
       float weight = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float f = exp2_of(red_stat[(w * kHeads + h) * 2] - top);
-        const float2 p = *reinterpret_cast<const float2 *>(red + (w * kHeads + h) * kDim + d);
+        const float f = exp2_of(red_stat[w][h].x - top);
+        const float2 p = *reinterpret_cast<const float2 *>(red_at[w] + h * kDim + d);
         v.x = fmaf(f, p.x, v.x);
         v.y = fmaf(f, p.y, v.y);
-        weight = fmaf(f, red_stat[(w * kHeads + h) * 2 + 1], weight);
+        weight = fmaf(f, red_stat[w][h].y, weight);
       }
       if (d == 0 && a.head_stat) {
         float2 *const to = first_part ? a.head_stat + (static_cast<int64_t>(unit) * a.parts + part) * kHeads

@@ -14,7 +14,9 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -816,6 +818,20 @@ def gated_ffn_backward(dh, ckpt_x: Block8, ckpt_g: Block8, ckpt_u: Block8, wg, w
 
 
 # ---- the packed key-value cache ----------------------------------------------------
+#
+# A decoder makes these calls for every layer and token, and the smallest ones take less time on the GPU than their checks
+# here: a call first asks whether all is as it has to be, and only then what is not.
+
+
+def _address(t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        raise ValueError("libsamd takes device tensors")
+    return t.data_ptr()
+
+
+# samd_cache and samd_cache_seqs, laid out as C lays them out: half the time of a structure's constructor
+_CACHE_BYTES = struct.Struct("@4i4BiQQQQ").pack
+_SEQS_BYTES = struct.Struct("@iiqQQ").pack
 
 
 class PagedCache:
@@ -823,40 +839,29 @@ class PagedCache:
     int32, the rows as samd_pack writes them in the format cache_fmt(bits); k_scales and v_scales (pages, heads, page,
     dim // 32) float16 or bfloat16. The lane width follows from the shapes."""
 
-    __slots__ = ("k_lanes", "k_scales", "v_lanes", "v_scales", "bits", "dim", "_desc")
+    __slots__ = ("k_lanes", "k_scales", "v_lanes", "v_scales", "bits", "dim", "heads", "page", "dtype", "_desc")
 
     def __init__(self, k_lanes, k_scales, v_lanes, v_scales):
-        rows, words, blocks = k_lanes.shape[:-1], k_lanes.shape[-1], k_scales.shape[-1]
-        if len(rows) != 3 or blocks < 1 or words not in (4 * blocks, 8 * blocks):
-            raise ValueError(f"lanes (pages, heads, page, words) and scales (pages, heads, page, dim // 32) of 4 or 8 bits "
-                             f"are wanted, got {tuple(k_lanes.shape)} and {tuple(k_scales.shape)}")
-        t = k_scales.dtype
-        if t is not torch.float16 and t is not torch.bfloat16:
-            raise ValueError(f"scales: {t}, wanted float16 or bfloat16")
-        for lanes, scales in ((k_lanes, k_scales), (v_lanes, v_scales)):
-            if lanes.dtype is not torch.int32 or lanes.shape != (*rows, words) or not lanes.is_contiguous():
-                raise ValueError(f"lanes: a contiguous {(*rows, words)} int32 tensor is wanted")
-            if scales.dtype is not t or scales.shape != (*rows, blocks) or not scales.is_contiguous():
-                raise ValueError(f"scales: a contiguous {(*rows, blocks)} {t} tensor is wanted")
-        if max(rows) >> 31:
-            _past_int(*rows)
+        lanes, scales, t = k_lanes.shape, k_scales.shape, k_scales.dtype
+        if (len(lanes) != 4 or lanes[:3] != scales[:-1] or v_lanes.shape != lanes or v_scales.shape != scales or
+                (t is not torch.bfloat16 and t is not torch.float16) or v_scales.dtype is not t or
+                k_lanes.dtype is not torch.int32 or v_lanes.dtype is not torch.int32 or not k_lanes.is_contiguous() or
+                not k_scales.is_contiguous() or not v_lanes.is_contiguous() or not v_scales.is_contiguous()):
+            raise ValueError(f"contiguous int32 lanes (pages, heads, page, words) and float16 or bfloat16 scales (pages, heads, "
+                             f"page, dim // 32) are wanted, the same for keys and values, got {tuple(lanes)}, {tuple(scales)}, "
+                             f"{tuple(v_lanes.shape)}, {tuple(v_scales.shape)} of {t}")
+        pages, heads, page, words = lanes
+        blocks = scales[3]
+        bits = words // blocks if blocks else 0
+        if bits not in (4, 8) or bits * blocks != words:
+            raise ValueError(f"rows of {words} words with {blocks} scales: 4 or 8 of them for a scale are wanted")
+        if (pages | heads | page) >> 31:
+            _past_int(pages, heads, page)
         self.k_lanes, self.k_scales, self.v_lanes, self.v_scales = k_lanes, k_scales, v_lanes, v_scales
-        self.bits, self.dim = words // blocks, 32 * blocks
-        pages, heads, page = rows
-        self._desc = samd_cache(pages, page, heads, self.dim, cache_fmt(self.bits), DTYPES[t], _ptr(k_lanes), _ptr(k_scales),
-                                _ptr(v_lanes), _ptr(v_scales))
-
-    @property
-    def heads(self) -> int:
-        return self._desc.heads
-
-    @property
-    def page(self) -> int:
-        return self._desc.page
-
-    @property
-    def dtype(self) -> torch.dtype:
-        return self.k_scales.dtype
+        self.bits, self.dim, self.heads, self.page, self.dtype = bits, 32 * blocks, heads, page, t
+        self._desc = samd_cache.from_buffer_copy(_CACHE_BYTES(
+            pages, page, heads, 32 * blocks, bits, 1, 0, 32, DTYPES[t], _address(k_lanes), _address(k_scales),
+            _address(v_lanes), _address(v_scales)))
 
 
 def cache_fmt(bits: int) -> samd_fmt:
@@ -887,18 +892,19 @@ def _cache_seqs(table, lengths) -> samd_cache_seqs:
         raise ValueError(f"lengths: a contiguous ({seqs},) tensor is wanted, got {tuple(lengths.shape)}")
     if (seqs | width) >> 31:
         _past_int(seqs, width)
-    return samd_cache_seqs(seqs, width, ld, _ptr(table), _ptr(lengths))
+    return samd_cache_seqs.from_buffer_copy(_SEQS_BYTES(seqs, width, ld, _address(table), _address(lengths)))
 
 
 def _token_rows(x, what: str, heads: int, dim: int, dtype, tokens: int | None = None) -> int:
     """Checks a (tokens, heads, dim) tensor whose tokens lie whole in memory, and returns the stride of a token."""
     shape = x.shape
+    if (x.dtype is dtype and len(shape) == 3 and shape[1] == heads and shape[2] == dim and
+            (tokens is None or shape[0] == tokens) and x.is_contiguous()):
+        return heads * dim
     if len(shape) != 3 or shape[1] != heads or shape[2] != dim or (tokens is not None and shape[0] != tokens):
         raise ValueError(f"{what}: shape {tuple(shape)}, wanted ({tokens if tokens is not None else 'any'}, {heads}, {dim})")
     if x.dtype is not dtype:
         raise ValueError(f"{what}: {x.dtype}, wanted {dtype}")
-    if x.is_contiguous():
-        return heads * dim
     if x.stride(2) != 1 or (heads > 1 and x.stride(1) != dim):
         raise ValueError(f"{what}: the heads of a token one behind the other are wanted, got strides {x.stride()}")
     return x.stride(0) if shape[0] > 1 else heads * dim
@@ -917,12 +923,21 @@ def _scores_ld(scores, seqs: int, heads: int) -> int:
     return scores.shape[2]
 
 
+def _new(like, shape, dtype, stream) -> torch.Tensor:
+    """An uninitialised tensor beside `like`, of the stream that is going to use it."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with _on(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
 def cache_append(cache: PagedCache, k, v, table, lengths, starts=None, stream=None) -> None:
     """Writes new tokens' keys and values (tokens, heads, dim) into the cache. lengths counts them already: rows
     starts[b] .. starts[b + 1] - 1 are the last tokens of sequence b; without starts every sequence has one, row b."""
-    ldk = _token_rows(k, "k", cache.heads, cache.dim, cache.dtype)
+    heads, dim, t = cache.heads, cache.dim, cache.dtype
+    ldk = _token_rows(k, "k", heads, dim, t)
     tokens = k.shape[0]
-    ldv = _token_rows(v, "v", cache.heads, cache.dim, cache.dtype, tokens)
+    ldv = _token_rows(v, "v", heads, dim, t, tokens)
     s = _cache_seqs(table, lengths)
     if tokens >> 31:
         _past_int(tokens)
@@ -932,15 +947,28 @@ def cache_append(cache: PagedCache, k, v, table, lengths, starts=None, stream=No
 def cache_read(cache: PagedCache, tokens: int, table, lengths, starts=None, k=None, v=None, stream=None):
     """(k, v): the values (tokens, heads, dim) of the rows that cache_append with the same table, lengths and starts
     wrote, in the scales' type. Rows of no sequence are left as they are in k and v."""
+    heads, dim, t = cache.heads, cache.dim, cache.dtype
     s = _cache_seqs(table, lengths)
     if not 0 <= tokens < 1 << 31:
         _past_int(tokens)
-    with _on(stream):
-        k, v = (torch.empty((tokens, cache.heads, cache.dim), dtype=cache.dtype, device=table.device) if x is None else x
-                for x in (k, v))
-    ldk, ldv = (_token_rows(x, n, cache.heads, cache.dim, cache.dtype, tokens) for x, n in ((k, "k"), (v, "v")))
+    ldk = ldv = heads * dim
+    if k is None:
+        k = _new(cache.k_scales, (tokens, heads, dim), t, stream)
+    else:
+        ldk = _token_rows(k, "k", heads, dim, t, tokens)
+    if v is None:
+        v = _new(cache.k_scales, (tokens, heads, dim), t, stream)
+    else:
+        ldv = _token_rows(v, "v", heads, dim, t, tokens)
     samd_cache_read(cache._desc, s, _starts(starts, s.seqs), tokens, k, ldk, v, ldv, stream)
     return k, v
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_workspace(device: int, pages, page, heads, dim, bits, seqs, max_pages, q_heads, scores) -> int:
+    """Bytes of workspace by sizes alone: they are the same for every layer of a model."""
+    c = samd_cache(pages, page, heads, dim, cache_fmt(bits), SAMD_F16, None, None, None, None)
+    return samd_paged_attention_workspace_size(c, samd_cache_seqs(seqs, max_pages, max_pages, None, None), q_heads, scores)
 
 
 def paged_attention(q, cache: PagedCache, table, lengths, scale: float | None = None, scores=None, out=None,
@@ -949,24 +977,23 @@ def paged_attention(q, cache: PagedCache, table, lengths, scale: float | None = 
     query heads; scale defaults to dim ** -0.5. scores (sequences, heads, any) float32: each token's weight is added to
     it, for cache_evict."""
     s = _cache_seqs(table, lengths)
+    seqs, heads, dim = s.seqs, cache.heads, cache.dim
     q_heads = q.shape[1] if q.dim() == 3 else 0
-    ldq = _token_rows(q, "q", q_heads, cache.dim, cache.dtype, s.seqs)
-    if q_heads < 1 or q_heads % cache.heads or q_heads >> 31:
-        raise ValueError(f"q: {q_heads} heads, wanted a multiple of the cache's {cache.heads}")
-    ld_scores = 0 if scores is None else _scores_ld(scores, s.seqs, cache.heads)
-    if scale is None:
-        scale = cache.dim ** -0.5
-    with _on(stream):
-        if out is None:
-            out = torch.empty((s.seqs, q_heads, cache.dim), dtype=q.dtype, device=q.device)
-            ldo = q_heads * cache.dim
-        else:
-            ldo = _token_rows(out, "out", q_heads, cache.dim, q.dtype, s.seqs)
-        if workspace is None:
-            n = samd_paged_attention_workspace_size(cache._desc, s, q_heads, scores is not None)
-            workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    samd_paged_attention(cache._desc, s, q_heads, q, ldq, scale, out, ldo, scores if ld_scores else None, ld_scores,
-                         workspace, stream=stream)
+    ldq = _token_rows(q, "q", q_heads, dim, cache.dtype, seqs)
+    if q_heads < 1 or q_heads % heads or q_heads >> 31:
+        raise ValueError(f"q: {q_heads} heads, wanted a multiple of the cache's {heads}")
+    ld_scores = 0 if scores is None else _scores_ld(scores, seqs, heads)
+    if out is None:
+        out, ldo = _new(q, (seqs, q_heads, dim), None, stream), q_heads * dim
+    else:
+        ldo = _token_rows(out, "out", q_heads, dim, q.dtype, seqs)
+    nb = None
+    if workspace is None:
+        nb = _attention_workspace(q.get_device(), cache._desc.pages, cache.page, heads, dim, cache.bits, seqs, s.max_pages, q_heads,
+                                  ld_scores > 0)
+        workspace = _new(q, (nb,), torch.uint8, stream) if nb else None
+    samd_paged_attention(cache._desc, s, q_heads, q, ldq, dim ** -0.5 if scale is None else scale, out, ldo,
+                         scores if ld_scores else None, ld_scores, workspace, nb, stream)
     return out
 
 
@@ -976,18 +1003,18 @@ def cache_evict(cache: PagedCache, table, lengths, scores, dst_table, keep: int,
     sequences'). (kept, new lengths, new scores): the kept tokens' places (sequences, heads, keep), -1 behind the last,
     and their scores, 0 behind it; dst_table with the new lengths and scores is the cache to go on with."""
     s = _cache_seqs(table, lengths)
-    ld_scores = _scores_ld(scores, s.seqs, cache.heads)
+    seqs, heads = s.seqs, cache.heads
+    ld_scores = _scores_ld(scores, seqs, heads)
     if not 0 <= recent <= keep or keep < 1:
         raise ValueError(f"keep {keep}, recent {recent}: 0 <= recent <= keep, and a keep of 1 or more, are wanted")
     if keep >> 31:
         _past_int(keep)
-    if dst_table.dtype is not torch.int32 or dst_table.shape[0] != s.seqs or dst_table.shape[1] * cache.page < keep:
-        raise ValueError(f"dst_table: ({s.seqs}, {-(-keep // cache.page)}) int32 pages are wanted")
+    if dst_table.dtype is not torch.int32 or dst_table.shape[0] != seqs or dst_table.shape[1] * cache.page < keep:
+        raise ValueError(f"dst_table: ({seqs}, {-(-keep // cache.page)}) int32 pages are wanted")
     ld_dst = _rows(dst_table, "dst_table")
-    with _on(stream):
-        kept = torch.empty((s.seqs, cache.heads, keep), dtype=torch.int32, device=scores.device)
-        new_lengths = torch.empty(s.seqs, dtype=torch.int32, device=scores.device)
-        new_scores = torch.empty((s.seqs, cache.heads, keep), dtype=torch.float32, device=scores.device)
+    kept = _new(scores, (seqs, heads, keep), torch.int32, stream)
+    new_lengths = _new(scores, (seqs,), torch.int32, stream)
+    new_scores = _new(scores, (seqs, heads, keep), None, stream)
     samd_cache_evict(cache._desc, s, scores, ld_scores, keep, recent, dst_table, ld_dst, kept, new_lengths, new_scores, stream)
     return kept, new_lengths, new_scores
 
@@ -1010,24 +1037,36 @@ def _moe_desc(x, E: int, topk: int, F: int = 32, group: int = 32, ldy: int = 0, 
     return samd_moe_desc(M, K, F, E, topk, group, ldx, ldy or K, DTYPES[t], _act(act))
 
 
-def moe_route(x, router, topk: int, normalize: bool = True, ids=None, weights=None, stream=None):
-    """(ids, weights), (M, topk) int32 and float32: the experts with the largest logits of x (M, K) by router (E, K), the
-    largest first, and the softmax of their logits, over themselves (normalize) or over all experts."""
+def _check_router(router, x, topk: int) -> None:
     if router.dtype is not x.dtype or router.dim() != 2 or router.shape[1] != x.shape[-1] or not router.is_contiguous():
         raise ValueError(f"router: a contiguous (experts, {x.shape[-1]}) {x.dtype} tensor is wanted")
     if topk > router.shape[0]:
         raise ValueError(f"{topk} experts of {router.shape[0]} are wanted")
+
+
+def moe_route(x, router, topk: int, normalize: bool = True, ids=None, weights=None, stream=None):
+    """(ids, weights), (M, topk) int32 and float32: the experts with the largest logits of x (M, K) by router (E, K), the
+    largest first, and the softmax of their logits, over themselves (normalize) or over all experts."""
+    _check_router(router, x, topk)
     d = _moe_desc(x, router.shape[0], topk)
     for o, what, t in ((ids, "ids", torch.int32), (weights, "weights", torch.float32)):
         if o is not None and (o.dtype is not t or o.shape != (d.M, topk) or not o.is_contiguous()):
             raise ValueError(f"{what}: a contiguous ({d.M}, {topk}) {t} tensor is wanted")
-    with _on(stream):
-        if ids is None:
-            ids = torch.empty((d.M, topk), dtype=torch.int32, device=x.device)
-        if weights is None:
-            weights = torch.empty((d.M, topk), dtype=torch.float32, device=x.device)
+    if ids is None:
+        ids = _new(x, (d.M, topk), torch.int32, stream)
+    if weights is None:
+        weights = _new(x, (d.M, topk), torch.float32, stream)
     samd_moe_route(d, normalize, x, router, ids, weights, stream)
     return ids, weights
+
+
+def _are_weights4(w, rows: int, groups: int, words: int, word, dtype) -> bool:
+    lanes, scales = w[0], w[1]
+    if (lanes.dtype is not word or scales.dtype is not dtype or scales.shape != (rows, groups) or lanes.numel() != rows * words or
+            not lanes.is_contiguous() or not scales.is_contiguous()):
+        return False
+    zeros = w[2] if len(w) > 2 else None
+    return zeros is None or (zeros.dtype is torch.uint8 and zeros.shape == (rows, groups) and zeros.is_contiguous())
 
 
 def _experts4(gate, up, down, K: int, group: int, f: samd_fmt, dtype) -> tuple[int, int]:
@@ -1035,11 +1074,14 @@ def _experts4(gate, up, down, K: int, group: int, f: samd_fmt, dtype) -> tuple[i
     scales (rows of all experts, groups of a row) say how many rows there are."""
     rows, n = gate[1].shape[0], down[1].shape[0]
     E = n // K if K else 0
-    if E < 1 or n != E * K or rows % E:
+    if E < 1 or n != E * K or rows % E or group < 1:
         raise ValueError(f"gate, down: scales of {rows} and {n} rows, wanted a multiple of the experts, and {K} times them")
-    F = rows // E
-    for w, r, k in ((gate, E * F, K), (up, E * F, K), (down, E * K, F)):
-        _check_weights4(w[0], w[1], w[2] if len(w) > 2 else None, r, k, group, f, dtype)
+    F, L, word = rows // E, f.word_bits // 4, word_dtype(f)
+    gk, wk = -(-K // group), -(-K // L)
+    if not (_are_weights4(gate, rows, gk, wk, word, dtype) and _are_weights4(up, rows, gk, wk, word, dtype) and
+            _are_weights4(down, n, -(-F // group), -(-F // L), word, dtype)):
+        for w, r, k in ((gate, rows, K), (up, rows, K), (down, n, F)):  # which, and what
+            _check_weights4(w[0], w[1], w[2] if len(w) > 2 else None, r, k, group, f, dtype)
     return E, F
 
 
@@ -1056,18 +1098,36 @@ def moe4(x, ids, weights, gate, up, down, group: int, f: samd_fmt, act="silu", o
         raise ValueError(f"weights: a contiguous {tuple(ids.shape)} float32 tensor is wanted")
     ldy = K if out is None else _ld8(out, "out", M, K, x.dtype)
     d = _moe_desc(x, E, topk, F, group, ldy, act)
-    with _on(stream):
-        if out is None:
-            out = torch.empty((M, K), dtype=x.dtype, device=x.device)
-        if workspace is None:
-            workspace = torch.empty(samd_moe4_workspace_size(d), dtype=torch.uint8, device=x.device)
-    gate, up, down = (w if len(w) > 2 else (*w, None) for w in (gate, up, down))
-    samd_moe4(d, f, x, ids, weights, gate, up, down, out, workspace, stream=stream)
+    if out is None:
+        out = _new(x, (M, K), None, stream)
+    if workspace is None:
+        workspace = _new(x, (samd_moe4_workspace_size(d),), torch.uint8, stream)
+    samd_moe4(d, f, x, ids, weights, _three(gate), _three(up), _three(down), out, workspace, None, stream)
     return out
+
+
+def _three(w):
+    return w if len(w) > 2 else (*w, None)
 
 
 def moe_layer4(x, router, topk: int, gate, up, down, group: int, f: samd_fmt, act="silu", normalize: bool = True, out=None,
                workspace=None, stream=None):
     """A whole layer of experts: moe_route, and moe4 on its choice."""
-    ids, weights = moe_route(x, router, topk, normalize, stream=stream)
-    return moe4(x, ids, weights, gate, up, down, group, f, act, out, workspace, stream)
+    if workspace is not None:
+        ids, weights = moe_route(x, router, topk, normalize, stream=stream)
+        return moe4(x, ids, weights, gate, up, down, group, f, act, out, workspace, stream)
+    M, K = x.shape
+    E, F = _experts4(gate, up, down, K, group, f, x.dtype)
+    _check_router(router, x, topk)
+    if router.shape[0] != E:
+        raise ValueError(f"router: {router.shape[0]} experts, wanted {E}")
+    d = _moe_desc(x, E, topk, F, group, K if out is None else _ld8(out, "out", M, K, x.dtype), act)
+    if out is None:
+        out = _new(x, (M, K), None, stream)
+    # the choice and the layer's workspace in one allocation
+    part = -(-4 * M * topk // 128) * 128
+    buf = _new(x, (2 * part + samd_moe4_workspace_size(d),), torch.uint8, stream)
+    at = _address(buf)
+    samd_moe_route(d, normalize, x, router, at, at + part, stream)
+    samd_moe4(d, f, x, at, at + part, _three(gate), _three(up), _three(down), out, at + 2 * part, buf.numel() - 2 * part, stream)
+    return out

@@ -122,7 +122,7 @@ def paged(pages=4, heads=2, page=16, dim=64, bits=8, t=torch.bfloat16):
 
 
 def test_the_binding_checks_its_tensors(monkeypatch):
-    monkeypatch.setattr(samd, "_ptr", lambda t: None)
+    monkeypatch.setattr(samd, "_address", lambda t: 16)
     l, s = paged()
     c = samd.PagedCache(l, s, l, s)
     assert (c.bits, c.dim, c.heads, c.page, c.dtype) == (8, 64, 2, 16, torch.bfloat16)
