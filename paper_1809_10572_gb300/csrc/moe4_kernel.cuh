@@ -133,13 +133,14 @@ __device__ __forceinline__ void mma_pure(float (&d)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 
-// Minus the power and the zero point z (in both halves), for the nibbles at bit 0 (lo) and bit 4 (hi).
+// Minus the power and the zero point z (in both halves), for the nibbles at bit 0 (lo) and bit 4 (hi); by multiply-adds,
+// which leave the pipe of the logic operations alone.
 template <typename T>
 __device__ __forceinline__ void minus(uint32_t zz, uint32_t &lo, uint32_t &hi) {
   if constexpr (std::is_same<T, __half>::value)
-    lo = 0xE400E400u | zz, hi = 0xD400D400u | zz << 4;
+    lo = 0xE400E400u + zz, hi = zz * 16u + 0xD400D400u;
   else
-    lo = hi = 0xC300C300u | zz;
+    lo = hi = 0xC300C300u + zz;
 }
 
 // The eight lanes of a word as four pairs (i, i + 4), each plus its power; flip is 8 for signed lanes (both halves).
@@ -382,12 +383,12 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
         less[q][0] = less[q][1] = plain_lo, less[q][2] = less[q][3] = plain_hi;
         if constexpr (kZeros) {
           if ((gi & 3) == 0) {
-            zc[q][0] = __shfl_sync(0xffffffffu, z[gi / 4], 16 * q + g);
-            zc[q][1] = __shfl_sync(0xffffffffu, z[gi / 4], 16 * q + g + 8);
+            zc[q][0] = __shfl_sync(0xffffffffu, z[gi / 4], 16 * q + g) & 0x0F0F0F0Fu;
+            zc[q][1] = __shfl_sync(0xffffffffu, z[gi / 4], 16 * q + g + 8) & 0x0F0F0F0Fu;
           }
           const int sel = 0x4040 | (gi & 3) | (gi & 3) << 8;
-          minus<T>(__byte_perm(zc[q][0], 0, sel) & 0x000F000Fu, less[q][0], less[q][2]);
-          minus<T>(__byte_perm(zc[q][1], 0, sel) & 0x000F000Fu, less[q][1], less[q][3]);
+          minus<T>(__byte_perm(zc[q][0], 0, sel), less[q][0], less[q][2]);
+          minus<T>(__byte_perm(zc[q][1], 0, sel), less[q][1], less[q][3]);
         }
       }
       float d[RT][4];

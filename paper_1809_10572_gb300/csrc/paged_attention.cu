@@ -16,6 +16,7 @@ constexpr int kWholeSteps = 16;
 struct JoinArgs {
   AttArgs a;
   int dim;
+  int joins;  // CTAs of the grid's second axis that join a head; those behind them count weights
   float *scores;
   int64_t ld_scores;
 };
@@ -79,7 +80,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join(const JoinA
   const int head0 = kv_head * a.group + part * a.per;
   const int len = static_cast<int>(length_of(a.s, b));
 
-  if (!a.whole) {
+  if (static_cast<int>(blockIdx.y) < j.joins) {
     const int2 span = a.span[unit_part];  // (not yet written where there are no tokens)
     if (len == 0) {
       uint32_t *const out = reinterpret_cast<uint32_t *>(a.out + b * a.ldo + static_cast<int64_t>(head0) * j.dim * 2);
@@ -91,7 +92,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join(const JoinA
     if (n > 1) {
       // columns of four elements by groups of threads that take parts in turn
       const int cols = j.dim / 4, groups = kJoinThreads / cols, col = tid % cols, grp = tid / cols;
-      for (int h = blockIdx.y; h < n_heads; h += gridDim.y) {
+      for (int h = blockIdx.y; h < n_heads; h += j.joins) {
         Joined mine = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), -3e38f, 0.0f};
         if (grp < groups)
 #pragma unroll 4
@@ -114,9 +115,11 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join(const JoinA
         __syncthreads();
       }
     }
+    return;
   }
 
-  if (!j.scores || part != 0) return;
+  if (part != 0 || len == 0) return;
+  const int slice = blockIdx.y - j.joins, slices = gridDim.y - j.joins;
   for (int i = warp; i < a.group; i += kJoinThreads / 32) {
     const int p = i / a.per;
     const int2 span = a.whole ? make_int2(0, 0) : a.span[unit_part + p];
@@ -127,7 +130,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join(const JoinA
   const int64_t tokens = static_cast<int64_t>(a.s.max_pages) << a.s.page_shift;
   const int64_t end = len < j.ld_scores ? len : j.ld_scores;
   float *const row = j.scores + unit * j.ld_scores;
-  for (int64_t t = static_cast<int64_t>(blockIdx.y) * kJoinThreads + tid; t < end; t += static_cast<int64_t>(gridDim.y) * kJoinThreads) {
+  for (int64_t t = static_cast<int64_t>(slice) * kJoinThreads + tid; t < end; t += static_cast<int64_t>(slices) * kJoinThreads) {
     float w = 0.0f;
     for (int p = 0; p < a.parts; ++p) {
       const float4 *const lp = reinterpret_cast<const float4 *>(a.logits + ((unit_part + p) * tokens + t) * kHeads);
@@ -219,12 +222,16 @@ cudaError_t launch_paged_attention(const samd_cache &c, const samd_cache_seqs &s
   if (e != cudaSuccess || (p.whole && !scores)) return e;
   // few heads: more CTAs for each
   const int64_t ups = p.units * p.parts;
-  const int64_t most = scores ? (static_cast<int64_t>(s.max_pages) * c.page + kJoinThreads - 1) / kJoinThreads : p.per;
-  int64_t z = (4 * sm_count() + ups - 1) / ups;
-  z = z < most ? z : most;
-  const JoinArgs j = {a, c.dim, scores, ld_scores};
+  auto share = [](int64_t all, int64_t of, int64_t most) {
+    const int64_t n = (all + of - 1) / of;
+    return static_cast<int>(n < 1 ? 1 : n < most ? n : most);
+  };
+  const int joins = p.whole ? 0 : share(4 * sm_count(), ups, p.per);
+  const int64_t runs = (static_cast<int64_t>(s.max_pages) * c.page + kJoinThreads - 1) / kJoinThreads;
+  const int slices = !scores ? 0 : share(8 * sm_count(), p.units, runs < 60000 ? runs < 1 ? 1 : runs : 60000);
+  const JoinArgs j = {a, c.dim, joins, scores, ld_scores};
   const size_t smem = scores ? static_cast<size_t>(a.group) * sizeof(float2) : 0;
-  const dim3 jgrid(static_cast<unsigned>(ups), static_cast<unsigned>(z < 1 ? 1 : z));
+  const dim3 jgrid(static_cast<unsigned>(ups), static_cast<unsigned>(joins + slices));
   return c.type == SAMD_BF16 ? launch_dependent(paged_attention_join<__nv_bfloat16>, jgrid, kJoinThreads, smem, stream, 1, j)
                              : launch_dependent(paged_attention_join<__half>, jgrid, kJoinThreads, smem, stream, 1, j);
 }
