@@ -51,7 +51,7 @@ namespace kv {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kHeads = 8;     // query heads of a CTA: the MMA's columns
-constexpr int kMinSteps = 8;  // a CTA is not used for fewer
+constexpr int kMinSteps = kWarps;  // a CTA is not used for fewer, unless a head has fewer
 
 struct AttArgs {
   Seqs s;
@@ -80,37 +80,43 @@ __host__ __device__ __forceinline__ int steps_of(const Seqs &s, int b) {
   return static_cast<int>((length_of(s, b) + kStep - 1) / kStep);
 }
 
-// CTAs that are used for so many steps, and the steps of one of them.
-__host__ __device__ __forceinline__ int64_t used_of(int64_t all, int slots) {
-  const int64_t most = (all + kMinSteps - 1) / kMinSteps;
+// CTAs that are used for so many steps of so many heads that have any, and the steps of one of them.
+__host__ __device__ __forceinline__ int64_t used_of(int64_t all, int64_t units, int slots) {
+  const int64_t steps = (all + kMinSteps - 1) / kMinSteps, most = steps > units ? steps : units;
   return most < slots ? most : slots;
 }
 __host__ __device__ __forceinline__ int64_t begin_of(int64_t slot, int64_t all, int64_t used) { return slot * all / used; }
 
 // By the whole CTA: its steps [begin, end), the sequence that the first lies in, and the step's place from that
-// sequence's first, *rem. Returns the number of all steps. tmp: kWarps + 2.
+// sequence's first, *rem; *used: the CTAs that have steps. Returns the number of all steps. tmp: 2 kWarps + 2.
 __device__ __forceinline__ int64_t locate(const Seqs &s, int heads, int slot, int slots, int64_t *tmp, int *b_out,
-                                          int64_t *begin, int64_t *end, int64_t *rem) {
+                                          int64_t *begin, int64_t *end, int64_t *rem, int64_t *used_out) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int chunk = (s.seqs + kThreads - 1) / kThreads, b0 = tid * chunk;
   int64_t mine = 0;
-  for (int b = b0; b < min(b0 + chunk, s.seqs); ++b) mine += steps_of(s, b);
+  int some = 0;  // sequences with steps
+  for (int b = b0; b < min(b0 + chunk, s.seqs); ++b) {
+    const int n = steps_of(s, b);
+    mine += n, some += n > 0;
+  }
+  some = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(some)));
   int64_t incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += up;
   }
-  if (lane == 31) tmp[warp] = incl;
+  if (lane == 31) tmp[warp] = incl, tmp[kWarps + 2 + warp] = some;
   __syncthreads();
-  int64_t before = 0, all = 0;
+  int64_t before = 0, all = 0, units = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
     if (w < warp) before += tmp[w];
     all += tmp[w];
+    units += tmp[kWarps + 2 + w];
   }
   all *= heads;
-  const int64_t used = used_of(all, slots);
+  const int64_t used = *used_out = used_of(all, units * heads, slots);
   *begin = *end = 0;
   if (slot < used) {
     *begin = begin_of(slot, all, used);
@@ -326,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   constexpr int kTiles = kDim / 16;  // of 16 elements
   constexpr float kLow = -3e38f;     // a reference before any token
   extern __shared__ __align__(256) uint8_t smem[];
-  __shared__ int64_t tmp[kWarps + 2];
+  __shared__ int64_t tmp[2 * kWarps + 2];
   __shared__ float2 red_stat[kWarps][kHeads];  // references and sums of weights
   __shared__ float *red_at[kWarps];            // the warps' sums
   // (the warp's number by a shuffle: what follows from it is the same in all lanes, and the compiler knows)
@@ -346,8 +352,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   } else {
     int b;
     int64_t begin, end, rem;
-    all = locate(a.s, a.heads, slot, a.slots, tmp, &b, &begin, &end, &rem);
-    used = used_of(all, a.slots);
+    all = locate(a.s, a.heads, slot, a.slots, tmp, &b, &begin, &end, &rem, &used);
     if (begin >= end) return;
     have.start(a, b, rem, end - begin);
   }

@@ -367,14 +367,14 @@ samd_status cache_shape_checks(const samd_cache *c, const samd_cache_seqs *s) {
       c->heads > 65536)
     return SAMD_EUNSUP;
   // rows are counted in an int64, tokens of a sequence and pairs of a sequence and a head in an int
-  if (static_cast<int64_t>(s->max_pages) * c->page > kMaxDim || static_cast<int64_t>(s->seqs) * c->heads > kMaxDim)
-    return SAMD_EUNSUP;
+  const int64_t tokens = static_cast<int64_t>(s->max_pages) * c->page, rows = static_cast<int64_t>(s->seqs) * c->heads;
+  if (tokens > kMaxDim || rows > kMaxDim || (tokens > 0 && rows > (int64_t(1) << 50) / tokens)) return SAMD_EUNSUP;
   return SAMD_OK;
 }
 
 samd_status cache_address_checks(const samd_cache *c, const samd_cache_seqs *s) {
-  if (!c->k_lanes || !c->k_scales || !c->v_lanes || !c->v_scales || !s->lengths || (!s->table && s->max_pages > 0))
-    return SAMD_EINVAL;
+  if (c->pages > 0 && (!c->k_lanes || !c->k_scales || !c->v_lanes || !c->v_scales)) return SAMD_EINVAL;
+  if (!s->lengths || (!s->table && s->max_pages > 0)) return SAMD_EINVAL;
   if (!aligned16(c->k_lanes) || !aligned16(c->k_scales) || !aligned16(c->v_lanes) || !aligned16(c->v_scales) ||
       !aligned4(s->table) || !aligned4(s->lengths))
     return SAMD_EALIGN;
@@ -398,11 +398,14 @@ samd_status cache_rows_checks(const samd_cache *c, const samd_cache_seqs *s, con
   return cache_address_checks(c, s);
 }
 
-samd_status attention_shape_checks(const samd_cache *c, const samd_cache_seqs *s, int q_heads) {
+samd_status attention_shape_checks(const samd_cache *c, const samd_cache_seqs *s, int q_heads, bool scores) {
   const samd_status st = cache_shape_checks(c, s);
   if (st != SAMD_OK) return st;
   if (q_heads < 1 || q_heads % c->heads != 0) return SAMD_ESHAPE;
   if (q_heads / c->heads > 256 || static_cast<int64_t>(s->seqs) * q_heads > kMaxDim) return SAMD_EUNSUP;
+  // the logits' bytes: up to 15 query heads' room for one
+  const int64_t tokens = static_cast<int64_t>(s->max_pages) * c->page;
+  if (scores && tokens > 0 && static_cast<int64_t>(s->seqs) * q_heads > (int64_t(1) << 50) / tokens) return SAMD_EUNSUP;
   return SAMD_OK;
 }
 }  // namespace
@@ -424,14 +427,14 @@ samd_status samd_cache_read(const samd_cache *c, const samd_cache_seqs *s, const
 }
 
 size_t samd_paged_attention_workspace_size(const samd_cache *c, const samd_cache_seqs *s, int q_heads, int scores) {
-  if (attention_shape_checks(c, s, q_heads) != SAMD_OK || s->seqs == 0) return 0;
+  if (attention_shape_checks(c, s, q_heads, scores != 0) != SAMD_OK || s->seqs == 0) return 0;
   return paged_attention_workspace(*c, *s, q_heads, scores != 0);
 }
 
 samd_status samd_paged_attention(const samd_cache *c, const samd_cache_seqs *s, int q_heads, const void *q,
                                  int64_t ldq, float scale, void *out, int64_t ldo, float *scores, int64_t ld_scores,
                                  void *workspace, size_t workspace_bytes, samd_stream_t stream) {
-  samd_status st = attention_shape_checks(c, s, q_heads);
+  samd_status st = attention_shape_checks(c, s, q_heads, scores != nullptr);
   if (st != SAMD_OK) return st;
   if (!(scale - scale == 0.0f)) return SAMD_EINVAL;
   const int64_t row = static_cast<int64_t>(q_heads) * c->dim;

@@ -924,11 +924,11 @@ def _scores_ld(scores, seqs: int, heads: int) -> int:
 
 
 def _new(like, shape, dtype, stream) -> torch.Tensor:
-    """An uninitialised tensor beside `like`, of the stream that is going to use it."""
+    """An uninitialised tensor on the device of `like`, of the stream that is going to use it."""
     if stream is None:
-        return like.new_empty(shape, dtype=dtype)
+        return torch.empty(shape, dtype=dtype, device=like.device)
     with _on(stream):
-        return like.new_empty(shape, dtype=dtype)
+        return torch.empty(shape, dtype=dtype, device=like.device)
 
 
 def cache_append(cache: PagedCache, k, v, table, lengths, starts=None, stream=None) -> None:
@@ -984,7 +984,7 @@ def paged_attention(q, cache: PagedCache, table, lengths, scale: float | None = 
         raise ValueError(f"q: {q_heads} heads, wanted a multiple of the cache's {heads}")
     ld_scores = 0 if scores is None else _scores_ld(scores, seqs, heads)
     if out is None:
-        out, ldo = _new(q, (seqs, q_heads, dim), None, stream), q_heads * dim
+        out, ldo = _new(q, (seqs, q_heads, dim), cache.dtype, stream), q_heads * dim
     else:
         ldo = _token_rows(out, "out", q_heads, dim, q.dtype, seqs)
     nb = None
@@ -1014,7 +1014,7 @@ def cache_evict(cache: PagedCache, table, lengths, scores, dst_table, keep: int,
     ld_dst = _rows(dst_table, "dst_table")
     kept = _new(scores, (seqs, heads, keep), torch.int32, stream)
     new_lengths = _new(scores, (seqs,), torch.int32, stream)
-    new_scores = _new(scores, (seqs, heads, keep), None, stream)
+    new_scores = _new(scores, (seqs, heads, keep), torch.float32, stream)
     samd_cache_evict(cache._desc, s, scores, ld_scores, keep, recent, dst_table, ld_dst, kept, new_lengths, new_scores, stream)
     return kept, new_lengths, new_scores
 
@@ -1099,7 +1099,7 @@ def moe4(x, ids, weights, gate, up, down, group: int, f: samd_fmt, act="silu", o
     ldy = K if out is None else _ld8(out, "out", M, K, x.dtype)
     d = _moe_desc(x, E, topk, F, group, ldy, act)
     if out is None:
-        out = _new(x, (M, K), None, stream)
+        out = _new(x, (M, K), x.dtype, stream)
     if workspace is None:
         workspace = _new(x, (samd_moe4_workspace_size(d),), torch.uint8, stream)
     samd_moe4(d, f, x, ids, weights, _three(gate), _three(up), _three(down), out, workspace, None, stream)
@@ -1123,7 +1123,7 @@ def moe_layer4(x, router, topk: int, gate, up, down, group: int, f: samd_fmt, ac
         raise ValueError(f"router: {router.shape[0]} experts, wanted {E}")
     d = _moe_desc(x, E, topk, F, group, K if out is None else _ld8(out, "out", M, K, x.dtype), act)
     if out is None:
-        out = _new(x, (M, K), None, stream)
+        out = _new(x, (M, K), x.dtype, stream)
     # the choice and the layer's workspace in one allocation
     part = -(-4 * M * topk // 128) * 128
     buf = _new(x, (2 * part + samd_moe4_workspace_size(d),), torch.uint8, stream)

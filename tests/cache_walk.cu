@@ -40,7 +40,9 @@ static void walk(const std::vector<int32_t> &lengths, int heads, int slots, int 
   for (int b = 0; b < a.s.seqs; ++b)
     for (int h = 0; h < heads; ++h) first.push_back(all), all += steps_of(a.s, b);
   const int units = a.s.seqs * heads;
-  const int64_t used = whole ? slots : used_of(all, slots);
+  int64_t some = 0;
+  for (int b = 0; b < a.s.seqs; ++b) some += steps_of(a.s, b) > 0;
+  const int64_t used = whole ? slots : used_of(all, some * heads, slots);
   std::vector<int> done(units, 0), seen(units, 0), last_slot(units, -1), said(units, -2);
   for (int slot = 0; slot < slots; ++slot) {
     Walk w;

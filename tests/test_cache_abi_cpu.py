@@ -31,7 +31,8 @@ BAD_CACHES = [(dict(type=samd.SAMD_F32), EINVAL), (dict(type=9), EINVAL), (dict(
               (dict(page=8), EUNSUP), (dict(page=24), EUNSUP), (dict(page=1 << 17), EUNSUP), (dict(dim=48), EUNSUP),
               (dict(dim=288), EUNSUP), (dict(heads=65537), EUNSUP)]
 BAD_SEQS = [(dict(seqs=-1), ESHAPE), (dict(max_pages=-1), ESHAPE), (dict(ld=1), ESHAPE),
-            (dict(max_pages=1 << 27, ld=1 << 27), EUNSUP), (dict(seqs=1 << 30), EUNSUP)]
+            (dict(max_pages=1 << 27, ld=1 << 27), EUNSUP), (dict(seqs=1 << 30), EUNSUP),
+            (dict(seqs=1 << 28, max_pages=1 << 26, ld=1 << 26), EUNSUP)]
 BAD_ADDRESSES = [(dict(kl=None), {}, EINVAL), (dict(vs=None), {}, EINVAL), (dict(ks=8), {}, EALIGN), (dict(vl=4), {}, EALIGN),
                  ({}, dict(table=None), EINVAL), ({}, dict(lengths=None), EINVAL), ({}, dict(table=6), EALIGN),
                  ({}, dict(lengths=9), EALIGN)]

@@ -306,6 +306,26 @@ def test_strides_streams_graphs_and_repeats(samd_lib):
     assert_status_clean()
 
 
+def test_a_cache_without_pages(samd_lib):
+    cache = samd.cache_empty(0, 16, 2, 64, 8, BF16)
+    table, lens = torch.zeros((3, 40), dtype=torch.int32, device="cuda"), torch.tensor([0, 5, 600], dtype=torch.int32, device="cuda")
+    q, k = ref.normal(92, (3, 4, 64), BF16), ref.normal(93, (3, 2, 64), BF16)
+    scores = torch.ones((3, 2, 640), device="cuda")
+    assert not samd.paged_attention(q, cache, table, lens, scores=scores).any() and (scores == 1).all()
+    samd.cache_append(cache, k, k, table, lens)
+    assert not samd.cache_read(cache, 3, table, lens)[0].any()
+
+
+@pytest.mark.parametrize("lengths", [[1] * 40, [3] * 7 + [0] * 30, [20, 1, 1, 1, 1000, 1], [17] * 300], ids=lambda n: f"{len(n)}x{n[0]}")
+def test_short_sequences_in_long_tables(samd_lib, lengths):
+    """Fewer steps than a CTA's warps for a head, in tables with room for many."""
+    cache, table, lens, k, v = make(95, lengths, 3, 64, 8, 16, F16, capacity=1500)
+    q = ref.normal(96, (len(lengths), 6, 64), F16)
+    scores = torch.zeros((len(lengths), 3, 1500), device="cuda")
+    got = samd.paged_attention(q, cache, table, lens, scores=scores)
+    check(got, q, table, lengths, k, v, 16, 0.125, F16, scores, torch.zeros_like(scores))
+
+
 def test_empty_calls(samd_lib):
     cache, table, lens, k, v = make(91, [5], 2, 64, 8, 16, BF16)
     q = torch.empty((0, 4, 64), dtype=BF16, device="cuda")
