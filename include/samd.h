@@ -448,8 +448,9 @@ SAMD_API samd_status samd_gated_ffn_backward(const samd_ffn_desc *desc, const vo
  * (tables, lengths, starts, scores, kept places) need no more than the 4-byte
  * alignment of their elements.
  *
- * A cache is `pages` pages of `page` tokens (a power of two, 16 or more) for
- * `heads` key heads of `dim` elements (a multiple of 32, 32 .. 256). A row is
+ * A cache is `pages` pages of `page` tokens (a power of two, 16 .. 65536) for
+ * `heads` key heads (up to 65536, and 2^30 rows a page) of `dim` elements (a
+ * multiple of 32, 32 .. 256). A row is
  * one token's key or value of one head: its lanes as samd_pack writes them
  * (signed, 4 or 8 bits, 32-bit words, no spacers), and a scale of `type`
  * (SAMD_F16 or SAMD_BF16) for every 32 of them. All four arrays hold their rows

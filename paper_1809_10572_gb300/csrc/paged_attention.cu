@@ -207,6 +207,7 @@ cudaError_t launch_paged_attention(const samd_cache &c, const samd_cache_seqs &s
   a.ldq = ldq * 2, a.ldo = ldo * 2;
   a.scale = scale * 1.4426950408889634f;
   a.heads = c.heads, a.group = q_heads / c.heads;
+  a.page_rows = static_cast<uint32_t>(c.heads) * static_cast<uint32_t>(c.page);
   a.parts = p.parts, a.per = p.per, a.slots = p.slots, a.whole = p.whole;
   if (!p.whole) {
     a.sums = reinterpret_cast<float *>(ws + p.sums);

@@ -61,6 +61,7 @@ struct AttArgs {
   int64_t ldq, ldo;  // bytes
   float scale;       // with log2(e)
   int heads;         // of keys
+  uint32_t page_rows;  // rows of a page: heads x slots
   int group;         // query heads of a key head
   int parts;         // CTAs that share a key head's pages: ceil(group / per)
   int per;           // query heads of a CTA
@@ -370,9 +371,11 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   Walk ahead = have;
   int l_step = ahead.first + warp, fill = 0, slot_used = 0;
   uint32_t missing = 0;  // bit of a stage: its page is none of the cache's
-  int l_page = -1;
+  int l_pages = -1, l_page = -1, l_turn = 0;  // pages of the warp's next 32 steps, a step a lane; of the next one
+  uint32_t head_rows = 0;  // of a page, before the key head in hand
   // brings `ahead` and l_step to the next step of this warp, and its page
   auto seek = [&]() {
+    bool fresh = false;
     while (l_step >= ahead.last) {
       const int was = ahead.b * a.heads + ahead.h;
       ahead.next(a);
@@ -382,8 +385,15 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
         return;
       }
       l_step = ahead.first + warp;
+      fresh = true;
     }
-    l_page = page_of(a.s, ahead.b, static_cast<int64_t>(l_step) * kStep);
+    if (fresh || l_turn == 32) {
+      head_rows = static_cast<uint32_t>(ahead.h) << a.s.page_shift;
+      const int step = l_step + kWarps * lane;
+      l_pages = step < ahead.last ? page_of(a.s, ahead.b, static_cast<int64_t>(step) * kStep) : -1;
+      l_turn = 0;
+    }
+    l_page = __shfl_sync(0xffffffffu, l_pages, l_turn++);
   };
   auto load_next = [&]() {
     if (l_step >= 0) {
@@ -391,8 +401,8 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       // (a page that is none of the cache's: the stage keeps what it holds, and the step counts nothing)
       missing = l_page >= 0 ? missing & ~(1u << fill) : missing | 1u << fill;
       if (l_page >= 0) {
-        const int pos = (l_step * kStep) & ((1 << a.s.page_shift) - 1);  // (tokens are counted in an int)
-        const int64_t row = ((static_cast<int64_t>(l_page) * a.heads + ahead.h) << a.s.page_shift) + pos;
+        const uint32_t pos = static_cast<uint32_t>(l_step * kStep) & ((1u << a.s.page_shift) - 1);  // (tokens are counted in an int)
+        const uint64_t row = static_cast<uint64_t>(static_cast<uint32_t>(l_page)) * a.page_rows + (head_rows + pos);
         const uint8_t *const kp = k_lane + row * P::kRow, *const vp = v_lane + row * P::kRow;
 #pragma unroll
         for (int i = 0; i < kCopies; ++i)
@@ -408,6 +418,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
     ptx::cp_async_commit();
     fill = fill + 1 == kStages ? 0 : fill + 1;
   };
+  l_turn = 32;
   seek();
 #pragma unroll 1
   for (int i = 0; i < kStages - 1; ++i) load_next();
@@ -565,13 +576,13 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       }
 
       float e[4];
-      bool over[2] = {false, false};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        e[j] = exp2_of(x[j] - ref[j & 1]);
-        over[j & 1] |= !(e[j] * vmax[j >> 1] <= 32768.0f);
-      }
-      if (__any_sync(0xffffffffu, over[0] | over[1])) {
+      for (int j = 0; j < 4; ++j) e[j] = exp2_of(x[j] - ref[j & 1]);
+      const bool past = !(fmaxf(e[0], e[1]) * vmax[0] <= 32768.0f) || !(fmaxf(e[2], e[3]) * vmax[1] <= 32768.0f);
+      if (__any_sync(0xffffffffu, past)) {
+        bool over[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) over[c] = !(e[c] * vmax[0] <= 32768.0f) || !(e[2 + c] * vmax[1] <= 32768.0f);
         float top[2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {

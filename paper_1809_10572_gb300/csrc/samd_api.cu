@@ -364,7 +364,7 @@ samd_status cache_shape_checks(const samd_cache *c, const samd_cache_seqs *s) {
       s->ld < s->max_pages)
     return SAMD_ESHAPE;
   if (c->page < 16 || c->page > 65536 || (c->page & (c->page - 1)) != 0 || c->dim % 32 != 0 || c->dim > 256 ||
-      c->heads > 65536)
+      c->heads > 65536 || static_cast<int64_t>(c->heads) * c->page > kMaxDim)
     return SAMD_EUNSUP;
   // rows are counted in an int64, tokens of a sequence and pairs of a sequence and a head in an int
   const int64_t tokens = static_cast<int64_t>(s->max_pages) * c->page, rows = static_cast<int64_t>(s->seqs) * c->heads;

@@ -29,7 +29,7 @@ BAD_CACHES = [(dict(type=samd.SAMD_F32), EINVAL), (dict(type=9), EINVAL), (dict(
               (dict(fmt=samd.fmt(4, True, 1)), EUNSUP), (dict(fmt=samd.fmt(4, True, 0, 64)), EUNSUP),
               (dict(pages=-1), ESHAPE), (dict(page=0), ESHAPE), (dict(heads=0), ESHAPE), (dict(dim=0), ESHAPE),
               (dict(page=8), EUNSUP), (dict(page=24), EUNSUP), (dict(page=1 << 17), EUNSUP), (dict(dim=48), EUNSUP),
-              (dict(dim=288), EUNSUP), (dict(heads=65537), EUNSUP)]
+              (dict(dim=288), EUNSUP), (dict(heads=65537), EUNSUP), (dict(heads=1 << 16, page=1 << 15), EUNSUP)]
 BAD_SEQS = [(dict(seqs=-1), ESHAPE), (dict(max_pages=-1), ESHAPE), (dict(ld=1), ESHAPE),
             (dict(max_pages=1 << 27, ld=1 << 27), EUNSUP), (dict(seqs=1 << 30), EUNSUP),
             (dict(seqs=1 << 28, max_pages=1 << 26, ld=1 << 26), EUNSUP)]
