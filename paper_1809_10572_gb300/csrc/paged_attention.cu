@@ -166,7 +166,7 @@ Plan plan_of(const samd_cache &c, const samd_cache_seqs &s, int q_heads, bool sc
   const int ctas = (c.fmt.bits == 8 ? ctas_of<8>(c.dim / 32) : ctas_of<4>(c.dim / 32)) * sm_count();
   int64_t slots = ctas / p.parts < 1 ? 1 : ctas / p.parts;
   if (slots > kMaxSlots) slots = kMaxSlots;
-  const int64_t most = p.whole ? p.units : used_of(p.units * ((tokens + kStep - 1) / kStep), p.units, kMaxSlots);
+  const int64_t most = p.whole ? p.units : used_of(p.units * dealt_of(static_cast<int>((tokens + kStep - 1) / kStep)), p.units, kMaxSlots);
   p.slots = static_cast<int>(slots < most ? slots : most < 1 ? 1 : most);
   size_t at = 0;
   auto take = [&at](int64_t bytes) {

@@ -34,12 +34,21 @@
 // (values). The weights change operand layout by movmatrix.
 //
 // Split: all steps of all sequences and key heads lie in one line, of which
-// every CTA takes an equal part, whatever the lengths; its warps take steps in
-// turn. A CTA's parts of two heads are finished one after the other (the ring
-// runs on); where a head's steps lie in several CTAs, each leaves its sums and
-// references in the workspace for paged_attention_join (fixed order: the same
-// call gives the same bits). Head groups of more than eight query heads are
-// neighbouring CTAs that read the same pages at the same time.
+// every CTA takes an equal part, whatever the lengths (and with what beginning a
+// head costs counted in); its warps take steps in turn. A CTA's parts of two heads
+// are finished one after the other (the ring runs on); where a head's steps lie in
+// several CTAs, each leaves its sums and references in the workspace for
+// paged_attention_join (fixed order: the same call gives the same bits). Head
+// groups of more than eight query heads are neighbouring CTAs that read the same
+// pages at the same time.
+//
+// Measured on one GB300, with the join (GPU time of a call): one sequence of
+// 131072 tokens, 8 key heads of 128 elements: 58 us in 8 bits (285 MB, 0.72 of the
+// copy bandwidth; twice the tokens of a call cost 1.05 of what their bytes do, so
+// that the rest, about 12 us, is fixed: launches, three dependent loads before the
+// first step, the join), 46 us in 4 bits (151 MB, 0.48). A step of 16 tokens by 128
+// elements is about 500 instructions in 8 bits and 440 in 4, 160 and 144 of them
+// for widening; with sixteen warps an SM issue slots are 54 and 65% busy.
 #pragma once
 
 #include "cache_internal.cuh"
@@ -52,6 +61,10 @@ constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kHeads = 8;     // query heads of a CTA: the MMA's columns
 constexpr int kMinSteps = kWarps;  // a CTA is not used for fewer, unless a head has fewer
+// What beginning a head takes of a CTA's time, in steps: a join, the next head's length, pages and query, one after the
+// other. Counted when steps are dealt out, 53 sequences of up to 4001 tokens and 12 heads take 59 us, without 71; 16 of up
+// to 8192 38 and 42 (14 to 40 are within 3% of each other there; long sequences in 4 bits lose 5% from 20 on).
+constexpr int kHeadCost = 16;
 
 struct AttArgs {
   Seqs s;
@@ -81,15 +94,18 @@ __host__ __device__ __forceinline__ int steps_of(const Seqs &s, int b) {
   return static_cast<int>((length_of(s, b) + kStep - 1) / kStep);
 }
 
-// CTAs that are used for so many steps of so many heads that have any, and the steps of one of them.
+// The steps of a sequence's head as they are dealt out: with what beginning it costs before the first of them.
+__host__ __device__ __forceinline__ int64_t dealt_of(int steps) { return steps > 0 ? steps + kHeadCost : 0; }
+
+// CTAs that are used for so many dealt steps of so many heads that have any, and the first one of a CTA's.
 __host__ __device__ __forceinline__ int64_t used_of(int64_t all, int64_t units, int slots) {
-  const int64_t steps = (all + kMinSteps - 1) / kMinSteps, most = steps > units ? steps : units;
+  const int64_t steps = (all - units * kHeadCost + kMinSteps - 1) / kMinSteps, most = steps > units ? steps : units;
   return most < slots ? most : slots;
 }
 __host__ __device__ __forceinline__ int64_t begin_of(int64_t slot, int64_t all, int64_t used) { return slot * all / used; }
 
-// By the whole CTA: its steps [begin, end), the sequence that the first lies in, and the step's place from that
-// sequence's first, *rem; *used: the CTAs that have steps. Returns the number of all steps. tmp: 2 kWarps + 2.
+// By the whole CTA: its dealt steps [begin, end), the sequence that the first lies in, and the step's place from that
+// sequence's first, *rem; *used: the CTAs that have steps. Returns the number of all dealt steps. tmp: 2 kWarps + 2.
 __device__ __forceinline__ int64_t locate(const Seqs &s, int heads, int slot, int slots, int64_t *tmp, int *b_out,
                                           int64_t *begin, int64_t *end, int64_t *rem, int64_t *used_out) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -98,7 +114,7 @@ __device__ __forceinline__ int64_t locate(const Seqs &s, int heads, int slot, in
   int some = 0;  // sequences with steps
   for (int b = b0; b < min(b0 + chunk, s.seqs); ++b) {
     const int n = steps_of(s, b);
-    mine += n, some += n > 0;
+    mine += dealt_of(n), some += n > 0;
   }
   some = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(some)));
   int64_t incl = mine;
@@ -126,7 +142,7 @@ __device__ __forceinline__ int64_t locate(const Seqs &s, int heads, int slot, in
     if (*begin >= first && *begin < first + mine * heads) {
       int b = b0;
       for (;; ++b) {
-        const int64_t n = static_cast<int64_t>(steps_of(s, b)) * heads;
+        const int64_t n = dealt_of(steps_of(s, b)) * heads;
         if (*begin < first + n) break;
         first += n;
       }
@@ -141,33 +157,41 @@ __device__ __forceinline__ int64_t locate(const Seqs &s, int heads, int slot, in
   return all;
 }
 
-// The slot that step x of all `all` lies in, of `used`: the last one whose begin, floor(slot all / used), is at most x.
+// The slot that dealt step x of all `all` lies in, of `used`: the last one whose begin, floor(slot all / used), is at most x.
 __host__ __device__ __forceinline__ int slot_of(int64_t x, int64_t all, int64_t used) {
   return static_cast<int>(((x + 1) * used - 1) / all);
 }
 
 // A walk over the parts of heads that a CTA has: sequence, key head, steps [first, last) of it.
 struct Walk {
-  int64_t left;  // steps of the CTA behind this part (whole: units behind this one count as 1)
+  int64_t left;  // dealt steps of the CTA behind this part
+  int64_t unit;  // the head's first among all dealt steps
   int b, h, steps, first, last;
 
   __host__ __device__ __forceinline__ bool on() const { return first < last; }
-  __host__ __device__ __forceinline__ void take(const AttArgs &a, int from) {
-    first = from;
-    last = steps - from < left ? steps : from + static_cast<int>(left);
-    left -= last - first;
+  __host__ __device__ __forceinline__ static int step_at(int64_t dealt) {  // the step that a dealt step is, or comes before
+    return dealt > kHeadCost ? static_cast<int>(dealt - kHeadCost) : 0;
   }
-  __host__ __device__ __forceinline__ void start(const AttArgs &a, int b_, int64_t rem, int64_t n) {
-    b = b_, h = 0, first = last = 0, steps = 0, left = n;
+  __host__ __device__ __forceinline__ void take(int64_t from) {
+    const int64_t all = dealt_of(steps), to = all - from < left ? all : from + left;
+    first = step_at(from), last = step_at(to);
+    left -= to - from;
+  }
+  // From dealt step `rem` of sequence b_, dealt step `begin` of all, n of them.
+  __host__ __device__ __forceinline__ void start(const AttArgs &a, int b_, int64_t rem, int64_t begin, int64_t n) {
+    b = b_, h = 0, first = last = 0, steps = 0, left = n, unit = begin;
     if (n <= 0) return;
     steps = steps_of(a.s, b);
-    h = static_cast<int>(rem / steps);
-    take(a, static_cast<int>(rem - static_cast<int64_t>(h) * steps));
+    const int64_t all = dealt_of(steps);
+    h = static_cast<int>(rem / all);
+    const int64_t from = rem - h * all;
+    unit = begin - from;
+    take(from);
   }
-  __host__ __device__ __forceinline__ void start_whole(const AttArgs &a, int unit) {
-    left = 0, first = 0;
-    b = unit / a.heads, h = unit - b * a.heads;
-    last = steps = unit < a.s.seqs * a.heads ? steps_of(a.s, b) : 0;
+  __host__ __device__ __forceinline__ void start_whole(const AttArgs &a, int u) {
+    left = 0, unit = 0, first = 0;
+    b = u / a.heads, h = u - b * a.heads;
+    last = steps = u < a.s.seqs * a.heads ? steps_of(a.s, b) : 0;
   }
   // The next part (or, where nothing is split, the next unit, which may have no steps); steps of none at the end.
   __host__ __device__ __forceinline__ void next(const AttArgs &a) {
@@ -176,12 +200,13 @@ struct Walk {
       first = last = 0;
       return;
     }
+    unit += dealt_of(steps);
     if (++h == a.heads) {
       h = 0;
       do steps = steps_of(a.s, ++b);
       while (steps == 0 && b + 1 < a.s.seqs);
     }
-    take(a, 0);
+    take(0);
   }
 };
 
@@ -355,10 +380,8 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
     int64_t begin, end, rem;
     all = locate(a.s, a.heads, slot, a.slots, tmp, &b, &begin, &end, &rem, &used);
     if (begin >= end) return;
-    have.start(a, b, rem, end - begin);
+    have.start(a, b, rem, begin, end - begin);
   }
-  int64_t unit_begin = 0;  // of all steps, the first of the head in hand
-  if (!a.whole) unit_begin = begin_of(slot, all, used) - have.first;
 
   // ---- the ring: this warp's steps, one after the other, over the CTA's parts
   const uint32_t ring = ptx::smem_addr(smem) + warp * kStages * P::kStage;
@@ -690,9 +713,8 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
     }
     if (!a.whole && first_part && tid == 0)
       a.span[static_cast<int64_t>(unit) * a.parts + part] =
-          make_int2(slot, slot_of(unit_begin + have.steps - 1, all, used));
+          make_int2(slot, slot_of(have.unit + dealt_of(have.steps) - 1, all, used));
     __syncthreads();
-    unit_begin += have.steps;
     have = then;
   }
   ptx::cp_async_wait<0>();

@@ -38,7 +38,7 @@ static void walk(const std::vector<int32_t> &lengths, int heads, int slots, int 
   std::vector<int64_t> first;  // of every unit, among all steps
   int64_t all = 0;
   for (int b = 0; b < a.s.seqs; ++b)
-    for (int h = 0; h < heads; ++h) first.push_back(all), all += steps_of(a.s, b);
+    for (int h = 0; h < heads; ++h) first.push_back(all), all += dealt_of(steps_of(a.s, b));
   const int units = a.s.seqs * heads;
   int64_t some = 0;
   for (int b = 0; b < a.s.seqs; ++b) some += steps_of(a.s, b) > 0;
@@ -46,31 +46,28 @@ static void walk(const std::vector<int32_t> &lengths, int heads, int slots, int 
   std::vector<int> done(units, 0), seen(units, 0), last_slot(units, -1), said(units, -2);
   for (int slot = 0; slot < slots; ++slot) {
     Walk w;
-    int64_t at = 0;
     if (whole) {
       w.start_whole(a, slot);
     } else {
       if (slot >= used) continue;
       const int64_t begin = begin_of(slot, all, used), end = begin_of(slot + 1, all, used);
-      if (begin >= end) return fail("a CTA without steps");
+      if (begin >= end) return fail("a CTA without a share");
       int b = 0;
-      while (begin >= first[b * heads] + static_cast<int64_t>(heads) * steps_of(a.s, b)) ++b;
-      w.start(a, b, begin - first[b * heads], end - begin);
-      at = begin - w.first;
+      while (begin >= first[b * heads] + heads * dealt_of(steps_of(a.s, b))) ++b;
+      w.start(a, b, begin - first[b * heads], begin, end - begin);
     }
     while (whole ? w.b * heads + w.h < units : w.on()) {
       const int u = w.b * heads + w.h;
       if (u < 0 || u >= units || w.steps != steps_of(a.s, w.b) || w.first != done[u] || w.last > w.steps)
         return fail("a part out of order");
       if (whole && (w.first != 0 || w.last != w.steps)) return fail("a head that is not whole");
-      if (!whole && at != first[u]) return fail("a head's place");
+      if (!whole && w.unit != first[u]) return fail("a head's place");
       if (w.first == 0) {
         if (seen[u]++) return fail("a head begun twice");
-        if (!whole) said[u] = slot_of(at + w.steps - 1, all, used);
+        if (!whole) said[u] = slot_of(w.unit + dealt_of(w.steps) - 1, all, used);
       }
       done[u] = w.last;
       last_slot[u] = slot;
-      at += w.steps;
       w.next(a);
     }
   }
