@@ -394,9 +394,9 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   Walk ahead = have;
   int l_step = ahead.first + warp, fill = 0, slot_used = 0;
   uint32_t missing = 0;  // bit of a stage: its page is none of the cache's
-  int l_pages = -1, l_page = -1, l_turn = 0;  // pages of the warp's next 32 steps, a step a lane; of the next one
+  int l_pages = -1, l_turn = 0;  // pages of the warp's next 32 steps, a step a lane; which of them is next
   uint32_t head_rows = 0;  // of a page, before the key head in hand
-  // brings `ahead` and l_step to the next step of this warp, and its page
+  // brings `ahead` and l_step to the next step of this warp, and asks for its page, which the next load waits for
   auto seek = [&]() {
     bool fresh = false;
     while (l_step >= ahead.last) {
@@ -416,12 +416,12 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       l_pages = step < ahead.last ? page_of(a.s, ahead.b, static_cast<int64_t>(step) * kStep) : -1;
       l_turn = 0;
     }
-    l_page = __shfl_sync(0xffffffffu, l_pages, l_turn++);
   };
   auto load_next = [&]() {
     if (l_step >= 0) {
       const uint32_t st = ring + fill * P::kStage;
       // (a page that is none of the cache's: the stage keeps what it holds, and the step counts nothing)
+      const int l_page = __shfl_sync(0xffffffffu, l_pages, l_turn++);
       missing = l_page >= 0 ? missing & ~(1u << fill) : missing | 1u << fill;
       if (l_page >= 0) {
         const uint32_t pos = static_cast<uint32_t>(l_step * kStep) & ((1u << a.s.page_shift) - 1);  // (tokens are counted in an int)
