@@ -28,9 +28,10 @@
 // lane r, a block ahead, dealt out by shuffles.
 //
 // Split: first kernel: tiles of all experts' rows in turn over one wave of
-// CTAs, whose warps share a tile's inputs; second: a tile's pairs and inputs
-// over the warps of a cluster of one to eight CTAs, each warp with its own sums
-// of all tokens in shared memory, joined in a fixed order.
+// warps, where there are enough, or of CTAs, whose warps share a tile's inputs;
+// second: a tile's pairs and inputs in runs over the warps of a cluster of one to
+// eight CTAs, each warp with its own sums of all tokens in shared memory, joined
+// in a fixed order.
 #pragma once
 
 #include "matvec4_kernel.cuh"
@@ -177,7 +178,8 @@ struct Moe {
   static constexpr size_t smem(bool gated, int tokens) { return static_cast<size_t>(kRing) + red_bytes(gated, tokens); }
 };
 
-template <typename T, bool kGated, bool kZeros, int RT, int CH, int CPG>
+// kOwn (first kernel): a tile is one warp's, over all inputs; else the CTA's, and its warps share the inputs.
+template <typename T, bool kGated, bool kOwn, bool kZeros, int RT, int CH, int CPG>
 __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
   using P = Moe<RT, CH, CPG>;
   constexpr int KB = P::KB, kRows = P::kRows, kPitch = P::kPitch, kStages = P::kStages, kG = P::kGroups;
@@ -198,37 +200,52 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
     for (int i = tid; i < kWarps * kRows * (a.M | 1); i += kThreads) red[i] = 0.0f;
   __syncthreads();
 
-  // A warp's blocks, one after the other. First kernel: the CTA's items (pass and tile) in turn, every eighth block of
-  // each; second: the CTA's tile, the warp's share of the blocks of all passes.
+  // A warp's blocks, one after the other. First kernel: items (pass and tile) of the warp, with all of their blocks, or of
+  // the CTA, with every eighth; second: the CTA's tile, and of the blocks of all passes a run (which ends few passes, where
+  // sums change hands).
   const int rank = kGated ? 0 : blockIdx.x % a.splits;
-  const int stride = kGated ? kWarps : kWarps * a.splits;
   const int passes = lists.passes, items = passes * a.tiles;
+  const int first_blk = kGated && !kOwn ? warp : 0, stride = kGated && !kOwn ? kWarps : 1;
+  const int first_item = kOwn ? static_cast<int>(blockIdx.x) * kWarps + warp : static_cast<int>(blockIdx.x);
+  const int item_step = kOwn ? static_cast<int>(gridDim.x) * kWarps : static_cast<int>(gridDim.x);
   struct At {
-    int item, pass, tile, blk;
+    int item, pass, tile, blk;  // item: second kernel: blocks of the run from this one on
   };
-  auto settle = [&](At &w) {  // true where the pass or the tile is another one
-    if (w.blk < a.nblk) return false;
+  auto seek_item = [&](At &w) {
+    w.pass = passes;
+    if (w.item < items) {
+      w.pass = w.item / a.tiles;
+      w.tile = w.item - w.pass * a.tiles;
+    }
+  };
+  auto advance = [&](At &w) {  // to the next block; true where the pass or the tile is another one
+    w.blk += stride;
     if constexpr (kGated) {
-      w.blk = warp;
-      w.item += gridDim.x;
-      if (w.item >= items) {
-        w.pass = passes;
-      } else {
-        w.pass = w.item / a.tiles;
-        w.tile = w.item - w.pass * a.tiles;
-      }
+      if (w.blk < a.nblk) return false;
+      w.blk = first_blk;
+      w.item += item_step;
+      seek_item(w);
     } else {
-      do w.blk -= a.nblk, ++w.pass;
-      while (w.blk >= a.nblk);
+      if (--w.item <= 0) {
+        w.pass = passes;
+        return true;
+      }
+      if (w.blk < a.nblk) return false;
+      w.blk = 0;
+      ++w.pass;
     }
     return true;
   };
-  At have = {static_cast<int>(blockIdx.x), 0, kGated ? 0 : static_cast<int>(blockIdx.x) / a.splits, kGated ? warp : rank * kWarps + warp};
+  At have = {first_item, 0, kGated ? 0 : static_cast<int>(blockIdx.x) / a.splits, first_blk};
   if constexpr (kGated) {
-    have.pass = have.item / a.tiles, have.tile = have.item - have.pass * a.tiles;
-    if (have.item >= items || warp >= a.nblk) have.pass = passes;  // nothing is this warp's
+    seek_item(have);
+    if (first_blk >= a.nblk) have.pass = passes;  // nothing is this warp's
   } else {
-    settle(have);
+    const int64_t all = static_cast<int64_t>(passes) * a.nblk, me = rank * kWarps + warp, of = kWarps * a.splits;
+    const int begin = static_cast<int>(all * me / of);
+    have.item = static_cast<int>(all * (me + 1) / of) - begin;
+    have.pass = have.item > 0 ? begin / a.nblk : passes;
+    have.blk = begin % a.nblk;
   }
 
   // ---- loading. Row r of a tile: 16-row tiles of eight rows of each matrix, or of sixteen of the one.
@@ -263,8 +280,7 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
           ptx::cp_async_16(st + (copy_at ^ ((r >> kSwz) & (CH - 1)) * 16) + r * kPitch, w_row[m] + n * a.row_bytes + at);
         }
       }
-      ahead.blk += stride;
-      if (settle(ahead)) seek();
+      if (advance(ahead)) seek();
     }
     ptx::cp_async_commit();
     fill = fill + 1 == kStages ? 0 : fill + 1;
@@ -358,8 +374,7 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
     for (int i = 0; i < kSW; ++i) s[i] = s_next[i];
 #pragma unroll
     for (int i = 0; i < kZW; ++i) z[i] = z_next[i];
-    have.blk += stride;
-    const bool other = settle(have);
+    const bool other = advance(have);
     if (other) {
       seek_scales(have);
       seek_inputs(have.pass);
@@ -424,7 +439,27 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
     return other;
   };
 
-  if constexpr (kGated) {
+  if constexpr (kOwn) {
+    // gate and up of a hidden column are the same thread's
+    while (have.pass < passes) {
+      const int pass = have.pass, n0 = have.tile * kOut;
+      while (!block()) {
+      }
+      const int first = lists.first[pass], n = min(static_cast<int>(lists.first[pass + 1]) - first, kCols);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (2 * t + i < n) {
+          const int c = first + 2 * t + i;
+          T *const to = reinterpret_cast<T *>(a.y + lists.order[c] * a.ldy) + n0 + g;
+#pragma unroll
+          for (int q = 0; q < RT; ++q) to[8 * q] = from_f32<T>(lists.weight[c] * (act_of(a.act, acc[q][i]) * acc[q][2 + i]));
+        }
+#pragma unroll
+      for (int q = 0; q < RT; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[q][i] = 0.0f;
+    }
+  } else if constexpr (kGated) {
     int buf = 0, turn = 0;
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
       const int pass = item / a.tiles, n0 = (item - pass * a.tiles) * kOut;
@@ -516,21 +551,21 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
   ptx::cp_async_wait<0>();
 }
 
-template <typename T, bool kGated, bool kZeros, int RT, int CH, int CPG>
+template <typename T, bool kGated, bool kOwn, bool kZeros, int RT, int CH, int CPG>
 cudaError_t launch_as(MoeArgs a, cudaStream_t s) {
   using P = Moe<RT, CH, CPG>;
   a.nblk = (a.K + P::KB - 1) / P::KB;
   a.tiles = a.N / (kGated ? 8 * RT : 16 * RT);
   a.s_vec = a.groups % P::kGroups == 0 && (1 << a.group_shift) * P::kGroups == P::KB;
-  constexpr auto kern = moe4_kernel<T, kGated, kZeros, RT, CH, CPG>;
-  const size_t smem = P::smem(kGated, a.M);
+  constexpr auto kern = moe4_kernel<T, kGated, kOwn, kZeros, RT, CH, CPG>;
+  const size_t smem = kOwn ? P::kRing : P::smem(kGated, a.M);
   const cudaError_t e = conv::ensure_smem_attr(reinterpret_cast<const void *>(kern), smem);
   if (e != cudaSuccess) return e;
   const int64_t pairs = static_cast<int64_t>(a.M) * a.topk;
   const int slots = 2 * sm_count();
   a.splits = 1;
   if (kGated) {
-    const int64_t most = pairs * a.tiles;
+    const int64_t most = kOwn ? (pairs * a.tiles + kWarps - 1) / kWarps : pairs * a.tiles;
     return launch_dependent(kern, dim3(static_cast<unsigned>(most < slots ? most : slots)), kThreads, smem, s, 1, a);
   }
   // a tile's blocks over as many CTAs as fill the GPU, while each warp still has a block
@@ -539,21 +574,32 @@ cudaError_t launch_as(MoeArgs a, cudaStream_t s) {
   return launch_dependent(kern, dim3(a.tiles * a.splits), kThreads, smem, s, a.splits, a);
 }
 
-template <typename T, bool kGated, bool kZeros, int RT, int CH>
+template <typename T, bool kGated, bool kOwn, bool kZeros, int RT>
 cudaError_t launch_grouped(const MoeArgs &a, cudaStream_t s) {
-  if (a.group_shift == 5) return launch_as<T, kGated, kZeros, RT, CH, 1>(a, s);
-  if (a.group_shift == 6) return launch_as<T, kGated, kZeros, RT, CH, 2>(a, s);
-  return launch_as<T, kGated, kZeros, RT, CH, 4>(a, s);
+  if (a.group_shift == 5) return launch_as<T, kGated, kOwn, kZeros, RT, 4, 1>(a, s);
+  if (a.group_shift == 6) return launch_as<T, kGated, kOwn, kZeros, RT, 4, 2>(a, s);
+  return launch_as<T, kGated, kOwn, kZeros, RT, 4, 4>(a, s);
 }
 
-// Tiles of 32 rows where there are two for each place of a CTA (second kernel: where the warps of that many get a block),
-// else of 16: inputs are put in order and looked up for twice the weights.
+// First kernel: tiles of 32 rows are a warp's where there are one and a half times as many as warps or more, or three
+// quarters where a CTA's warps would have one block each of a tile (13 tokens, 46 of 64 experts of 2048 x 1408: 82 us a
+// layer, with the CTA's tiles 97; 32 tokens, 32 of 1024 x 1024: 48 and 55; but 4 tokens, 8 of 4096 x 4096: 53 and 46);
+// else the CTA's, of 32 rows (inputs are put in order and looked up for twice the weights: 46 us of the last, of 16 rows
+// 54) where they give every SM four, else of 16. Second: of 32 rows where the warps of twice as many CTAs as fit get a block.
 template <typename T, bool kGated, bool kZeros>
 cudaError_t launch_sized(const MoeArgs &a, cudaStream_t s) {
   const int64_t pairs = static_cast<int64_t>(a.M) * a.topk, experts = pairs < a.E ? pairs : a.E;
-  const int64_t work = kGated ? experts * (a.N / 16) : experts * (a.N / 32) * ((a.K + 127) / 128) / kWarps;
-  return work >= 4 * sm_count() ? launch_grouped<T, kGated, kZeros, 2, 4>(a, s)
-                                : launch_grouped<T, kGated, kZeros, 1, 4>(a, s);
+  if constexpr (kGated) {
+    const int64_t tiles = experts * (a.N / 8), warps = 2 * kWarps * sm_count();
+    const int64_t per_warp = (a.K + 127) / 128 <= kWarps ? 3 * warps / 2 : 3 * warps;  // tiles of eight rows of each matrix
+    if (tiles >= per_warp) return launch_grouped<T, true, true, kZeros, 2>(a, s);
+    if (tiles >= 8 * sm_count()) return launch_grouped<T, true, false, kZeros, 2>(a, s);
+    return launch_grouped<T, true, false, kZeros, 1>(a, s);
+  } else {
+    const int64_t work = experts * (a.N / 32) * ((a.K + 127) / 128) / kWarps;
+    return work >= 4 * sm_count() ? launch_grouped<T, false, false, kZeros, 2>(a, s)
+                                  : launch_grouped<T, false, false, kZeros, 1>(a, s);
+  }
 }
 
 template <typename T>
