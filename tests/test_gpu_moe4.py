@@ -89,7 +89,8 @@ def choose(seed, M, E, topk):
 
 SHAPES = [(1, 64, 32, 1, 1, 32), (1, 2048, 256, 8, 2, 64), (2, 32, 64, 4, 4, 32), (3, 256, 96, 5, 3, 128), (1, 544, 1056, 16, 8, 64),
           (9, 288, 160, 3, 2, 32), (13, 1024, 352, 64, 6, 64), (33, 96, 64, 2, 2, 256), (64, 128, 128, 8, 4, 32),
-          (70, 64, 96, 4, 2, 64), (40, 64, 32, 40, 32, 32), (5, 2080, 2336, 6, 2, 32), (2, 4096, 64, 2, 1, 8192)]
+          (70, 64, 96, 4, 2, 64), (40, 64, 32, 40, 32, 32), (5, 2080, 2336, 6, 2, 32), (2, 4096, 64, 2, 1, 8192),
+          (40, 96, 768, 40, 4, 32), (18, 1056, 928, 64, 4, 64)]  # the last two: tiles that are a warp's
 
 
 @pytest.mark.parametrize("t", [BF16, F16])
@@ -112,7 +113,7 @@ def test_normal_data(samd_lib, shape, zeros, t):
 @pytest.mark.parametrize("t", [BF16, F16])
 @pytest.mark.parametrize("zeros", [None, False, True])
 @pytest.mark.parametrize("word_bits", [32, 64])
-@pytest.mark.parametrize("shape", [(1, 64, 32, 2, 1, 32), (3, 288, 160, 7, 3, 64), (20, 2048, 96, 4, 2, 128), (66, 96, 256, 5, 4, 32)], ids=str)
+@pytest.mark.parametrize("shape", [(1, 64, 32, 2, 1, 32), (3, 288, 160, 7, 3, 64), (20, 2048, 96, 4, 2, 128), (66, 96, 256, 5, 4, 32), (40, 96, 768, 40, 4, 64)], ids=str)
 def test_integers_are_exact(samd_lib, shape, word_bits, zeros, t):
     """One input of a token is 1 or -1, lanes lie within 2 of the zero point, scales are 1/2 .. 2: g and u are at most 4 in
     halves, h (weights of 1/2) at most 8 in eighths, exact in both types; a group's sum of offsets and lanes is at most
