@@ -549,8 +549,8 @@ SAMD_API samd_status samd_cache_evict(const samd_cache *cache, const samd_cache_
  * y: ldy; multiples of 8, else SAMD_EALIGN), F hidden columns; all of `type`
  * (SAMD_F16 or SAMD_BF16). `group` as in samd_matvec_desc. SAMD_EINVAL: another
  * type, act or group; SAMD_ESHAPE: M < 0, E < 1, topk < 1 (or above E, for
- * samd_moe_route), K or F < 1, a stride below its row's length; SAMD_EUNSUP: K or F not a multiple of 32 or
- * above 2^20, E above 1024, topk above 32.
+ * samd_moe_route), K or F < 1, a stride below its row's length; SAMD_EUNSUP: K or
+ * F not a multiple of 32 or above 2^20, E above 1024, topk above 32.
  */
 typedef struct {
   int M, K, F, E, topk, group;

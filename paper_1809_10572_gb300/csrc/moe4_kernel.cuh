@@ -183,7 +183,8 @@ template <typename T, bool kGated, bool kOwn, bool kZeros, int RT, int CH, int C
 __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
   using P = Moe<RT, CH, CPG>;
   constexpr int KB = P::KB, kRows = P::kRows, kPitch = P::kPitch, kStages = P::kStages, kG = P::kGroups;
-  constexpr int kSwz = CH >= 8 ? 0 : 1;            // rows that share a 128-byte line: 2^kSwz
+  static_assert(CH == 4, "a row of a stage is 64 bytes");
+  constexpr int kSwz = 1;                          // rows that share a 128-byte line: 2^kSwz
   constexpr int kOut = kGated ? kRows / 2 : kRows; // rows of a matrix in a tile
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Lists lists;
@@ -302,14 +303,7 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
     const uint16_t *const sp = s_base + s_row + grp;
     const uint8_t *const zp = z_base + s_row + grp;
     if (kG > 1 && a.s_vec) {
-      if constexpr (kG == 8) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(sp);
-        s[0] = v.x, s[1] = v.y, s[2] = v.z, s[3] = v.w;
-        if constexpr (kZeros) {
-          const uint2 q = *reinterpret_cast<const uint2 *>(zp);
-          z[0] = q.x, z[1] = q.y;
-        }
-      } else if constexpr (kG == 4) {
+      if constexpr (kG == 4) {
         const uint2 v = *reinterpret_cast<const uint2 *>(sp);
         s[0] = v.x, s[1] = v.y;
         if constexpr (kZeros) z[0] = *reinterpret_cast<const uint32_t *>(zp);
