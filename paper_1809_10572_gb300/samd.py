@@ -1113,9 +1113,6 @@ def _three(w):
 def moe_layer4(x, router, topk: int, gate, up, down, group: int, f: samd_fmt, act="silu", normalize: bool = True, out=None,
                workspace=None, stream=None):
     """A whole layer of experts: moe_route, and moe4 on its choice."""
-    if workspace is not None:
-        ids, weights = moe_route(x, router, topk, normalize, stream=stream)
-        return moe4(x, ids, weights, gate, up, down, group, f, act, out, workspace, stream)
     M, K = x.shape
     E, F = _experts4(gate, up, down, K, group, f, x.dtype)
     _check_router(router, x, topk)
@@ -1124,10 +1121,12 @@ def moe_layer4(x, router, topk: int, gate, up, down, group: int, f: samd_fmt, ac
     d = _moe_desc(x, E, topk, F, group, K if out is None else _ld8(out, "out", M, K, x.dtype), act)
     if out is None:
         out = _new(x, (M, K), x.dtype, stream)
-    # the choice and the layer's workspace in one allocation
+    # the choice and, where the caller has none, the layer's workspace in one allocation
     part = -(-4 * M * topk // 128) * 128
-    buf = _new(x, (2 * part + samd_moe4_workspace_size(d),), torch.uint8, stream)
-    at = _address(buf)
+    buf = _new(x, (2 * part + (samd_moe4_workspace_size(d) if workspace is None else 0),), torch.uint8, stream)
+    at, nb = _address(buf), None
+    if workspace is None:
+        workspace, nb = at + 2 * part, buf.numel() - 2 * part
     samd_moe_route(d, normalize, x, router, at, at + part, stream)
-    samd_moe4(d, f, x, at, at + part, _three(gate), _three(up), _three(down), out, at + 2 * part, buf.numel() - 2 * part, stream)
+    samd_moe4(d, f, x, at, at + part, _three(gate), _three(up), _three(down), out, workspace, nb, stream)
     return out
