@@ -966,7 +966,8 @@ def cache_read(cache: PagedCache, tokens: int, table, lengths, starts=None, k=No
 
 @functools.lru_cache(maxsize=1024)
 def _attention_workspace(device: int, pages, page, heads, dim, bits, seqs, max_pages, q_heads, scores) -> int:
-    """Bytes of workspace by sizes alone: they are the same for every layer of a model."""
+    """Bytes of workspace by the current device, whose SMs the library goes by, and sizes alone: they are the same for
+    every layer of a model."""
     c = samd_cache(pages, page, heads, dim, cache_fmt(bits), SAMD_F16, None, None, None, None)
     return samd_paged_attention_workspace_size(c, samd_cache_seqs(seqs, max_pages, max_pages, None, None), q_heads, scores)
 
@@ -989,8 +990,8 @@ def paged_attention(q, cache: PagedCache, table, lengths, scale: float | None = 
         ldo = _token_rows(out, "out", q_heads, dim, q.dtype, seqs)
     nb = None
     if workspace is None:
-        nb = _attention_workspace(q.get_device(), cache._desc.pages, cache.page, heads, dim, cache.bits, seqs, s.max_pages, q_heads,
-                                  ld_scores > 0)
+        nb = _attention_workspace(torch.cuda.current_device(), cache._desc.pages, cache.page, heads, dim, cache.bits, seqs,
+                                  s.max_pages, q_heads, ld_scores > 0)
         workspace = _new(q, (nb,), torch.uint8, stream) if nb else None
     samd_paged_attention(cache._desc, s, q_heads, q, ldq, dim ** -0.5 if scale is None else scale, out, ldo,
                          scores if ld_scores else None, ld_scores, workspace, nb, stream)

@@ -20,3 +20,26 @@ def test_a_layers_router_has_as_many_rows_as_there_are_experts():
                 samd.moe_layer4(x, torch.zeros((rows, K), dtype=t), 2, *mats, G, samd.fmt(4, True), workspace=workspace)
         with pytest.raises(ValueError, match="device"):  # as many: nothing is wrong but that it all lies on the host
             samd.moe_layer4(x, torch.zeros((E, K), dtype=t), 2, *mats, G, samd.fmt(4, True), workspace=workspace)
+
+
+def test_the_attentions_workspace_is_the_current_devices(monkeypatch):
+    """Its size goes by the current device's SMs, as the library's call does, wherever q lies."""
+    given = []
+    current = [0]
+    monkeypatch.setattr(samd, "_address", lambda t: 16)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(samd, "samd_paged_attention_workspace_size", lambda *a: 128 * (current[0] + 1))
+    monkeypatch.setattr(samd, "samd_paged_attention", lambda *a: given.append(a[-2]))
+    samd._attention_workspace.cache_clear()
+
+    def meta(*shape, dtype=torch.int32):
+        return torch.empty(shape, dtype=dtype, device="meta")
+
+    t = torch.bfloat16
+    lanes, scales = meta(4, 2, 16, 16), meta(4, 2, 16, 2, dtype=t)
+    cache = samd.PagedCache(lanes, scales, lanes, scales)
+    for device in (0, 1, 0, 1):
+        current[0] = device
+        samd.paged_attention(meta(3, 4, 64, dtype=t), cache, meta(3, 40), meta(3))
+    samd._attention_workspace.cache_clear()
+    assert given == [128, 256, 128, 256]
