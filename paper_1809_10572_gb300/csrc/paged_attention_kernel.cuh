@@ -23,7 +23,7 @@
 // when a weight passes 2^15 (nine doublings later), so that a step's common
 // path has no reduction over tokens. Weights below 2^-30 of the largest seen
 // are rounded at 2^-31 of it. Logits, weights' sums and outputs are in fp32.
-// (Scales outside 2^-90 .. 2^110 are taken for the nearer bound in ref: values
+// (Scales outside 2^-80 .. 2^110 are taken for the nearer bound in ref: values
 // that small are lost, values that large may come out infinite.)
 //
 // Layout: a warp takes 16 tokens (one step, never more than one page) through a
@@ -345,10 +345,15 @@ __device__ __forceinline__ float scale_at(const uint32_t *w, int g) {
   return g & 1 ? f.y : f.x;
 }
 
-// log2 of a scale's magnitude, rounded down, within -90 .. 110.
+// The least scale that moves a reference, and what smaller ones (a row of zeros) count as. Both where overflow is looked
+// for and where the reference goes: a weight is then 2^95 at most, and 2^30 of them stay within fp32.
+constexpr int kLeast = -80;
+constexpr float kLeastScale = 8.271806125530277e-25f;  // 2^kLeast
+
+// log2 of a scale's magnitude, rounded down, within kLeast .. 110.
 __device__ __forceinline__ float log2_down(float s) {
   const int e = static_cast<int>((__float_as_uint(s) & 0x7FFFFFFFu) >> 23) - 127;
-  return static_cast<float>(e < -90 ? -90 : e > 110 ? 110 : e);
+  return static_cast<float>(e < kLeast ? kLeast : e > 110 ? 110 : e);
 }
 
 template <typename T, int NB, int BITS>
@@ -584,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
             x[2 * r] = x[2 * r + 1] = -INFINITY;
           }
       }
-      float vs[2][NB], vmax[2] = {0.0f, 0.0f};
+      float vs[2][NB], vmax[2] = {kLeastScale, kLeastScale};
 #pragma unroll
       for (int r = 0; r < 2; ++r)
 #pragma unroll

@@ -1,0 +1,100 @@
+"""samd_paged_attention on finite values of every range, and on infinities, against its definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import cache_ref as ref
+from paper_1809_10572_gb300 import samd
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16 = torch.bfloat16, torch.float16
+PAGE = 16
+
+
+def one_sequence(kl, ks, vl, vs, bits, width=0):
+    """(cache, table, lengths, key values, value values in pages) of one sequence whose rows are given as (heads, tokens,
+    ..); slots behind it have NaN scales. width: entries of the table at least (those behind the sequence name no page);
+    with more than 16 of 16 tokens a head is dealt out over CTAs."""
+    n = kl.shape[1]
+
+    def paged(x, fill):
+        more = x.new_full((x.shape[0], -n % PAGE, x.shape[2]), fill)
+        return torch.cat((x, more), 1).unflatten(1, (-1, PAGE)).transpose(0, 1).contiguous()
+
+    kl, ks, vl, vs = paged(kl, 3), paged(ks, math.nan), paged(vl, 3), paged(vs, math.nan)
+    table = torch.full((1, max(width, kl.shape[0])), -1, dtype=torch.int32, device="cuda")
+    table[0, :kl.shape[0]] = torch.arange(kl.shape[0])
+    cache = samd.PagedCache(ref.pack(kl, bits), ks, ref.pack(vl, bits), vs)
+    return cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), ref.values(kl, ks), ref.values(vl, vs)
+
+
+def check(got, q, n, k, v, scale, t, scores=None, before=None):
+    """Of one sequence. A weight below 2^-126 of the largest is 0 in fp32: n times that of the largest value at most."""
+    kb, vb = (x.transpose(0, 1).flatten(1, 2)[:, :n] for x in (k, v))
+    want, p, x = ref.attention(q[0], kb, vb, scale)
+    bound, delta = ref.attention_bound(q[0], kb, vb, scale, p, x, want, t)
+    bound = bound + n * 2.0 ** -126 * vb.abs().max()
+    err = (got[0].double() - want).abs()
+    assert (err <= bound).all(), float((err / bound).max())
+    if scores is not None:
+        group = q.shape[1] // kb.shape[0]
+        w = p.view(kb.shape[0], group, n)
+        total = before[0, :, :n].double() + w.sum(1)
+        # a weight's error twice (its own, the sum's), the sums over n and over the group, one addition to the old
+        lim = (w * (2 * delta.view(-1, group, 1) + (n / 16 + 64 + group) * 2.0 ** -23)).sum(1) + group * 2.0 ** -126
+        assert ((scores[0, :, :n].double() - total).abs() <= lim + 2.0 ** -24 * (total + lim)).all()
+        assert torch.equal(scores[0, :, n:], before[0, :, n:])
+
+
+def rising(steps, heads, dim, bits, t, rise):
+    """Keys and a scale that make the logits `rise` times `steps` (0 .. 1, a token each) for a query of 1 in element 0."""
+    most = 2 ** (bits - 1) - 1
+    kl = torch.zeros((heads, len(steps), dim), dtype=torch.int64, device="cuda")
+    kl[:, :, 0] = torch.round(most * steps).long()
+    return kl, torch.ones((heads, len(steps), dim // 32), dtype=t, device="cuda"), rise / most
+
+
+@pytest.mark.parametrize("t", [BF16, F16])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("rise", [15, 22, 40, 88, 100, 180])
+@pytest.mark.parametrize("zero", ["all", "front", "all but the last", "odd"])
+def test_rows_of_zero_values(samd_lib, zero, rise, bits, t):
+    """Values that are zero in whole rows, while the logits rise along the sequence by `rise` in all: such tokens weigh as
+    much as others, and the sum of weights stays finite."""
+    heads, dim, n = 2, 64, 333
+    kl, ks, scale = rising(torch.linspace(0, 1, n, device="cuda"), heads, dim, bits, t, rise)
+    vl, vs = ref.random_rows(3, (heads, n), dim, bits, t)
+    at = torch.arange(n, device="cuda")
+    gone = {"all": at >= 0, "front": at < 300, "all but the last": at < n - 1, "odd": at % 2 == 1}[zero]
+    vl[:, gone], vs[:, gone] = 0, 0.0
+    cache, table, lens, k, v = one_sequence(kl, ks, vl, vs, bits)
+    q = torch.zeros((1, 6, dim), dtype=t, device="cuda")
+    q[0, :, 0] = torch.tensor([1, 0.75, 0.5, 0.25, -1, 0.125])
+    scores = torch.rand((1, heads, n + 3), generator=ref.gen(4)).cuda()
+    before = scores.clone()
+    got = samd.paged_attention(q, cache, table, lens, scale=scale, scores=scores)
+    check(got, q, n, k, v, scale, t, scores, before)
+    assert torch.equal(got, samd.paged_attention(q, cache, table, lens, scale=scale))
+
+
+@pytest.mark.parametrize("t", [BF16, F16])
+@pytest.mark.parametrize("width", [0, 20])
+@pytest.mark.parametrize("last", [31.0, 60.0])
+@pytest.mark.parametrize("runs", [1, 4])
+def test_zero_values_before_the_first_that_are_not(samd_lib, runs, last, width, t):
+    """Logits in units of log2: tokens with zero values at 0, as many at 31.5, then some with values: every partial sum of
+    weights is far within fp32 for any reference near the largest logit."""
+    dim, n = 64, 48 * runs
+    run = torch.arange(n, device="cuda") // (16 * runs)
+    kl, ks, scale = rising(torch.tensor([0.0, 31.5, last], device="cuda")[run] * 2 / 127, 1, dim, 8, t, 127 / 2 * math.log(2))
+    vl = torch.ones((1, n, dim), dtype=torch.int64, device="cuda")
+    vs = torch.ones((1, n, 2), dtype=t, device="cuda")
+    vl[:, run < 2], vs[:, run < 2] = 0, 0.0
+    cache, table, lens, k, v = one_sequence(kl, ks, vl, vs, 8, width)
+    q = torch.zeros((1, 1, dim), dtype=t, device="cuda")
+    q[..., 0] = 1
+    scores = torch.zeros((1, 1, n), device="cuda")
+    got = samd.paged_attention(q, cache, table, lens, scale=scale, scores=scores)
+    check(got, q, n, k, v, scale, t, scores, torch.zeros_like(scores))
