@@ -512,7 +512,8 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
 #pragma unroll
         for (int i = 0; i < kQ / 2; ++i)  // the word's pairs: lanes (i, i + half of them)
           qb[u][i] = pack2<__half>(f[u][i] * up0 * up1, f[u][i + kQ / 2] * up0 * up1);
-      const float m = a.scale * down * down1;
+      // (an infinity: all logits are NaNs, also where the products would be infinities of one sign)
+      const float m = top <= 3.402823466e38f ? a.scale * down * down1 : NAN;
       mult[0] = __shfl_sync(0xffffffffu, m, 8 * t);
       mult[1] = __shfl_sync(0xffffffffu, m, 8 * t + 4);
     }

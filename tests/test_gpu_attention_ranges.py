@@ -98,3 +98,26 @@ def test_zero_values_before_the_first_that_are_not(samd_lib, runs, last, width, 
     scores = torch.zeros((1, 1, n), device="cuda")
     got = samd.paged_attention(q, cache, table, lens, scale=scale, scores=scores)
     check(got, q, n, k, v, scale, t, scores, torch.zeros_like(scores))
+
+
+@pytest.mark.parametrize("t", [BF16, F16])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+@pytest.mark.parametrize("n,width", [(1, 0), (1, 20), (40, 0), (40, 20), (700, 0)])
+def test_an_infinity_in_q_gives_nans(samd_lib, n, width, value, bits, t):
+    """Also where the keys' lanes at its element have one sign, so that all products are infinities of one sign."""
+    heads, dim = 2, 64
+    kl, ks = ref.random_rows(11, (heads, n), dim, bits, t)
+    vl, vs = ref.random_rows(13, (heads, n), dim, bits, t)
+    q = ref.normal(15, (1, 4, dim), t)
+    for lane in (-3, 3):
+        kl[:, :, 5] = lane
+        cache, table, lens, *_ = one_sequence(kl, ks, vl, vs, bits, width)
+        clean, hit = q.clone(), q.clone()
+        hit[0, 1, 5] = value
+        scores = torch.zeros((2, 1, heads, n), device="cuda")
+        a = samd.paged_attention(clean, cache, table, lens, scores=scores[0])
+        b = samd.paged_attention(hit, cache, table, lens, scores=scores[1])
+        assert torch.isnan(b[0, 1]).all() and torch.isnan(scores[1, 0, 0]).all()
+        assert torch.equal(a[0, [0, 2, 3]], b[0, [0, 2, 3]]) and torch.equal(scores[0, 0, 1], scores[1, 0, 1])
+        assert torch.isfinite(a).all() and torch.isfinite(scores[0]).all()
