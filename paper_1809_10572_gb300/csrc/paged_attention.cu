@@ -205,7 +205,7 @@ cudaError_t launch_paged_attention(const samd_cache &c, const samd_cache_seqs &s
   a.ks = static_cast<const uint8_t *>(c.k_scales), a.vs = static_cast<const uint8_t *>(c.v_scales);
   a.q = static_cast<const uint8_t *>(q), a.out = static_cast<uint8_t *>(out);
   a.ldq = ldq * 2, a.ldo = ldo * 2;
-  a.scale = scale * 1.4426950408889634f;
+  a.scale = scale;
   a.heads = c.heads, a.group = q_heads / c.heads;
   a.page_rows = static_cast<uint32_t>(c.heads) * static_cast<uint32_t>(c.page);
   a.parts = p.parts, a.per = p.per, a.slots = p.slots, a.whole = p.whole;

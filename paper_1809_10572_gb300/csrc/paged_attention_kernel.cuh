@@ -72,7 +72,7 @@ struct AttArgs {
   const uint8_t *q;
   uint8_t *out;
   int64_t ldq, ldo;  // bytes
-  float scale;       // with log2(e)
+  float scale;
   int heads;         // of keys
   uint32_t page_rows;  // rows of a page: heads x slots
   int group;         // query heads of a key head
@@ -513,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
         for (int i = 0; i < kQ / 2; ++i)  // the word's pairs: lanes (i, i + half of them)
           qb[u][i] = pack2<__half>(f[u][i] * up0 * up1, f[u][i + kQ / 2] * up0 * up1);
       // (an infinity: all logits are NaNs, also where the products would be infinities of one sign)
-      const float m = top <= 3.402823466e38f ? a.scale * down * down1 : NAN;
+      const float m = top <= 3.402823466e38f ? a.scale * down * down1 * 1.4426950408889634f : NAN;
       mult[0] = __shfl_sync(0xffffffffu, m, 8 * t);
       mult[1] = __shfl_sync(0xffffffffu, m, 8 * t + 4);
     }

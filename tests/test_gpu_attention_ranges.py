@@ -121,3 +121,15 @@ def test_an_infinity_in_q_gives_nans(samd_lib, n, width, value, bits, t):
         assert torch.isnan(b[0, 1]).all() and torch.isnan(scores[1, 0, 0]).all()
         assert torch.equal(a[0, [0, 2, 3]], b[0, [0, 2, 3]]) and torch.equal(scores[0, 0, 1], scores[1, 0, 1])
         assert torch.isfinite(a).all() and torch.isfinite(scores[0]).all()
+
+
+@pytest.mark.parametrize("scale", [3e38, -3.4e38])
+def test_scales_next_to_the_largest_float(samd_lib, scale):
+    """log2(e) times them is past fp32; with a small q the logits are ordinary numbers."""
+    heads, dim, n, t = 2, 64, 300, BF16
+    kl, ks = ref.random_rows(21, (heads, n), dim, 8, t)
+    vl, vs = ref.random_rows(23, (heads, n), dim, 8, t)
+    cache, table, lens, k, v = one_sequence(kl, ks, vl, vs, 8)
+    q = ref.normal(25, (1, 4, dim), torch.float64).mul_(2.0 ** -126).to(t)
+    got = samd.paged_attention(q, cache, table, lens, scale=scale)
+    check(got, q, n, k, v, torch.tensor(scale).float().item(), t)
