@@ -17,14 +17,19 @@
 // largest magnitude to 2^13 .. 2^14: bfloat16's eight and fp16's eleven bits are
 // kept, what lies 2^-27 below the largest is rounded at 2^-38 of it). The sums
 // of 32 elements are scaled in fp32. For the second product the weight of a
-// token and the scale of its 32 values go together, p = 2^(x - ref) s, rounded
-// once to fp16 (2^-11, as a result in fp16 is). ref is a running
-// reference of each head: the largest x + log2 s seen, less 6; it moves only
-// when a weight passes 2^15 (nine doublings later), so that a step's common
-// path has no reduction over tokens. Weights below 2^-30 of the largest seen
-// are rounded at 2^-31 of it. Logits, weights' sums and outputs are in fp32.
-// (Scales outside 2^-80 .. 2^110 are taken for the nearer bound in ref: values
-// that small are lost, values that large may come out infinite.)
+// token and the scale of its 32 values go together, p = 2^(x - ref + up) s,
+// rounded once to fp16 (2^-11, as a result in fp16 is; in 16 bits because the
+// lanes are the MMA's other operand). ref is a running reference of each head,
+// the largest x rounded up to an integer; up belongs to a head and a block of 32
+// elements, and brings the block's largest weight times scale to 2^6 .. 2^7, so
+// that an output keeps its bits whatever lies in other elements of the rows and
+// in other heads. Both move only when a p passes 2^15 (nine doublings later) or
+// a weight 2^16, so that a step's common path has no reduction over tokens; being
+// integers, they move the sums by powers of two, exactly. Of a block's weights
+// times scales those below 2^-20 of the largest are rounded at 2^-31 of it. Logits,
+// weights' sums and outputs are in fp32: weights below 2^-126 of the largest are
+// 0. (up ends at 2^120: values' scales below 2^-114 lose bits. Sums of values above
+// 2^115 may pass fp32, and keys' scales above 2^100 in a logit.)
 //
 // Layout: a warp takes 16 tokens (one step, never more than one page) through a
 // ring of its own in shared memory, filled by cp.async of 16 bytes a lane; rows
@@ -65,6 +70,8 @@ constexpr int kMinSteps = kWarps;  // a CTA is not used for fewer, unless a head
 // other. Counted when steps are dealt out, 53 sequences of up to 4001 tokens and 12 heads take 59 us, without 71; 16 of up
 // to 8192 38 and 42 (14 to 40 are within 3% of each other there; long sequences in 4 bits lose 5% from 20 on).
 constexpr int kHeadCost = 16;
+constexpr int kMostUp = 120;             // largest power of a block's weights (log2)
+constexpr float kMostWeight = 65536.0f;  // a weight above it moves the reference, whatever its values are
 
 struct AttArgs {
   Seqs s;
@@ -345,15 +352,15 @@ __device__ __forceinline__ float scale_at(const uint32_t *w, int g) {
   return g & 1 ? f.y : f.x;
 }
 
-// The least scale that moves a reference, and what smaller ones (a row of zeros) count as. Both where overflow is looked
-// for and where the reference goes: a weight is then 2^95 at most, and 2^30 of them stay within fp32.
-constexpr int kLeast = -80;
-constexpr float kLeastScale = 8.271806125530277e-25f;  // 2^kLeast
-
-// log2 of a scale's magnitude, rounded down, within kLeast .. 110.
-__device__ __forceinline__ float log2_down(float s) {
-  const int e = static_cast<int>((__float_as_uint(s) & 0x7FFFFFFFu) >> 23) - 127;
-  return static_cast<float>(e < kLeast ? kLeast : e > 110 ? 110 : e);
+// 2^n, 0 below fp32's normal range (n up to 127).
+__device__ __forceinline__ float power_of_two(int n) { return n < -126 ? 0.0f : __int_as_float((127 + n) << 23); }
+// The power of two at or below a magnitude (subnormal ones and 0: 2^-127).
+__device__ __forceinline__ int log2_down(float v) { return static_cast<int>((__float_as_uint(v) & 0x7FFFFFFFu) >> 23) - 127; }
+// The larger magnitude in both halves, under any sign; NaN where either is one.
+__device__ __forceinline__ uint32_t max_abs_h2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
 }
 
 template <typename T, int NB, int BITS>
@@ -366,6 +373,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   __shared__ int64_t tmp[2 * kWarps + 2];
   __shared__ float2 red_stat[kWarps][kHeads];  // references and sums of weights
   __shared__ float *red_at[kWarps];            // the warps' sums
+  __shared__ Walk walks[2][kWarps];            // where a warp's loads are, and its sums
   // (the warp's number by a shuffle: what follows from it is the same in all lanes, and the compiler knows)
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t = lane & 3;
   const Powers<BITS> power;
@@ -396,31 +404,37 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   for (int i = 0; i < kCopies; ++i) copy_at[i] = P::at((i * 32 + lane) / kUnits, (i * 32 + lane) % kUnits);
   const uint8_t *const k_lane = a.k + lane * 16, *const v_lane = a.v + lane * 16;
   const uint8_t *const s_lane = lane < 2 * NB ? a.ks + lane * 16 : a.vs + (lane - 2 * NB) * 16;  // (lanes below 4 NB)
-  Walk ahead = have;
-  int l_step = ahead.first + warp, fill = 0, slot_used = 0;
+  // (what a step has no use for lies in shared memory: the loop has no register left)
+  Walk *const ahead = &walks[0][warp], *const kept = &walks[1][warp];
+  if (lane == 0) *ahead = have;
+  __syncwarp();
+  int l_step = have.first + warp, l_last = have.last, fill = 0, slot_used = 0;
   uint32_t missing = 0;  // bit of a stage: its page is none of the cache's
   int l_pages = -1, l_turn = 0;  // pages of the warp's next 32 steps, a step a lane; which of them is next
   uint32_t head_rows = 0;  // of a page, before the key head in hand
   // brings `ahead` and l_step to the next step of this warp, and asks for its page, which the next load waits for
   auto seek = [&]() {
+    if (l_step < l_last && l_turn < 32) return;
+    Walk w = *ahead;
     bool fresh = false;
-    while (l_step >= ahead.last) {
-      const int was = ahead.b * a.heads + ahead.h;
-      ahead.next(a);
-      if (a.whole ? was + a.slots >= a.s.seqs * a.heads : !ahead.on()) {
-        ahead.last = ahead.first = 0;
+    while (l_step >= w.last) {
+      const int was = w.b * a.heads + w.h;
+      w.next(a);
+      if (a.whole ? was + a.slots >= a.s.seqs * a.heads : !w.on()) {
         l_step = -1;
         return;
       }
-      l_step = ahead.first + warp;
+      l_step = w.first + warp;
       fresh = true;
     }
-    if (fresh || l_turn == 32) {
-      head_rows = static_cast<uint32_t>(ahead.h) << a.s.page_shift;
-      const int step = l_step + kWarps * lane;
-      l_pages = step < ahead.last ? page_of(a.s, ahead.b, static_cast<int64_t>(step) * kStep) : -1;
-      l_turn = 0;
-    }
+    __syncwarp();
+    if (fresh && lane == 0) *ahead = w;
+    __syncwarp();
+    l_last = w.last;
+    head_rows = static_cast<uint32_t>(w.h) << a.s.page_shift;
+    const int step = l_step + kWarps * lane;
+    l_pages = step < w.last ? page_of(a.s, w.b, static_cast<int64_t>(step) * kStep) : -1;
+    l_turn = 0;
   };
   auto load_next = [&]() {
     if (l_step >= 0) {
@@ -481,10 +495,8 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   auto goes_on = [&](const Walk &w) { return a.whole ? w.b * a.heads + w.h < total_units : w.on(); };
   if (goes_on(have)) load_q(have);
   while (goes_on(have)) {
-    const int unit = have.b * a.heads + have.h;
-    const int head0 = have.h * a.group + part * a.per;  // the CTA's first query head
-    const int n_heads = min(a.per, a.group - part * a.per);
     const int len = static_cast<int>(length_of(a.s, have.b));
+    float *const logits = a.logits ? a.logits + ((static_cast<int64_t>(have.b * a.heads + have.h) * a.parts + part) * span_tokens + g) * kHeads + 2 * t : nullptr;
 
     // q of head g in the MMA's order, in fp16 under a power of two
     uint32_t qb[kUnits][16 / BITS];  // pairs of a unit of 16 bytes: 2 (8 bits) or 4 (4 bits) words
@@ -519,13 +531,20 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
     }
 
     float o[kTiles][4], ref[2] = {kLow, kLow}, sum[2] = {0.0f, 0.0f};
+    float up[NB][2];  // 2^up of every block, for each of the two heads
+#pragma unroll
+    for (int i = 0; i < NB; ++i) up[i][0] = up[i][1] = power_of_two(kMostUp);
 #pragma unroll
     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
 
+    const int last = have.last;
+    int step = have.first + warp;
+    if (lane == 0) *kept = have;
+    __syncwarp();
 #pragma unroll 1
-    for (int step = have.first + warp; step < have.last; step += kWarps) {
+    for (; step < last; step += kWarps) {
       ptx::cp_async_wait<kStages - 2>();
       __syncwarp();  // every lane's copies are in, and the stage filled next has been read by every lane
       const bool gone = (missing >> slot_used & 1) != 0;
@@ -590,16 +609,8 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
             x[2 * r] = x[2 * r + 1] = -INFINITY;
           }
       }
-      float vs[2][NB], vmax[2] = {kLeastScale, kLeastScale};
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-          vs[r][i] = scale_at<T>(vw[r], i);
-          vmax[r] = fmaxf(vmax[r], fabsf(vs[r][i]));
-        }
-      if (a.logits) {
-        float *const lp = a.logits + ((static_cast<int64_t>(unit) * a.parts + part) * span_tokens + tok) * kHeads + 2 * t;
+      if (logits) {
+        float *const lp = logits + static_cast<int64_t>(step) * (kStep * kHeads);
         *reinterpret_cast<float2 *>(lp) = make_float2(x[0], x[1]);
         *reinterpret_cast<float2 *>(lp + 8 * kHeads) = make_float2(x[2], x[3]);
       }
@@ -607,29 +618,69 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       float e[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) e[j] = exp2_of(x[j] - ref[j & 1]);
-      const bool past = !(fmaxf(e[0], e[1]) * vmax[0] <= 32768.0f) || !(fmaxf(e[2], e[3]) * vmax[1] <= 32768.0f);
-      if (__any_sync(0xffffffffu, past)) {
-        bool over[2];
+      uint32_t w[NB][2];  // weights times scales, of the thread's two tokens
+      auto weigh = [&]() {
+        uint32_t most[NB];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) over[c] = !(e[c] * vmax[0] <= 32768.0f) || !(e[2 + c] * vmax[1] <= 32768.0f);
-        float top[2];
+        for (int i = 0; i < NB; ++i) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          top[c] = fmaxf(x[c] + log2_down(vmax[0]), x[2 + c] + log2_down(vmax[1])) - 6.0f;
-          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 4));
-          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 8));
-          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 16));
-          // (of this head's column alone: a head's bits do not depend on its neighbours)
-          const bool moves = (__ballot_sync(0xffffffffu, over[c]) & 0x11111111u << t) != 0;
-          top[c] = moves ? fmaxf(top[c], ref[c]) : ref[c];
-          const float f = exp2_of(ref[c] - top[c]);
-          ref[c] = top[c];
-          sum[c] *= f;
-#pragma unroll
-          for (int i = 0; i < kTiles; ++i) o[i][c] *= f, o[i][2 + c] *= f;
+          for (int r = 0; r < 2; ++r) {
+            const float s = scale_at<T>(vw[r], i);
+            w[i][r] = pack2<__half>(e[2 * r] * s * up[i][0], e[2 * r + 1] * s * up[i][1]);
+          }
+          most[i] = max_abs_h2(w[i][0], w[i][1]);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) e[j] = exp2_of(x[j] - ref[j & 1]);
+        for (int n = 1; n < NB; n *= 2)
+#pragma unroll
+          for (int i = 0; i + n < NB; i += 2 * n) most[i] = max_abs_h2(most[i], most[i + n]);
+        return most[0] & 0x7FFF7FFFu;
+      };
+      const uint32_t most = weigh();
+      // (a half above 2^15 carries into its sign)
+      const bool past = ((most + 0x07FF07FFu) & 0x80008000u) != 0 ||
+                        fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])) > kMostWeight;
+      if (__any_sync(0xffffffffu, past)) {
+        int by[2];
+        bool moves[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          // (of this head's column alone: a head's bits do not depend on its neighbours)
+          const bool over = (most >> 16 * c & 0x7FFFu) > 0x7800u || fmaxf(e[c], e[2 + c]) > kMostWeight;
+          moves[c] = (__ballot_sync(0xffffffffu, over) & 0x11111111u << t) != 0;
+          float top = fmaxf(x[c], x[2 + c]);
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+          top = moves[c] ? fmaxf(ceilf(top), ref[c]) : ref[c];
+          const float far = top - ref[c];
+          by[c] = far < 512.0f ? static_cast<int>(far) : 512;
+          ref[c] = top;
+          sum[c] *= power_of_two(-by[c]);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) e[2 * r + c] = exp2_of(x[2 * r + c] - top);
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          uint32_t sizes = 0;  // exponents of the largest weight times scale, of both heads
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            sizes |= static_cast<uint32_t>(log2_down(fmaxf(fabsf(e[c] * scale_at<T>(vw[0], i)), fabsf(e[2 + c] * scale_at<T>(vw[1], i)))) + 127) << 16 * c;
+          sizes = __vmaxu2(sizes, __shfl_xor_sync(0xffffffffu, sizes, 4));
+          sizes = __vmaxu2(sizes, __shfl_xor_sync(0xffffffffu, sizes, 8));
+          sizes = __vmaxu2(sizes, __shfl_xor_sync(0xffffffffu, sizes, 16));
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            // what the block's power is under the new reference, and with it what its sums are worth
+            const int had = log2_down(up[i][c]) + by[c], size = static_cast<int>(sizes >> 16 * c & 0xFFFFu) - 127;
+            int now = had < kMostUp ? had : kMostUp;
+            if (moves[c] && size + now >= 15) now = 6 - size;
+            up[i][c] = power_of_two(now);
+            const float f = power_of_two(now - had);
+            o[2 * i][c] *= f, o[2 * i][2 + c] *= f, o[2 * i + 1][c] *= f, o[2 * i + 1][2 + c] *= f;
+          }
+        }
+        weigh();
       }
       sum[0] += e[0] + e[2];
       sum[1] += e[1] + e[3];
@@ -638,8 +689,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       uint32_t r[4];
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
-        const uint32_t b0 = transpose8x8(pack2<__half>(e[0] * vs[0][blk], e[1] * vs[0][blk]));
-        const uint32_t b1 = transpose8x8(pack2<__half>(e[2] * vs[1][blk], e[3] * vs[1][blk]));
+        const uint32_t b0 = transpose8x8(w[blk][0]), b1 = transpose8x8(w[blk][1]);
         if (BITS == 8 || (blk & 1) == 0) ldsm4_trans(pair_at(st, 1, BITS == 8 ? blk : blk / 2), r);
         uint32_t lo[16 / BITS], hi[16 / BITS];
         if constexpr (BITS == 8) {
@@ -658,6 +708,10 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       }
     }
 
+    have = *kept;
+    const int unit = have.b * a.heads + have.h;
+    const int head0 = have.h * a.group + part * a.per;  // the CTA's first query head
+    const int n_heads = min(a.per, a.group - part * a.per);
     Walk then = have;
     then.next(a);
     if (goes_on(then)) load_q(then);  // on its way while the warps join
@@ -668,6 +722,12 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 4);
       sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 8);
       sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 16);
+      // the sum of weights to 1 .. 2, and the blocks' powers off: what is left is the size of values, in any scales
+      const int size = sum[c] > 0.0f ? log2_down(sum[c]) : 0;
+      ref[c] += static_cast<float>(size);
+      sum[c] *= power_of_two(-size);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) up[i][c] = power_of_two(-size - log2_down(up[i][c]));
     }
     if (g == 0) {
 #pragma unroll
@@ -684,7 +744,7 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       for (int j = 0; j < 4; ++j) {
         // row g (and g + 8) of tile i is this element
         const int d = BITS == 8 ? 16 * i + 2 * g + (j >> 1) : 32 * (i / 2) + 4 * g + 2 * (i & 1) + (j >> 1);
-        red[(2 * t + (j & 1)) * kDim + d] = o[i][j];
+        red[(2 * t + (j & 1)) * kDim + d] = o[i][j] * up[i / 2][j & 1];
       }
     __syncthreads();
     const bool first_part = have.first == 0, last_part = have.last == have.steps;

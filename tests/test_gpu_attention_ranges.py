@@ -30,14 +30,19 @@ def one_sequence(kl, ks, vl, vs, bits, width=0):
     return cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), ref.values(kl, ks), ref.values(vl, vs)
 
 
-def check(got, q, n, k, v, scale, t, scores=None, before=None):
-    """Of one sequence. A weight below 2^-126 of the largest is 0 in fp32: n times that of the largest value at most."""
+def check(got, q, n, k, v, scale, t, scores=None, before=None, own=False):
+    """Of one sequence; own: every output against its own block's magnitudes, so that what lies in other elements of the
+    rows does not count. A weight below 2^-126 of the largest is 0 in fp32: n times that of the largest value at most."""
     kb, vb = (x.transpose(0, 1).flatten(1, 2)[:, :n] for x in (k, v))
     want, p, x = ref.attention(q[0], kb, vb, scale)
-    bound, delta = ref.attention_bound(q[0], kb, vb, scale, p, x, want, t)
-    bound = bound + n * 2.0 ** -126 * vb.abs().max()
-    err = (got[0].double() - want).abs()
-    assert (err <= bound).all(), float((err / bound).max())
+    width = ref.BLOCK if own else vb.shape[2]
+    for at in range(0, vb.shape[2], width):
+        part = slice(at, at + width)
+        vp = vb[:, :, part].contiguous()
+        bound, delta = ref.attention_bound(q[0], kb, vp, scale, p, x, want[:, part], t)
+        bound = bound + n * 2.0 ** -126 * vp.abs().max()
+        err = (got[0, :, part].double() - want[:, part]).abs()
+        assert (err <= bound).all(), (at, float((err / bound).max()))
     if scores is not None:
         group = q.shape[1] // kb.shape[0]
         w = p.view(kb.shape[0], group, n)
@@ -133,3 +138,47 @@ def test_scales_next_to_the_largest_float(samd_lib, scale):
     q = ref.normal(25, (1, 4, dim), torch.float64).mul_(2.0 ** -126).to(t)
     got = samd.paged_attention(q, cache, table, lens, scale=scale)
     check(got, q, n, k, v, torch.tensor(scale).float().item(), t)
+
+
+def test_values_of_tiny_scales_before_large_ones(samd_lib):
+    """Scales of 2^-110 in front: their weights are summed as those of zero rows are."""
+    heads, dim, n, t = 2, 64, 333, BF16
+    for rise in (22, 40, 100):
+        kl, ks, scale = rising(torch.linspace(0, 1, n, device="cuda"), heads, dim, 8, t, rise)
+        vl, vs = ref.random_rows(5, (heads, n), dim, 8, t)
+        vs[:, :300] = 2.0 ** -110
+        cache, table, lens, k, v = one_sequence(kl, ks, vl, vs, 8)
+        q = torch.zeros((1, 4, dim), dtype=t, device="cuda")
+        q[..., 0] = torch.tensor([1, 0.5, -1, 0.125])
+        scores = torch.zeros((1, heads, n), device="cuda")
+        got = samd.paged_attention(q, cache, table, lens, scale=scale, scores=scores)
+        check(got, q, n, k, v, scale, t, scores, torch.zeros_like(scores))
+
+
+@pytest.mark.parametrize("t", [BF16, F16])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_blocks_of_any_size_beside_each_other(samd_lib, dim, bits, t):
+    """Blocks of 32 elements with scales of their own: the same ratio in all tokens, growing along the sequence, falling,
+    and any in any token, some of them zero. An output depends on its own block's values alone."""
+    heads, n, nb = 2, 700, dim // 32
+    lo, hi = (-100, 100) if t is BF16 else (-24, 8)
+    kl, ks = ref.random_rows(31, (heads, n), dim, bits, t)
+    vl, _ = ref.random_rows(33, (heads, n), dim, bits, t)
+    q = ref.normal(35, (1, 6, dim), t, 2.0)
+    i, blk = torch.arange(n, device="cuda")[:, None], torch.arange(nb, device="cuda")[None]
+    span = hi - lo
+    exps = {"own ratio": hi - (blk * 29) % (span + 1) + 0 * i, "rising": lo + (i * span // n + blk * 7) % (span + 1),
+            "falling": hi - (i * span // n + blk * 7) % (span + 1), "tiny": lo + 0 * (i + blk),
+            "any": ref.ints(37, (n, nb), lo, hi)}
+    for name, e in exps.items():
+        vs = torch.exp2(e.double()).expand(heads, n, nb).clone()
+        if name == "any":
+            vs *= ref.ints(39, (heads, n, nb), 0, 9) > 0
+        cache, table, lens, k, v = one_sequence(kl, ks, vl, vs.to(t), bits)
+        for factor in (1.0, 8.0):
+            scale = factor * dim ** -0.5
+            check(samd.paged_attention(q, cache, table, lens, scale=scale), q, n, k, v, scale, t, own=True)
+        # the same tokens in one CTA
+        cache, table, lens, k, v = one_sequence(*(x[:, :200] for x in (kl, ks, vl, vs.to(t))), bits)
+        check(samd.paged_attention(q, cache, table, lens, scale=dim ** -0.5), q, 200, k, v, dim ** -0.5, t, own=True)
