@@ -584,10 +584,11 @@ SAMD_API size_t samd_moe4_workspace_size(const samd_moe_desc *desc);
  * rows of K weights, down E times K rows of F, one expert behind the other, as
  * samd_matvec4 takes them (fw: 4-bit lanes without spacers, 32- or 64-bit words);
  * all three have zero points or none has. weights * act * up is rounded to
- * `type` before the last product, everything else is in fp32 and rounded once.
+ * `type` before the last product (past fp16's range to an infinity), everything
+ * else is in fp32 and rounded once; the products are those of the integers.
  * Made for few tokens (an expert's weights are read once for every eight tokens
  * that chose it); any M is right. The same call gives the same bits. A token
- * with an infinity or a NaN gives NaNs, in its own row only.
+ * with an infinity or a NaN gives infinities or NaNs, in its own row only.
  */
 SAMD_API samd_status samd_moe4(const samd_moe_desc *desc, samd_fmt fw, const void *x, const int32_t *ids,
                                const float *weights, samd_weights4 gate, samd_weights4 up, samd_weights4 down, void *y,

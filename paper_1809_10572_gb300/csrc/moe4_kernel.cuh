@@ -10,14 +10,14 @@
 // byte each, come once for every eight pairs. An SM receives about 47 weights a
 // clock, so what counts is instructions for a weight. The products go through
 // mma.sync (m16n8k16: 16 rows of weights by eight pairs). A nibble over the
-// mantissa of a power of two is that power plus the nibble; it is not taken off
-// the weight, which would be an instruction for two of them, but off the sum:
-// the accumulator starts with minus the power and the zero point times the same
-// inputs, an MMA whose first operand is a constant row by row. Both products
-// are exact; the sum of 32 .. 128 inputs then carries fp32's rounding of terms
-// up to 1040 (fp16) or 143 (bf16) times an input, 2^-14 and 2^-17 of it at
-// most: below the result's own rounding. (An infinity among a token's inputs
-// gives that token NaNs.)
+// mantissa of a power of two is that power plus the nibble; the power and the zero
+// point are taken off it, exactly, so that the products are those of the integers
+// and a sum knows nothing of inputs whose weights are zero. Taken off the sums
+// instead (an MMA with a constant operand for each of these) a channel 1000 times
+// the others left half of fp16's rounding in them, and the time is the same: the
+// subtraction has a pipe of its own, and the chains of MMAs are half as long (13
+// tokens, 46 of 64 experts of 2048 x 1408, bf16: 79.9 us a layer, off the sums 80.5;
+// with zero points in fp16 83.4 and 82.1).
 //
 // Layout: as in matvec4_kernel.cuh: a word holds lanes 8w .. 8w + 7, one mask
 // takes lanes i and i + 4 out together, so inputs run in the order (0,4),
@@ -132,32 +132,6 @@ __device__ __forceinline__ void mma_pure(float (&d)[4], const uint32_t (&a)[4], 
         "%12, %13};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
-}
-
-// Minus the power and the zero point z (in both halves), for the nibbles at bit 0 (lo) and bit 4 (hi); by multiply-adds,
-// which leave the pipe of the logic operations alone.
-template <typename T>
-__device__ __forceinline__ void minus(uint32_t zz, uint32_t &lo, uint32_t &hi) {
-  if constexpr (std::is_same<T, __half>::value)
-    lo = 0xE400E400u + zz, hi = zz * 16u + 0xD400D400u;
-  else
-    lo = hi = 0xC300C300u + zz;
-}
-
-// The eight lanes of a word as four pairs (i, i + 4), each plus its power; flip is 8 for signed lanes (both halves).
-template <typename T>
-__device__ __forceinline__ void widen(uint32_t w, uint32_t flip, uint32_t (&p)[4]) {
-  if constexpr (std::is_same<T, __half>::value) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t v = w >> 8 * i;
-      p[2 * i] = (v & 0x000F000Fu) ^ (0x64006400u | flip);
-      p[2 * i + 1] = (v & 0x00F000F0u) ^ (0x54005400u | flip << 4);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = ((w >> 4 * i) & 0x000F000Fu) ^ (0x43004300u | flip);
-  }
 }
 
 // RT: row tiles of 16 rows in a tile; CH: chunks of 32 inputs in a block; CPG: chunks of a block that share a scale.
@@ -346,8 +320,8 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
 
   const uint32_t lm = (lane & 15) * kPitch + ((lane >> 4) ^ (((lane & 15) >> kSwz) & (CH - 1))) * 16;
   const uint32_t flip = a.is_signed ? 0x00080008u : 0u;
-  uint32_t plain_lo, plain_hi;
-  minus<T>(flip, plain_lo, plain_hi);
+  mv::Offset<T> plain;
+  plain.set(flip);
 
   float acc[RT][4] = {};
   int slot = 0;
@@ -382,22 +356,22 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
     uint32_t words[RT][4], sc[RT][2] = {}, zc[RT][2] = {};
 #pragma unroll
     for (int gi = 0; gi < kG; ++gi) {
-      uint32_t less[RT][4];
+      mv::Offset<T> less[RT][2];
 #pragma unroll
       for (int q = 0; q < RT; ++q) {
         if ((gi & 1) == 0) {
           sc[q][0] = __shfl_sync(0xffffffffu, s[gi / 2], 16 * q + g);
           sc[q][1] = __shfl_sync(0xffffffffu, s[gi / 2], 16 * q + g + 8);
         }
-        less[q][0] = less[q][1] = plain_lo, less[q][2] = less[q][3] = plain_hi;
+        less[q][0] = less[q][1] = plain;
         if constexpr (kZeros) {
           if ((gi & 3) == 0) {
             zc[q][0] = __shfl_sync(0xffffffffu, z[gi / 4], 16 * q + g) & 0x0F0F0F0Fu;
             zc[q][1] = __shfl_sync(0xffffffffu, z[gi / 4], 16 * q + g + 8) & 0x0F0F0F0Fu;
           }
           const int sel = 0x4040 | (gi & 3) | (gi & 3) << 8;
-          minus<T>(__byte_perm(zc[q][0], 0, sel), less[q][0], less[q][2]);
-          minus<T>(__byte_perm(zc[q][1], 0, sel), less[q][1], less[q][3]);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) less[q][r].set(__byte_perm(zc[q][r], 0, sel));
         }
       }
       float d[RT][4];
@@ -413,12 +387,10 @@ __global__ void __launch_bounds__(kThreads, 2) moe4_kernel(const MoeArgs a) {
 #pragma unroll
         for (int q = 0; q < RT; ++q) {
           uint32_t lo[4], hi[4];
-          widen<T>(words[q][2 * (c & 1)], flip, lo);
-          widen<T>(words[q][2 * (c & 1) + 1], flip, hi);
-          mma_pure<T>(d[q], less[q], b0, b1, cc > 0);
-          mma_pure<T>(d[q], less[q], b2, b3, true);
+          mv::widen(words[q][2 * (c & 1)], flip, less[q][0], lo);
+          mv::widen(words[q][2 * (c & 1) + 1], flip, less[q][1], hi);
           const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
-          mma_pure<T>(d[q], a0, b0, b1, true);
+          mma_pure<T>(d[q], a0, b0, b1, cc > 0);
           mma_pure<T>(d[q], a1, b2, b3, true);
         }
       }
