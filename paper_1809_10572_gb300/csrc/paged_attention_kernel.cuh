@@ -722,8 +722,10 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
       sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 4);
       sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 8);
       sum[c] += __shfl_xor_sync(0xffffffffu, sum[c], 16);
-      // the sum of weights to 1 .. 2, and the blocks' powers off: what is left is the size of values, in any scales
-      const int size = sum[c] > 0.0f ? log2_down(sum[c]) : 0;
+      // the sum of weights to 1 .. 2, and the blocks' powers off: what is left is the size of values, in any scales (past
+      // 2^24 a reference may not hold the sum's power, which then stays where it is)
+      int size = sum[c] > 0.0f ? log2_down(sum[c]) : 0;
+      if (ref[c] + static_cast<float>(size) - ref[c] != static_cast<float>(size)) size = 0;
       ref[c] += static_cast<float>(size);
       sum[c] *= power_of_two(-size);
 #pragma unroll

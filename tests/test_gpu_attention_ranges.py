@@ -182,3 +182,26 @@ def test_blocks_of_any_size_beside_each_other(samd_lib, dim, bits, t):
         # the same tokens in one CTA
         cache, table, lens, k, v = one_sequence(*(x[:, :200] for x in (kl, ks, vl, vs.to(t))), bits)
         check(samd.paged_attention(q, cache, table, lens, scale=dim ** -0.5), q, 200, k, v, dim ** -0.5, t, own=True)
+
+
+@pytest.mark.parametrize("t", [BF16, F16])
+@pytest.mark.parametrize("n,width", [(33, 0), (33, 20), (200, 20), (333, 0), (700, 0)])
+def test_equal_logits_of_any_size(samd_lib, n, width, t):
+    """The same key for all tokens, logits up to 2^40: whatever a logit's rounding is, it is the same for all, and all
+    weigh 1 / n. (A weight times its scale is rounded by 2^-11; sums as everywhere.)"""
+    heads, dim = 2, 64
+    vl, vs = ref.random_rows(41, (heads, n), dim, 8, t)
+    kl = torch.zeros((heads, n, dim), dtype=torch.int64, device="cuda")
+    kl[..., 0], kl[..., 33] = 127, -100
+    cache, table, lens, k, v = one_sequence(kl, torch.ones_like(vs), vl, vs, 8, width)
+    vb = v.transpose(0, 1).flatten(1, 2)[:, :n].repeat_interleave(2, 0)
+    want = vb.mean(1)
+    lim = (2.0 ** -11 + (n / 16 + 64) * 2.0 ** -23) * vb.abs().mean(1)
+    for size in (1.0, 2.0 ** 15, -2.0 ** 12):
+        for scale in (0.125, 2.0 ** 17, 2.0 ** 18 / 3):
+            q = torch.zeros((1, 4, dim), dtype=t, device="cuda")
+            q[0, :, 0] = torch.tensor([1, -1, 0.75, 0.01]) * size
+            scores = torch.zeros((1, heads, n), device="cuda")
+            got = samd.paged_attention(q, cache, table, lens, scale=scale, scores=scores)
+            assert ((got[0].double() - want).abs() <= ref.UNIT[t] * (want.abs() + lim) + lim).all(), (size, scale)
+            assert ((scores.double() - 2 / n).abs() <= 2 / n * (n / 16 + 66) * 2.0 ** -23).all(), (size, scale)
