@@ -205,3 +205,21 @@ def test_equal_logits_of_any_size(samd_lib, n, width, t):
             got = samd.paged_attention(q, cache, table, lens, scale=scale, scores=scores)
             assert ((got[0].double() - want).abs() <= ref.UNIT[t] * (want.abs() + lim) + lim).all(), (size, scale)
             assert ((scores.double() - 2 / n).abs() <= 2 / n * (n / 16 + 66) * 2.0 ** -23).all(), (size, scale)
+
+
+@pytest.mark.slow
+def test_counted_weights_past_two_to_the_31(samd_lib):
+    """A workspace whose logits take 2.4 GB, the last sequence's at its end."""
+    heads, dim, n, t, seqs, pages = 8, 32, 3000, F16, 9, 65536
+    rows = [x for s in (51, 53) for x in ref.random_rows(s, (heads, n), dim, 4, t)]
+    cache, one, _, k, v = one_sequence(*rows, 4)
+    table = torch.full((seqs, pages), -1, dtype=torch.int32, device="cuda")
+    table[0, :one.shape[1]] = table[-1, :one.shape[1]] = one[0]
+    lens = torch.tensor([100] + [0] * (seqs - 2) + [n], dtype=torch.int32, device="cuda")
+    assert samd.samd_paged_attention_workspace_size(cache._desc, samd._cache_seqs(table, lens), heads, True) > 1 << 31
+    q = ref.normal(55, (seqs, heads, dim), t, 2.0)
+    scores = torch.zeros((seqs, heads, n), device="cuda")
+    got = samd.paged_attention(q, cache, table, lens, scores=scores)
+    for b, m in ((0, 100), (seqs - 1, n)):
+        check(got[b:b + 1], q[b:b + 1], m, k, v, dim ** -0.5, t, scores[b:b + 1], torch.zeros_like(scores[:1]))
+    assert not got[1:-1].any() and not scores[1:-1].any()

@@ -1,5 +1,5 @@
 """samd_moe4 with channels far above the others, against its definition in 64 bits within a bound that knows only the
-products of the integers."""
+products of the integers; and matrices past 2^31 bytes."""
 import pytest
 import torch
 
@@ -72,3 +72,35 @@ def test_channels_far_above_the_others(samd_lib, M, K, F, E, topk, G, zeros, t):
         err = (got.double() - want).abs()
         assert torch.isfinite(want.to(t)).all() and (err <= ref.UNIT[t] * (want.abs() + lim) + lim + ref.TINY).all()
         assert float(err.norm()) <= ref.UNIT[t] * float(want.norm())
+
+
+@pytest.mark.slow
+def test_matrices_past_two_to_the_31_bytes(samd_lib):
+    """The last experts of matrices of 4.3 GB each."""
+    E, K, F, G, topk, t = 512, 4096, 4096, 128, 3, BF16
+    g = torch.Generator(device="cuda").manual_seed(3)
+
+    def rows(n, k):
+        return (torch.randint(-(1 << 31), (1 << 31) - 1, (n, k // 8), dtype=torch.int32, device="cuda", generator=g),
+                (torch.rand((n, k // G), device="cuda", generator=g) + 0.5).mul_(0.01).to(t))
+
+    mats = gate, up, down = rows(E * F, K), rows(E * F, K), rows(E * K, F)
+    assert gate[0].numel() * 4 > 1 << 31
+    x = ref.normal(4, (2, K), t)
+    ids = torch.tensor([[511, 0, 260], [255, 510, 511]], dtype=torch.int32, device="cuda")
+    w = torch.tensor([[0.5, 0.25, 0.25], [0.125, 0.5, 0.375]], device="cuda")
+    got = samd.moe4(x, ids, w, gate, up, down, G, samd.fmt(4, True), "silu")
+    want = torch.zeros((2, K), dtype=torch.float64, device="cuda")
+    lim = torch.zeros_like(want)
+    for m in range(2):
+        for j, e in enumerate(ids[m].tolist()):
+            own = []
+            for (lanes, scales), n, k in zip(mats, (F, F, K), (K, K, F)):
+                b = lanes.view(E, n, -1)[e].contiguous().view(torch.uint8).view(n, -1)
+                q = torch.stack((b & 15, b >> 4), -1).flatten(1).long()
+                own.append(ref.weights4(torch.where(q > 7, q - 16, q), scales.view(E, n, -1)[e], None, G)[None])
+            one = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+            a = x[m:m + 1], one, w[m:m + 1, j:j + 1], *own, "silu"
+            want[m] += plain(*a)[0]
+            lim[m] += bound(*a, t)[0]
+    assert ((got.double() - want).abs() <= ref.UNIT[t] * (want.abs() + lim) + lim + ref.TINY).all()
