@@ -548,10 +548,16 @@ cudaError_t launch_grouped(const MoeArgs &a, cudaStream_t s) {
 }
 
 // First kernel: tiles of 32 rows are a warp's where there are one and a half times as many as warps or more, or three
-// quarters where a CTA's warps would have one block each of a tile (13 tokens, 46 of 64 experts of 2048 x 1408: 82 us a
-// layer, with the CTA's tiles 97; 32 tokens, 32 of 1024 x 1024: 48 and 55; but 4 tokens, 8 of 4096 x 4096: 53 and 46);
-// else the CTA's, of 32 rows (inputs are put in order and looked up for twice the weights: 46 us of the last, of 16 rows
-// 54) where they give every SM four, else of 16. Second: of 32 rows where the warps of twice as many CTAs as fit get a block.
+// quarters where a CTA's warps would have one block each of a tile; else the CTA's, of 32 rows (inputs are put in order and
+// looked up for twice the weights) where they give every SM four, else of 16. us of a layer with a warp's tiles, the CTA's
+// of 32 rows, of 16 (tokens, experts of each, K x F; groups of 64): 13, 6 of 64, 2048 x 1408: 80, 88, 107; 32, 4 of 32, 1024
+// x 1024: 47, 54, 60; 24, 4 of 64, 512 x 1024: 37, 43, 53; 3, 8 of 64, 7168 x 2048: 169, 172, 209; 8, 4 of 16, 2048 x 2048:
+// 44, 44, 53; 4, 2 of 8, 4096 x 4096: 56, 47, 55; 6, 4 of 32, 4096 x 1408: 70, 60, 68; 1, 2 of 8, 4096 x 8192: 47, 46, 51.
+// Where the rule is not the best: 16, 2 of 16, 1024 x 2048: 39, 34, 49 (it takes the warp's); 1, 8 of 64, 2048 x 768: 27,
+// 20.5, 22.4 and 2, 2 of 16, 4096 x 2048: 41, 30, 34 (it takes those of 16 rows).
+// Second: of 32 rows where the warps of twice as many CTAs as fit get a block. A layer with 32 and 16 rows: 80 and 85, 172
+// and 179, 47 and 49 us for the first, the fourth and the sixth of these; but 47 and 36 for the second, 37 and 33
+// for the third, 39 and 28 for the 16 tokens: many pairs of few columns, for which the rule is wrong.
 template <typename T, bool kGated, bool kZeros>
 cudaError_t launch_sized(const MoeArgs &a, cudaStream_t s) {
   const int64_t pairs = static_cast<int64_t>(a.M) * a.topk, experts = pairs < a.E ? pairs : a.E;

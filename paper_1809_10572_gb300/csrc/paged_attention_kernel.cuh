@@ -48,12 +48,15 @@
 // pages at the same time.
 //
 // Measured on one GB300, with the join (GPU time of a call): one sequence of
-// 131072 tokens, 8 key heads of 128 elements: 58 us in 8 bits (285 MB, 0.72 of the
-// copy bandwidth; twice the tokens of a call cost 1.05 of what their bytes do, so
-// that the rest, about 12 us, is fixed: launches, three dependent loads before the
-// first step, the join), 46 us in 4 bits (151 MB, 0.48). A step of 16 tokens by 128
-// elements is about 500 instructions in 8 bits and 440 in 4, 160 and 144 of them
-// for widening; with sixteen warps an SM issue slots are 54 and 65% busy.
+// 131072 tokens, 8 key heads of 128 elements: 59 us in 8 bits (285 MB, 0.71 of the
+// copy bandwidth; twice the tokens of a call cost 1.04 of what their bytes do, so
+// that the rest, about 14 us, is fixed: launches, three dependent loads before the
+// first step, the join), 49 us in 4 bits (151 MB, 0.46). A step of 16 tokens by 128
+// elements is 468 instructions in 4 bits (160 of the logic pipe, 144 for widening)
+// and about 580 in 8 (16 sequences of up to 8192 tokens, what beginning their heads
+// takes among them); with sixteen warps an SM issue slots are 64 and 58% busy. Blocks'
+// own powers cost 24 multiplications and maxima a step: 3 us of the 49, nothing
+// where HBM bounds (one range for all blocks of a head: 45.7 and 59.1 us).
 #pragma once
 
 #include "cache_internal.cuh"
@@ -67,8 +70,10 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kHeads = 8;     // query heads of a CTA: the MMA's columns
 constexpr int kMinSteps = kWarps;  // a CTA is not used for fewer, unless a head has fewer
 // What beginning a head takes of a CTA's time, in steps: a join, the next head's length, pages and query, one after the
-// other. Counted when steps are dealt out, 53 sequences of up to 4001 tokens and 12 heads take 59 us, without 71; 16 of up
-// to 8192 38 and 42 (14 to 40 are within 3% of each other there; long sequences in 4 bits lose 5% from 20 on).
+// other. Counted when steps are dealt out; us of a call with 1, 8, 12, 16, 20, 24 and 32 for it: 53 sequences of up to 4001
+// tokens, 12 heads of 96: 73, 64, 59, 56, 58, 59, 58; 16 of up to 8192, 8 heads of 128: 41, 40, 37, 38, 38, 39, 38; 8 of up
+// to 16000 in 4 bits with scores: 29.0, 27.8, 27.4, 26.5, 26.4, 25.8, 25.2; one of 131072 in 4 bits: 49 up to 24, 51 with
+// 32; one in 8 bits, of any length: within 3% of each other.
 constexpr int kHeadCost = 16;
 constexpr int kMostUp = 120;             // largest power of a block's weights (log2)
 constexpr float kMostWeight = 65536.0f;  // a weight above it moves the reference, whatever its values are
