@@ -519,11 +519,11 @@ SAMD_API size_t samd_paged_attention_workspace_size(const samd_cache *cache, con
  * of sums changes with the batch's lengths. q, key and value of infinity or NaN
  * give NaNs in their own head only. |scale| has to be finite (SAMD_EINVAL).
  * Logits, weights and sums are in fp32 (a weight below 2^-126 of the largest is
- * 0); but a weight times the scale of 32 values is rounded to 11 bits before it
- * meets the lanes: up to 2^-11 of sum_t p_t |V_td|, and 2^-31 of a term of the
- * block's largest weight times scale, for each token. bfloat16: keys' scales
- * above 2^100 and values above 2^115 may pass fp32's range, values' scales below
- * 2^-114 lose bits.
+ * 0; elements of q are taken to 2^-38 of their head's largest); but a weight
+ * times the scale of 32 values is rounded to 11 bits before it meets the lanes:
+ * up to 2^-11 of sum_t p_t |V_td|, and 2^-31 of a term of the block's largest
+ * weight times scale, for each token. bfloat16: keys' scales above 2^100 and
+ * values above 2^115 may pass fp32's range, values' scales below 2^-114 lose bits.
  */
 SAMD_API samd_status samd_paged_attention(const samd_cache *cache, const samd_cache_seqs *seqs, int q_heads,
                                           const void *q, int64_t ldq, float scale, void *out, int64_t ldo,

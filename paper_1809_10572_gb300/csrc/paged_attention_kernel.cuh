@@ -322,7 +322,8 @@ struct Att {
   static constexpr int kSums = kHeads * kDim * 4;
   static constexpr bool kInStage = kStage >= kSums;
   static constexpr int bytes(int stages) { return kWarps * (stages * kStage + (kInStage ? 0 : kSums)); }
-  static constexpr bool fits(int stages, int ctas) { return ctas * (bytes(stages) + 1024 + 512) <= 228 * 1024; }
+  // (with what the system keeps of a CTA's shared memory, and the kernel's own)
+  static constexpr bool fits(int stages, int ctas) { return ctas * (bytes(stages) + 1024 + 768) <= 228 * 1024; }
   // CTAs of an SM by their registers (128 a thread with four, 168 with three); then as many stages a warp as fit, up to four
   static constexpr int kCtas = NB <= 4 && fits(2, 4) ? 4 : NB <= 6 && fits(2, 3) ? 3 : 2;
   static constexpr int kStages = fits(4, kCtas) ? 4 : fits(3, kCtas) ? 3 : 2;
@@ -501,7 +502,9 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
   if (goes_on(have)) load_q(have);
   while (goes_on(have)) {
     const int len = static_cast<int>(length_of(a.s, have.b));
-    float *const logits = a.logits ? a.logits + ((static_cast<int64_t>(have.b * a.heads + have.h) * a.parts + part) * span_tokens + g) * kHeads + 2 * t : nullptr;
+    float *logits = nullptr;  // the thread's two heads of the first token that it has
+    if (a.logits)
+      logits = a.logits + ((static_cast<int64_t>(have.b * a.heads + have.h) * a.parts + part) * span_tokens + g) * kHeads + 2 * t;
 
     // q of head g in the MMA's order, in fp16 under a power of two
     uint32_t qb[kUnits][16 / BITS];  // pairs of a unit of 16 bytes: 2 (8 bits) or 4 (4 bits) words
@@ -669,8 +672,10 @@ __global__ void __launch_bounds__(kThreads, Att<NB, BITS>::kCtas) paged_attentio
         for (int i = 0; i < NB; ++i) {
           uint32_t sizes = 0;  // exponents of the largest weight times scale, of both heads
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-            sizes |= static_cast<uint32_t>(log2_down(fmaxf(fabsf(e[c] * scale_at<T>(vw[0], i)), fabsf(e[2 + c] * scale_at<T>(vw[1], i)))) + 127) << 16 * c;
+          for (int c = 0; c < 2; ++c) {
+            const float m = fmaxf(fabsf(e[c] * scale_at<T>(vw[0], i)), fabsf(e[2 + c] * scale_at<T>(vw[1], i)));
+            sizes |= static_cast<uint32_t>(log2_down(m) + 127) << 16 * c;
+          }
           sizes = __vmaxu2(sizes, __shfl_xor_sync(0xffffffffu, sizes, 4));
           sizes = __vmaxu2(sizes, __shfl_xor_sync(0xffffffffu, sizes, 8));
           sizes = __vmaxu2(sizes, __shfl_xor_sync(0xffffffffu, sizes, 16));
